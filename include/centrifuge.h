@@ -284,6 +284,151 @@ cf_status cf_layer_bwd_lora(const cf_layer_desc* desc, const cf_saved* saved, co
                             int32_t* n_kept_dev_out, int32_t* n_kept_host, void* ws, size_t ws_bytes,
                             cf_stream stream);
 
+/* ---- query/key norm with rotary embedding (model families that normalise the heads) --------
+ * Every head of the projected queries and keys is normalised by its own root mean square, scaled by a gain that all heads of
+ * its kind share and, where tables are given, rotated at its token's position, all in one pass:
+ *   n = x * rstd,  rstd = (mean(x^2) + rms_eps)^(-1/2),  y = R(pos) (n * g)
+ * with the rotation R of cf_saved (half-split pairs).  Arithmetic is fp32; y is rounded once.
+ *   Uses only S, Hq, Hkv, d, dtype and rms_eps of desc (Hq % Hkv == 0 is not asked for).  d is a power of two, 16 to 256
+ *   in CF_BF16 and 8 to 256 in CF_F32; another multiple of 8 in CF_BF16 is CF_ERR_UNSUPPORTED.
+ *   Row t of the full-length tensors has position positions[t], or t mod S without positions; a position outside [0, S),
+ *   the rows of the tables, is taken for the nearest one inside.  n_rows and rows read through idx are at most 2^30. */
+typedef struct {
+    void *q, *k;                   /* rows of [Hq*d] and [Hkv*d] elements, 16-byte aligned          */
+    int64_t q_stride, k_stride;    /* elements from row to row, 0 = dense; multiples of 16 bytes    */
+} cf_qk;
+
+typedef struct {
+    const void *gq, *gk;           /* [d] gains of the queries' and the keys' norm                  */
+    const float *rope_cos, *rope_sin;   /* [S, d/2] fp32; both NULL = no rotation                   */
+    const int32_t* positions;      /* nullable                                                      */
+} cf_qk_norm;
+
+/* out = norm and rotation of in, n_rows rows of each.  out may be in itself (same pointers and strides); no other overlap. */
+cf_status cf_qk_norm_rope_fwd(const cf_layer_desc* desc, const cf_qk_norm* p, const cf_qk* in, int32_t n_rows,
+                              const cf_qk* out, cf_stream stream);
+
+/* The backward pass on kept rows.  in: the tensors before the norm, full length, read through idx (NULL: row j is row j); dy,
+ * dx: compact, one row per kept token; dx may be dy itself (same pointers and strides), no other overlap.  n_kept_dev and max_kept as for
+ * cf_gather_rows.  dgq, dgk [d] (both or neither NULL: frozen gains): gain gradients, overwritten in the storage dtype, or
+ * (main_grad 1) fp32 buffers that the call adds to; zero rows give zero gradients.  The sums' order depends on the sizes alone.
+ * ws is needed for the gain gradients only. */
+size_t cf_qk_norm_workspace_bytes(const cf_layer_desc* desc, int32_t max_kept);
+cf_status cf_qk_norm_rope_bwd(const cf_layer_desc* desc, const cf_qk_norm* p, const cf_qk* in, const cf_qk* dy_kept,
+                              const int32_t* idx, const int32_t* n_kept_dev, int32_t max_kept, const cf_qk* dx_kept,
+                              void* dgq, void* dgk, int32_t main_grad, void* ws, size_t ws_bytes, cf_stream stream);
+
+/* The layer calls for models with that norm: saved->q and saved->k are, as always, what attention used (after norm and rotation),
+ * qk has the projections' outputs ahead of them and the gains.  dq and dk go back through the rotation and the norm at each kept
+ * row, in place, before the projections' backward.  dgq, dgk [d]: in the storage dtype, overwritten, or with grads->main_grad fp32 and
+ * added to; both NULL: frozen gains (always so in the adapter call, whose dgq and dgk have to be NULL).  Everything else as for the calls of the same name without
+ * _qk (the compact call: cf_layer_bwd_compact_dev with n_kept_dev, and cf_layer_bwd_compact of max_kept rows with NULL), the workspace too, but for its
+ * size: cf_layer_qk_workspace_bytes / cf_lora_qk_workspace_bytes. */
+typedef struct {
+    const void *q_pre, *k_pre;     /* [T,Hq*d], [T,Hkv*d] projected queries and keys                */
+    const void *gq, *gk;           /* [d] gains                                                     */
+    float eps;                     /* of this norm                                                  */
+    void *dgq, *dgk;
+} cf_layer_qk;
+
+size_t cf_layer_qk_workspace_bytes(const cf_layer_desc* desc, int32_t max_kept);
+size_t cf_lora_qk_workspace_bytes(const cf_layer_desc* desc, int32_t rank, int32_t max_kept);
+cf_status cf_layer_bwd_filtered_qk(const cf_layer_desc* desc, const cf_saved* saved, const cf_weights* w, const cf_layer_qk* qk,
+                                   const void* dy_full, const uint8_t* mask, int32_t max_kept, cf_grads* grads,
+                                   int32_t* idx_out, int32_t* cu_kept_out, int32_t* n_kept_dev_out, int32_t* n_kept_host,
+                                   void* ws, size_t ws_bytes, cf_stream stream);
+cf_status cf_layer_bwd_compact_qk(const cf_layer_desc* desc, const cf_saved* saved, const cf_weights* w, const cf_layer_qk* qk,
+                                  const void* dy_kept, const int32_t* idx, const int32_t* cu_kept, const int32_t* n_kept_dev,
+                                  int32_t max_kept, cf_grads* grads, void* ws, size_t ws_bytes, cf_stream stream);
+cf_status cf_layer_bwd_dense_qk(const cf_layer_desc* desc, const cf_saved* saved, const cf_weights* w, const cf_layer_qk* qk,
+                                const void* dy_full, cf_grads* grads, void* ws, size_t ws_bytes, cf_stream stream);
+cf_status cf_layer_bwd_lora_qk(const cf_layer_desc* desc, const cf_saved* saved, const cf_weights* w, const cf_layer_qk* qk,
+                               const cf_lora* lora, const void* dy_full, const uint8_t* mask, int32_t max_kept,
+                               cf_lora_grads* grads, int32_t* idx_out, int32_t* cu_kept_out, int32_t* n_kept_dev_out,
+                               int32_t* n_kept_host, void* ws, size_t ws_bytes, cf_stream stream);
+
+/* ---- losses of kept tokens with their gradient towards the logits --------------------------
+ * What stands ahead of the layers: the gradient is [N_k,V], the compact upstream gradient of the head's reduced linear backward.
+ * With s = logit_scale, l a kept token's logits and y its target, lp = s*l_y - log(sum_c exp(s*l_c)) and
+ *   CF_LOSS_NLL     L = -lp                                   (Sec. 2.1 Eq. 1 with norm = 0: the mean over kept tokens)
+ *   CF_LOSS_POLICY  L = -min(r*A, clip(r, 1-clip_lo, 1+clip_hi)*A) + kl_coef*k,  r = exp(lp - old_logp),
+ *                   k = exp(ref_logp - lp) - (ref_logp - lp) - 1   (ref_logp NULL: k = 0)
+ *   loss = sum_j w_j*L_j / norm,   dlogits[j,c] = w_j/norm * dL/dlp * s * ([c == y] - exp(s*l_c - logsumexp)),
+ * with dL/dlp of the first term 0 where the clipped product is the smaller one and -r*A elsewhere.  norm 0 stands for the
+ * number of live rows.  A row whose target lies outside [0,V) or whose weight is 0 is left out whatever it holds (infinities
+ * and NaN included): its logp and its gradient are 0; it counts in the number of live rows.  A logit of -inf has probability 0.
+ *   logits   [rows,V], row stride logits_stride elements (0 = V); kept row j is row idx[j] (NULL: row j).  Any alignment of rows:
+ *            pointers need their element's only, multiples of 16 bytes are faster
+ *   targets, old_logp, ref_logp, advantages, weights   one per row of logits, read at the same idx[j].  weights NULL: 1
+ *   dlogits  [max_kept,V], row stride dlogits_stride (nullable: not wanted).  May be logits itself (same stride) without idx
+ *   logp     [max_kept] fp32 (nullable): lp.  For the same logits it has the same bits with and without dlogits, so that old_logp
+ *            from a call without gradient makes r exactly 1
+ *   stats    [4] fp32 (nullable): loss, its first term, the mean k, the share of clipped tokens (all weighted by w/norm)
+ * At least one of dlogits, logp, stats is wanted.  n_kept_dev and max_kept as for cf_gather_rows; rows behind the live ones are
+ * left as they were.  ws: cf_token_loss_workspace_bytes(max_kept), 16-byte aligned. */
+typedef enum { CF_LOSS_NLL = 0, CF_LOSS_POLICY = 1 } cf_loss_kind;
+
+typedef struct {
+    int32_t kind;                  /* cf_loss_kind                              */
+    int32_t V;                     /* vocabulary                                */
+    int32_t dtype;                 /* cf_dtype of logits and dlogits            */
+    float logit_scale;             /* 0 => 1 (one over a sampling temperature)  */
+    float clip_lo, clip_hi;        /* policy: 0 <= clip_lo <= 1, clip_hi >= 0   */
+    float kl_coef;                 /* policy; 0 without ref_logp                */
+    float norm;                    /* 0 => the number of live rows              */
+} cf_loss_desc;
+
+size_t cf_token_loss_workspace_bytes(int32_t max_kept);
+cf_status cf_token_loss(const cf_loss_desc* desc, const void* logits, int64_t logits_stride, const int64_t* targets,
+                        const float* old_logp, const float* ref_logp, const float* advantages, const float* weights,
+                        const int32_t* idx, const int32_t* n_kept_dev, int32_t max_kept, void* dlogits,
+                        int64_t dlogits_stride, float* logp, float* stats, void* ws, size_t ws_bytes, cf_stream stream);
+
+/* ---- AdamW over many tensors ---------------------------------------------------------------
+ * What takes cf_grads (and cf_lora_grads): one launch per 40 tensors, of any sizes,
+ *   g' = grad_scale * g * min(1, max_norm / (norm + 1e-6))
+ *   m = beta1*m + (1-beta1)*g',  v = beta2*v + (1-beta2)*g'^2
+ *   p = p - lr*weight_decay*p - lr * (m / (1-beta1^step)) / (sqrt(v / (1-beta2^step)) + eps)
+ * in fp32.  norm_dev (device, nullable: no clipping) is what cf_grad_norm left; where it is not finite the call changes nothing.
+ * step_dev, lr_dev (device, nullable) replace step and lr, for a call captured into a graph.
+ *   p        CF_F32 parameters, or CF_BF16 ones with (master) or without an fp32 master copy; p is the rounded master
+ *   m, v     state_bits 32: fp32.  state_bits 8: e4m3 bytes that stand for m / m_scale and sqrt(v) / v_scale, with a scale for every
+ *            256 elements (ceil(n/256) of them): the block's largest absolute value / 448.  m is rounded to nearest.  sqrt(v) is rounded up with the
+ *            probability of what is cut off, by 20 bits of a hash of (seed, step, tensor's number in the call, element): to nearest, an average over
+ *            1/(1-beta2) steps would stand still, since a step changes it by less than half a step of 8 bits; and never
+ *            to 0 unless it is 0, which a later division by eps would blow up.
+ * All pointers 16-byte aligned (scales: 4); no overlap.  The tensors array is read on the host during the call. */
+typedef struct {
+    void* p;
+    float* master;                 /* CF_BF16 parameters: NULL or the fp32 master copy; CF_F32: NULL */
+    const void* g;
+    void *m, *v;
+    float *m_scale, *v_scale;      /* state_bits 8                              */
+    int64_t n;                     /* elements, 0 to 2^35                       */
+    float weight_decay;
+} cf_adamw_tensor;
+
+typedef struct {
+    double lr, beta1, beta2, eps;
+    int32_t step;                  /* 1 for the first                           */
+    int32_t p_dtype, g_dtype;      /* cf_dtype of all parameters, of all gradients */
+    int32_t state_bits;            /* 32 or 8                                   */
+    uint32_t seed;                 /* state_bits 8                              */
+    float grad_scale;
+    float max_norm;                /* > 0 where norm_dev is given               */
+    const float* norm_dev;
+    const int32_t* step_dev;
+    const float* lr_dev;
+} cf_adamw_desc;
+
+cf_status cf_adamw_step(const cf_adamw_desc* desc, const cf_adamw_tensor* tensors, int32_t n_tensors, cf_stream stream);
+
+/* norm (device, [1] fp32) = |grad_scale| * sqrt(sum of the squares of all tensors' elements), summed in fp64 in a fixed order.  grads: host array
+ * of n_tensors 16-byte aligned device pointers, sizes: their elements. */
+size_t cf_grad_norm_workspace_bytes(int32_t n_tensors);
+cf_status cf_grad_norm(const void* const* grads, const int64_t* sizes, int32_t n_tensors, int32_t g_dtype, float grad_scale,
+                       float* norm, void* ws, size_t ws_bytes, cf_stream stream);
+
 /* ---- measurement probes (for the rooflines of Sec. 3.2's GEMMs and of the gather / row-local
  * kernels; not part of the method) ------------------------------------------------------------
  * cf_probe_mfma_bf16: n_blocks blocks of four waves; every wave runs `iters` passes over an 8 x 8

@@ -17,6 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libcentrifuge.so")
 
 CF_BF16, CF_F32 = 0, 1
+CF_LOSS_NLL, CF_LOSS_POLICY = 0, 1
 _STATUS = {0: "CF_OK", 1: "CF_ERR_NULL", 2: "CF_ERR_SHAPE", 3: "CF_ERR_DTYPE", 4: "CF_ERR_WORKSPACE",
            5: "CF_ERR_UNSUPPORTED", 6: "CF_ERR_HIP"}
 
@@ -28,6 +29,9 @@ EXPORTS = (
     "cf_layer_bwd_dense",
     "cf_lora_workspace_bytes", "cf_layer_bwd_lora", "cf_probe_mfma_bf16", "cf_probe_mfma_lds_bf16",
     "cf_probe_copy",
+    "cf_qk_norm_rope_fwd", "cf_qk_norm_workspace_bytes", "cf_qk_norm_rope_bwd", "cf_layer_qk_workspace_bytes",
+    "cf_lora_qk_workspace_bytes", "cf_layer_bwd_filtered_qk", "cf_layer_bwd_compact_qk", "cf_layer_bwd_dense_qk", "cf_layer_bwd_lora_qk",
+    "cf_token_loss_workspace_bytes", "cf_token_loss", "cf_adamw_step", "cf_grad_norm_workspace_bytes", "cf_grad_norm",
 )
 
 
@@ -68,6 +72,35 @@ class Lora(C.Structure):
 
 class LoraGrads(C.Structure):
     _fields_ = [("d" + n, C.c_void_p) for n in _LORA_T] + [("dx", C.c_void_p)]
+
+
+class Qk(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("q_stride", C.c_int64), ("k_stride", C.c_int64)]
+
+
+class QkNorm(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("gq", "gk", "rope_cos", "rope_sin", "positions")]
+
+
+class LayerQk(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q_pre", "k_pre", "gq", "gk")] + [("eps", C.c_float)] + \
+               [(n, C.c_void_p) for n in ("dgq", "dgk")]
+
+
+class LossDesc(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("V", C.c_int32), ("dtype", C.c_int32)] + \
+               [(n, C.c_float) for n in ("logit_scale", "clip_lo", "clip_hi", "kl_coef", "norm")]
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("p", "master", "g", "m", "v", "m_scale", "v_scale")] + \
+               [("n", C.c_int64), ("weight_decay", C.c_float)]
+
+
+class AdamwDesc(C.Structure):
+    _fields_ = [(n, C.c_double) for n in ("lr", "beta1", "beta2", "eps")] + \
+               [(n, C.c_int32) for n in ("step", "p_dtype", "g_dtype", "state_bits")] + [("seed", C.c_uint32)] + \
+               [("grad_scale", C.c_float), ("max_norm", C.c_float)] + [(n, C.c_void_p) for n in ("norm_dev", "step_dev", "lr_dev")]
 
 
 _lib = None
@@ -130,6 +163,25 @@ def lib() -> C.CDLL:
     L.cf_probe_mfma_lds_bf16.argtypes = [i32, i32, i32, vp, C.POINTER(C.c_double), vp]
     L.cf_probe_copy.restype = C.c_int
     L.cf_probe_copy.argtypes = [vp, vp, sz, vp]
+    desc, qk, qkn = C.POINTER(LayerDesc), C.POINTER(Qk), C.POINTER(QkNorm)
+    layer = [desc, C.POINTER(Saved), C.POINTER(Weights), C.POINTER(LayerQk)]
+    for name, res, args in (
+            ("cf_qk_norm_rope_fwd", C.c_int, [desc, qkn, qk, i32, qk, vp]),
+            ("cf_qk_norm_workspace_bytes", sz, [desc, i32]),
+            ("cf_qk_norm_rope_bwd", C.c_int, [desc, qkn, qk, qk, vp, vp, i32, qk, vp, vp, i32, vp, sz, vp]),
+            ("cf_layer_qk_workspace_bytes", sz, [desc, i32]),
+            ("cf_lora_qk_workspace_bytes", sz, [desc, i32, i32]),
+            ("cf_layer_bwd_filtered_qk", C.c_int, layer + [vp, vp, i32, C.POINTER(Grads), vp, vp, vp, C.POINTER(i32), vp, sz, vp]),
+            ("cf_layer_bwd_compact_qk", C.c_int, layer + [vp, vp, vp, vp, i32, C.POINTER(Grads), vp, sz, vp]),
+            ("cf_layer_bwd_dense_qk", C.c_int, layer + [vp, C.POINTER(Grads), vp, sz, vp]),
+            ("cf_layer_bwd_lora_qk", C.c_int, layer + [C.POINTER(Lora), vp, vp, i32, C.POINTER(LoraGrads), vp, vp, vp, C.POINTER(i32),
+                                                       vp, sz, vp]),
+            ("cf_token_loss_workspace_bytes", sz, [i32]),
+            ("cf_token_loss", C.c_int, [C.POINTER(LossDesc), vp, i64, vp, vp, vp, vp, vp, vp, vp, i32, vp, i64, vp, vp, vp, sz, vp]),
+            ("cf_adamw_step", C.c_int, [C.POINTER(AdamwDesc), C.POINTER(AdamwTensor), i32, vp]),
+            ("cf_grad_norm_workspace_bytes", sz, [i32]),
+            ("cf_grad_norm", C.c_int, [C.POINTER(vp), C.POINTER(i64), i32, i32, f32, vp, vp, sz, vp])):
+        getattr(L, name).restype, getattr(L, name).argtypes = res, args
     _lib = L
     return L
 
@@ -296,8 +348,10 @@ _WEIGHTS = ("wq", "wk", "wv", "wo", "wg", "wu", "wd", "g1", "g2")
 class LayerBackward:
     """Pre-allocated outputs + workspace for repeated calls on one layer shape."""
 
-    def __init__(self, desc: LayerDesc, device="cuda:0", max_kept: int | None = None, main_grad: bool = False):
-        """main_grad: the parameter gradients are fp32 buffers, zeroed here, that every call adds to."""
+    def __init__(self, desc: LayerDesc, device="cuda:0", max_kept: int | None = None, main_grad: bool = False,
+                 qk_norm_eps: float | None = None):
+        """main_grad: the parameter gradients are fp32 buffers, zeroed here, that every call adds to.  qk_norm_eps: the layer normalises its
+        query and key heads; saved then holds q_pre and k_pre as well, weights gq and gk, and the gradients dgq and dgk."""
         self.desc = desc
         self.device = torch.device(device)
         dt = torch_dtype(desc)
@@ -308,11 +362,15 @@ class LayerBackward:
         p = (lambda *s: torch.zeros(s, dtype=torch.float32, device=self.device)) if main_grad else e
         self.grads = dict(dwq=p(H, Nq), dwk=p(H, Nkv), dwv=p(H, Nkv), dwo=p(Nq, H), dwg=p(H, F), dwu=p(H, F),
                           dwd=p(F, H), dg1=p(H), dg2=p(H), dx=e(T, H))
+        self.qk_norm_eps = qk_norm_eps
+        if qk_norm_eps is not None:
+            self.grads.update(dgq=p(desc.d), dgk=p(desc.d))
         # zeros, not empty: entries past N_k are never written, and must stay valid row numbers for a
         # caller that passes a wrong count to filtered_known
         self.idx = torch.zeros(T, dtype=torch.int32, device=self.device)
         self.cu_kept = torch.empty(desc.B + 1, dtype=torch.int32, device=self.device)
-        self.ws_bytes = lib().cf_layer_workspace_bytes(C.byref(desc), self.max_kept)
+        size = lib().cf_layer_workspace_bytes if qk_norm_eps is None else lib().cf_layer_qk_workspace_bytes
+        self.ws_bytes = size(C.byref(desc), self.max_kept)
         if self.ws_bytes == 0:
             raise CfError(2, "cf_layer_workspace_bytes")
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
@@ -327,18 +385,25 @@ class LayerBackward:
         w = Weights(*[weights[n].data_ptr() for n in _WEIGHTS])
         return sv, w
 
+    def _call(self, name: str, saved: dict, weights: dict, *args):
+        """cf_<name>, or cf_<name>_qk for a layer with query/key norm, with the arguments behind the weights."""
+        sv, w = self._pack(saved, weights)
+        if self.qk_norm_eps is None:
+            _check(getattr(lib(), "cf_" + name)(C.byref(self.desc), C.byref(sv), C.byref(w), *args), "cf_" + name)
+            return
+        name = {"layer_bwd_compact_dev": "layer_bwd_compact"}.get(name, name) + "_qk"
+        qk = LayerQk(*[t.data_ptr() for t in (saved["q_pre"], saved["k_pre"], weights["gq"], weights["gk"])], self.qk_norm_eps,
+                     _addr(self.grads.get("dgq")), _addr(self.grads.get("dgk")))
+        _check(getattr(lib(), "cf_" + name)(C.byref(self.desc), C.byref(sv), C.byref(w), C.byref(qk), *args), "cf_" + name)
+
     def filtered_async(self, saved: dict, weights: dict, dy: torch.Tensor, mask: torch.Tensor) -> None:
         """Enqueues cf_layer_bwd_filtered and returns at once: nothing is read back and the stream is
         not synchronised.  Results land in self.grads (dx: first N_k rows), self.idx, self.cu_kept,
         self.n_kept_dev; the page-locked word behind n_kept() holds N_k once the stream has run."""
-        sv, w = self._pack(saved, weights)
         self._n_host[0] = -1
-        _check(lib().cf_layer_bwd_filtered(C.byref(self.desc), C.byref(sv), C.byref(w), _ptr(dy), _ptr(mask),
-                                           self.max_kept, C.byref(self._g), _ptr(self.idx), _ptr(self.cu_kept),
-                                           _ptr(self.n_kept_dev),
-                                           C.cast(self._n_host.data_ptr(), C.POINTER(C.c_int32)), _ptr(self.ws),
-                                           self.ws_bytes, _stream()),
-               "cf_layer_bwd_filtered")
+        self._call("layer_bwd_filtered", saved, weights, _ptr(dy), _ptr(mask), self.max_kept, C.byref(self._g), _ptr(self.idx),
+                   _ptr(self.cu_kept), _ptr(self.n_kept_dev), C.cast(self._n_host.data_ptr(), C.POINTER(C.c_int32)), _ptr(self.ws),
+                   self.ws_bytes, _stream())
 
     def n_kept(self) -> int:
         """N_k of the last filtered call (synchronises the current stream)."""
@@ -370,27 +435,19 @@ class LayerBackward:
                     cu_kept: torch.Tensor, n_kept_dev: torch.Tensor) -> None:
         """cf_layer_bwd_compact_dev: a layer below the index-building one, with the count still on the
         device (no host read anywhere in the stack)."""
-        sv, w = self._pack(saved, weights)
-        _check(lib().cf_layer_bwd_compact_dev(C.byref(self.desc), C.byref(sv), C.byref(w), _ptr(dy_kept), _ptr(idx),
-                                              _ptr(cu_kept), _ptr(n_kept_dev), self.max_kept, C.byref(self._g),
-                                              _ptr(self.ws), self.ws_bytes, _stream()),
-               "cf_layer_bwd_compact_dev")
+        self._call("layer_bwd_compact_dev", saved, weights, _ptr(dy_kept), _ptr(idx), _ptr(cu_kept), _ptr(n_kept_dev), self.max_kept,
+                   C.byref(self._g), _ptr(self.ws), self.ws_bytes, _stream())
 
     def compact(self, saved: dict, weights: dict, dy_kept: torch.Tensor, idx: torch.Tensor,
                 cu_kept: torch.Tensor, n_kept: int) -> None:
         """Runs cf_layer_bwd_compact for a layer below the one that built (idx, cu_kept); results
         land in self.grads (dx: first n_kept rows).  No host synchronisation."""
-        sv, w = self._pack(saved, weights)
-        _check(lib().cf_layer_bwd_compact(C.byref(self.desc), C.byref(sv), C.byref(w), _ptr(dy_kept), _ptr(idx),
-                                          _ptr(cu_kept), n_kept, C.byref(self._g), _ptr(self.ws),
-                                          self.ws_bytes, _stream()),
-               "cf_layer_bwd_compact")
+        count = (n_kept,) if self.qk_norm_eps is None else (None, n_kept)
+        self._call("layer_bwd_compact", saved, weights, _ptr(dy_kept), _ptr(idx), _ptr(cu_kept), *count, C.byref(self._g), _ptr(self.ws),
+                   self.ws_bytes, _stream())
 
     def dense(self, saved: dict, weights: dict, dy: torch.Tensor) -> None:
-        sv, w = self._pack(saved, weights)
-        _check(lib().cf_layer_bwd_dense(C.byref(self.desc), C.byref(sv), C.byref(w), _ptr(dy),
-                                        C.byref(self._g), _ptr(self.ws), self.ws_bytes, _stream()),
-               "cf_layer_bwd_dense")
+        self._call("layer_bwd_dense", saved, weights, _ptr(dy), C.byref(self._g), _ptr(self.ws), self.ws_bytes, _stream())
 
 
 def layer_bwd_filtered(desc, saved, weights, dy, mask):
@@ -410,8 +467,9 @@ def layer_bwd_dense(desc, saved, weights, dy):
 class LoraBackward(LayerBackward):
     """Pre-allocated adapter gradients + workspace for cf_layer_bwd_lora (base weights frozen)."""
 
-    def __init__(self, desc: LayerDesc, rank: int, device="cuda:0"):
+    def __init__(self, desc: LayerDesc, rank: int, device="cuda:0", qk_norm_eps: float | None = None):
         self.desc = desc
+        self.qk_norm_eps = qk_norm_eps
         self.device = torch.device(device)
         self.rank = rank
         dt = torch_dtype(desc)
@@ -424,7 +482,8 @@ class LoraBackward(LayerBackward):
         # caller that passes a wrong count to filtered_known
         self.idx = torch.zeros(T, dtype=torch.int32, device=self.device)
         self.cu_kept = torch.empty(desc.B + 1, dtype=torch.int32, device=self.device)
-        self.ws_bytes = lib().cf_lora_workspace_bytes(C.byref(desc), rank, T)
+        size = lib().cf_lora_workspace_bytes if qk_norm_eps is None else lib().cf_lora_qk_workspace_bytes
+        self.ws_bytes = size(C.byref(desc), rank, T)
         if self.ws_bytes == 0:
             raise CfError(2, "cf_lora_workspace_bytes")
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
@@ -436,18 +495,226 @@ class LoraBackward(LayerBackward):
     def run_async(self, saved: dict, weights: dict, lora: dict, dy: torch.Tensor, mask: torch.Tensor | None) -> None:
         """mask None: every token kept (the dense LoRA backward).  Nothing synchronises: the kept count is
         in self.n_kept_dev, and n_kept() reads the page-locked copy after waiting for the stream."""
-        sv, w = self._pack(saved, weights)
         lo = Lora(*([lora[n].data_ptr() for n in _LORA_T] + [self.rank, float(lora["scale"])]))
         self._n_host[0] = -1
-        _check(lib().cf_layer_bwd_lora(C.byref(self.desc), C.byref(sv), C.byref(w), C.byref(lo), _ptr(dy),
-                                       _ptr(mask), self.max_kept, C.byref(self._g), _ptr(self.idx),
-                                       _ptr(self.cu_kept), _ptr(self.n_kept_dev),
-                                       C.cast(self._n_host.data_ptr(), C.POINTER(C.c_int32)), _ptr(self.ws),
-                                       self.ws_bytes, _stream()),
-               "cf_layer_bwd_lora")
+        self._call("layer_bwd_lora", saved, weights, C.byref(lo), _ptr(dy), _ptr(mask), self.max_kept, C.byref(self._g), _ptr(self.idx),
+                   _ptr(self.cu_kept), _ptr(self.n_kept_dev), C.cast(self._n_host.data_ptr(), C.POINTER(C.c_int32)), _ptr(self.ws),
+                   self.ws_bytes, _stream())
 
     def run(self, saved: dict, weights: dict, lora: dict, dy: torch.Tensor, mask: torch.Tensor | None) -> int:
         """run_async, then waits for the stream and returns N_k."""
         self.run_async(saved, weights, lora, dy, mask)
         torch.cuda.current_stream().synchronize()
         return int(self._n_host[0])
+
+
+# --------------------------------------------------------------------------
+# around the layer calls: query/key norm with rotation, losses, AdamW
+# --------------------------------------------------------------------------
+
+def _need(ok, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _on(device, **tensors):
+    """Every tensor given lies on `device`, which has to be the current one: the library launches on its current stream."""
+    _need(device.type == "cuda" and device.index == torch.cuda.current_device(), "tensors have to be on the current GPU, not on %s" % device)
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
+
+
+def _qk_rows(desc: LayerDesc, q, k, what: str, dtype):
+    """A cf_qk of q [n, Hq*d] and k [n, Hkv*d]: dense columns, any stride from row to row."""
+    for t, h in ((q, desc.Hq), (k, desc.Hkv)):
+        if not (t.dim() == 2 and t.shape[1] == h * desc.d and t.dtype == dtype and (t.stride(1) == 1 or t.numel() == 0)):
+            raise ValueError("%s: expected %s [rows, %d] with dense columns, got %s %s, strides %s" %
+                             (what, dtype, h * desc.d, t.dtype, tuple(t.shape), t.stride()))
+    n = q.shape[0]
+    _need(k.shape[0] == n, "%s: q has %d rows, k %d" % (what, n, k.shape[0]))
+    # the stride of a single row means nothing
+    return Qk(_ptr(q), _ptr(k), q.stride(0) if n > 1 else 0, k.stride(0) if n > 1 else 0)
+
+
+def _qk_norm(desc: LayerDesc, gq, gk, rope_cos, rope_sin, positions, rows: int, dtype):
+    for g in (gq, gk):
+        _need(g.dtype == dtype and g.shape == (desc.d,) and g.is_contiguous(), "gains have to be %s [%d]" % (dtype, desc.d))
+    _need((rope_cos is None) == (rope_sin is None), "rope_cos and rope_sin: both or neither")
+    for t in (rope_cos, rope_sin):
+        _need(t is None or (t.dtype == torch.float32 and t.shape == (desc.S, desc.d // 2) and t.is_contiguous()),
+              "rotary tables have to be fp32 [%d, %d], contiguous" % (desc.S, desc.d // 2))
+    _need(positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() >= rows),
+          "positions have to be int32, contiguous, one per row")
+    return QkNorm(gq.data_ptr(), gk.data_ptr(), _addr(rope_cos), _addr(rope_sin), None if positions is None else _ptr(positions))
+
+
+def qk_norm_rope_fwd(desc: LayerDesc, q, k, gq, gk, rope_cos=None, rope_sin=None, positions=None, out=None):
+    """Norm of every query and key head and its rotation at positions[row] (row mod S without positions).  q [n, Hq*d] and k [n, Hkv*d] may be columns
+    of a longer row (a fused projection).  out: a pair to write to, q and k themselves for a pass in place."""
+    dt = torch_dtype(desc)
+    rows = _qk_rows(desc, q, k, "q, k", dt)
+    n = q.shape[0]
+    p = _qk_norm(desc, gq, gk, rope_cos, rope_sin, positions, n, dt)
+    dev = q.device
+    if out is None:
+        out = (torch.empty((n, desc.Hq * desc.d), dtype=dt, device=dev), torch.empty((n, desc.Hkv * desc.d), dtype=dt, device=dev))
+    to = _qk_rows(desc, out[0], out[1], "out", dt)
+    _need(out[0].shape[0] == n, "out has %d rows, not %d" % (out[0].shape[0], n))
+    _on(dev, k=k, gq=gq, gk=gk, rope_cos=rope_cos, rope_sin=rope_sin, positions=positions, out_q=out[0], out_k=out[1])
+    _check((_lib or lib()).cf_qk_norm_rope_fwd(C.byref(desc), C.byref(p), C.byref(rows), n, C.byref(to), _stream()), "cf_qk_norm_rope_fwd")
+    return out
+
+
+def _kept_count(idx, n_kept_dev, rows: int, kept: int):
+    _need(idx is None or (idx.dtype == torch.int32 and idx.is_contiguous() and idx.numel() >= kept), "idx has to be int32, one per kept row")
+    _need(idx is not None or kept <= rows, "without idx there are at most %d rows" % rows)
+    _need(n_kept_dev is None or (n_kept_dev.dtype == torch.int32 and n_kept_dev.numel() == 1), "n_kept_dev has to be one int32")
+
+
+def qk_norm_rope_bwd(desc: LayerDesc, q, k, gq, gk, dq, dk, rope_cos=None, rope_sin=None, positions=None, idx=None, n_kept_dev=None,
+                     need_gains: bool = True, main_grads=None, out=None):
+    """Backward of qk_norm_rope_fwd for compact dq [n, Hq*d], dk [n, Hkv*d]; q and k are its inputs at full length.  Returns (dx of q, dx of k, dgq, dgk).
+    n_kept_dev: only the first min(*n_kept_dev, n) rows.  main_grads: fp32 (dgq, dgk) that are added to.  out: as in the forward pass."""
+    dt = torch_dtype(desc)
+    x, dy = _qk_rows(desc, q, k, "q, k", dt), _qk_rows(desc, dq, dk, "dq, dk", dt)
+    n, dev = dq.shape[0], dq.device
+    _kept_count(idx, n_kept_dev, q.shape[0], n)
+    p = _qk_norm(desc, gq, gk, rope_cos, rope_sin, positions, q.shape[0], dt)
+    if out is None:
+        out = (torch.empty((n, desc.Hq * desc.d), dtype=dt, device=dev), torch.empty((n, desc.Hkv * desc.d), dtype=dt, device=dev))
+    dx = _qk_rows(desc, out[0], out[1], "out", dt)
+    _need(out[0].shape[0] == n, "out has %d rows, not %d" % (out[0].shape[0], n))
+    dg, wsb, ws = (None, None), 0, None
+    if main_grads is not None or need_gains:
+        dg = main_grads if main_grads is not None else tuple(torch.empty(desc.d, dtype=dt, device=dev) for _ in range(2))
+        for t in dg:
+            _need(t.dtype == (dt if main_grads is None else torch.float32) and t.shape == (desc.d,) and t.is_contiguous(),
+                  "main_grads have to be fp32 [%d]" % desc.d)
+        wsb = lib().cf_qk_norm_workspace_bytes(C.byref(desc), n)
+        ws = torch.empty(wsb, dtype=torch.uint8, device=dev)
+    _on(dev, q=q, k=k, dk=dk, gq=gq, gk=gk, rope_cos=rope_cos, rope_sin=rope_sin, positions=positions, idx=idx, n_kept_dev=n_kept_dev,
+        out_q=out[0], out_k=out[1], dgq=dg[0], dgk=dg[1])
+    _check((_lib or lib()).cf_qk_norm_rope_bwd(C.byref(desc), C.byref(p), C.byref(x), C.byref(dy), None if idx is None else _ptr(idx),
+                                               _addr(n_kept_dev), n, C.byref(dx), _addr(dg[0]), _addr(dg[1]), int(main_grads is not None),
+                                               _addr(ws), wsb, _stream()), "cf_qk_norm_rope_bwd")
+    return out[0], out[1], dg[0], dg[1]
+
+
+def token_loss(logits, targets, old_logp=None, advantages=None, ref_logp=None, weights=None, clip=(0.2, 0.2), kl_coef: float = 0.0,
+               logit_scale: float = 1.0, norm: float = 0.0, idx=None, n_kept_dev=None, max_kept: int | None = None, need_grad: bool = True, out=None):
+    """Loss of the kept rows of logits [rows, V] (dense columns, any stride) and its gradient: the mean NLL of targets [rows] int64, or with advantages
+    the clipped policy loss.  Per-row tensors are fp32 [rows] and read, like logits, at idx[j] (row j without idx).  Returns (stats [4]: loss, its first term, KL, clipped share;
+    logp [max_kept]; dlogits [max_kept, V] or None).  max_kept: by default all of idx, or all rows.  out: dlogits to write to,
+    logits itself for a gradient in place (without idx)."""
+    _need(logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] == 1), "logits have to be [rows, V] with dense columns")
+    rows, V = logits.shape
+    dev = logits.device
+    n = max_kept if max_kept is not None else rows if idx is None else idx.numel()
+    _kept_count(idx, n_kept_dev, rows, n)
+    _need(targets.dtype == torch.int64 and targets.shape == (rows,) and targets.is_contiguous(), "targets have to be int64 [%d]" % rows)
+    policy = advantages is not None
+    _need(policy or (old_logp is None and ref_logp is None), "old_logp and ref_logp belong to a loss with advantages")
+    per_row = dict(old_logp=old_logp, advantages=advantages, ref_logp=ref_logp, weights=weights)
+    for name, t in per_row.items():
+        if t is not None and not (t.dtype == torch.float32 and t.shape == (rows,) and t.is_contiguous()):
+            raise ValueError("%s has to be fp32 [%d]" % (name, rows))
+    code = _dtype_code(logits)
+    if out is None:
+        out = torch.empty((n, V), dtype=logits.dtype, device=dev) if need_grad else None
+    else:
+        _need(out.dim() == 2 and out.dtype == logits.dtype and out.shape[0] >= n and out.shape[1] == V and (out.stride(1) == 1 or V == 1),
+              "out has to be %s [%d, %d] with dense columns" % (logits.dtype, n, V))
+        _need(out.shape[0] < 2 or out.stride(0) >= V, "rows of out must not overlap")
+    _on(dev, targets=targets, idx=idx, n_kept_dev=n_kept_dev, out=out, **per_row)
+    logp = torch.empty(n, dtype=torch.float32, device=dev)
+    stats = torch.empty(4, dtype=torch.float32, device=dev)
+    L = _lib or lib()
+    wsb = L.cf_token_loss_workspace_bytes(n)
+    ws = torch.empty(wsb, dtype=torch.uint8, device=dev)
+    d = LossDesc(CF_LOSS_POLICY if policy else CF_LOSS_NLL, V, code, logit_scale, clip[0], clip[1], kl_coef, norm)
+    stride = lambda t: t.stride(0) if t.shape[0] > 1 else 0
+    _check(L.cf_token_loss(C.byref(d), _ptr(logits), stride(logits), _ptr(targets), _addr(old_logp), _addr(ref_logp), _addr(advantages),
+                           _addr(weights), None if idx is None else _ptr(idx), _addr(n_kept_dev), n, None if out is None else _ptr(out),
+                           0 if out is None else stride(out), _ptr(logp), stats.data_ptr(), ws.data_ptr(), wsb, _stream()), "cf_token_loss")
+    return stats, logp, out
+
+
+STATE_BLOCK = 256       # elements that share a scale of an 8-bit state
+
+
+def adamw_state_values(q: torch.Tensor, scale: torch.Tensor):
+    """The fp32 values that an 8-bit state stands for (of v: its square root)."""
+    n = q.numel()
+    return (q.reshape(-1).float() * scale.repeat_interleave(STATE_BLOCK)[:n]).view(q.shape)
+
+
+class AdamW:
+    """AdamW over a list of parameters and the list of their gradients (LayerBackward.grads, main gradients or not; contiguous, one dtype each).  The plan
+    keeps the tensors' addresses: gradients are new values in the same buffers.  One call at a time: its norm and workspace are its own."""
+
+    def __init__(self, params, grads, lr: float, betas=(0.9, 0.95), eps: float = 1e-8, weight_decay=0.0, max_norm: float | None = None,
+                 grad_scale: float = 1.0, state_bits: int = 32, master=None, state=None, seed: int = 0, step_dev=None, lr_dev=None):
+        """weight_decay: a number, or one per parameter.  max_norm: clip by the global norm, which step() leaves in grad_norm; a norm that is not
+        finite leaves everything unchanged.  master: None, True (made here from bf16 parameters) or a list of fp32 copies.  state: lists (m, v) in
+        fp32 or (m, v, m_scale, v_scale) in 8 bits; None: zeros of state_bits.  step_dev, lr_dev: int32 / fp32 tensors that replace step() 's own
+        count and lr, for steps captured into a graph."""
+        self.params, self.grads_list = list(params), list(grads)
+        n = len(self.params)
+        _need(n > 0 and n == len(self.grads_list), "one gradient per parameter, and at least one")
+        self.device = dev = self.params[0].device
+        p_dt, g_dt = self.params[0].dtype, self.grads_list[0].dtype
+        size = [p.numel() for p in self.params]
+        self.master = [p.float() for p in self.params] if master is True else list(master) if master else None
+        if state is None:
+            _need(state_bits in (8, 32), "state_bits has to be 8 or 32")
+            z = lambda: [torch.zeros(p.shape, dtype=torch.float32 if state_bits == 32 else torch.float8_e4m3fn, device=dev) for p in self.params]
+            sc = lambda: [torch.zeros(-(-k // STATE_BLOCK), dtype=torch.float32, device=dev) for k in size]
+            state = (z(), z()) if state_bits == 32 else (z(), z(), sc(), sc())
+        self.m, self.v = list(state[0]), list(state[1])
+        self.m_scale, self.v_scale = (list(state[2]), list(state[3])) if len(state) == 4 else (None, None)
+        bits = 32 if self.m_scale is None else 8
+        wd = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else [float(x) for x in weight_decay]
+        _need(len(wd) == n, "one weight_decay per parameter")
+
+        def check(ts, what, dtype, numel=lambda i: size[i]):
+            _need(len(ts) == n, "%s: one tensor per parameter" % what)
+            for i, t in enumerate(ts):
+                _need(t.dtype == dtype and t.numel() == numel(i) and t.is_contiguous() and t.device == dev,
+                      "%s[%d] has to be %s, contiguous, of %d elements on %s" % (what, i, dtype, numel(i), dev))
+        check(self.params, "params", p_dt)
+        check(self.grads_list, "grads", g_dt)
+        if self.master is not None:
+            check(self.master, "master", torch.float32)
+        for ts, what in ((self.m, "m"), (self.v, "v")):
+            check(ts, what, torch.float32 if bits == 32 else torch.float8_e4m3fn)
+        if bits == 8:
+            for ts, what in ((self.m_scale, "m_scale"), (self.v_scale, "v_scale")):
+                check(ts, what, torch.float32, lambda i: -(-size[i] // STATE_BLOCK))
+        for t, dt in ((step_dev, torch.int32), (lr_dev, torch.float32)):
+            _need(t is None or (t.dtype == dt and t.numel() == 1 and t.device == dev), "step_dev: one int32, lr_dev: one fp32, on %s" % dev)
+        self.step_dev, self.lr_dev = step_dev, lr_dev
+        at = lambda ts, i: ts[i].data_ptr() if ts is not None else None
+        self._t = (AdamwTensor * n)(*[AdamwTensor(at(self.params, i), at(self.master, i), at(self.grads_list, i), at(self.m, i), at(self.v, i),
+                                                  at(self.m_scale, i), at(self.v_scale, i), size[i], wd[i]) for i in range(n)])
+        self.grad_norm, self.t = None, 0
+        if max_norm is not None:
+            self.grad_norm = torch.zeros(1, dtype=torch.float32, device=dev)
+            self._g = (C.c_void_p * n)(*[g.data_ptr() for g in self.grads_list])
+            self._n = (C.c_int64 * n)(*size)
+            self._ws = torch.empty(lib().cf_grad_norm_workspace_bytes(n), dtype=torch.uint8, device=dev)
+        self._d = AdamwDesc(lr, betas[0], betas[1], eps, 0, _dtype_code(self.params[0]), _dtype_code(self.grads_list[0]), bits, seed & 0xFFFFFFFF,
+                            grad_scale, 0.0 if max_norm is None else max_norm, _addr(self.grad_norm), _addr(step_dev), _addr(lr_dev))
+
+    def step(self, lr: float | None = None, step: int | None = None) -> None:
+        """One update.  step: its number, 1 for the first; by default one more than the last call's."""
+        _on(self.device)
+        L, st, d = _lib or lib(), _stream(), self._d
+        d.step = self.t + 1 if step is None else step
+        if lr is not None:
+            d.lr = lr
+        if self.grad_norm is not None:
+            _check(L.cf_grad_norm(self._g, self._n, len(self._t), d.g_dtype, d.grad_scale, d.norm_dev, self._ws.data_ptr(), self._ws.numel(), st),
+                   "cf_grad_norm")
+        _check(L.cf_adamw_step(C.byref(d), self._t, len(self._t), st), "cf_adamw_step")
+        self.t = d.step

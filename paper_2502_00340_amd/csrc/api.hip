@@ -127,6 +127,7 @@ struct LayerWs {
     void *dy_k, *bufF0, *bufF1, *bufF2, *bufHa, *bufHb, *dr, *a_k, *da, *q_k, *dq, *dk, *dv;
     void* attn_ws;
     float *dg_partial1, *dg_partial2;       // of the two norms
+    float* qk_partial = nullptr;            // of the gains of the query/key norm, behind everything else
     float* slots;                           // fp32 parts of a product (NtParts), from its launch to its reader's; null in fp32
     size_t total;
 };
@@ -198,6 +199,15 @@ cf_status attn_dispatch(const cf_layer_desc& L, const void* q_kept, const void* 
     return CF_OK;
 }
 
+// dq and dk, which leave the attention backward rotated back, through the norm of the heads, in place
+hipError_t qk_norm_back(const cf_layer_desc& L, const cf_layer_qk& qk, const LayerWs& w, const int32_t* idx, RowCount rows, bool acc_f32,
+                        hipStream_t st) {
+    cf_layer_desc D = L;
+    D.rms_eps = qk.eps;
+    const cf_qk in{const_cast<void*>(qk.q_pre), const_cast<void*>(qk.k_pre), 0, 0}, dy{w.dq, w.dk, 0, 0};
+    return launch_qk_norm_bwd(D, cf_qk_norm{qk.gq, qk.gk, nullptr, nullptr, nullptr}, in, dy, idx, rows, dy, qk.dgq, qk.dgk, acc_f32, w.qk_partial, st);
+}
+
 // Everything after the keep index is launched.  rows: the live rows (a host count, or a device count
 // with its upper bound); idx == nullptr means the dense backward (row j is token j).
 // dy: the upstream gradient, compact [rows,H] when dy_is_full == false; when dy_is_full it is the
@@ -206,7 +216,7 @@ cf_status attn_dispatch(const cf_layer_desc& L, const void* q_kept, const void* 
 // over the kept tokens).
 cf_status layer_core(const cf_layer_desc& L, const cf_saved& sv, const cf_weights& W,
                      const void* dy, bool dy_is_full, const int32_t* idx,
-                     const int32_t* cu_kept, RowCount rows, cf_grads& G, const LayerWs& w, hipStream_t st) {
+                     const int32_t* cu_kept, RowCount rows, cf_grads& G, const LayerWs& w, const cf_layer_qk* qk, hipStream_t st) {
     const int dt = L.dtype;
     const size_t e = dtype_size(dt);
     const int N = rows.n;
@@ -221,6 +231,8 @@ cf_status layer_core(const cf_layer_desc& L, const cf_saved& sv, const cf_weight
         size_t sz[9] = {(size_t)H * Nq, (size_t)H * Nkv, (size_t)H * Nkv, (size_t)Nq * H,
                         (size_t)H * F, (size_t)H * F, (size_t)F * H, (size_t)H, (size_t)H};
         for (int i = 0; i < 9; ++i) CF_HIP(launch_fill_zero(outs[i], sz[i] * e, st));
+        if (qk && qk->dgq)
+            for (void* p : {qk->dgq, qk->dgk}) CF_HIP(launch_fill_zero(p, L.d * e, st));
         return CF_OK;
     }
     if (dy_is_full && !idx) return CF_ERR_NULL;
@@ -239,8 +251,9 @@ cf_status layer_core(const cf_layer_desc& L, const cf_saved& sv, const cf_weight
         const struct { const void* p; size_t bytes; } outs[] = {
             {G.dx, n * H * e}, {G.dg1, H * ps}, {G.dg2, H * ps}, {G.dwq, (size_t)H * Nq * ps}, {G.dwk, (size_t)H * Nkv * ps},
             {G.dwv, (size_t)H * Nkv * ps}, {G.dwo, (size_t)Nq * H * ps}, {G.dwg, (size_t)H * F * ps}, {G.dwu, (size_t)H * F * ps},
-            {G.dwd, (size_t)F * H * ps}};
+            {G.dwd, (size_t)F * H * ps}, {qk ? qk->dgq : nullptr, L.d * ps}, {qk ? qk->dgk : nullptr, L.d * ps}};
         for (const auto& o : outs) {
+            if (!o.p) continue;
             own_dy = own_dy || overlap(o.p, o.bytes, dy, n * H * e);
             late_dwo = late_dwo && (idx || !overlap(o.p, o.bytes, a_rows, n * Nq * e));
         }
@@ -297,6 +310,7 @@ cf_status layer_core(const cf_layer_desc& L, const cf_saved& sv, const cf_weight
                                  w.dk, w.dv, w.attn_ws, st, idx ? sv.attn_out : nullptr, idx ? sv.q : nullptr, sv.rope_cos,
                                  sv.rope_sin, parts);
     if (as != CF_OK) return as;
+    if (qk) CF_HIP(qk_norm_back(L, *qk, w, idx, rows, mg, st));
     dw(a_rows, w.dr, G.dwo, Nq, H);                  // dWo = a^T * dr      [Nq,H]
     if (!late_dwo) CF_HIP(dw_launch(&dws[--n_dw], 1));
 
@@ -344,7 +358,7 @@ LoraWs carve_lora(const cf_layer_desc& L, int rank, int max_kept, void* ws) {
 cf_status layer_core_lora(const cf_layer_desc& L, const cf_saved& sv, const cf_weights& W,
                           const cf_lora& A, const void* dy, bool dy_is_full, const int32_t* idx,
                           const int32_t* cu_kept, RowCount rows, cf_lora_grads& G, const LoraWs& lw,
-                          hipStream_t st) {
+                          const cf_layer_qk* qk, hipStream_t st) {
     const LayerWs& w = lw.base;
     const int dt = L.dtype;
     const size_t e = dtype_size(dt);
@@ -397,6 +411,7 @@ cf_status layer_core_lora(const cf_layer_desc& L, const cf_saved& sv, const cf_w
                                  w.dk, w.dv, w.attn_ws, st, idx ? sv.attn_out : nullptr, idx ? sv.q : nullptr, sv.rope_cos,
                                  sv.rope_sin, parts);
     if (as != CF_OK) return as;
+    if (qk) CF_HIP(qk_norm_back(L, *qk, w, idx, rows, false, st));
     // ---- adapted Q, K, V projections: input h1 [N,H]
     CF_HIP(group({{w.dq, A.bq, lw.tq, N, R, Nq, 0, A.scale},
                   {w.dk, A.bk, lw.tk, N, R, Nkv, 0, A.scale},
@@ -455,6 +470,43 @@ cf_status check_rope(const cf_layer_desc* L, const cf_saved* sv) {
     return (L->d % 2 == 0 && (L->d / 2) % vn == 0) ? CF_OK : CF_ERR_SHAPE;
 }
 
+// what the query/key norm asks of a head: a power of two that a wave's lanes share out in 16-byte pieces of both halves
+cf_status check_qk_heads(const cf_layer_desc* L) {
+    if (!L) return CF_ERR_NULL;
+    const cf_status s = check_dtype(L->dtype);
+    if (s != CF_OK) return s;
+    if (L->S <= 0 || L->Hq <= 0 || L->Hkv <= 0 || L->d <= 0 || (int64_t)(L->Hq + (int64_t)L->Hkv) * L->d > 1 << 24) return CF_ERR_SHAPE;
+    if (!(L->rms_eps >= 0.f) || L->rms_eps > 3e38f) return CF_ERR_SHAPE;
+    if (L->dtype == CF_BF16 && L->d % 8 == 0 && (!pow2(L->d) || L->d < 16 || L->d > 256)) return CF_ERR_UNSUPPORTED;
+    return pow2(L->d) && L->d >= (L->dtype == CF_BF16 ? 16 : 8) && L->d <= 256 ? CF_OK : CF_ERR_SHAPE;
+}
+
+cf_status check_qk_norm(const cf_qk_norm* p) {
+    if (!p || !p->gq || !p->gk || (p->rope_cos == nullptr) != (p->rope_sin == nullptr)) return CF_ERR_NULL;
+    for (const void* q : {p->gq, p->gk, (const void*)p->rope_cos, (const void*)p->rope_sin})
+        if (misaligned(q)) return CF_ERR_SHAPE;
+    return misaligned(p->positions, 4) ? CF_ERR_SHAPE : CF_OK;
+}
+
+cf_status check_qk_rows(const cf_layer_desc& L, const cf_qk* r) {
+    if (!r || !r->q || !r->k) return CF_ERR_NULL;
+    const int vn = L.dtype == CF_BF16 ? 8 : 4;
+    if (misaligned(r->q) || misaligned(r->k) || r->q_stride % vn || r->k_stride % vn) return CF_ERR_SHAPE;
+    if ((r->q_stride && r->q_stride < (int64_t)L.Hq * L.d) || (r->k_stride && r->k_stride < (int64_t)L.Hkv * L.d)) return CF_ERR_SHAPE;
+    return CF_OK;
+}
+
+cf_status check_layer_qk(const cf_layer_desc* L, const cf_layer_qk* qk, bool lora) {
+    if (!qk || !qk->q_pre || !qk->k_pre || !qk->gq || !qk->gk || (qk->dgq == nullptr) != (qk->dgk == nullptr)) return CF_ERR_NULL;
+    cf_layer_desc D = *L;
+    D.rms_eps = qk->eps;
+    const cf_status s = check_qk_heads(&D);
+    if (s != CF_OK) return s;
+    for (const void* p : {qk->q_pre, qk->k_pre, qk->gq, qk->gk, (const void*)qk->dgq, (const void*)qk->dgk})
+        if (misaligned(p)) return CF_ERR_SHAPE;
+    return lora && qk->dgq ? CF_ERR_SHAPE : CF_OK;
+}
+
 // Both products of a linear on 128x128 tiles fit one round of the CUs.
 bool linear_in_one_round(int n, int in, int out) {
     return (int64_t)ceil_div(in, 128) * (ceil_div(n, 128) + ceil_div(out, 128)) <= compute_units();
@@ -479,6 +531,145 @@ bool linear_in_parts(int n, int in, int out) {
     // the grouped launch's reduction takes longer: 32 steps 17 and 22 us, 48 steps 22 and 21, 64 steps in two parts 30 and 33, in more 26
     // and 21
     return pairs - std::max<int64_t>(per, w_steps) >= (one_round ? GROUP_GAIN : 28);
+}
+
+// The gains' partials of the query/key norm lie behind a call's other scratch, `used` bytes of it; false: the workspace is too small.
+bool take_qk_partial(const cf_layer_desc& L, const cf_layer_qk* qk, int max_kept, size_t used, void* ws, size_t ws_bytes, float*& partial) {
+    if (qk) partial = reinterpret_cast<float*>(static_cast<unsigned char*>(ws) + used);
+    return ws_bytes >= used + (qk ? qk_norm_partial_bytes(L.d, max_kept) : 0);
+}
+
+cf_status layer_bwd_filtered(const cf_layer_desc* desc, const cf_saved* saved, const cf_weights* w, const cf_layer_qk* qk,
+                                const void* dy_full, const uint8_t* mask, int32_t max_kept, cf_grads* grads,
+                                int32_t* idx_out, int32_t* cu_kept_out, int32_t* n_kept_dev_out,
+                                int32_t* n_kept_host, void* ws, size_t ws_bytes, cf_stream stream) {
+    cf_status s = check_layer_desc(desc);
+    if (s != CF_OK) return s;
+    s = check_layer_ptrs(saved, w, dy_full, grads);
+    if (s != CF_OK) return s;
+    s = check_rope(desc, saved);
+    if (s != CF_OK) return s;
+    if (qk && (s = check_layer_qk(desc, qk, false)) != CF_OK) return s;
+    if (!mask) return CF_ERR_NULL;
+    if ((idx_out && misaligned(idx_out, 4)) || (cu_kept_out && misaligned(cu_kept_out, 4)) ||
+        (n_kept_dev_out && misaligned(n_kept_dev_out, 4)))
+        return CF_ERR_SHAPE;
+    const int T = desc->B * desc->S;
+    if (max_kept < 0) return CF_ERR_SHAPE;
+    if (max_kept == 0 || max_kept > T) max_kept = T;
+    if (!ws || misaligned(ws, 256)) return CF_ERR_WORKSPACE;
+    LayerWs wk = carve_layer(*desc, max_kept, ws);
+    if (!take_qk_partial(*desc, qk, max_kept, wk.total, ws, ws_bytes, wk.qk_partial)) return CF_ERR_WORKSPACE;
+    hipStream_t st = as_stream(stream);
+    int32_t* idx = idx_out ? idx_out : wk.idx;
+    int32_t* cu = cu_kept_out ? cu_kept_out : wk.cu_kept;
+    int32_t* n_dev = n_kept_dev_out ? n_kept_dev_out : wk.n_kept_dev;
+    CF_HIP(launch_keep_index(mask, desc->B, desc->S, idx, cu, n_dev, wk.index_ws, st));
+    // the count stays on the device: every later kernel reads it there, nothing waits for the host
+    s = layer_core(*desc, *saved, *w, dy_full, true, idx, cu, RowCount{max_kept, n_dev}, *grads, wk, qk, st);
+    if (s != CF_OK) return s;
+    // The host's copy of the count is queued behind the layer's kernels: the caller can read it only
+    // after synchronising with the stream anyway, and ahead of them the copy would sit in their way.
+    if (n_kept_host)
+        CF_HIP(hipMemcpyAsync(n_kept_host, n_dev, sizeof(int32_t), hipMemcpyDeviceToHost, st));
+    return CF_OK;
+}
+
+cf_status layer_bwd_compact_dev(const cf_layer_desc* desc, const cf_saved* saved, const cf_weights* w, const cf_layer_qk* qk,
+                                   const void* dy_kept, const int32_t* idx, const int32_t* cu_kept,
+                                   const int32_t* n_kept_dev, int32_t max_kept, cf_grads* grads, void* ws,
+                                   size_t ws_bytes, cf_stream stream) {
+    cf_status s = check_layer_desc(desc);
+    if (s != CF_OK) return s;
+    s = check_layer_ptrs(saved, w, dy_kept, grads);
+    if (s != CF_OK) return s;
+    s = check_rope(desc, saved);
+    if (s != CF_OK) return s;
+    if (qk && (s = check_layer_qk(desc, qk, false)) != CF_OK) return s;
+    if (!idx || !cu_kept || (!n_kept_dev && !qk)) return CF_ERR_NULL;      // with qk a count that the host knows, too
+    if (misaligned(idx, 4) || misaligned(cu_kept, 4) || misaligned(n_kept_dev, 4)) return CF_ERR_SHAPE;
+    const int T = desc->B * desc->S;
+    if (max_kept < 0 || (!n_kept_dev && max_kept > T)) return CF_ERR_SHAPE;
+    if (n_kept_dev && (max_kept == 0 || max_kept > T)) max_kept = T;
+    if (!ws || misaligned(ws, 256)) return CF_ERR_WORKSPACE;
+    LayerWs wk = carve_layer(*desc, max_kept, ws);
+    if (!take_qk_partial(*desc, qk, max_kept, wk.total, ws, ws_bytes, wk.qk_partial)) return CF_ERR_WORKSPACE;
+    return layer_core(*desc, *saved, *w, dy_kept, false, idx, cu_kept, RowCount{max_kept, n_kept_dev}, *grads,
+                      wk, qk, as_stream(stream));
+}
+
+cf_status layer_bwd_dense(const cf_layer_desc* desc, const cf_saved* saved, const cf_weights* w, const cf_layer_qk* qk,
+                             const void* dy_full, cf_grads* grads, void* ws, size_t ws_bytes,
+                             cf_stream stream) {
+    cf_status s = check_layer_desc(desc);
+    if (s != CF_OK) return s;
+    s = check_layer_ptrs(saved, w, dy_full, grads);
+    if (s != CF_OK) return s;
+    s = check_rope(desc, saved);
+    if (s != CF_OK) return s;
+    if (qk && (s = check_layer_qk(desc, qk, false)) != CF_OK) return s;
+    const int T = desc->B * desc->S;
+    if (!ws || misaligned(ws, 256)) return CF_ERR_WORKSPACE;
+    LayerWs wk = carve_layer(*desc, T, ws);
+    if (!take_qk_partial(*desc, qk, T, wk.total, ws, ws_bytes, wk.qk_partial)) return CF_ERR_WORKSPACE;
+    return layer_core(*desc, *saved, *w, dy_full, false, nullptr, nullptr, RowCount{T, nullptr}, *grads, wk, qk,
+                      as_stream(stream));
+}
+
+cf_status layer_bwd_lora(const cf_layer_desc* desc, const cf_saved* saved, const cf_weights* w, const cf_layer_qk* qk,
+                            const cf_lora* lora, const void* dy_full, const uint8_t* mask, int32_t max_kept,
+                            cf_lora_grads* grads, int32_t* idx_out, int32_t* cu_kept_out,
+                            int32_t* n_kept_dev_out, int32_t* n_kept_host, void* ws, size_t ws_bytes,
+                            cf_stream stream) {
+    cf_status s = check_layer_desc(desc);
+    if (s != CF_OK) return s;
+    if (!saved || !w || !lora || !dy_full || !grads) return CF_ERR_NULL;
+    {
+        const void* req[] = {saved->x, saved->q, saved->k, saved->v, saved->attn_out, saved->lse, saved->r,
+                             saved->gate, saved->up, w->wq, w->wk, w->wv, w->wo, w->wg, w->wu, w->wd, w->g1,
+                             w->g2, lora->aq, lora->bq, lora->ak, lora->bk, lora->av, lora->bv, lora->ao,
+                             lora->bo, grads->daq, grads->dbq, grads->dak, grads->dbk, grads->dav,
+                             grads->dbv, grads->dao, grads->dbo, grads->dx, dy_full};
+        for (const void* p : req)
+            if (!p) return CF_ERR_NULL;
+        for (const void* p : req)
+            if (misaligned(p)) return CF_ERR_SHAPE;
+    }
+    if ((saved->rope_cos == nullptr) != (saved->rope_sin == nullptr)) return CF_ERR_NULL;
+    s = check_rope(desc, saved);
+    if (s != CF_OK) return s;
+    if (qk && (s = check_layer_qk(desc, qk, true)) != CF_OK) return s;
+    const int mult = desc->dtype == CF_BF16 ? 8 : 4;
+    if (lora->rank <= 0 || lora->rank % mult || lora->rank > 1024) return CF_ERR_SHAPE;
+    if (!(lora->scale == lora->scale)) return CF_ERR_SHAPE;
+    if ((idx_out && misaligned(idx_out, 4)) || (cu_kept_out && misaligned(cu_kept_out, 4)) ||
+        (n_kept_dev_out && misaligned(n_kept_dev_out, 4)))
+        return CF_ERR_SHAPE;
+    if (!ws || misaligned(ws, 256)) return CF_ERR_WORKSPACE;
+    const int T = desc->B * desc->S;
+    if (max_kept < 0) return CF_ERR_SHAPE;
+    if (max_kept == 0 || max_kept > T) max_kept = T;
+    hipStream_t st = as_stream(stream);
+    if (!mask) {
+        LoraWs lw = carve_lora(*desc, lora->rank, T, ws);
+        if (!take_qk_partial(*desc, qk, T, lw.total, ws, ws_bytes, lw.base.qk_partial)) return CF_ERR_WORKSPACE;
+        if (n_kept_host) *n_kept_host = T;
+        return layer_core_lora(*desc, *saved, *w, *lora, dy_full, false, nullptr, nullptr, RowCount{T, nullptr}, *grads,
+                               lw, qk, st);
+    }
+    LoraWs lw = carve_lora(*desc, lora->rank, max_kept, ws);
+    if (!take_qk_partial(*desc, qk, max_kept, lw.total, ws, ws_bytes, lw.base.qk_partial)) return CF_ERR_WORKSPACE;
+    int32_t* idx = idx_out ? idx_out : lw.base.idx;
+    int32_t* cu = cu_kept_out ? cu_kept_out : lw.base.cu_kept;
+    int32_t* n_dev = n_kept_dev_out ? n_kept_dev_out : lw.base.n_kept_dev;
+    CF_HIP(launch_keep_index(mask, desc->B, desc->S, idx, cu, n_dev, lw.base.index_ws, st));
+    // the count stays on the device, as in cf_layer_bwd_filtered: nothing here waits for the host
+    const RowCount rows{max_kept, n_dev};
+    s = layer_core_lora(*desc, *saved, *w, *lora, dy_full, true, idx, cu, rows, *grads, lw, qk, st);
+    if (s != CF_OK) return s;
+    if (n_kept_host)
+        CF_HIP(hipMemcpyAsync(n_kept_host, n_dev, sizeof(int32_t), hipMemcpyDeviceToHost, st));
+    return CF_OK;
 }
 
 }  // namespace
@@ -644,35 +835,17 @@ cf_status cf_layer_bwd_filtered(const cf_layer_desc* desc, const cf_saved* saved
                                 const void* dy_full, const uint8_t* mask, int32_t max_kept, cf_grads* grads,
                                 int32_t* idx_out, int32_t* cu_kept_out, int32_t* n_kept_dev_out,
                                 int32_t* n_kept_host, void* ws, size_t ws_bytes, cf_stream stream) {
-    cf_status s = check_layer_desc(desc);
-    if (s != CF_OK) return s;
-    s = check_layer_ptrs(saved, w, dy_full, grads);
-    if (s != CF_OK) return s;
-    s = check_rope(desc, saved);
-    if (s != CF_OK) return s;
-    if (!mask) return CF_ERR_NULL;
-    if ((idx_out && misaligned(idx_out, 4)) || (cu_kept_out && misaligned(cu_kept_out, 4)) ||
-        (n_kept_dev_out && misaligned(n_kept_dev_out, 4)))
-        return CF_ERR_SHAPE;
-    const int T = desc->B * desc->S;
-    if (max_kept < 0) return CF_ERR_SHAPE;
-    if (max_kept == 0 || max_kept > T) max_kept = T;
-    if (!ws || misaligned(ws, 256)) return CF_ERR_WORKSPACE;
-    LayerWs wk = carve_layer(*desc, max_kept, ws);
-    if (ws_bytes < wk.total) return CF_ERR_WORKSPACE;
-    hipStream_t st = as_stream(stream);
-    int32_t* idx = idx_out ? idx_out : wk.idx;
-    int32_t* cu = cu_kept_out ? cu_kept_out : wk.cu_kept;
-    int32_t* n_dev = n_kept_dev_out ? n_kept_dev_out : wk.n_kept_dev;
-    CF_HIP(launch_keep_index(mask, desc->B, desc->S, idx, cu, n_dev, wk.index_ws, st));
-    // the count stays on the device: every later kernel reads it there, nothing waits for the host
-    s = layer_core(*desc, *saved, *w, dy_full, true, idx, cu, RowCount{max_kept, n_dev}, *grads, wk, st);
-    if (s != CF_OK) return s;
-    // The host's copy of the count is queued behind the layer's kernels: the caller can read it only
-    // after synchronising with the stream anyway, and ahead of them the copy would sit in their way.
-    if (n_kept_host)
-        CF_HIP(hipMemcpyAsync(n_kept_host, n_dev, sizeof(int32_t), hipMemcpyDeviceToHost, st));
-    return CF_OK;
+    return layer_bwd_filtered(desc, saved, w, nullptr, dy_full, mask, max_kept, grads, idx_out, cu_kept_out, n_kept_dev_out, n_kept_host, ws,
+                              ws_bytes, stream);
+}
+
+cf_status cf_layer_bwd_filtered_qk(const cf_layer_desc* desc, const cf_saved* saved, const cf_weights* w, const cf_layer_qk* qk,
+                                   const void* dy_full, const uint8_t* mask, int32_t max_kept, cf_grads* grads,
+                                   int32_t* idx_out, int32_t* cu_kept_out, int32_t* n_kept_dev_out, int32_t* n_kept_host,
+                                   void* ws, size_t ws_bytes, cf_stream stream) {
+    if (!qk) return CF_ERR_NULL;
+    return layer_bwd_filtered(desc, saved, w, qk, dy_full, mask, max_kept, grads, idx_out, cu_kept_out, n_kept_dev_out, n_kept_host, ws,
+                              ws_bytes, stream);
 }
 
 cf_status cf_layer_bwd_compact(const cf_layer_desc* desc, const cf_saved* saved, const cf_weights* w,
@@ -692,7 +865,7 @@ cf_status cf_layer_bwd_compact(const cf_layer_desc* desc, const cf_saved* saved,
     if (!ws || misaligned(ws, 256)) return CF_ERR_WORKSPACE;
     LayerWs wk = carve_layer(*desc, n_kept, ws);
     if (ws_bytes < wk.total) return CF_ERR_WORKSPACE;
-    return layer_core(*desc, *saved, *w, dy_kept, false, idx, cu_kept, RowCount{n_kept, nullptr}, *grads, wk,
+    return layer_core(*desc, *saved, *w, dy_kept, false, idx, cu_kept, RowCount{n_kept, nullptr}, *grads, wk, nullptr,
                       as_stream(stream));
 }
 
@@ -700,39 +873,26 @@ cf_status cf_layer_bwd_compact_dev(const cf_layer_desc* desc, const cf_saved* sa
                                    const void* dy_kept, const int32_t* idx, const int32_t* cu_kept,
                                    const int32_t* n_kept_dev, int32_t max_kept, cf_grads* grads, void* ws,
                                    size_t ws_bytes, cf_stream stream) {
-    cf_status s = check_layer_desc(desc);
-    if (s != CF_OK) return s;
-    s = check_layer_ptrs(saved, w, dy_kept, grads);
-    if (s != CF_OK) return s;
-    s = check_rope(desc, saved);
-    if (s != CF_OK) return s;
-    if (!idx || !cu_kept || !n_kept_dev) return CF_ERR_NULL;
-    if (misaligned(idx, 4) || misaligned(cu_kept, 4) || misaligned(n_kept_dev, 4)) return CF_ERR_SHAPE;
-    const int T = desc->B * desc->S;
-    if (max_kept < 0) return CF_ERR_SHAPE;
-    if (max_kept == 0 || max_kept > T) max_kept = T;
-    if (!ws || misaligned(ws, 256)) return CF_ERR_WORKSPACE;
-    LayerWs wk = carve_layer(*desc, max_kept, ws);
-    if (ws_bytes < wk.total) return CF_ERR_WORKSPACE;
-    return layer_core(*desc, *saved, *w, dy_kept, false, idx, cu_kept, RowCount{max_kept, n_kept_dev}, *grads,
-                      wk, as_stream(stream));
+    return layer_bwd_compact_dev(desc, saved, w, nullptr, dy_kept, idx, cu_kept, n_kept_dev, max_kept, grads, ws, ws_bytes, stream);
+}
+
+cf_status cf_layer_bwd_compact_qk(const cf_layer_desc* desc, const cf_saved* saved, const cf_weights* w, const cf_layer_qk* qk,
+                                  const void* dy_kept, const int32_t* idx, const int32_t* cu_kept, const int32_t* n_kept_dev,
+                                  int32_t max_kept, cf_grads* grads, void* ws, size_t ws_bytes, cf_stream stream) {
+    if (!qk) return CF_ERR_NULL;
+    return layer_bwd_compact_dev(desc, saved, w, qk, dy_kept, idx, cu_kept, n_kept_dev, max_kept, grads, ws, ws_bytes, stream);
 }
 
 cf_status cf_layer_bwd_dense(const cf_layer_desc* desc, const cf_saved* saved, const cf_weights* w,
                              const void* dy_full, cf_grads* grads, void* ws, size_t ws_bytes,
                              cf_stream stream) {
-    cf_status s = check_layer_desc(desc);
-    if (s != CF_OK) return s;
-    s = check_layer_ptrs(saved, w, dy_full, grads);
-    if (s != CF_OK) return s;
-    s = check_rope(desc, saved);
-    if (s != CF_OK) return s;
-    const int T = desc->B * desc->S;
-    if (!ws || misaligned(ws, 256)) return CF_ERR_WORKSPACE;
-    LayerWs wk = carve_layer(*desc, T, ws);
-    if (ws_bytes < wk.total) return CF_ERR_WORKSPACE;
-    return layer_core(*desc, *saved, *w, dy_full, false, nullptr, nullptr, RowCount{T, nullptr}, *grads, wk,
-                      as_stream(stream));
+    return layer_bwd_dense(desc, saved, w, nullptr, dy_full, grads, ws, ws_bytes, stream);
+}
+
+cf_status cf_layer_bwd_dense_qk(const cf_layer_desc* desc, const cf_saved* saved, const cf_weights* w, const cf_layer_qk* qk,
+                                const void* dy_full, cf_grads* grads, void* ws, size_t ws_bytes, cf_stream stream) {
+    if (!qk) return CF_ERR_NULL;
+    return layer_bwd_dense(desc, saved, w, qk, dy_full, grads, ws, ws_bytes, stream);
 }
 
 size_t cf_lora_workspace_bytes(const cf_layer_desc* desc, int32_t rank, int32_t max_kept) {
@@ -745,53 +905,60 @@ cf_status cf_layer_bwd_lora(const cf_layer_desc* desc, const cf_saved* saved, co
                             cf_lora_grads* grads, int32_t* idx_out, int32_t* cu_kept_out,
                             int32_t* n_kept_dev_out, int32_t* n_kept_host, void* ws, size_t ws_bytes,
                             cf_stream stream) {
-    cf_status s = check_layer_desc(desc);
+    return layer_bwd_lora(desc, saved, w, nullptr, lora, dy_full, mask, max_kept, grads, idx_out, cu_kept_out, n_kept_dev_out, n_kept_host, ws,
+                          ws_bytes, stream);
+}
+
+size_t cf_layer_qk_workspace_bytes(const cf_layer_desc* desc, int32_t max_kept) {
+    const size_t n = cf_layer_workspace_bytes(desc, max_kept);
+    return n && check_qk_heads(desc) == CF_OK ? n + qk_norm_partial_bytes(desc->d, max_kept) : 0;
+}
+
+size_t cf_lora_qk_workspace_bytes(const cf_layer_desc* desc, int32_t rank, int32_t max_kept) {
+    const size_t n = cf_lora_workspace_bytes(desc, rank, max_kept);
+    return n && check_qk_heads(desc) == CF_OK ? n + qk_norm_partial_bytes(desc->d, max_kept) : 0;
+}
+
+cf_status cf_layer_bwd_lora_qk(const cf_layer_desc* desc, const cf_saved* saved, const cf_weights* w, const cf_layer_qk* qk,
+                               const cf_lora* lora, const void* dy_full, const uint8_t* mask, int32_t max_kept,
+                               cf_lora_grads* grads, int32_t* idx_out, int32_t* cu_kept_out, int32_t* n_kept_dev_out,
+                               int32_t* n_kept_host, void* ws, size_t ws_bytes, cf_stream stream) {
+    if (!qk) return CF_ERR_NULL;
+    return layer_bwd_lora(desc, saved, w, qk, lora, dy_full, mask, max_kept, grads, idx_out, cu_kept_out, n_kept_dev_out, n_kept_host, ws,
+                          ws_bytes, stream);
+}
+
+size_t cf_qk_norm_workspace_bytes(const cf_layer_desc* desc, int32_t max_kept) {
+    if (check_qk_heads(desc) != CF_OK || max_kept < 0) return 0;
+    return align_up(qk_norm_partial_bytes(desc->d, max_kept), 256);
+}
+
+cf_status cf_qk_norm_rope_fwd(const cf_layer_desc* desc, const cf_qk_norm* p, const cf_qk* in, int32_t n_rows, const cf_qk* out,
+                              cf_stream stream) {
+    cf_status s = check_qk_heads(desc);
+    if (s == CF_OK) s = check_qk_norm(p);
+    if (s == CF_OK) s = check_qk_rows(*desc, in);
+    if (s == CF_OK) s = check_qk_rows(*desc, out);
     if (s != CF_OK) return s;
-    if (!saved || !w || !lora || !dy_full || !grads) return CF_ERR_NULL;
-    {
-        const void* req[] = {saved->x, saved->q, saved->k, saved->v, saved->attn_out, saved->lse, saved->r,
-                             saved->gate, saved->up, w->wq, w->wk, w->wv, w->wo, w->wg, w->wu, w->wd, w->g1,
-                             w->g2, lora->aq, lora->bq, lora->ak, lora->bk, lora->av, lora->bv, lora->ao,
-                             lora->bo, grads->daq, grads->dbq, grads->dak, grads->dbk, grads->dav,
-                             grads->dbv, grads->dao, grads->dbo, grads->dx, dy_full};
-        for (const void* p : req)
-            if (!p) return CF_ERR_NULL;
-        for (const void* p : req)
-            if (misaligned(p)) return CF_ERR_SHAPE;
-    }
-    if ((saved->rope_cos == nullptr) != (saved->rope_sin == nullptr)) return CF_ERR_NULL;
-    s = check_rope(desc, saved);
+    if (n_rows < 0 || n_rows > 1 << 30) return CF_ERR_SHAPE;
+    CF_HIP(launch_qk_norm_fwd(*desc, *p, *in, n_rows, *out, as_stream(stream)));
+    return CF_OK;
+}
+
+cf_status cf_qk_norm_rope_bwd(const cf_layer_desc* desc, const cf_qk_norm* p, const cf_qk* in, const cf_qk* dy_kept, const int32_t* idx,
+                              const int32_t* n_kept_dev, int32_t max_kept, const cf_qk* dx_kept, void* dgq, void* dgk, int32_t main_grad,
+                              void* ws, size_t ws_bytes, cf_stream stream) {
+    cf_status s = check_qk_heads(desc);
+    if (s == CF_OK) s = check_qk_norm(p);
+    for (const cf_qk* r : {in, dy_kept, dx_kept})
+        if (s == CF_OK) s = check_qk_rows(*desc, r);
     if (s != CF_OK) return s;
-    const int mult = desc->dtype == CF_BF16 ? 8 : 4;
-    if (lora->rank <= 0 || lora->rank % mult || lora->rank > 1024) return CF_ERR_SHAPE;
-    if (!(lora->scale == lora->scale)) return CF_ERR_SHAPE;
-    if ((idx_out && misaligned(idx_out, 4)) || (cu_kept_out && misaligned(cu_kept_out, 4)) ||
-        (n_kept_dev_out && misaligned(n_kept_dev_out, 4)))
-        return CF_ERR_SHAPE;
-    if (!ws || misaligned(ws, 256)) return CF_ERR_WORKSPACE;
-    const int T = desc->B * desc->S;
-    if (max_kept < 0) return CF_ERR_SHAPE;
-    if (max_kept == 0 || max_kept > T) max_kept = T;
-    hipStream_t st = as_stream(stream);
-    if (!mask) {
-        LoraWs lw = carve_lora(*desc, lora->rank, T, ws);
-        if (ws_bytes < lw.total) return CF_ERR_WORKSPACE;
-        if (n_kept_host) *n_kept_host = T;
-        return layer_core_lora(*desc, *saved, *w, *lora, dy_full, false, nullptr, nullptr, RowCount{T, nullptr}, *grads,
-                               lw, st);
-    }
-    LoraWs lw = carve_lora(*desc, lora->rank, max_kept, ws);
-    if (ws_bytes < lw.total) return CF_ERR_WORKSPACE;
-    int32_t* idx = idx_out ? idx_out : lw.base.idx;
-    int32_t* cu = cu_kept_out ? cu_kept_out : lw.base.cu_kept;
-    int32_t* n_dev = n_kept_dev_out ? n_kept_dev_out : lw.base.n_kept_dev;
-    CF_HIP(launch_keep_index(mask, desc->B, desc->S, idx, cu, n_dev, lw.base.index_ws, st));
-    // the count stays on the device, as in cf_layer_bwd_filtered: nothing here waits for the host
-    const RowCount rows{max_kept, n_dev};
-    s = layer_core_lora(*desc, *saved, *w, *lora, dy_full, true, idx, cu, rows, *grads, lw, st);
-    if (s != CF_OK) return s;
-    if (n_kept_host)
-        CF_HIP(hipMemcpyAsync(n_kept_host, n_dev, sizeof(int32_t), hipMemcpyDeviceToHost, st));
+    if ((dgq == nullptr) != (dgk == nullptr)) return CF_ERR_NULL;
+    if (max_kept < 0 || max_kept > 1 << 30 || (main_grad != 0 && main_grad != 1)) return CF_ERR_SHAPE;
+    if (misaligned(idx, 4) || misaligned(n_kept_dev, 4) || misaligned(dgq, 4) || misaligned(dgk, 4)) return CF_ERR_SHAPE;
+    if (dgq && (!ws || misaligned(ws, 256) || ws_bytes < qk_norm_partial_bytes(desc->d, max_kept))) return CF_ERR_WORKSPACE;
+    CF_HIP(launch_qk_norm_bwd(*desc, *p, *in, *dy_kept, idx, RowCount{max_kept, n_kept_dev}, *dx_kept, dgq, dgk, main_grad != 0,
+                              static_cast<float*>(ws), as_stream(stream)));
     return CF_OK;
 }
 

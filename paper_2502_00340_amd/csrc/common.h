@@ -254,6 +254,14 @@ hipError_t launch_attn_rowdot(int dtype, const void* da, const void* a, RowCount
                               float* D, hipStream_t st, const int32_t* a_idx = nullptr, void* a_out = nullptr,
                               const void* q_src = nullptr, void* q_out = nullptr);
 hipError_t launch_fill_zero(void* p, size_t bytes, hipStream_t st);
+
+// qk_norm.hip: the entry points' norm and rotation of query and key heads; strides of 0 are dense rows.  dgq, dgk null: frozen gains;
+// else partial holds qk_norm_partial_bytes(d, rows.n).  acc_f32: they are fp32 and added to.
+hipError_t launch_qk_norm_fwd(const cf_layer_desc& L, const cf_qk_norm& p, const cf_qk& in, int n_rows, const cf_qk& out, hipStream_t st);
+size_t qk_norm_partial_bytes(int d, int n_rows);
+hipError_t launch_qk_norm_bwd(const cf_layer_desc& L, const cf_qk_norm& p, const cf_qk& in, const cf_qk& dy, const int32_t* idx,
+                              RowCount rows, const cf_qk& dx, void* dgq, void* dgk, bool acc_f32, float* partial, hipStream_t st);
+
 // CUs of the current device (cached per device ordinal; 256 if the query fails)
 inline int compute_units() {
     static std::atomic<int> cache[64];

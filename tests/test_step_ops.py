@@ -1,0 +1,1059 @@
+"""What stands around the layer calls in a training step: query/key norm with rotation (alone and in the layer calls), the token
+losses with their gradient, AdamW.  Each against a plain implementation in 64 bits, whose own gradients are pinned by differences.
+
+Tolerances count roundings: a stored value is off by half a step of its type (EPS: half of finfo.eps, relative), an fp32 sum of n
+terms by (its depth) * 2^-24 of the sum of their absolute values, a function of the hardware or the library by a few 2^-24."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import layer_oracle as O
+from paper_2502_00340_amd import binding as Bn
+from paper_2502_00340_amd import workloads as WL
+from tests import harness as Hn
+
+DEV = "cuda:0"
+F64, F32, BF = torch.float64, torch.float32, torch.bfloat16
+U = 2.0 ** -24
+EPS = {BF: 2.0 ** -8, F32: U}
+FAKE = 0x10000          # never dereferenced: the calls it goes into fail validation first
+gpu = pytest.mark.gpu
+
+
+def say(*a):
+    print("[case]", *a, flush=True)
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def randn(g, *shape, std=1.0, mean=0.0, dtype=F32, device=DEV):
+    return (torch.randn(shape, generator=g, dtype=F32) * std + mean).to(dtype).to(device)
+
+
+def close(got, ref, tol, what=""):
+    """Every element within its own bound; NaN and infinities where the reference has them."""
+    got, ref = got.to(F64).cpu(), ref.to(F64).cpu()
+    tol = torch.as_tensor(tol, dtype=F64).cpu().expand(ref.shape)
+    assert got.shape == ref.shape, (what, got.shape, ref.shape)
+    fine = ref.isfinite()
+    assert torch.equal(got.isnan(), ref.isnan()) and torch.equal(got[~fine & ~ref.isnan()], ref[~fine & ~ref.isnan()]), what
+    over = ((got - ref).abs() - tol)[fine]
+    assert over.numel() == 0 or float(over.max()) <= 0.0, "%s: %g over the bound, worst difference %g" % (
+        what, float(over.max()), float((got - ref).abs()[fine].max()))
+
+
+# ---- plain forms in 64 bits --------------------------------------------------------------------------------
+
+def qk_ref(x, g, d, eps, cos=None, sin=None, pos=None):
+    """Norm of every head of x [n, heads*d] and its rotation."""
+    y = x.to(F64).reshape(x.shape[0], x.shape[1] // d, d)
+    y = y / (y.square().mean(-1, keepdim=True) + eps).sqrt() * g.to(F64)
+    if cos is not None:
+        c, s = cos.to(F64)[pos][:, None], sin.to(F64)[pos][:, None]
+        lo, hi = y[..., :d // 2], y[..., d // 2:]
+        y = torch.cat((lo * c - hi * s, hi * c + lo * s), -1)
+    return y.reshape(x.shape)
+
+
+def qk_ref_bwd(x, g, dy, d, eps, cos=None, sin=None, pos=None):
+    """dx, dg, and what bounds dx's and dg's rounding: the absolute values of the terms they are sums of."""
+    y = x.to(F64).reshape(x.shape[0], x.shape[1] // d, d)
+    u = dy.to(F64).reshape(y.shape)
+    mag = u.abs()
+    if cos is not None:
+        c, s = cos.to(F64)[pos][:, None], sin.to(F64)[pos][:, None]
+        lo, hi = u[..., :d // 2], u[..., d // 2:]
+        mag = torch.cat((lo.abs() * c.abs() + hi.abs() * s.abs(), hi.abs() * c.abs() + lo.abs() * s.abs()), -1)
+        u = torch.cat((lo * c + hi * s, hi * c - lo * s), -1)
+    rstd = 1.0 / (y.square().mean(-1, keepdim=True) + eps).sqrt()
+    n, a = y * rstd, u * g.to(F64)
+    dx = rstd * (a - n * (a * n).mean(-1, keepdim=True))
+    ga = mag * g.to(F64).abs()
+    bound = rstd * (ga + n.abs() * (ga * n.abs()).mean(-1, keepdim=True))
+    return dx.reshape(x.shape), (u * n).sum((0, 1)), bound.reshape(x.shape), (mag * n.abs()).sum((0, 1))
+
+
+def loss_ref(l, y, policy=None, w=None, scale=1.0, norm=0.0):
+    """(stats, logp, dlogits, row coefficients) of live rows l [n, V]; policy: (old, adv, ref or None, lo, hi, kl_coef)."""
+    l, n, V = l.to(F64), l.shape[0], l.shape[1]
+    live = (y >= 0) & (y < V)
+    w = torch.ones(n, dtype=F64, device=l.device) if w is None else w.to(F64)
+    live &= w != 0
+    at = y.clamp(0, V - 1)[:, None]
+    p = torch.softmax(l * scale, 1)
+    lp = torch.log_softmax(l * scale, 1).gather(1, at).squeeze(1)
+    if policy is None:
+        first, k, cut, slope = -lp, torch.zeros_like(lp), torch.zeros_like(lp), -torch.ones_like(lp)
+        kl = 0.0
+    else:
+        old, adv, ref, lo, hi, kl = policy
+        r, A = (lp - old.to(F64)).exp(), adv.to(F64)
+        rc = r.clamp(1.0 - lo, 1.0 + hi)
+        cut = (r * A > rc * A).to(F64)
+        first = -torch.minimum(r * A, rc * A)
+        q = torch.zeros_like(lp) if ref is None else ref.to(F64) - lp
+        k = q.exp() - q - 1.0
+        slope = torch.where(cut > 0, 0.0, -r * A) + kl * (1.0 - q.exp())
+    by = norm if norm else float(n)
+    zero = torch.zeros((), dtype=F64, device=l.device)
+    keep = lambda t: torch.where(live, t, zero)
+    stats = torch.stack([keep(w * t).sum() / by for t in (first + kl * k, first, k, cut)])
+    coef = keep(w / by * slope * scale)
+    hot = torch.zeros_like(p).scatter_(1, at, 1.0)
+    return stats, keep(lp), torch.where((coef != 0)[:, None], coef[:, None] * (hot - p), zero), coef
+
+
+def adam_ref(p, g, m, v, step, lr, b1, b2, eps, wd, clip=1.0):
+    g = g * clip
+    m, v = b1 * m + (1 - b1) * g, b2 * v + (1 - b2) * g * g
+    upd = lr * (m / (1 - b1 ** step)) / (torch.sqrt(v / (1 - b2 ** step)) + eps)
+    return p - lr * wd * p - upd, m, v, upd
+
+
+# ---- the plain forms' gradients against differences (CPU) ---------------------------------------------------
+
+def test_qk_reference_gradients_against_differences():
+    g0, d, n = gen(1), 8, 5
+    x, g, dy = (randn(g0, *s, dtype=F64, device="cpu") for s in ((n, 3 * d), (d,), (n, 3 * d)))
+    a = torch.rand((7, d // 2), generator=g0, dtype=F64) * 6
+    pos = torch.tensor([0, 6, 3, 3, 1])
+    f = lambda x_, g_: (qk_ref(x_, g_, d, 1e-3, a.cos(), a.sin(), pos) * dy).sum()
+    dx, dg, _, _ = qk_ref_bwd(x, g, dy, d, 1e-3, a.cos(), a.sin(), pos)
+    h = 1e-5
+    for t, grad in ((x, dx), (g, dg)):
+        for i in range(t.numel()):
+            e = torch.zeros(t.numel(), dtype=F64)
+            e[i] = h
+            e = e.view(t.shape)
+            diff = (f(x + e, g) - f(x - e, g)) if t is x else (f(x, g + e) - f(x, g - e))
+            assert abs(float(diff) / (2 * h) - float(grad.view(-1)[i])) < 1e-7
+
+
+@pytest.mark.parametrize("policy", [False, True])
+def test_loss_reference_gradient_against_differences(policy):
+    g0, n, V = gen(2), 9, 6
+    l = randn(g0, n, V, dtype=F64, device="cpu")
+    y = torch.randint(0, V, (n,), generator=g0)
+    y[3] = -100
+    w = torch.rand(n, generator=g0, dtype=F64)
+    w[5] = 0.0
+    lp = torch.log_softmax(0.7 * l, 1).gather(1, y.clamp(0)[:, None]).squeeze(1)
+    x = torch.tensor([0.5, -0.6, 0.1, 0.0, 0.6, 0.2, -0.05, -0.4, 0.45], dtype=F64)        # on both sides of both borders, off them
+    pol = (lp - x, randn(g0, n, dtype=F64, device="cpu"), lp + 0.3, 0.2, 0.3, 0.1) if policy else None
+    f = lambda t: float(loss_ref(t, y, pol, w, 0.7, 4.0)[0][0])
+    grad, h = loss_ref(l, y, pol, w, 0.7, 4.0)[2], 1e-6
+    assert policy is False or 0 < float(loss_ref(l, y, pol, w, 0.7, 4.0)[0][3])
+    for i in range(n):
+        for c in range(V):
+            e = torch.zeros_like(l)
+            e[i, c] = h
+            assert abs((f(l + e) - f(l - e)) / (2 * h) - float(grad[i, c])) < 1e-8
+
+
+# ---- refusals (CPU) ----------------------------------------------------------------------------------------
+
+@pytest.fixture(scope="module")
+def L():
+    if not __import__("os").path.exists(Bn.LIB_PATH):
+        from paper_2502_00340_amd import build
+        build.build_library(verbose=False)
+    return Bn.lib()
+
+
+def _desc(**kw):
+    return Bn.make_desc(**{**dict(B=2, S=64, H=256, Hq=4, Hkv=2, d=64, F=512, dtype="bf16"), **kw})
+
+
+def test_qk_norm_refusals(L):
+    ok = dict(desc=_desc(), p=Bn.QkNorm(FAKE, FAKE, None, None, None), x=Bn.Qk(FAKE, FAKE, 0, 0), y=Bn.Qk(FAKE, FAKE, 0, 0), n=4)
+
+    def fwd(**kw):
+        a = {**ok, **kw}
+        ref = lambda s: None if s is None else C.byref(s)
+        return L.cf_qk_norm_rope_fwd(ref(a["desc"]), ref(a["p"]), ref(a["x"]), a["n"], ref(a["y"]), None)
+
+    for kw, code in (
+            (dict(desc=None), 1), (dict(p=None), 1), (dict(x=None), 1), (dict(y=None), 1), (dict(n=-1), 2),
+            (dict(p=Bn.QkNorm(None, FAKE, None, None, None)), 1), (dict(p=Bn.QkNorm(FAKE, FAKE, FAKE, None, None)), 1),
+            (dict(p=Bn.QkNorm(FAKE + 8, FAKE, None, None, None)), 2), (dict(p=Bn.QkNorm(FAKE, FAKE, FAKE, FAKE + 4, None)), 2),
+            (dict(p=Bn.QkNorm(FAKE, FAKE, None, None, FAKE + 2)), 2),
+            (dict(x=Bn.Qk(None, FAKE, 0, 0)), 1), (dict(x=Bn.Qk(FAKE, FAKE + 2, 0, 0)), 2), (dict(x=Bn.Qk(FAKE, FAKE, 260, 0)), 2),
+            (dict(x=Bn.Qk(FAKE, FAKE, 248, 0)), 2), (dict(y=Bn.Qk(FAKE, FAKE, 0, 120)), 2), (dict(y=Bn.Qk(FAKE, FAKE, 0, -128)), 2),
+            (dict(desc=_desc(d=80)), 5), (dict(desc=_desc(d=512)), 5), (dict(desc=_desc(d=8)), 5), (dict(desc=_desc(d=60)), 2),
+            (dict(desc=_desc(d=4, dtype="f32")), 2), (dict(desc=_desc(d=512, dtype="f32")), 2), (dict(desc=_desc(rms_eps=-1.0)), 2),
+            (dict(desc=_desc(rms_eps=float("nan"))), 2), (dict(desc=_desc(S=0)), 2), (dict(desc=_desc(Hkv=0)), 2)):
+        assert fwd(**kw) == code, kw
+    bad = _desc()
+    bad.dtype = 7
+    assert fwd(desc=bad) == 3
+    d, p, x = ok["desc"], ok["p"], ok["x"]
+    need = L.cf_qk_norm_workspace_bytes(C.byref(d), 100)
+    assert 0 < need < L.cf_qk_norm_workspace_bytes(C.byref(d), 100000) and L.cf_qk_norm_workspace_bytes(C.byref(d), -1) == 0
+    assert L.cf_qk_norm_workspace_bytes(C.byref(_desc(d=80)), 100) == 0
+
+    def bwd(idx=FAKE, nd=None, n=100, dgq=FAKE, dgk=FAKE, main=0, ws=FAKE, wsb=need):
+        return L.cf_qk_norm_rope_bwd(C.byref(d), C.byref(p), C.byref(x), C.byref(x), idx, nd, n, C.byref(x), dgq, dgk, main, ws, wsb, None)
+
+    for kw, code in ((dict(dgk=None), 1), (dict(dgq=None), 1), (dict(n=-1), 2), (dict(main=2), 2), (dict(idx=FAKE + 1), 2), (dict(nd=FAKE + 2), 2),
+                     (dict(dgq=FAKE + 1), 2), (dict(ws=None), 4), (dict(ws=FAKE + 16), 4), (dict(wsb=need - 512), 4)):
+        assert bwd(**kw) == code, kw
+
+
+def test_layer_qk_refusals(L):
+    d = _desc()
+    sv, w = Bn.Saved(*([FAKE] * 9)), Bn.Weights(*([FAKE] * 9))
+    grads, lora, lg = Bn.Grads(*([FAKE] * 10)), Bn.Lora(*([FAKE] * 8), 8, 1.0), Bn.LoraGrads(*([FAKE] * 9))
+    need = L.cf_layer_qk_workspace_bytes(C.byref(d), 128)
+    assert need > L.cf_layer_workspace_bytes(C.byref(d), 128)
+    assert L.cf_lora_qk_workspace_bytes(C.byref(d), 8, 128) > L.cf_lora_workspace_bytes(C.byref(d), 8, 128)
+    good = [FAKE] * 4 + [1e-6, FAKE, FAKE]
+
+    def calls(qk, ws=FAKE, wsb=1 << 40):
+        q = None if qk is None else C.byref(Bn.LayerQk(*qk))
+        head = (C.byref(d), C.byref(sv), C.byref(w), q)
+        yield L.cf_layer_bwd_filtered_qk(*head, FAKE, FAKE, 0, C.byref(grads), None, None, None, None, ws, wsb, None)
+        yield L.cf_layer_bwd_compact_qk(*head, FAKE, FAKE, FAKE, FAKE, 0, C.byref(grads), ws, wsb, None)
+        yield L.cf_layer_bwd_dense_qk(*head, FAKE, C.byref(grads), ws, wsb, None)
+        if qk is None or not qk[5]:
+            yield L.cf_layer_bwd_lora_qk(*head, C.byref(lora), FAKE, FAKE, 0, C.byref(lg), None, None, None, None, ws, wsb, None)
+
+    at = lambda i, v: good[:i] + [v] + good[i + 1:]
+    for qk, code in ((None, 1), (at(0, None), 1), (at(3, None), 1), (at(5, None), 1), (at(1, FAKE + 2), 2), (at(6, FAKE + 2), 2), (at(4, -1.0), 2)):
+        assert set(calls(qk)) == {code}, (qk, code)
+    frozen = good[:5] + [None, None]
+    assert set(calls(frozen, wsb=4096)) == {4} and set(calls(good, ws=None)) == {4} and set(calls(frozen, ws=FAKE + 16)) == {4}
+    head = (C.byref(d), C.byref(sv), C.byref(w))
+    assert L.cf_layer_bwd_lora_qk(*head, C.byref(Bn.LayerQk(*good)), C.byref(lora), FAKE, FAKE, 0, C.byref(lg), None, None, None, None, FAKE, 1 << 40,
+                                  None) == 2      # the adapter call has no gain gradients
+    # a count that the host knows is not clamped
+    assert L.cf_layer_bwd_compact_qk(*head, C.byref(Bn.LayerQk(*good)), FAKE, FAKE, FAKE, None, 129, C.byref(grads), FAKE, 1 << 40, None) == 2
+    bad = _desc(d=4, dtype="f32")
+    assert L.cf_layer_qk_workspace_bytes(C.byref(bad), 16) == 0
+
+
+def test_token_loss_refusals(L):
+    def call(desc=(1, 100, 0, 0.0, 0.2, 0.2, 0.1, 0.0), logits=FAKE, ls=0, y=FAKE, old=FAKE, ref=FAKE, adv=FAKE, w=None, idx=None, nd=None, n=10,
+             dl=FAKE * 2, ds=0, lp=FAKE, st=FAKE, ws=FAKE, wsb=1 << 20):
+        return L.cf_token_loss(None if desc is None else C.byref(Bn.LossDesc(*desc)), logits, ls, y, old, ref, adv, w, idx, nd, n, dl, ds, lp, st, ws,
+                               wsb, None)
+    D = lambda **kw: tuple({**dict(kind=1, V=100, dtype=0, scale=0.0, lo=0.2, hi=0.2, kl=0.1, norm=0.0), **kw}.values())
+    nan, inf = float("nan"), float("inf")
+    for kw, code in ((dict(desc=None), 1), (dict(logits=None), 1), (dict(y=None), 1), (dict(old=None), 1), (dict(adv=None), 1),
+                     (dict(dl=None, lp=None, st=None), 1), (dict(desc=D(dtype=2)), 3), (dict(desc=D(kind=2)), 2), (dict(desc=D(V=0)), 2),
+                     (dict(desc=D(scale=-1.0)), 2), (dict(desc=D(scale=inf)), 2), (dict(desc=D(lo=-0.1)), 2), (dict(desc=D(lo=1.1)), 2),
+                     (dict(desc=D(hi=-0.1)), 2), (dict(desc=D(hi=nan)), 2), (dict(desc=D(kl=nan)), 2), (dict(desc=D(norm=nan)), 2), (dict(ref=None), 2),
+                     (dict(n=-1), 2), (dict(ls=99), 2), (dict(ds=99), 2), (dict(ls=-100), 2), (dict(logits=FAKE + 1), 2), (dict(dl=FAKE + 1), 2), (dict(y=FAKE + 4), 2),
+                     (dict(w=FAKE + 2), 2), (dict(idx=FAKE + 2), 2), (dict(nd=FAKE + 1), 2), (dict(lp=FAKE + 2), 2), (dict(st=FAKE + 2), 2),
+                     (dict(dl=FAKE, idx=FAKE), 2), (dict(dl=FAKE, ds=200), 2), (dict(ws=None), 4), (dict(ws=FAKE + 8), 4), (dict(wsb=100), 4)):
+        assert call(**kw) == code, kw
+    assert L.cf_token_loss_workspace_bytes(-1) == 0 and L.cf_token_loss_workspace_bytes(0) > 0
+
+
+def test_adamw_refusals(L):
+    base = dict(lr=1e-3, b1=0.9, b2=0.99, eps=1e-8, step=1, p=0, g=1, bits=32, seed=0, scale=1.0, max_norm=0.0, norm=None, sd=None, ld=None)
+
+    def call(t=(), n=1, **kw):
+        a = {**base, **kw}
+        ts = {**dict(p=FAKE, w=FAKE, g=FAKE, m=FAKE, v=FAKE, ms=None, vs=None, n=8, wd=0.1), **dict(t)}
+        return L.cf_adamw_step(C.byref(Bn.AdamwDesc(*a.values())), C.byref(Bn.AdamwTensor(*ts.values())), n, None)
+    nan = float("nan")
+    for kw, code in ((dict(p=3), 3), (dict(g=-1), 3), (dict(bits=16), 2), (dict(step=0), 2), (dict(lr=-1.0), 2), (dict(lr=nan), 2), (dict(b1=1.0), 2),
+                     (dict(b2=1.0), 2), (dict(b2=nan), 2), (dict(eps=0.0), 2), (dict(eps=1e-60), 2), (dict(scale=nan), 2), (dict(norm=FAKE), 2),
+                     (dict(norm=FAKE + 2, max_norm=1.0), 2), (dict(sd=FAKE + 2), 2), (dict(n=-1), 2), (dict(t=dict(n=-1)), 2), (dict(t=dict(n=1 << 36)), 2),
+                     (dict(t=dict(wd=-1.0)), 2), (dict(t=dict(wd=nan)), 2), (dict(t=dict(p=None)), 1), (dict(t=dict(m=None)), 1), (dict(bits=8), 1),
+                     (dict(t=dict(g=FAKE + 8)), 2), (dict(t=dict(w=FAKE + 4)), 2), (dict(p=1), 2), (dict(bits=8, t=dict(ms=FAKE, vs=FAKE + 2)), 2)):
+        assert call(**kw) == code, kw
+    two = (Bn.AdamwTensor * 2)(Bn.AdamwTensor(FAKE, FAKE, FAKE, FAKE, FAKE, None, None, 8, 0.0), Bn.AdamwTensor(FAKE, None, FAKE, FAKE, FAKE, None, None, 8, 0.0))
+    assert L.cf_adamw_step(C.byref(Bn.AdamwDesc(*base.values())), two, 2, None) == 2       # one with a master copy, one without
+    assert L.cf_adamw_step(None, two, 2, None) == 1 and L.cf_adamw_step(C.byref(Bn.AdamwDesc(*base.values())), None, 1, None) == 1
+    g, n = (C.c_void_p * 1)(FAKE), (C.c_int64 * 1)(8)
+
+    def norm(g=g, n=n, k=1, dt=1, scale=1.0, out=FAKE, ws=FAKE, wsb=1 << 20):
+        return L.cf_grad_norm(g, n, k, dt, scale, out, ws, wsb, None)
+    for kw, code in ((dict(g=None), 1), (dict(n=None), 1), (dict(out=None), 1), (dict(dt=2), 3), (dict(k=-1), 2), (dict(scale=nan), 2), (dict(out=FAKE + 2), 2),
+                     (dict(n=(C.c_int64 * 1)(-1)), 2), (dict(n=(C.c_int64 * 1)(1 << 36)), 2), (dict(g=(C.c_void_p * 1)(None)), 1), (dict(g=(C.c_void_p * 1)(FAKE + 4)), 2),
+                     (dict(ws=None), 4), (dict(ws=FAKE + 8), 4), (dict(wsb=64), 4)):
+        assert norm(**kw) == code, kw
+    assert L.cf_grad_norm_workspace_bytes(-1) == 0 < L.cf_grad_norm_workspace_bytes(0) <= L.cf_grad_norm_workspace_bytes(1000)
+
+
+def test_binding_refuses_what_the_library_cannot_see(L):
+    """Shapes, types and strides that a pointer does not carry, and tensors that are not on the GPU."""
+    d = _desc()
+    q, k, g, idx = torch.zeros(6, 256, dtype=BF), torch.zeros(6, 128, dtype=BF), torch.ones(64, dtype=BF), torch.zeros(6, dtype=torch.int32)
+    cos = torch.zeros(64, 32)
+    for a in ((q[:, :128], k, g, g), (q, k[:5], g, g), (q.float(), k, g, g), (q, k, g[:32], g), (q, k, g.float(), g), (q.t().contiguous().t(), k, g, g),
+              (q, k, g, g, cos), (q, k, g, g, cos[:10], cos), (q, k, g, g, None, None, idx[:3]), (q, k, g, g, None, None, idx.long()), (q, k, g, g)):
+        with pytest.raises(ValueError):
+            Bn.qk_norm_rope_fwd(d, *a)
+    for kw in (dict(idx=idx.long()), dict(idx=idx[:2]), dict(n_kept_dev=idx), dict(main_grads=(g, g)), dict(out=(q[:2], k[:2])), {}):
+        with pytest.raises(ValueError):
+            Bn.qk_norm_rope_bwd(d, q, k, g, g, q, k, **kw)
+    l, y, f = torch.zeros(6, 10), torch.zeros(6, dtype=torch.int64), torch.zeros(6)
+    for a, kw in (((l, y.int()), {}), ((l, y[:5]), {}), ((l.t(), y), {}), ((l, y), dict(old_logp=f)), ((l, y, f, f[:3]), {}), ((l, y, f, f.double()), {}),
+                  ((l, y), dict(max_kept=7)), ((l, y), dict(idx=idx[:2], max_kept=3)), ((l, y), dict(out=l[:3])), ((l, y), dict(out=l.to(BF))),
+                  ((l, y), dict(weights=f[:2])), ((l, y), {})):
+        with pytest.raises(ValueError):
+            Bn.token_loss(*a, **kw)
+    with pytest.raises(TypeError):
+        Bn.token_loss(l.half(), y)
+    p = [torch.zeros(8, 8)]
+    for a, kw in (((p, []), {}), (([], []), {}), ((p, [torch.zeros(8)]), {}), ((p, [torch.zeros(8, 8).t()[::2].repeat(2, 1).t()]), {}), ((p, p), dict(state_bits=16)),
+                  ((p, p), dict(weight_decay=[0.1, 0.2])), ((p, p), dict(state=(p, [p[0].to(BF)]))), ((p, p), dict(step_dev=torch.zeros(1))),
+                  ((p + [p[0].to(BF)], p + p), {})):
+        with pytest.raises(ValueError):
+            Bn.AdamW(*a, lr=1e-3, **kw)
+    with pytest.raises(ValueError):
+        Bn.AdamW(p, [torch.zeros(8, 8)], lr=1e-3).step()          # not on a GPU
+
+
+# ---- query/key norm and rotation ---------------------------------------------------------------------------
+
+EPS_N = 1e-6
+# sums over a head: 2*VN terms in a lane and a few steps across lanes; rsqrt, products, rotation
+QK_OPS = 48
+
+
+def _qk_case(seed, dtype, n, Hq, Hkv, d, table, strided=False):
+    g0 = gen(seed)
+    pad = (24, 40) if strided else (0, 0)
+    q, k = (randn(g0, n, h * d + p, std=1.5, dtype=dtype)[:, :h * d] for h, p in ((Hq, pad[0]), (Hkv, pad[1])))
+    gq, gk = randn(g0, d, std=0.3, mean=1.0, dtype=dtype), randn(g0, d, std=0.3, mean=1.0, dtype=dtype)
+    cos, sin = WL.rope_tables(table, d)
+    return g0, q, k, gq, gk, torch.from_numpy(cos).to(DEV), torch.from_numpy(sin).to(DEV)
+
+
+SHAPES = [(1, 32, 8, 128, 4096), (7, 32, 4, 64, 5), (513, 3, 1, 128, 200), (130, 24, 8, 128, 65), (33, 1, 1, 16, 33), (70, 5, 2, 32, 9), (64, 12, 4, 256, 100),
+          (2100, 4, 1, 128, 700), (19, 65, 1, 64, 19)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n,Hq,Hkv,d,table", SHAPES)
+def test_qk_norm_forward(dtype, n, Hq, Hkv, d, table):
+    """Rows of all head layouts, with strides, with and without positions and tables, and in place."""
+    say("qk fwd", dtype, n, Hq, Hkv, d, table)
+    g0, q, k, gq, gk, cos, sin = _qk_case(n + d, dtype, n, Hq, Hkv, d, table, strided=n % 2 == 1)
+    desc = Bn.make_desc(1, table, 256, Hq, Hkv, d, 256, dtype, rms_eps=EPS_N)
+    places = torch.randint(0, table, (n,), generator=g0).int().to(DEV)
+    for tabs, pos in (((cos, sin), None), ((cos, sin), places), ((None, None), None)):
+        at = torch.arange(n, device=DEV) % table if pos is None else pos.long()
+        oq, ok = Bn.qk_norm_rope_fwd(desc, q, k, gq, gk, *tabs, positions=pos)
+        for x, g, o in ((q, gq, oq), (k, gk, ok)):
+            ref = qk_ref(x, g, d, EPS_N, *tabs, at)
+            plain = qk_ref(x, g, d, EPS_N).reshape(n, -1, 2, d // 2).abs().amax(2, keepdim=True).expand(-1, -1, 2, -1).reshape(ref.shape)
+            close(o, ref, EPS[dtype] * ref.abs() + QK_OPS * U * 2 * plain, "forward")
+    a, b = q.clone(), k.clone()
+    Bn.qk_norm_rope_fwd(desc, a, b, gq, gk, cos, sin, positions=places, out=(a, b))
+    ref = Bn.qk_norm_rope_fwd(desc, q, k, gq, gk, cos, sin, positions=places)
+    assert torch.equal(a, ref[0]) and torch.equal(b, ref[1])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n,Hq,Hkv,d,table", SHAPES)
+@pytest.mark.parametrize("main", [False, True])
+def test_qk_norm_backward(dtype, n, Hq, Hkv, d, table, main):
+    """Kept rows through an index, fewer live rows than the bound, gains overwritten and added to; rows behind the live ones stay."""
+    say("qk bwd", dtype, n, Hq, Hkv, d, table, main)
+    g0, q, k, gq, gk, cos, sin = _qk_case(3 * n + d, dtype, n, Hq, Hkv, d, table, strided=n % 2 == 1)
+    desc = Bn.make_desc(1, table, 256, Hq, Hkv, d, 256, dtype, rms_eps=EPS_N)
+    kept = max(1, (2 * n) // 3)
+    idx = torch.randperm(n, generator=g0)[:kept].sort().values.int().to(DEV)
+    for live, rows in ((kept, idx), (kept // 2, idx), (0, idx), (n, None)):
+        m = n if rows is None else kept
+        dq, dk = randn(g0, m, Hq * d, dtype=dtype), randn(g0, m, Hkv * d, dtype=dtype)
+        nd = None if live == m else torch.tensor([live], dtype=torch.int32, device=DEV)
+        acc = tuple(randn(g0, d, std=5.0) for _ in range(2)) if main else None
+        out = (torch.full_like(dq, 7.0), torch.full_like(dk, 7.0))
+        before = None if acc is None else [t.clone() for t in acc]
+        xq, xk, dgq, dgk = Bn.qk_norm_rope_bwd(desc, q, k, gq, gk, dq, dk, cos, sin, idx=rows, n_kept_dev=nd, main_grads=acc, out=out)
+        at = torch.arange(n, device=DEV)[:live] if rows is None else rows.long()[:live]
+        for i, (x, g, dy, dx, dg, h) in enumerate(((q, gq, dq, xq, dgq, Hq), (k, gk, dk, xk, dgk, Hkv))):
+            ref, rg, bx, bg = qk_ref_bwd(x[at], g, dy[:live], d, EPS_N, cos, sin, at % table)
+            close(dx[:live], ref, EPS[dtype] * ref.abs() + QK_OPS * U * bx, "dx")
+            assert bool((dx[live:] == 7.0).all())
+            if main:
+                rg = rg + before[i].to(F64)
+                bg = bg + before[i].abs().to(F64)
+            # fp32 sums: a lane's items one after the other, then lanes, waves and blocks
+            close(dg, rg, EPS[F32 if main else dtype] * rg.abs() + 256 * U * bg, "gain")
+        again = Bn.qk_norm_rope_bwd(desc, q, k, gq, gk, dq, dk, cos, sin, idx=rows, n_kept_dev=nd, main_grads=None if acc is None else before,
+                                    out=(torch.empty_like(dq), torch.empty_like(dk)))
+        assert torch.equal(again[2], dgq) and torch.equal(again[3], dgk), "the same bits on every call"
+    a, b = dq.clone(), dk.clone()
+    got = Bn.qk_norm_rope_bwd(desc, q, k, gq, gk, a, b, cos, sin, need_gains=False, out=(a, b))
+    assert got[2] is None and torch.equal(a, xq) and torch.equal(b, xk)
+
+
+@gpu
+def test_qk_norm_positions_outside_the_tables_and_zero_rows():
+    say("qk positions")
+    g0, q, k, gq, gk, cos, sin = _qk_case(5, BF, 8, 4, 2, 64, 10)
+    desc = Bn.make_desc(1, 10, 256, 4, 2, 64, 256, BF, rms_eps=EPS_N)
+    wild = torch.tensor([0, 9, 10, -1, 2 ** 31 - 1, -2 ** 31, 5, 11], dtype=torch.int32, device=DEV)
+    tame = torch.tensor([0, 9, 9, 0, 9, 0, 5, 9], dtype=torch.int32, device=DEV)
+    for f in (lambda p: Bn.qk_norm_rope_fwd(desc, q, k, gq, gk, cos, sin, positions=p), lambda p: Bn.qk_norm_rope_bwd(desc, q, k, gq, gk, q, k, cos, sin, positions=p)):
+        for a, b in zip(f(wild), f(tame)):
+            assert torch.equal(a, b)
+    zq, zk = torch.zeros_like(q), torch.zeros_like(k)
+    assert not any(bool(t.any()) for t in Bn.qk_norm_rope_fwd(desc, zq, zk, gq, gk, cos, sin))     # a head of zeros: rstd is eps^-1/2
+    out = Bn.qk_norm_rope_fwd(desc, q[:0], k[:0], gq, gk, cos, sin)
+    assert out[0].shape == (0, 256) and out[1].shape == (0, 128)
+    got = Bn.qk_norm_rope_bwd(desc, q, k, gq, gk, q[:0], k[:0], cos, sin)
+    assert not bool(got[2].any()) and not bool(got[3].any())
+
+
+@gpu
+def test_qk_norm_gradient_against_differences():
+    """fp32 differences of the forward kernel along random directions: truncation h^2/6 * |f'''| and rounding 2^-24 * |f| * sqrt(n) / h
+    at h = 2^-6, |f| of order one an element, 3000 elements: 1e-3 of the derivative's scale."""
+    say("qk differences")
+    n, Hq, Hkv, d = 10, 3, 2, 64
+    g0, q, k, gq, gk, cos, sin = _qk_case(9, F32, n, Hq, Hkv, d, 20)
+    desc = Bn.make_desc(1, 20, 256, Hq, Hkv, d, 256, F32, rms_eps=EPS_N)
+    dq, dk = randn(g0, n, Hq * d), randn(g0, n, Hkv * d)
+    f = lambda *a: sum(float((o.double() * w.double()).sum()) for o, w in zip(Bn.qk_norm_rope_fwd(desc, *a, cos, sin), (dq, dk)))
+    grads = Bn.qk_norm_rope_bwd(desc, q, k, gq, gk, dq, dk, cos, sin)
+    h = 2.0 ** -6
+    for i, t in enumerate((q, k, gq, gk)):
+        for _ in range(3):
+            e = randn(g0, *t.shape)
+            args = [q, k, gq, gk]
+            up, down = [*args], [*args]
+            up[i], down[i] = t + h * e, t - h * e
+            got = (f(*up) - f(*down)) / (2 * h)
+            want = float((grads[i].double() * e.double()).sum())
+            scale = float(((grads[i].double() * e.double()) ** 2).sum()) ** 0.5
+            assert abs(got - want) < 0.02 * scale, (i, got, want, scale)
+
+
+def _layer_qk_problem(dtype, B=2, S=96, rope=True, seed=3, H=256, Hq=4, Hkv=2, d=64, F=512):
+    """A layer with query/key norm, everything consistent, in fp64 and quantised."""
+    rng = np.random.default_rng(seed)
+    shape = WL.LayerShape("qk", B=B, S=S, H=H, Hq=Hq, Hkv=Hkv, d=d, F=F, dtype="bf16" if dtype == BF else "f32")
+    qz = lambda a: Hn.quantize(a, shape.dtype)
+    W = {n: qz(v) for n, v in WL.make_weights(shape, rng).items()}
+    W["gq"], W["gk"] = qz(1.0 + 0.2 * rng.standard_normal(d)), qz(1.0 + 0.2 * rng.standard_normal(d))
+    tabs = WL.rope_tables(S, d) if rope else None
+    W64 = {n: v.astype(np.float64) for n, v in W.items()}
+    x = qz(rng.standard_normal((B * S, H)))
+    h1, _ = O.rmsnorm_fwd(x.astype(np.float64), W64["g1"], 1e-5)
+    sv = dict(x=x, q_pre=qz(h1 @ W64["wq"]), k_pre=qz(h1 @ W64["wk"]), v=qz(h1 @ W64["wv"]))
+    pos = torch.arange(B * S) % S
+    t = lambda a: torch.from_numpy(np.ascontiguousarray(a))
+    args = (t(tabs[0]), t(tabs[1]), pos) if rope else ()
+    for n in "qk":
+        sv[n] = qz(qk_ref(t(sv[n + "_pre"]), t(W["g" + n]), d, EPS_N, *args).numpy())
+    a, lse = O.attn_fwd(*(sv[n].astype(np.float64) for n in "qkv"), B, S, Hq, Hkv, d, 1 / math.sqrt(d))
+    sv["attn_out"], sv["lse"] = qz(a), lse.astype(np.float32)
+    sv["r"] = qz(x + sv["attn_out"].astype(np.float64) @ W64["wo"])
+    h2, _ = O.rmsnorm_fwd(sv["r"].astype(np.float64), W64["g2"], 1e-5)
+    sv["gate"], sv["up"] = qz(h2 @ W64["wg"]), qz(h2 @ W64["wu"])
+    return shape, W, sv, tabs, rng
+
+
+def _layer_qk_ref(shape, W, sv, tabs, dy, mask, lora=None):
+    """The oracle's layer backward with the norm of the heads put in between attention and projections."""
+    kw = dict(B=shape.B, S=shape.S, Hq=shape.Hq, Hkv=shape.Hkv, d=shape.d)
+    sv, W = ({n: v.astype(np.float64) for n, v in x.items()} for x in (sv, W))
+    ref = O.layer_bwd(sv, W, dy.astype(np.float64), mask, rope=tabs, lora=lora, **kw)
+    h1, _ = O.rmsnorm_fwd(sv["x"], W["g1"], 1e-5)
+    dh = {}
+    for n in "qk":
+        dx, dg, _, _ = qk_ref_bwd(torch.from_numpy(sv[n + "_pre"]), torch.from_numpy(W["g" + n]), torch.from_numpy(ref["_d" + n]), shape.d, EPS_N)
+        ref["dg" + n] = dg.numpy()
+        dh[n], ref["dw" + n], ref["da" + n], ref["db" + n] = O.lora_linear_bwd(h1, dx.numpy(), W["w" + n], lora, n)
+    dhv, _, _, _ = O.lora_linear_bwd(h1, ref["_dv"], W["wv"], lora, "v")
+    dxn, ref["dg1"] = O.rmsnorm_bwd(dh["q"] + dh["k"] + dhv, sv["x"], W["g1"], 1e-5)
+    ref["dx"] = ref["_dr"] + dxn
+    return ref
+
+
+def _layer_qk_device(shape, W, sv, tabs):
+    to = lambda a: Hn.to_dev(a, shape.dtype)
+    dsv = {n: (torch.from_numpy(v).to(DEV) if n == "lse" else to(v)) for n, v in sv.items()}
+    if tabs is not None:
+        dsv["rope_cos"], dsv["rope_sin"] = (torch.from_numpy(t).to(DEV) for t in tabs)
+    return dsv, {n: to(v) for n, v in W.items()}
+
+
+def _layer_qk_check(shape, grads, ref, rows, names):
+    tol, line = Hn.TOL[shape.dtype], Hn.TOL_LINE[shape.dtype]       # those of the layer's other parity tests
+    for n in names:
+        got, want = Hn.to_np(grads[n]), ref[n]
+        if n == "dx":
+            got, want = got[:len(rows)], want[rows]
+        assert Hn.rel_fro(got, want) <= tol and Hn.line_err(got, want) <= line, (n, Hn.rel_fro(got, want), Hn.line_err(got, want))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rope", [False, True])
+@pytest.mark.parametrize("main", [False, True])
+def test_layer_calls_with_query_key_norm(dtype, rope, main):
+    say("layer qk", dtype, rope, main)
+    shape, W, sv, tabs, rng = _layer_qk_problem(dtype, rope=rope)
+    dsv, dW = _layer_qk_device(shape, W, sv, tabs)
+    dy = Hn.quantize(rng.standard_normal((shape.T, shape.H)), shape.dtype)
+    ddy = Hn.to_dev(dy, shape.dtype)
+    names = Hn.GRADS + ("dgq", "dgk", "dx")
+    desc = Bn.make_desc(shape.B, shape.S, shape.H, shape.Hq, shape.Hkv, shape.d, shape.F, shape.dtype)
+    new = lambda: Bn.LayerBackward(desc, main_grad=main, qk_norm_eps=EPS_N)
+    mask = WL.mask_topk(rng, shape.B, shape.S, 0.6)
+    rows = np.flatnonzero(mask.reshape(-1))
+    ref = _layer_qk_ref(shape, W, sv, tabs, dy, mask)
+    plan = new()
+    n = plan.filtered(dsv, dW, ddy, torch.from_numpy(mask).to(DEV))
+    assert n == len(rows)
+    _layer_qk_check(shape, plan.grads, ref, rows, names)
+    kept = ddy[torch.from_numpy(rows).to(DEV)].contiguous()
+    for call in (lambda p: p.compact(dsv, dW, kept, plan.idx, plan.cu_kept, n),
+                 lambda p: p.compact_dev(dsv, dW, kept, plan.idx, plan.cu_kept, plan.n_kept_dev),
+                 lambda p: p.filtered_known(dsv, dW, ddy, torch.from_numpy(mask).to(DEV), n)):
+        other = new()
+        call(other)
+        torch.cuda.synchronize()
+        for k in names:
+            assert torch.equal(other.grads[k][:n] if k == "dx" else other.grads[k], plan.grads[k][:n] if k == "dx" else plan.grads[k]), k
+    dense = new()
+    dense.dense(dsv, dW, ddy)
+    _layer_qk_check(shape, dense.grads, _layer_qk_ref(shape, W, sv, tabs, dy, None), np.arange(shape.T), names)
+    none = new()
+    for g in none.grads.values():
+        g.fill_(3.0)
+    assert none.filtered(dsv, dW, ddy, torch.zeros((shape.B, shape.S), dtype=torch.uint8, device=DEV)) == 0
+    none.compact(dsv, dW, kept, plan.idx, plan.cu_kept, 0)
+    for k in names[:-1]:
+        assert bool((none.grads[k] == (3.0 if main else 0.0)).all()), k
+
+
+@gpu
+@pytest.mark.parametrize("masked", [False, True])
+def test_adapter_layer_call_with_query_key_norm(masked):
+    say("lora qk", masked)
+    shape, W, sv, tabs, rng = _layer_qk_problem(BF, seed=4)
+    rank = 8
+    H, Nq, Nkv = shape.H, shape.Nq, shape.Nkv
+    q = lambda *s: Hn.quantize(0.05 * rng.standard_normal(s), "bf16")
+    lora = dict(aq=q(H, rank), bq=q(rank, Nq), ak=q(H, rank), bk=q(rank, Nkv), av=q(H, rank), bv=q(rank, Nkv), ao=q(Nq, rank), bo=q(rank, H), scale=0.5)
+    dy = Hn.quantize(rng.standard_normal((shape.T, H)), "bf16")
+    mask = WL.mask_topk(rng, shape.B, shape.S, 0.5) if masked else None
+    rows = np.flatnonzero(mask.reshape(-1)) if masked else np.arange(shape.T)
+    ref = _layer_qk_ref(shape, W, sv, tabs, dy, mask, {k: v if k == "scale" else v.astype(np.float64) for k, v in lora.items()})
+    dsv, dW = _layer_qk_device(shape, W, sv, tabs)
+    desc = Bn.make_desc(shape.B, shape.S, H, shape.Hq, shape.Hkv, shape.d, shape.F, "bf16")
+    plan = Bn.LoraBackward(desc, rank, qk_norm_eps=EPS_N)
+    dl = {k: v if k == "scale" else Hn.to_dev(v, "bf16") for k, v in lora.items()}
+    n = plan.run(dsv, dW, dl, Hn.to_dev(dy, "bf16"), None if mask is None else torch.from_numpy(mask).to(DEV))
+    assert n == len(rows)
+    _layer_qk_check(shape, plan.grads, ref, rows, ["daq", "dbq", "dak", "dbk", "dav", "dbv", "dao", "dbo", "dx"])
+
+
+# ---- losses ------------------------------------------------------------------------------------------------
+
+def _loss_case(seed, dtype, rows, V, std=2.5):
+    g0 = gen(seed)
+    l = randn(g0, rows, V, std=std)
+    y = torch.randint(0, V, (rows,), generator=g0).to(DEV)
+    l.scatter_add_(1, y[:, None], randn(g0, rows, 1, std=3.0, mean=6.0))
+    return g0, l.to(dtype), y
+
+
+def _policy_inputs(g0, l, y, scale=1.0):
+    V = l.shape[1]
+    lp = torch.log_softmax(l.to(F64) * scale, 1).gather(1, y.clamp(0, V - 1)[:, None]).squeeze(1)
+    n = lp.numel()
+    x = torch.randn(n, generator=g0, dtype=F64).to(DEV) * 0.3
+    for b in (math.log(0.8), math.log(1.3)):        # the gradient jumps there: no ratio within a thousandth
+        x = torch.where((x - b).abs() < 1e-3, x + 4e-3, x)
+    old, ref = (lp - x).to(F32).nan_to_num(0.0, 0.0, 0.0), (lp + 0.3 * torch.randn(n, generator=g0, dtype=F64).to(DEV)).to(F32).nan_to_num(0.0, 0.0, 0.0)
+    return old, randn(g0, n), ref
+
+
+def _check_loss(got, want, l, y, dtype, scale, wsum, policy):
+    """Bounds.  The sum of V exponentials: at most V/256 + 40 additions one after the other, and each term's argument (up to 2^6 in
+    size) rounded: 2^6 + V/256 + 40 steps of 2^-24, which is logp's absolute error, next to its own rounding.  A ratio exp(lp - old) has that as relative
+    error."""
+    stats, lp, dl = got
+    rs, rlp, rd, coef = want
+    V = l.shape[1]
+    e = (64 + V / 256 + 40) * U * 2
+    fine = rlp.isfinite()
+    tol_lp = torch.where(fine, e + 4 * U * (rlp.abs() + (l.to(F64) * scale).abs().amax(1)), 0.0).nan_to_num(0.0, 0.0, 0.0)
+    close(lp, rlp, tol_lp, "logp")
+    worst = float(tol_lp.max()) if tol_lp.numel() else 0.0
+    if dl is not None:
+        rel = 8 * worst + 64 * U
+        # a row's coefficient and p are off by `rel`; where the policy's two terms cancel, by that of the larger: 4 * |w / norm| bounds them
+        tol = EPS[dtype] * rd.abs() + rel * (rd.abs() + (wsum[:, None] * (rd.abs() / coef.abs().clamp(min=1e-30)[:, None])))
+        # the target's value is coef * (1 - p), p = exp(lp): an error of lp moves it by coef * p * error, whatever is left of 1 - p
+        tol.scatter_add_(1, y.clamp(0, V - 1)[:, None], (worst * coef.abs() * rlp.exp()).nan_to_num(0.0, 0.0, 0.0)[:, None])
+        close(dl, rd, tol, "dlogits")
+    close(stats, rs, 16 * worst * float(wsum.sum()) + 4 * U * rs.abs().nan_to_num(0.0, 0.0, 0.0), "stats")
+
+
+LOSS = [(1, 1), (5, 7), (3, 8), (4, 9), (6, 64), (2, 511), (3, 512), (2, 4099), (9, 32000), (3, 50257), (2, 128256), (2, 131077), (1, 262147)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,V", LOSS)
+@pytest.mark.parametrize("policy", [False, True])
+def test_token_loss(dtype, rows, V, policy):
+    """Vocabularies around the sizes of a vector, a wave, a block and what a block keeps; rows that start on any element."""
+    say("loss", dtype, rows, V, policy)
+    g0, l, y = _loss_case(rows + V, dtype, rows, V)
+    w = (torch.rand(rows, generator=g0) + 0.5).to(DEV) if policy else None
+    scale = 0.75 if V % 2 else 1.0
+    kw = dict(weights=w, logit_scale=scale)
+    pol = None
+    if policy:
+        old, adv, ref = _policy_inputs(g0, l, y, scale)
+        kw.update(old_logp=old, advantages=adv, ref_logp=ref, clip=(0.2, 0.3), kl_coef=0.1)
+        pol = (old, adv, ref, 0.2, 0.3, 0.1)
+    want = loss_ref(l, y, pol, w, scale)
+    wsum = (torch.ones(rows, dtype=F64, device=DEV) if w is None else w.to(F64)) / rows
+    if policy:
+        wsum = wsum * (2.0 * adv.abs().to(F64) + 1.0)
+    got = Bn.token_loss(l, y, **kw)
+    _check_loss(got, want, l, y, dtype, scale, wsum, policy)
+    fwd = Bn.token_loss(l, y, need_grad=False, **kw)
+    assert fwd[2] is None and torch.equal(fwd[1], got[1]) and torch.equal(fwd[0], got[0]), "the same bits without a gradient"
+    # rows that begin on an odd element, far apart, and into rows of another stride
+    wide = torch.zeros(rows * (V + 3) + 1, dtype=dtype, device=DEV)
+    lv = wide[1:].view(rows, V + 3)[:, :V]
+    lv.copy_(l)
+    out = torch.full((rows, V + 5), 7.0, dtype=dtype, device=DEV)
+    odd = Bn.token_loss(lv, y, out=out[:, :V], **kw)
+    assert torch.equal(odd[1], got[1]) and torch.equal(out[:, :V], got[2]) and bool((out[:, V:] == 7.0).all())
+    # in place
+    Bn.token_loss(lv, y, out=lv, **kw)
+    assert torch.equal(lv, got[2]) and not bool(wide[1:].view(rows, V + 3)[:, V:].any()) and float(wide[0]) == 0.0
+
+
+@gpu
+@pytest.mark.parametrize("dtype,V", [(BF, 1003), (F32, 1003), (BF, 40960)])
+def test_token_loss_on_kept_rows(dtype, V):
+    """Through an index, with a bound above the live rows, ignored targets, weights of zero: what is left out may hold anything."""
+    say("loss kept", dtype, V)
+    rows = 37
+    g0, l, y = _loss_case(7, dtype, rows, V)
+    idx = torch.randperm(rows, generator=g0)[:21].sort().values.int().to(DEV)
+    at = idx.long()
+    w = (torch.rand(rows, generator=g0) + 0.5).to(DEV)
+    old, adv, ref = _policy_inputs(g0, l, y)
+    y[at[2]], y[at[9]], y[at[11]] = -100, V, 2 ** 40
+    w[at[4]] = 0.0
+    gone = torch.ones(rows, dtype=torch.bool, device=DEV)
+    gone[at] = False
+    for i in (2, 4, 9, 11):
+        gone[at[i]] = True
+    l[gone], old[gone], adv[gone] = float("nan"), float("inf"), float("nan")
+    ref[gone] = float("-inf")
+    w[gone & (w != 0)] = float("inf")
+    pol = (old[at], adv[at], ref[at], 0.2, 0.2, 0.05)
+    for live, norm in ((21, 0.0), (13, 5.0), (0, 0.0)):
+        nd = torch.tensor([live], dtype=torch.int32, device=DEV)
+        out = torch.full((21, V), 7.0, dtype=dtype, device=DEV)
+        stats, lp, dl = Bn.token_loss(l, y, old, adv, ref, w, (0.2, 0.2), 0.05, norm=norm, idx=idx, n_kept_dev=nd, out=out)
+        assert bool((dl[live:] == 7.0).all())
+        if live == 0:
+            assert not bool(stats.any())
+            continue
+        clean = lambda t: torch.where(gone[at], torch.zeros((), dtype=t.dtype, device=DEV), t)[:live]
+        ll, yy, ww = l[at][:live].clone(), y[at][:live], w[at][:live].clone()
+        ll[gone[at][:live]] = 0.0
+        ww[gone[at][:live]] = 0.0
+        want = loss_ref(ll, yy, (clean(pol[0]), clean(pol[1]), clean(pol[2]), 0.2, 0.2, 0.05), ww, norm=norm)
+        wsum = ww.to(F64) / (norm or live) * (2.0 * clean(pol[1]).abs().to(F64) + 1.0)
+        _check_loss((stats, lp[:live], dl[:live]), want, ll, yy, dtype, 1.0, wsum, True)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_token_loss_of_masked_and_extreme_logits(dtype):
+    """-inf and the type's lowest value as masks, rows that hold nothing else, values far apart, NaN and infinity."""
+    say("loss extremes", dtype)
+    low = torch.finfo(dtype).min
+    V = 1030
+    g0, l, y = _loss_case(11, dtype, 8, V)
+    y[:] = 5
+    l[0, 6:] = float("-inf")
+    l[1, :5], l[1, 6:] = float("-inf"), float("-inf")           # the target alone: logp 0, gradient 0
+    l[2] = low                                                  # uniform
+    l[3, 6:] = low
+    l[4, 100] = 30000.0                                         # the target has probability 0
+    l[5] = 0.0
+    l[6] = low
+    l[6, 5] = 3.0
+    l[7, 0:900] = low
+    stats, lp, dl = Bn.token_loss(l, y)
+    want = loss_ref(l, y)
+    _check_loss((stats, lp, dl), want, l.clamp(min=-100.0), y, dtype, 1.0, torch.full((8,), 1 / 8, dtype=F64, device=DEV) , False)
+    assert float(lp[1]) == 0.0 and not bool(dl[1].any()) and not bool(dl[0, 6:].any())
+    for bad in (float("nan"), float("inf")):
+        a = l.clone()
+        a[0, 17] = bad
+        _, lp, dl = Bn.token_loss(a, y)
+        assert math.isnan(float(lp[0])) and bool(dl[0].isnan().all()) and torch.equal(lp[1:], Bn.token_loss(l, y)[1][1:])
+    a = l.clone()
+    a[0] = float("-inf")                                        # no probability at all
+    assert math.isnan(float(Bn.token_loss(a, y)[1][0]))
+
+
+@gpu
+def test_token_loss_on_policy_ratio_is_one():
+    """old_logp from a call without gradient: every ratio is exactly 1, so nothing is clipped at any clip width, and the first term is -mean(A)."""
+    say("loss on policy")
+    for V, dtype in ((1003, BF), (32000, BF), (128256, BF), (50257, F32)):
+        g0, l, y = _loss_case(13, dtype, 6, V)
+        adv = torch.tensor([1.0, -2.0, 0.5, 0.0, 3.0, -1.0], device=DEV)
+        old = Bn.token_loss(l, y, need_grad=False)[1]
+        stats, lp, _ = Bn.token_loss(l, y, old, adv, old, clip=(0.0, 0.0), kl_coef=1.0)
+        assert torch.equal(lp, old) and float(stats[3]) == 0.0 and float(stats[2]) == 0.0
+        assert abs(float(stats[1]) + 0.25) < 1e-7
+
+
+@gpu
+def test_token_loss_gradient_against_differences():
+    """Differences of the kernel's own loss, summed over the rows: h = 2^-4, truncation h^2/6 of third derivatives below 0.1, rounding of an fp32 loss of
+    about 3 times 2^-24 over 2h: 1.5e-4 together."""
+    say("loss differences")
+    g0, l, y = _loss_case(17, F32, 4, 50, std=1.0)
+    old, adv, ref = _policy_inputs(g0, l, y)
+    old = torch.log_softmax(l, 1).gather(1, y[:, None]).squeeze(1) + 0.02       # inside the clip range with all steps
+    for kw in (dict(), dict(old_logp=old, advantages=adv, ref_logp=ref, clip=(0.9, 3.0), kl_coef=0.3)):
+        _, _, dl = Bn.token_loss(l, y, norm=1.0, **kw)
+        h = 2.0 ** -4
+        for i, c in ((0, 3), (1, int(y[1])), (2, 49), (3, int(y[3]))):
+            up, down = l.clone(), l.clone()
+            up[i, c] += h
+            down[i, c] -= h
+            a, b = (float(Bn.token_loss(t, y, norm=1.0, need_grad=False, **kw)[0][0]) for t in (up, down))
+            assert abs((a - b) / (2 * h) - float(dl[i, c])) < 2e-3 * max(1.0, abs(float(dl[i, c])))
+
+
+# ---- AdamW -------------------------------------------------------------------------------------------------
+
+B1, B2, AEPS, WD, LR = 0.9, 0.97, 1e-8, 0.1, 1e-2
+SIZES = [1, 3, 4, 255, 256, 257, 1023, 4096, 4097, 0, 12289]
+
+
+def _adam_case(seed, p_dtype, g_dtype, sizes, gstd=1e-2):
+    g0 = gen(seed)
+    p = [randn(g0, n, std=0.05, dtype=p_dtype) for n in sizes]
+    g = [randn(g0, n, std=gstd, dtype=g_dtype) for n in sizes]
+    m, v = [randn(g0, n, std=gstd / 3) for n in sizes], [randn(g0, n, std=gstd).square() for n in sizes]
+    return g0, p, g, m, v
+
+
+def _check_adam32(w, m, v, old, g, step, wd, clip=1.0):
+    """Counts: g*clip 3, the products and the sum of a moment 4; update: root, quotients and bias corrections 16, p and its decay 4."""
+    w0, m0, v0 = (t.to(F64) for t in old)
+    rw, rm, rv, upd = adam_ref(w0, g.to(F64), m0, v0, step, LR, B1, B2, AEPS, wd, clip)
+    gc = g.to(F64).abs() * clip
+    em = 8 * U * (B1 * m0.abs() + (1 - B1) * gc)
+    close(m, rm, em, "m")
+    close(v, rv, 10 * U * (B2 * v0 + (1 - B2) * gc ** 2), "v")
+    ew = EPS[w.dtype] * rw.abs() + 5 * U * w0.abs() + 24 * U * upd.abs()
+    ew = ew + LR * em / (1 - B1 ** step) / (torch.sqrt(rv / (1 - B2 ** step)) + AEPS)
+    close(w, rw, ew, "parameter")
+    return rw
+
+
+@gpu
+@pytest.mark.parametrize("p_dtype,master", [(F32, False), (BF, True), (BF, False)])
+@pytest.mark.parametrize("g_dtype", [BF, F32])
+def test_adamw_32_bit_states(p_dtype, master, g_dtype):
+    """Sizes around vectors, scale blocks and chunks, an empty tensor among them, over three steps; a weight decay for each."""
+    say("adamw32", p_dtype, master, g_dtype)
+    _, p, g, m, v = _adam_case(1, p_dtype, g_dtype, SIZES)
+    wd = [0.1 * (i % 3) for i in range(len(p))]
+    ms = [x.float() + 1e-4 for x in p] if master else None
+    opt = Bn.AdamW(p, g, lr=LR, betas=(B1, B2), eps=AEPS, weight_decay=wd, master=ms, state=(m, v))
+    for step in range(1, 4):
+        old = [tuple(t.clone() for t in ((ms or p)[i], m[i], v[i])) for i in range(len(p))]
+        opt.step()
+        assert opt.t == step
+        for i in range(len(p)):
+            if p[i].numel():
+                _check_adam32((ms or p)[i], m[i], v[i], old[i], g[i], step, wd[i])
+            if master:
+                assert torch.equal(p[i], ms[i].to(BF)), "the parameter is the rounded master"
+
+
+@gpu
+def test_adamw_first_step_from_zero_states_and_many_tensors():
+    """More tensors than one launch takes; from zeros a first step moves every parameter by lr (sign of its gradient)."""
+    say("adamw many")
+    sizes = [(7 * i) % 300 + 1 for i in range(95)]
+    for bits in (32, 8):
+        _, p, g, _, _ = _adam_case(2, F32, F32, sizes)
+        old = [x.clone() for x in p]
+        opt = Bn.AdamW(p, g, lr=LR, eps=1e-12, state_bits=bits)
+        opt.step()
+        for x, o, d in zip(p, old, g):
+            close(x, o.to(F64) - LR * d.to(F64).sign(), 64 * U * LR + 2 * U * o.abs().to(F64) + 1e-12 / d.abs().to(F64) * LR, "first step")
+
+
+@gpu
+@pytest.mark.parametrize("g_dtype", [BF, F32])
+def test_global_norm_and_clipping(g_dtype):
+    say("norm", g_dtype)
+    sizes = [1, 5, 4096, 8192, 8193, 0, 100003] + [17] * 200
+    _, p, g, m, v = _adam_case(3, F32, g_dtype, sizes, gstd=0.5)
+    want = math.sqrt(sum(float(x.double().square().sum()) for x in g))
+    for max_norm, scale in ((0.5 * want, 1.0), (4.0 * want, 1.0), (0.3 * want, 0.25)):
+        _, p, _, m, v = _adam_case(3, F32, g_dtype, sizes, gstd=0.5)
+        opt = Bn.AdamW(p, g, lr=LR, betas=(B1, B2), eps=AEPS, weight_decay=WD, max_norm=max_norm, grad_scale=scale, state=(m, v))
+        old = [tuple(t.clone() for t in (p[i], m[i], v[i])) for i in range(len(p))]
+        opt.step(step=7)
+        assert abs(float(opt.grad_norm) - want * scale) <= 2 * U * want * scale
+        clip = scale * min(1.0, max_norm / (want * scale + 1e-6))
+        for i in (0, 1, 2, 4, 6, 50, 206):
+            _check_adam32(p[i], m[i], v[i], old[i], g[i], 7, WD, clip)
+    # squares beyond fp32
+    big = [torch.full((5000,), 1e30, device=DEV)]
+    q, m1, v1 = torch.zeros(5000, device=DEV), torch.zeros(5000, device=DEV), torch.zeros(5000, device=DEV)
+    opt = Bn.AdamW([q], big, lr=LR, max_norm=1.0, state=([m1], [v1]))
+    opt.step()
+    assert abs(float(opt.grad_norm) / (1e30 * math.sqrt(5000.0)) - 1.0) < 4 * U and bool(q.isfinite().all())
+
+
+@gpu
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_adamw_leaves_everything_at_a_norm_that_is_not_finite(bits, bad):
+    say("adamw non-finite", bits, bad)
+    _, p, g, _, _ = _adam_case(4, BF, BF, [300, 5000])
+    opt = Bn.AdamW(p, g, lr=LR, max_norm=1.0, master=True, state_bits=bits)
+    opt.step()
+    held = [t for ts in (opt.params, opt.master, opt.m, opt.v, opt.m_scale or [], opt.v_scale or []) for t in ts]
+    before = [t.clone() for t in held]
+    keep = float(g[1][4999])
+    g[1][4999] = bad
+    opt.step()
+    assert not math.isfinite(float(opt.grad_norm))
+    for a, b in zip(held, before):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    g[1][4999] = keep
+    opt.step()
+    assert not torch.equal(opt.master[0], before[2])
+
+
+def _values(opt):
+    return ([Bn.adamw_state_values(q, s).double() for q, s in zip(opt.m, opt.m_scale)], [Bn.adamw_state_values(q, s).double() for q, s in zip(opt.v, opt.v_scale)])
+
+
+@gpu
+@pytest.mark.parametrize("p_dtype,master", [(F32, False), (BF, True), (BF, False)])
+@pytest.mark.parametrize("g_dtype", [BF, F32])
+def test_adamw_8_bit_states(p_dtype, master, g_dtype):
+    """The parameters move by the formulas from the states' values; the new states are the formulas' within a rounding: m half a step of e4m3 (2^-4 of the
+    value, 2^-10 of its block's unit), the root of v a whole step upwards or downwards, and a root that is not zero stays so."""
+    say("adamw8", p_dtype, master, g_dtype)
+    _, p, g, _, _ = _adam_case(5, p_dtype, g_dtype, SIZES)
+    for i, x in enumerate(g):
+        if x.numel() > 300:
+            x[256:270] *= 1e-6          # far below their block's largest
+            x[3] = 0.0
+    opt = Bn.AdamW(p, g, lr=LR, betas=(B1, B2), eps=AEPS, weight_decay=WD, master=master or None, state_bits=8, seed=99)
+    for step in range(1, 5):
+        w0 = [t.double() for t in (opt.master or p)]
+        m0, r0 = _values(opt)
+        opt.step()
+        m1, r1 = _values(opt)
+        for i in range(len(p)):
+            n = p[i].numel()
+            if n == 0:
+                continue
+            rw, rm, rv, upd = adam_ref(w0[i], g[i].double(), m0[i], r0[i] ** 2, step, LR, B1, B2, AEPS, WD)
+            w = (opt.master or p)[i]
+            close(w, rw, EPS[w.dtype] * rw.abs() + 5 * U * w0[i].abs() + 32 * U * upd.abs() +
+                  LR * 8 * U * (B1 * m0[i].abs() + (1 - B1) * g[i].double().abs()) / (1 - B1 ** step) / (torch.sqrt(rv / (1 - B2 ** step)) + AEPS), "parameter")
+            um, uv = (s[i].double().repeat_interleave(256)[:n] for s in (opt.m_scale, opt.v_scale))
+            slack = 16 * U
+            close(m1[i], rm, (2.0 ** -4 + slack) * rm.abs() + 2.0 ** -10 * um + 8 * U * (B1 * m0[i].abs() + (1 - B1) * g[i].double().abs()), "m")
+            root = rv.sqrt()
+            # a step is 2^-3 of a value's power of two, and 2^-9 units below the normal values; to the smallest value from anything above zero
+            close(r1[i], root, (2.0 ** -3 + slack) * root + 2.0 ** -9 * uv, "root of v")
+            assert torch.equal(r1[i] == 0, root == 0)
+            assert bool((opt.m[i].float().abs() <= 448).all()) and bool((opt.v[i].float() <= 448).all())
+            blocks = lambda t: torch.nn.functional.pad(t, (0, -n % 256)).view(-1, 256).abs().amax(1)
+            close(opt.m_scale[i], blocks(rm) / 448, 16 * U * blocks(rm) / 448 + 2.0 ** -120, "scale of m")
+            close(opt.v_scale[i], blocks(root).clamp(min=2.0 ** -100) / 448, 16 * U * blocks(root) / 448 + 2.0 ** -120, "scale of v")
+
+
+@gpu
+def test_adamw_8_bit_rounding_is_unbiased_and_reproducible():
+    """What is cut off is made up for on average: over n elements that each are off by less than a step s (uniform, variance below s^2/4) the mean is
+    within 6 * s / (2 * sqrt(n)).  The same seed and step give the same bits, others do not."""
+    say("adamw8 unbiased")
+    n = 1 << 18
+    g0 = gen(6)
+    g = [randn(g0, n, std=1e-2)]
+
+    def run(seed, step):
+        opt = Bn.AdamW([torch.zeros(n, device=DEV)], g, lr=LR, betas=(B1, B2), state_bits=8, seed=seed)
+        opt.step(step=step)
+        return opt
+    a, b, c, e = run(1, 1), run(1, 1), run(2, 1), run(1, 2)
+    bits = lambda o: o.v[0].view(torch.uint8)
+    assert torch.equal(bits(a), bits(b)) and not torch.equal(bits(a), bits(c)) and not torch.equal(bits(a), bits(e))
+    root = (g[0].double().square() * (1 - B2)).sqrt()
+    unit = a.v_scale[0].double().repeat_interleave(256)
+    y = root / unit
+    step = torch.exp2(torch.floor(torch.log2(y.clamp(min=2.0 ** -6))) - 3.0)
+    off = (Bn.adamw_state_values(a.v[0], a.v_scale[0]).double() / unit - y) / step
+    off = off[y > 2.0 ** -9]
+    assert float(off.abs().max()) <= 1.0 + 1e-4
+    assert abs(float(off.mean())) < 6 * 0.5 / math.sqrt(off.numel())
+    # 0.1 % a step is less than half a step of 8 bits: to nearest the average would stand still
+    opt = Bn.AdamW([torch.zeros(n, device=DEV)], g, lr=0.0, betas=(B1, 0.999), state_bits=8)
+    for _ in range(50):
+        opt.step()
+    v = Bn.adamw_state_values(opt.v[0], opt.v_scale[0]).double().square().sum()
+    want = float(g[0].double().square().sum()) * (1 - 0.999 ** 50)
+    assert abs(float(v) / want - 1.0) < 0.05        # roots of fresh roundings are squared: a bias of up to s^2/4 = 0.4 % of v a step, of what moves
+
+
+@gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_step_and_rate_on_the_device_in_a_graph(bits):
+    """A captured step replayed with other gradients, counts and rates, against eager steps of the same numbers."""
+    say("adamw graph", bits)
+    _, p, g, _, _ = _adam_case(8, F32, F32, [1000, 5000])
+    twin = [x.clone() for x in p]
+    count, rate = torch.ones(1, dtype=torch.int32, device=DEV), torch.full((1,), LR, device=DEV)
+    opt = Bn.AdamW(p, g, lr=0.0, state_bits=bits, max_norm=0.1, step_dev=count, lr_dev=rate)
+    ref = Bn.AdamW(twin, g, lr=LR, state_bits=bits, max_norm=0.1)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            opt.step(step=1)
+    torch.cuda.synchronize()
+    g0 = gen(9)
+    for t in range(1, 5):
+        for x in g:
+            x.copy_(randn(g0, x.numel(), std=1e-2))
+        count.fill_(t)
+        rate.fill_(LR / t)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        ref.step(lr=float(rate))
+        for a, b in zip(p, twin):
+            assert torch.equal(a, b), t
+
+
+# ---- as they are used together -----------------------------------------------------------------------------
+
+@gpu
+def test_token_loss_and_norm_in_a_graph_and_on_another_stream():
+    say("graph and stream")
+    g0, l, y = _loss_case(21, BF, 40, 5003)
+    mask = (torch.rand((2, 20), generator=g0) < 0.6).to(torch.uint8).to(DEV)
+    _, q, k, gq, gk, cos, sin = _qk_case(22, BF, 40, 4, 2, 64, 20)
+    desc = Bn.make_desc(2, 20, 256, 4, 2, 64, 256, BF, rms_eps=EPS_N)
+    dq, dk = randn(g0, 40, 256, dtype=BF), randn(g0, 40, 128, dtype=BF)
+
+    def call():
+        idx, cu, nd, _ = Bn.build_keep_index(mask, sync=False)
+        a = Bn.token_loss(l, y, idx=idx, n_kept_dev=nd)
+        b = Bn.qk_norm_rope_bwd(desc, q, k, gq, gk, dq, dk, cos, sin, idx=idx, n_kept_dev=nd)
+        return nd, a, b
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        call()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            held = call()
+    torch.cuda.synchronize()
+    for share in (0.3, 1.1, 0.0, 0.7):
+        mask.copy_((torch.rand((2, 20), generator=g0) < share).to(torch.uint8))
+        l.copy_(randn(g0, 40, 5003, dtype=BF))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        nd, a, b = call()
+        n = int(nd)
+        assert n == int(held[0]) == int(mask.sum())
+        for x, z in zip(held[1] + held[2][:2], a + b[:2]):
+            assert torch.equal(x if x.numel() == 4 else x[:n], z if z.numel() == 4 else z[:n])
+        assert torch.equal(held[2][2], b[2]) and torch.equal(held[2][3], b[3])
+        torch.cuda.synchronize()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_training_step_end_to_end(dtype):
+    """Norm and rotation, loss, head, layer and update as a program runs them, with every token kept: the gradients are those of the
+    whole function, which torch differentiates in 64 bits; then the parameters move by AdamW of these gradients."""
+    say("step", dtype)
+    V = 520
+    shape, W, sv, tabs, rng = _layer_qk_problem(dtype, seed=31)
+    B, S, H, Hq, Hkv, d = shape.B, shape.S, shape.H, shape.Hq, shape.Hkv, shape.d
+    T = shape.T
+    wh = Hn.quantize(0.05 * rng.standard_normal((H, V)), shape.dtype)
+    y = torch.from_numpy(rng.integers(0, V, T))
+    # the whole function in 64 bits
+    P = {n: torch.from_numpy(v.astype(np.float64)).requires_grad_() for n, v in {**W, "wh": wh}.items()}
+    rms = lambda x, g: x / (x.square().mean(-1, keepdim=True) + 1e-5).sqrt() * g
+    x = torch.from_numpy(sv["x"].astype(np.float64))
+    cos, sin, pos = torch.from_numpy(tabs[0]), torch.from_numpy(tabs[1]), torch.arange(T) % S
+    h1 = rms(x, P["g1"])
+    q, k, v = qk_ref(h1 @ P["wq"], P["gq"], d, EPS_N, cos, sin, pos), qk_ref(h1 @ P["wk"], P["gk"], d, EPS_N, cos, sin, pos), h1 @ P["wv"]
+    heads = lambda t, n: t.view(B, S, n, d).transpose(1, 2)
+    kk, vv = (heads(t, Hkv).repeat_interleave(Hq // Hkv, 1) for t in (k, v))
+    sc = (heads(q, Hq) @ kk.transpose(2, 3) / math.sqrt(d)).masked_fill(torch.triu(torch.ones(S, S, dtype=torch.bool), 1), -math.inf)
+    r = x + (torch.softmax(sc, -1) @ vv).transpose(1, 2).reshape(T, -1) @ P["wo"]
+    h2 = rms(r, P["g2"])
+    out = r + (torch.nn.functional.silu(h2 @ P["wg"]) * (h2 @ P["wu"])) @ P["wd"]
+    logits = out @ P["wh"]
+    loss = torch.nn.functional.cross_entropy(logits, y)
+    loss.backward()
+    # the same through the library
+    dsv, dW = _layer_qk_device(shape, W, sv, tabs)
+    desc = Bn.make_desc(B, S, H, Hq, Hkv, d, shape.F, shape.dtype, rms_eps=EPS_N)
+    fq, fk = Bn.qk_norm_rope_fwd(desc, dsv["q_pre"], dsv["k_pre"], dW["gq"], dW["gk"], dsv["rope_cos"], dsv["rope_sin"])
+    desc = Bn.make_desc(B, S, H, Hq, Hkv, d, shape.F, shape.dtype)
+    dsv["q"], dsv["k"] = fq, fk
+    yo = Hn.to_dev(Hn.quantize(out.detach().numpy(), shape.dtype), shape.dtype)
+    dwh = Hn.to_dev(wh, shape.dtype)
+    idx, cu, nd, n = Bn.build_keep_index(torch.ones((B, S), dtype=torch.uint8, device=DEV))
+    dl = (yo.float() @ dwh.float()).to(dtype)
+    stats, _, g = Bn.token_loss(dl, y.to(DEV), idx=idx, n_kept_dev=nd)
+    dy, gwh = Bn.linear_bwd_reduced(yo, g, dwh)
+    plan = Bn.LayerBackward(desc, main_grad=True, qk_norm_eps=EPS_N)
+    plan.compact_dev(dsv, dW, dy, idx, cu, nd)
+    tol = 3 * Hn.TOL[shape.dtype]           # the layer's, the head's and the loss's one after the other
+    assert abs(float(stats[0]) - float(loss)) < tol
+    grads = {("d" + n): t.grad.numpy() for n, t in P.items()}
+    for n in Hn.GRADS + ("dgq", "dgk"):
+        assert Hn.rel_fro(Hn.to_np(plan.grads[n]), grads[n]) <= tol, (n, Hn.rel_fro(Hn.to_np(plan.grads[n]), grads[n]))
+    assert Hn.rel_fro(Hn.to_np(gwh), grads["dwh"]) <= tol
+    names = ("wq", "wk", "wv", "wo", "wg", "wu", "wd", "g1", "g2", "gq", "gk")
+    for bits in (32, 8):
+        p = [dW[n].clone() for n in names]
+        gs = [plan.grads["d" + n] for n in names]
+        opt = Bn.AdamW(p, gs, lr=LR, betas=(B1, B2), eps=AEPS, weight_decay=[WD if n[0] == "w" else 0.0 for n in names], max_norm=0.1,
+                       master=True if dtype == BF else None, state_bits=bits)
+        opt.step()
+        norm = math.sqrt(sum(float(x.double().square().sum()) for x in gs))
+        assert abs(float(opt.grad_norm) - norm) <= 2 * U * norm
+        for i, n in enumerate(names):
+            z = torch.zeros_like(gs[i], dtype=F64)
+            rw, _, _, upd = adam_ref(dW[n].double(), gs[i].double(), z, z, 1, LR, B1, B2, AEPS, WD if n[0] == "w" else 0.0, min(1.0, 0.1 / (norm + 1e-6)))
+            w = (opt.master or p)[i]
+            # eps is next to sqrt(v) where a gradient is tiny: the clip's rounding moves the quotient by no more than itself
+            close(w, rw, EPS[F32] * rw.abs() + 5 * U * dW[n].double().abs() + 64 * U * upd.abs(), n)
