@@ -1,16 +1,14 @@
-// Losses of kept tokens and their gradient towards the logits: one block per kept row reads the row twice, first for the running
-// maximum and sum of the softmax, then (from the caches) for the gradient, which needs both.  HBM-bound: the kept rows of the
-// logits in, the gradient out.
+// Losses of kept tokens and their gradient towards the logits.  A block takes a row; one pass gives the running maximum and sum of its
+// softmax, a second one, which needs both, the gradient.  HBM-bound: the kept rows of the logits in, the gradient out, if the row stays in registers
+// between the passes; two exponentials an element are not far from what bounds it either.
 #include <math.h>
 
 #include "common.h"
 
 namespace cf {
 
-constexpr float LOG2E = 1.4426950408889634f;
-
 // 16 bytes at an address that need only be aligned to an element: rows of an odd vocabulary start anywhere
-struct __attribute__((packed, aligned(2))) Bytes16 { unsigned x, y, z, w; };
+typedef unsigned Bytes16 __attribute__((ext_vector_type(4), aligned(2)));
 
 template <typename T> __device__ __forceinline__ void widen(const Bytes16& b, float (&o)[Vec<T>::N]);
 template <> __device__ __forceinline__ void widen<float>(const Bytes16& b, float (&o)[4]) {
@@ -42,7 +40,7 @@ struct LossArgs {
     const float *old_logp, *ref_logp, *adv, *weights;
     const int32_t *idx, *n_dev;
     int n_max, V;
-    float scale;                // of the logits
+    float scale, k, klo;        // of the logits; times log2(e), and what rounding that left
     bool policy;
     float lo, hi, kl_coef;      // bounds of the ratio
     float norm;                 // 0: the number of live rows
@@ -57,50 +55,119 @@ struct RowLoss {
     float4 terms;
     float coef;
 };
-__device__ __forceinline__ RowLoss row_loss(const LossArgs& a, float lp, int64_t row, float w, float inv_norm) {
+// What a block knows of a row apart from its logits.  The same for all its threads, which the compiler cannot know of what it loads:
+// these go through the scalar path, apart from the vectors in flight (nothing in them is written during the kernel before it is read).
+template <typename U> __device__ __forceinline__ U scalar_load(const U* p) {
+    return *(const __attribute__((address_space(4))) U*)(uintptr_t)p;
+}
+template <typename T> __device__ __forceinline__ float scalar_load_f32(const void* base, int64_t i);
+template <> __device__ __forceinline__ float scalar_load_f32<float>(const void* base, int64_t i) { return scalar_load((const float*)base + i); }
+template <> __device__ __forceinline__ float scalar_load_f32<bf16_t>(const void* base, int64_t i) {
+    const uintptr_t at = (uintptr_t)base + 2 * i;       // the dword around it
+    const unsigned u = scalar_load((const unsigned*)(at & ~(uintptr_t)3));
+    return __uint_as_float((at & 2) ? u & 0xFFFF0000u : u << 16);
+}
+struct RowHead {
+    int row, y;             // y: -1 for a row that is left out
+    const void* l;
+    float w, ly, old, ref, adv;
+    __device__ __forceinline__ bool live() const { return y >= 0; }
+};
+template <typename T> __device__ __forceinline__ void find_row(const LossArgs& a, int j, RowHead& r) {
+    r.row = a.idx != nullptr ? scalar_load(a.idx + j) : j;
+    r.l = (const T*)a.logits + (int64_t)r.row * a.stride;
+}
+template <typename T> __device__ __forceinline__ void load_head(const LossArgs& a, RowHead& r) {
+    const int64_t y = scalar_load(a.targets + r.row);
+    r.w = a.weights != nullptr ? scalar_load(a.weights + r.row) : 1.f;
+    r.old = r.ref = r.adv = 0.f;
+    if (a.policy) {
+        r.old = scalar_load(a.old_logp + r.row);
+        r.adv = scalar_load(a.adv + r.row);
+        if (a.ref_logp != nullptr) r.ref = scalar_load(a.ref_logp + r.row);
+    }
+    r.y = y >= 0 && y < a.V && r.w != 0.f ? (int)y : -1;
+    r.ly = scalar_load_f32<T>(r.l, r.y < 0 ? 0 : r.y);
+}
+__device__ __forceinline__ RowLoss row_loss(const LossArgs& a, const RowHead& h, float lp, float inv_norm) {
+    const float w = h.w;
     if (!a.policy) return RowLoss{make_float4(-w * lp, -w * lp, 0.f, 0.f), -w * inv_norm};
-    const float A = a.adv[row], r = expf(lp - a.old_logp[row]);
+    const float A = h.adv, r = expf(lp - h.old);
     const float rc = fminf(fmaxf(r, a.lo), a.hi);
     const bool clipped = r * A > rc * A;
     const float first = clipped ? -rc * A : -r * A;
     float d = clipped ? 0.f : -r * A, k = 0.f;
     if (a.ref_logp != nullptr) {
-        const float q = a.ref_logp[row] - lp, e = expm1f(q);        // exp(q) - 1 as such: k is the small rest of it
+        const float q = h.ref - lp, e = expm1f(q);          // exp(q) - 1 as such: k is the small rest of it
         k = e - q;
         d -= a.kl_coef * e;
     }
     return RowLoss{make_float4(w * (first + a.kl_coef * k), w * first, w * k, clipped ? w : 0.f), w * inv_norm * d};
 }
 
-template <typename T, int NT>
-__global__ __launch_bounds__(NT) void token_loss_kernel(LossArgs a) {
-    constexpr int VN = Vec<T>::N, WAVES = NT / 64;
-    __shared__ float red[2 * WAVES];
-    const int n_rows = live_rows(a.n_max, a.n_dev), j = blockIdx.x, tid = threadIdx.x;
-    if (j >= n_rows) return;
-    const int64_t row = a.idx != nullptr ? a.idx[j] : j;
-    const T* l = (const T*)a.logits + row * a.stride;
-    T* dl = a.dlogits != nullptr ? (T*)a.dlogits + (int64_t)j * a.dstride : nullptr;
-    const int V = a.V, nv = V / VN;
-    const int64_t y = a.targets[row];
-    const float w = a.weights != nullptr ? a.weights[row] : 1.f;
-    const float inv_norm = 1.f / (a.norm != 0.f ? a.norm : (float)n_rows);
-    const float ks = a.scale * LOG2E;
-    float lp = 0.f, m = 0.f, inv_s = 0.f;
+// One exponential of a softmax, 2^(k*(x - m)).  For fp32 logits (EXACT) the roundings of k*(x - m) and of k itself, up to 2^-19 of a small
+// probability, are carried along and multiplied in; a bf16 gradient has 2^-8.
+struct Expo {
+    float m, k, klo;
+};
+template <bool EXACT> __device__ __forceinline__ float expo(const Expo& a, float x) {
+    const float d = x - a.m, hi = d * a.k, e = __builtin_amdgcn_exp2f(hi);
+    if (!EXACT) return e;
+    const float lo = fmaf(d, a.klo, fmaf(d, a.k, -hi));
+    return fmaf(e, hi > -200.f ? lo * 0.6931471805599453f : 0.f, e);       // behind a mask hi may be -inf, and lo NaN
+}
+
+// Maximum and sum of the block's threads: afterwards s is with respect to the common m
+template <int WAVES> __device__ __forceinline__ void block_softmax(float k, float& m, float& s, float (&red)[2 * WAVES]) {
+    float bm = m;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) bm = fmaxf(bm, __shfl_xor(bm, o, 64));
+    s = wave_sum(s * __builtin_amdgcn_exp2f((m - bm) * k));
+    if ((threadIdx.x & 63) == 0) { red[threadIdx.x >> 6] = bm; red[WAVES + (threadIdx.x >> 6)] = s; }
+    __syncthreads();
+    m = red[0];
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) m = fmaxf(m, red[i]);
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) s += red[WAVES + i] * __builtin_amdgcn_exp2f((red[i] - m) * k);
+}
+
+// The gradient's factors: neg times an exponential, at_y at the target.  `writes`: the thread that leaves what the row gives.
+struct RowEnd {
+    float neg, at_y;
+};
+__device__ __forceinline__ RowEnd row_end(const LossArgs& a, const RowHead& r, int j, float m, float s, float inv_norm, bool writes) {
+    float lp = 0.f;
     RowLoss rl{make_float4(0.f, 0.f, 0.f, 0.f), 0.f};
-    const bool live = y >= 0 && y < V && w != 0.f;
-    if (live) {
-        const float ly = to_f32<T>(l[y]);
-        float s = 0.f;
-        m = -3.402823466e38f;
+    if (r.live()) {
+        lp = (r.ly - m) * a.scale - logf(s);
+        rl = row_loss(a, r, lp, inv_norm);
+    }
+    if (writes) {
+        if (a.logp != nullptr) a.logp[j] = lp;
+        a.terms[j] = rl.terms;
+    }
+    const float cs = rl.coef * a.scale;
+    return RowEnd{-cs / s, -cs * expm1f(lp)};
+}
+
+// A row read twice, with no bound on its length
+template <typename T, int NT> __device__ __forceinline__ void stream_row(const LossArgs& a, const RowHead& r, int j, float inv_norm, float (&red)[NT / 32]) {
+    constexpr int VN = Vec<T>::N, WAVES = NT / 64;
+    const int tid = threadIdx.x, V = a.V, nv = V / VN;
+    const T* l = (const T*)r.l;
+    Expo ex{-3.402823466e38f, a.k, a.klo};
+    float s = 0.f;
+    if (r.live()) {
         auto take = [&](const float (&x)[VN]) {
-            float t = m;
+            float t = ex.m;
 #pragma unroll
             for (int e = 0; e < VN; ++e) t = fmaxf(t, x[e]);
-            s *= exp2f((m - t) * ks);
-            m = t;
+            s *= __builtin_amdgcn_exp2f((ex.m - t) * ex.k);
+            ex.m = t;
 #pragma unroll
-            for (int e = 0; e < VN; ++e) s += exp2f((x[e] - m) * ks);
+            for (int e = 0; e < VN; ++e) s += expo<true>(ex, x[e]);
         };
         for (int v = tid; v < nv; v += NT) {
             float x[VN];
@@ -114,55 +181,161 @@ __global__ __launch_bounds__(NT) void token_loss_kernel(LossArgs a) {
             for (int e = 1; e < VN; ++e) x[e] = -INFINITY;
             take(x);
         }
-        float bm = m;
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) bm = fmaxf(bm, __shfl_xor(bm, o, 64));
-        s = wave_sum(s * exp2f((m - bm) * ks));
-        if ((tid & 63) == 0) { red[tid >> 6] = bm; red[WAVES + (tid >> 6)] = s; }
-        __syncthreads();
-        m = red[0];
-#pragma unroll
-        for (int i = 1; i < WAVES; ++i) m = fmaxf(m, red[i]);
-        s = 0.f;
-#pragma unroll
-        for (int i = 0; i < WAVES; ++i) s += red[WAVES + i] * exp2f((red[i] - m) * ks);
-        inv_s = 1.f / s;
-        lp = (ly - m) * a.scale - logf(s);
-        rl = row_loss(a, lp, row, w, inv_norm);
+        block_softmax<WAVES>(ex.k, ex.m, s, red);
     }
-    if (tid == 0) {
-        if (a.logp != nullptr) a.logp[j] = lp;
-        a.terms[j] = rl.terms;
-    }
-    if (dl == nullptr) return;
-    if (!live || rl.coef == 0.f) {
-        const Bytes16 zero{0u, 0u, 0u, 0u};
-        for (int v = tid; v < nv; v += NT) reinterpret_cast<Bytes16*>(dl)[v] = zero;
-        if (int c = nv * VN + tid; c < V) dl[c] = one_from_f32<T>(0.f);
-        return;
-    }
-    const float cs = rl.coef * a.scale, neg = -cs * inv_s, at_y = -cs * expm1f(lp);
+    const RowEnd end = row_end(a, r, j, ex.m, s, inv_norm, threadIdx.x == 0);
+    if (a.dlogits == nullptr) return;
+    T* dl = (T*)a.dlogits + (int64_t)j * a.dstride;
     for (int v = tid; v < nv; v += NT) {
         float x[VN];
         widen<T>(reinterpret_cast<const Bytes16*>(l)[v], x);
 #pragma unroll
-        for (int e = 0; e < VN; ++e) x[e] = neg * exp2f((x[e] - m) * ks);
-        if (v == (int)y / VN) {
-#pragma unroll
-            for (int e = 0; e < VN; ++e) x[e] = e == (int)y % VN ? at_y : x[e];
-        }
+        for (int e = 0; e < VN; ++e) x[e] = !r.live() ? 0.f : v * VN + e == r.y ? end.at_y : end.neg * expo<true>(ex, x[e]);
         reinterpret_cast<Bytes16*>(dl)[v] = narrow<T>(x);
     }
-    if (int c = nv * VN + tid; c < V) dl[c] = one_from_f32<T>(c == (int)y ? at_y : neg * exp2f((to_f32<T>(l[c]) - m) * ks));
+    if (int c = nv * VN + tid; c < V)
+        dl[c] = one_from_f32<T>(!r.live() ? 0.f : c == r.y ? end.at_y : end.neg * expo<true>(ex, to_f32<T>(l[c])));
+}
+
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void token_loss_stream_kernel(LossArgs a) {
+    __shared__ float red[NT / 32];
+    const int n_rows = live_rows(a.n_max, a.n_dev), j = blockIdx.x;
+    if (j >= n_rows) return;
+    RowHead r;
+    find_row<T>(a, j, r);
+    load_head<T>(a, r);
+    stream_row<T, NT>(a, r, j, 1.f / (a.norm != 0.f ? a.norm : (float)n_rows), red);
+}
+
+// A row in a block's registers, NV vectors of 16 bytes a thread, so that it is read once.  The block walks through rows, and each vector of the next
+// row is asked for as soon as its register has given its part of the gradient (or of the sum, without a gradient): reads, arithmetic
+// and writes of neighbouring rows overlap.
+// Keeps a vector as it is stored, and the arithmetic where it stands: widened values of one pass are not to be kept for the next one.
+__device__ __forceinline__ void hold(Bytes16& b) { asm volatile("" : "+v"(b)); }
+__device__ __forceinline__ void hold(float& a, float& b) { asm volatile("" : "+v"(a), "+v"(b)); }
+
+template <typename T, int NT, int NV, bool GRAD>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void token_loss_kernel(LossArgs a) {
+    constexpr int VN = Vec<T>::N, WAVES = NT / 64;
+    constexpr bool EXACT = VN == 4;
+    __shared__ float red[2 * WAVES];
+    __shared__ float ends[3];
+    const int n_rows = live_rows(a.n_max, a.n_dev), tid = threadIdx.x, V = a.V, ct = V / VN * VN + tid;
+    int j = blockIdx.x, nv = V / VN;
+    if (j >= n_rows) return;
+    const float inv_norm = 1.f / (a.norm != 0.f ? a.norm : (float)n_rows);
+    Bytes16 x[NV];
+    // Lanes behind the row's last vector load that one again (or its first): a load without a condition has one register from issue to use.
+    auto load = [&](const void* l, int i) __attribute__((always_inline)) {
+        const int last = (nv - 1 - i * NT) * 16;
+        return *reinterpret_cast<const Bytes16*>((const char*)l + (last >= 0 ? i * NT * 16 : 0) + (unsigned)min(tid * 16, max(last, 0)));
+    };
+    // the row's last elements, one a thread
+    auto load_tail = [&](const void* l) __attribute__((always_inline)) { return ct < V ? to_f32<T>(((const T*)l)[ct]) : -INFINITY; };
+    RowHead r;
+    find_row<T>(a, j, r);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) x[i] = load(r.l, i);
+    float xt = load_tail(r.l);
+    for (;;) {
+        const int jn = j + (int)gridDim.x;
+        asm("" : "+s"(nv));             // or 2 * NV lane masks are kept in scalar registers from row to row
+        load_head<T>(a, r);
+        RowHead rn = r;                 // behind the last row its own vectors are asked for again
+        if (jn < n_rows) find_row<T>(a, jn, rn);
+        Expo ex{-3.402823466e38f, a.k, a.klo};
+        float s = 0.f;
+        const float tail = xt;
+        auto take = [&](const auto& o) __attribute__((always_inline)) {
+            constexpr int N = sizeof(o) / sizeof(float);
+            float t = ex.m;
+#pragma unroll
+            for (int e = 0; e < N; ++e) t = fmaxf(t, o[e]);
+            s *= __builtin_amdgcn_exp2f((ex.m - t) * ex.k);
+            ex.m = t;
+#pragma unroll
+            for (int e = 0; e < N; ++e) s += expo<EXACT>(ex, o[e]);
+            hold(ex.m, s);
+        };
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float o[VN];
+            hold(x[i]);
+            widen<T>(x[i], o);
+            if (nv - i * NT < NT) {
+#pragma unroll
+                for (int e = 0; e < VN; ++e) o[e] = tid < nv - i * NT ? o[e] : -INFINITY;
+            }
+            take(o);
+            if (!GRAD) x[i] = load(rn.l, i);
+        }
+        const float o1[1] = {tail};
+        take(o1);
+        if (!GRAD) xt = load_tail(rn.l);
+        // over the wave; the first wave adds up the waves and ends the row
+        float m = ex.m;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+        s = wave_sum(s * __builtin_amdgcn_exp2f((ex.m - m) * ex.k));
+        if ((tid & 63) == 0) { red[tid >> 6] = m; red[WAVES + (tid >> 6)] = s; }
+        __syncthreads();
+        if (tid < 64) {
+            const float wm = red[tid & (WAVES - 1)];
+            m = wm;
+            s = red[WAVES + (tid & (WAVES - 1))];
+#pragma unroll
+            for (int o = WAVES / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+            s *= __builtin_amdgcn_exp2f((wm - m) * ex.k);
+#pragma unroll
+            for (int o = WAVES / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+            const RowEnd end = row_end(a, r, j, m, s, inv_norm, tid == 0);
+            if (tid == 0) { ends[0] = m; ends[1] = end.neg; ends[2] = end.at_y; }
+        }
+        __syncthreads();
+        if (GRAD) {
+            ex.m = ends[0];
+            const float neg = ends[1], at_y = ends[2];
+            char* dl = (char*)((T*)a.dlogits + (int64_t)j * a.dstride);
+            const int yv = r.y >> (VN == 8 ? 3 : 2), ye = r.y & (VN - 1);       // yv < 0: a row that is left out
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                float o[VN];
+                hold(x[i]);
+                if (yv >= 0) {
+                    widen<T>(x[i], o);
+#pragma unroll
+                    for (int e = 0; e < VN; ++e) o[e] = neg * expo<EXACT>(ex, o[e]);
+                    if (tid == yv - i * NT) {
+#pragma unroll
+                        for (int e = 0; e < VN; ++e) o[e] = e == ye ? at_y : o[e];
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < VN; ++e) o[e] = 0.f;
+                }
+                Bytes16 g = narrow<T>(o);
+                hold(g);
+                if (tid < nv - i * NT) *reinterpret_cast<Bytes16*>(dl + i * NT * 16 + (unsigned)tid * 16u) = g;
+                x[i] = load(rn.l, i);
+            }
+            if (ct < V) ((T*)dl)[ct] = one_from_f32<T>(yv < 0 ? 0.f : ct == r.y ? at_y : neg * expo<EXACT>(ex, tail));
+            xt = load_tail(rn.l);
+        }
+        if (jn >= n_rows) return;
+        j = jn;
+        r = rn;
+    }
 }
 
 // stats = sums of the rows' terms over the live rows, in fp64 and in fixed order, over norm
-__global__ __launch_bounds__(256) void loss_stats_kernel(const float4* __restrict__ terms, int n_max, const int32_t* __restrict__ n_dev,
+__global__ __launch_bounds__(1024) void loss_stats_kernel(const float4* __restrict__ terms, int n_max, const int32_t* __restrict__ n_dev,
                                                          float norm, float* __restrict__ stats) {
-    __shared__ double red[4][4];
+    __shared__ double red[16][4];
     const int n_rows = live_rows(n_max, n_dev);
     double s[4] = {0., 0., 0., 0.};
-    for (int j = threadIdx.x; j < n_rows; j += 256) {
+#pragma unroll 4
+    for (int j = threadIdx.x; j < n_rows; j += 1024) {
         const float4 t = terms[j];
         s[0] += t.x; s[1] += t.y; s[2] += t.z; s[3] += t.w;
     }
@@ -174,10 +347,31 @@ __global__ __launch_bounds__(256) void loss_stats_kernel(const float4* __restric
     }
     __syncthreads();
     if (threadIdx.x < 4) {
-        const double t = red[0][threadIdx.x] + red[1][threadIdx.x] + red[2][threadIdx.x] + red[3][threadIdx.x];
+        double t = 0.;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) t += red[i][threadIdx.x];
         const double by = norm != 0.f ? (double)norm : (double)(n_rows > 0 ? n_rows : 1);
         stats[threadIdx.x] = (float)(t / by);
     }
+}
+
+template <typename T, int NT, int NV> static void launch_rows(const LossArgs& a, hipStream_t st) {
+    const int resident = compute_units() * (1024 / NT), grid = a.n_max < resident ? a.n_max : resident;
+    if (a.dlogits != nullptr) token_loss_kernel<T, NT, NV, true><<<grid, NT, 0, st>>>(a);
+    else token_loss_kernel<T, NT, NV, false><<<grid, NT, 0, st>>>(a);
+}
+
+// The smallest block whose registers hold a row.  A function of the vocabulary, the type and the scale alone: a row's sums, and its logp, are
+// added up in the same order in every call.
+template <typename T> static void launch_token_loss(const LossArgs& a, hipStream_t st) {
+    const int nv = a.V / Vec<T>::N;
+    if (nv < 1 || nv > 1024 * 20) token_loss_stream_kernel<T, 512><<<a.n_max, 512, 0, st>>>(a);
+    else if (nv <= 256 * 4) launch_rows<T, 256, 4>(a, st);
+    else if (nv <= 256 * 8) launch_rows<T, 256, 8>(a, st);
+    else if (nv <= 256 * 16) launch_rows<T, 256, 16>(a, st);
+    else if (nv <= 512 * 16) launch_rows<T, 512, 16>(a, st);
+    else if (nv <= 1024 * 16) launch_rows<T, 1024, 16>(a, st);
+    else launch_rows<T, 1024, 20>(a, st);
 }
 
 }  // namespace cf
@@ -218,13 +412,11 @@ cf_status cf_token_loss(const cf_loss_desc* desc, const void* logits, int64_t lo
     if (dlogits == logits && (idx || ls != ds)) return CF_ERR_SHAPE;     // a row would be written before another block has read it
     if (!ws || off(ws, 16) || ws_bytes < cf_token_loss_workspace_bytes(max_kept)) return CF_ERR_WORKSPACE;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    LossArgs a{logits, ls, targets, old_logp, ref_logp, advantages, weights, idx, n_kept_dev, max_kept, desc->V, scale, policy,
+    const double k = (double)scale * 1.4426950408889634;
+    LossArgs a{logits, ls, targets, old_logp, ref_logp, advantages, weights, idx, n_kept_dev, max_kept, desc->V, scale, (float)k, (float)(k - (float)k), policy,
                1.f - desc->clip_lo, 1.f + desc->clip_hi, policy ? desc->kl_coef : 0.f, desc->norm, dlogits, ds, logp, (float4*)ws};
-    if (max_kept > 0) {
-        if (desc->dtype == CF_F32) token_loss_kernel<float, 512><<<max_kept, 512, 0, st>>>(a);
-        else token_loss_kernel<bf16_t, 512><<<max_kept, 512, 0, st>>>(a);
-    }
-    if (stats) loss_stats_kernel<<<1, 256, 0, st>>>((const float4*)ws, max_kept, n_kept_dev, desc->norm, stats);
+    if (max_kept > 0) desc->dtype == CF_F32 ? launch_token_loss<float>(a, st) : launch_token_loss<bf16_t>(a, st);
+    if (stats) loss_stats_kernel<<<1, 1024, 0, st>>>((const float4*)ws, max_kept, n_kept_dev, desc->norm, stats);
     return hipGetLastError() == hipSuccess ? CF_OK : CF_ERR_HIP;
 }
 

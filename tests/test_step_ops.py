@@ -598,7 +598,7 @@ def _check_loss(got, want, l, y, dtype, scale, wsum, policy):
     close(stats, rs, 16 * worst * float(wsum.sum()) + 4 * U * rs.abs().nan_to_num(0.0, 0.0, 0.0), "stats")
 
 
-LOSS = [(1, 1), (5, 7), (3, 8), (4, 9), (6, 64), (2, 511), (3, 512), (2, 4099), (9, 32000), (3, 50257), (2, 128256), (2, 131077), (1, 262147)]
+LOSS = [(1, 1), (5, 7), (3, 8), (4, 9), (6, 64), (2, 511), (3, 512), (2, 1028), (2, 2056), (3, 2064), (2, 4099), (1, 32776), (2, 65544), (9, 32000), (3, 50257), (2, 128256), (2, 131077), (1, 262147)]
 
 
 @gpu
