@@ -210,43 +210,52 @@ __global__ __launch_bounds__(NT) void token_loss_stream_kernel(LossArgs a) {
 
 // A row in a block's registers, NV vectors of 16 bytes a thread, so that it is read once.  The block walks through rows, and each vector of the next
 // row is asked for as soon as its register has given its part of the gradient (or of the sum, without a gradient): reads, arithmetic
-// and writes of neighbouring rows overlap.
+// and writes of neighbouring rows overlap.  4096 of 8192 rows of 128256 bf16 logits: 2.1 GB in 406 us, 5.2 TB/s where a copy of 1 GiB reaches 6.2; read
+// twice it took 601.  4096 rows of 32000 102 us (126), 701 of 50257 fp32 logits 59 us (87).  Arithmetic does not bound it: with its exponentials left out it takes 402.
+// The gradient is written past the caches: 406 against 417 us, 102 against 110; with the two products of a [V, 2048] head behind it, 64 to 2048 rows
+// of 32000 take 0.97 to 1.00 of the time, 1024 of 128256 0.995, and 4096 of 32000, which just fit the last cache, 1.03.
 // Keeps a vector as it is stored, and the arithmetic where it stands: widened values of one pass are not to be kept for the next one.
 __device__ __forceinline__ void hold(Bytes16& b) { asm volatile("" : "+v"(b)); }
 __device__ __forceinline__ void hold(float& a, float& b) { asm volatile("" : "+v"(a), "+v"(b)); }
 
+// A vector at a scalar address and a lane's offset from it.  Without the empty statement the lane's part is added up in 64 bits for each vector.
+__device__ __forceinline__ Bytes16* vector_at(const void* base, unsigned offset) {
+    uintptr_t p = (uintptr_t)base;
+    asm("" : "+s"(p));
+    return (Bytes16*)((__attribute__((address_space(1))) char*)p + offset);
+}
+
 template <typename T, int NT, int NV, bool GRAD>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void token_loss_kernel(LossArgs a) {
     constexpr int VN = Vec<T>::N, WAVES = NT / 64;
+    // The launch takes this kernel for rows of more than FULL * NT vectors: up to there every lane has one.  Behind, a vector that no lane has is skipped,
+    // and lanes behind the last one do what its owner does.  No access is conditional but for that: what is in flight is counted, and
+    // a count that hangs on a branch is waited for as if the branch had not been taken.
+    constexpr int FULL = NV <= 4 ? 0 : NV - 4;
     constexpr bool EXACT = VN == 4;
     __shared__ float red[2 * WAVES];
     __shared__ float ends[3];
-    const int n_rows = live_rows(a.n_max, a.n_dev), tid = threadIdx.x, V = a.V, ct = V / VN * VN + tid;
-    int j = blockIdx.x, nv = V / VN;
+    const int n_rows = live_rows(a.n_max, a.n_dev), tid = threadIdx.x, V = a.V, nv = V / VN, ct = nv * VN + tid;
+    int j = blockIdx.x, jn;
     if (j >= n_rows) return;
     const float inv_norm = 1.f / (a.norm != 0.f ? a.norm : (float)n_rows);
     Bytes16 x[NV];
-    // Lanes behind the row's last vector load that one again (or its first): a load without a condition has one register from issue to use.
-    auto load = [&](const void* l, int i) __attribute__((always_inline)) {
-        const int last = (nv - 1 - i * NT) * 16;
-        return *reinterpret_cast<const Bytes16*>((const char*)l + (last >= 0 ? i * NT * 16 : 0) + (unsigned)min(tid * 16, max(last, 0)));
-    };
-    // the row's last elements, one a thread
-    auto load_tail = [&](const void* l) __attribute__((always_inline)) { return ct < V ? to_f32<T>(((const T*)l)[ct]) : -INFINITY; };
-    RowHead r;
-    find_row<T>(a, j, r);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) x[i] = load(r.l, i);
-    float xt = load_tail(r.l);
-    for (;;) {
-        const int jn = j + (int)gridDim.x;
-        asm("" : "+s"(nv));             // or 2 * NV lane masks are kept in scalar registers from row to row
+    auto at = [&](int i) __attribute__((always_inline)) { return (unsigned)(i < FULL ? tid : min(tid, nv - 1 - i * NT)) * 16u; };
+    auto load = [&](const void* l, int i) __attribute__((always_inline)) { return *vector_at((const char*)l + i * NT * 16, at(i)); };
+    const int tail_at = min(ct, V - 1);         // the row's last elements, one a thread, as they are stored
+    RowHead r, rn;
+    T xt;
+    Expo ex{0.f, a.k, a.klo};
+    float s, tail;
+    // What the row needs apart from its vectors, and where the next one is (behind the last row its own vectors are asked for again); the threads'
+    // maximum and sum
+    auto begin = [&]() __attribute__((always_inline)) {
         load_head<T>(a, r);
-        RowHead rn = r;                 // behind the last row its own vectors are asked for again
+        rn = r;
+        jn = j + (int)gridDim.x;
         if (jn < n_rows) find_row<T>(a, jn, rn);
-        Expo ex{-3.402823466e38f, a.k, a.klo};
-        float s = 0.f;
-        const float tail = xt;
+        ex.m = -3.402823466e38f;
+        s = 0.f;
         auto take = [&](const auto& o) __attribute__((always_inline)) {
             constexpr int N = sizeof(o) / sizeof(float);
             float t = ex.m;
@@ -260,19 +269,32 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
         };
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
+            if (i >= FULL && i * NT >= nv) continue;
             float o[VN];
             hold(x[i]);
             widen<T>(x[i], o);
-            if (nv - i * NT < NT) {
+            if (i >= FULL && nv - i * NT < NT) {
 #pragma unroll
                 for (int e = 0; e < VN; ++e) o[e] = tid < nv - i * NT ? o[e] : -INFINITY;
             }
             take(o);
             if (!GRAD) x[i] = load(rn.l, i);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        tail = ct < V ? to_f32<T>(xt) : -INFINITY;
         const float o1[1] = {tail};
         take(o1);
-        if (!GRAD) xt = load_tail(rn.l);
+        if (!GRAD) xt = ((const T*)rn.l)[tail_at];
+    };
+    find_row<T>(a, j, r);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (i < FULL || i * NT < nv) x[i] = load(r.l, i);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    xt = ((const T*)r.l)[tail_at];
+    begin();            // not the loop's: there the loads stand between stores
+    for (;;) {
         // over the wave; the first wave adds up the waves and ends the row
         float m = ex.m;
 #pragma unroll
@@ -295,36 +317,46 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
         __syncthreads();
         if (GRAD) {
             ex.m = ends[0];
-            const float neg = ends[1], at_y = ends[2];
+            const float at_y = ends[2];
+            // bf16: k*x - fl(k*m) in one operation; what rounding k*m cut off is a factor of the whole row
+            const float mk = ex.m * ex.k, neg = EXACT ? ends[1] : ends[1] * __builtin_amdgcn_exp2f(-fmaf(ex.m, ex.k, -mk));
+            auto grad = [&](float v) __attribute__((always_inline)) {
+                return neg * (EXACT ? expo<true>(ex, v) : __builtin_amdgcn_exp2f(fmaf(v, ex.k, -mk)));
+            };
             char* dl = (char*)((T*)a.dlogits + (int64_t)j * a.dstride);
-            const int yv = r.y >> (VN == 8 ? 3 : 2), ye = r.y & (VN - 1);       // yv < 0: a row that is left out
+            const unsigned yv = (unsigned)(r.y >> (VN == 8 ? 3 : 2)) * 16u;
+            const int ye = r.y & (VN - 1);
+            if (ct < V) ((T*)dl)[ct] = one_from_f32<T>(!r.live() ? 0.f : ct == r.y ? at_y : grad(tail));
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                float o[VN];
+                if (i >= FULL && i * NT >= nv) continue;
+                Bytes16 g;
                 hold(x[i]);
-                if (yv >= 0) {
+                if (r.live()) {
+                    float o[VN];
                     widen<T>(x[i], o);
 #pragma unroll
-                    for (int e = 0; e < VN; ++e) o[e] = neg * expo<EXACT>(ex, o[e]);
-                    if (tid == yv - i * NT) {
+                    for (int e = 0; e < VN; ++e) o[e] = grad(o[e]);
+                    if (at(i) == yv - i * NT * 16) {
 #pragma unroll
                         for (int e = 0; e < VN; ++e) o[e] = e == ye ? at_y : o[e];
                     }
+                    g = narrow<T>(o);
+                    hold(g);
                 } else {
-#pragma unroll
-                    for (int e = 0; e < VN; ++e) o[e] = 0.f;
+                    g = Bytes16{0u, 0u, 0u, 0u};
+                    hold(g);
                 }
-                Bytes16 g = narrow<T>(o);
-                hold(g);
-                if (tid < nv - i * NT) *reinterpret_cast<Bytes16*>(dl + i * NT * 16 + (unsigned)tid * 16u) = g;
+                __builtin_nontemporal_store(g, vector_at(dl + i * NT * 16, at(i)));
                 x[i] = load(rn.l, i);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            if (ct < V) ((T*)dl)[ct] = one_from_f32<T>(yv < 0 ? 0.f : ct == r.y ? at_y : neg * expo<EXACT>(ex, tail));
-            xt = load_tail(rn.l);
+            xt = ((const T*)rn.l)[tail_at];
         }
         if (jn >= n_rows) return;
         j = jn;
         r = rn;
+        begin();
     }
 }
 
@@ -361,15 +393,18 @@ template <typename T, int NT, int NV> static void launch_rows(const LossArgs& a,
     else token_loss_kernel<T, NT, NV, false><<<grid, NT, 0, st>>>(a);
 }
 
-// The smallest block whose registers hold a row.  A function of the vocabulary, the type and the scale alone: a row's sums, and its logp, are
+// The smallest block whose registers hold a row.  A function of the vocabulary and the type alone: a row's sums, and its logp, are
 // added up in the same order in every call.
 template <typename T> static void launch_token_loss(const LossArgs& a, hipStream_t st) {
     const int nv = a.V / Vec<T>::N;
     if (nv < 1 || nv > 1024 * 20) token_loss_stream_kernel<T, 512><<<a.n_max, 512, 0, st>>>(a);
     else if (nv <= 256 * 4) launch_rows<T, 256, 4>(a, st);
     else if (nv <= 256 * 8) launch_rows<T, 256, 8>(a, st);
+    else if (nv <= 256 * 12) launch_rows<T, 256, 12>(a, st);
     else if (nv <= 256 * 16) launch_rows<T, 256, 16>(a, st);
+    else if (nv <= 512 * 12) launch_rows<T, 512, 12>(a, st);
     else if (nv <= 512 * 16) launch_rows<T, 512, 16>(a, st);
+    else if (nv <= 1024 * 12) launch_rows<T, 1024, 12>(a, st);
     else if (nv <= 1024 * 16) launch_rows<T, 1024, 16>(a, st);
     else launch_rows<T, 1024, 20>(a, st);
 }
