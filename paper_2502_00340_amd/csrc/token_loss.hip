@@ -317,12 +317,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
         __syncthreads();
         if (GRAD) {
             ex.m = ends[0];
-            const float at_y = ends[2];
-            // bf16: k*x - fl(k*m) in one operation; what rounding k*m cut off is a factor of the whole row
-            const float mk = ex.m * ex.k, neg = EXACT ? ends[1] : ends[1] * __builtin_amdgcn_exp2f(-fmaf(ex.m, ex.k, -mk));
-            auto grad = [&](float v) __attribute__((always_inline)) {
-                return neg * (EXACT ? expo<true>(ex, v) : __builtin_amdgcn_exp2f(fmaf(v, ex.k, -mk)));
-            };
+            const float neg = ends[1], at_y = ends[2];
+            auto grad = [&](float v) __attribute__((always_inline)) { return neg * expo<EXACT>(ex, v); };
             char* dl = (char*)((T*)a.dlogits + (int64_t)j * a.dstride);
             const unsigned yv = (unsigned)(r.y >> (VN == 8 ? 3 : 2)) * 16u;
             const int ye = r.y & (VN - 1);

@@ -587,15 +587,14 @@ def _check_loss(got, want, l, y, dtype, scale, wsum, policy):
     fine = rlp.isfinite()
     tol_lp = torch.where(fine, e + 4 * U * (rlp.abs() + (l.to(F64) * scale).abs().amax(1)), 0.0).nan_to_num(0.0, 0.0, 0.0)
     close(lp, rlp, tol_lp, "logp")
-    worst = float(tol_lp.max()) if tol_lp.numel() else 0.0
+    rel = (8 * tol_lp + 64 * U)[:, None]
     if dl is not None:
-        rel = 8 * worst + 64 * U
         # a row's coefficient and p are off by `rel`; where the policy's two terms cancel, by that of the larger: 4 * |w / norm| bounds them
         tol = EPS[dtype] * rd.abs() + rel * (rd.abs() + (wsum[:, None] * (rd.abs() / coef.abs().clamp(min=1e-30)[:, None])))
         # the target's value is coef * (1 - p), p = exp(lp): an error of lp moves it by coef * p * error, whatever is left of 1 - p
-        tol.scatter_add_(1, y.clamp(0, V - 1)[:, None], (worst * coef.abs() * rlp.exp()).nan_to_num(0.0, 0.0, 0.0)[:, None])
+        tol.scatter_add_(1, y.clamp(0, V - 1)[:, None], (tol_lp * coef.abs() * rlp.exp()).nan_to_num(0.0, 0.0, 0.0)[:, None])
         close(dl, rd, tol, "dlogits")
-    close(stats, rs, 16 * worst * float(wsum.sum()) + 4 * U * rs.abs().nan_to_num(0.0, 0.0, 0.0), "stats")
+    close(stats, rs, 16 * float((tol_lp * wsum).sum()) + 4 * U * rs.abs().nan_to_num(0.0, 0.0, 0.0), "stats")
 
 
 LOSS = [(1, 1), (5, 7), (3, 8), (4, 9), (6, 64), (2, 511), (3, 512), (2, 1028), (2, 2056), (3, 2064), (2, 4099), (1, 32776), (2, 65544), (9, 32000), (3, 50257), (2, 128256), (2, 131077), (1, 262147)]
