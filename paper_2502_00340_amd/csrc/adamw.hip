@@ -2,15 +2,15 @@
 // parameter and states out.
 //
 // The tensors' pointers travel in the kernel arguments (4 KB at most), so that a call needs no table in device memory and can be captured;
-// a launch covers up to 40 tensors, a block CHUNK elements of one of them.  8-bit states have a scale for every 256 elements of a
-// tensor, which a wave owns four at a time.
+// a launch covers up to 40 tensors, a block CHUNK elements of one of them, a lane 8 of these.  8-bit states have a scale for every 256
+// elements of a tensor, the ones of half a wave.
 #include <initializer_list>
 
 #include "common.h"
 
 namespace cf {
 
-constexpr int ADAM_TENSORS = 40, CHUNK = 4096, QBLOCK = 256;
+constexpr int ADAM_TENSORS = 40, LANE = 8, CHUNK = 256 * LANE, QBLOCK = 256;
 
 struct AdamTensor {
     void* p;
@@ -20,50 +20,51 @@ struct AdamTensor {
     float *ms, *vs;
     int64_t n;
     float wd;
-    int32_t end;            // blocks of this tensor and the ones before it
 };
 struct AdamArgs {
-    double beta1, beta2, lr;
-    float b1, b2, c1, c2;   // beta, 1 - beta
-    float eps;
-    int32_t step;
-    uint32_t seed;
-    int32_t first;          // number of the first tensor in the call
+    int32_t end[ADAM_TENSORS];      // blocks of a tensor and the ones before it; of those behind the last INT_MAX
+    AdamTensor t[ADAM_TENSORS];
+    double beta1, beta2;
+    float b1, b2, c1, c2;           // beta, 1 - beta
+    float eps, lr, size, inv_root;  // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+    uint32_t step, seed;
+    int32_t first;                  // number of the first tensor in the call
     float grad_scale, max_norm;
     const float *norm_dev, *lr_dev;
     const int32_t* step_dev;
-    int32_t n_tensors;
-    AdamTensor t[ADAM_TENSORS];
 };
 static_assert(sizeof(AdamArgs) <= 4096, "kernel arguments");
 
 // A step's scalars, the same for all elements
 struct AdamStep {
-    float clip, size, inv_root, decay;      // of the gradient; lr / (1 - beta1^t); 1 / sqrt(1 - beta2^t); lr
+    float clip, size, inv_root, lr;
     uint32_t step;
 };
 
-__device__ __forceinline__ double int_pow(double b, unsigned n) {
+__host__ __device__ inline double int_pow(double b, unsigned n) {
     double r = 1.;
     for (; n != 0; n >>= 1, b *= b)
         if (n & 1) r *= b;
     return r;
 }
+__host__ __device__ inline void adam_scalars(double beta1, double beta2, double lr, unsigned step, float& size, float& inv_root) {
+    size = (float)(lr / (1. - int_pow(beta1, step)));
+    inv_root = (float)(1. / sqrt(1. - int_pow(beta2, step)));
+}
 
 // false: the norm is not finite, the step is left out
 __device__ __forceinline__ bool adam_step(const AdamArgs& a, AdamStep& s) {
-    s.clip = a.grad_scale;
+    s = AdamStep{a.grad_scale, a.size, a.inv_root, a.lr, a.step};
     if (a.norm_dev != nullptr) {
         const float norm = *a.norm_dev;
         if (!(norm - norm == 0.f)) return false;
         s.clip *= fminf(1.f, a.max_norm / (norm + 1e-6f));
     }
-    const int t = a.step_dev != nullptr ? *a.step_dev : a.step;
-    s.step = t < 1 ? 1 : t;
-    const double lr = a.lr_dev != nullptr ? (double)*a.lr_dev : a.lr;
-    s.decay = (float)lr;
-    s.size = (float)(lr / (1. - int_pow(a.beta1, s.step)));
-    s.inv_root = (float)(1. / sqrt(1. - int_pow(a.beta2, s.step)));
+    if (a.step_dev != nullptr || a.lr_dev != nullptr) {
+        if (a.lr_dev != nullptr) s.lr = *a.lr_dev;
+        if (a.step_dev != nullptr) { const int t = *a.step_dev; s.step = t < 1 ? 1 : t; }
+        adam_scalars(a.beta1, a.beta2, s.lr, s.step, s.size, s.inv_root);
+    }
     return true;
 }
 
@@ -76,85 +77,146 @@ __device__ __forceinline__ float rounded(float a, float b) {
     return p;
 }
 
-__device__ __forceinline__ void adam_one(const AdamArgs& a, const AdamStep& s, float wd, float g, float& w, float& m, float& v) {
-    g = rounded(g, s.clip);
-    m = rounded(a.b1, m) + rounded(a.c1, g);
-    v = rounded(a.b2, v) + rounded(a.c2, rounded(g, g));
-    w = w - s.decay * wd * w - s.size * m / (sqrtf(v) * s.inv_root + a.eps);
+// The square root of a normal number to half a step: the hardware's, which is off by one, and what a fused residual says is missing.  A third of the
+// instructions of sqrtf, which an element of an 8-bit state has not the time for next to its 18 bytes.
+__device__ __forceinline__ float root(float v) {
+    const float s = __builtin_amdgcn_sqrtf(v);
+    return fmaf(fmaf(-s, s, v), 0.5f * __builtin_amdgcn_rcpf(fmaxf(s, 0x1p-70f)), s);
 }
 
-// four elements from i on, of which `left` exist
-template <typename T> __device__ __forceinline__ void load4(const T* p, int64_t left, float (&o)[4]);
-template <> __device__ __forceinline__ void load4<float>(const float* p, int64_t left, float (&o)[4]) {
-    if (left >= 4) Vec<float>::load(p, o);
-    else
+// LANE elements from i on, of which `left` exist: all of them, unless TAIL
+template <typename T, bool TAIL> __device__ __forceinline__ void load_lane(const T* p, int64_t left, float (&o)[LANE]) {
+    if (TAIL && left < LANE) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = e < left ? p[e] : 0.f;
-}
-template <> __device__ __forceinline__ void load4<bf16_t>(const bf16_t* p, int64_t left, float (&o)[4]) {
-    if (left >= 4) {
-        const uint2 u = *reinterpret_cast<const uint2*>(p);
-        o[0] = __uint_as_float(u.x << 16); o[1] = __uint_as_float(u.x & 0xFFFF0000u);
-        o[2] = __uint_as_float(u.y << 16); o[3] = __uint_as_float(u.y & 0xFFFF0000u);
-    } else
+        for (int e = 0; e < LANE; ++e) o[e] = e < left ? to_f32<T>(p[e]) : 0.f;
+        return;
+    }
+    constexpr int VN = Vec<T>::N;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = e < left ? bf16_to_f32(p[e]) : 0.f;
+    for (int q = 0; q < LANE / VN; ++q) Vec<T>::load(p + q * VN, reinterpret_cast<float (&)[VN]>(o[q * VN]));
 }
-template <typename T> __device__ __forceinline__ void store4(T* p, int64_t left, const float (&o)[4]);
-template <> __device__ __forceinline__ void store4<float>(float* p, int64_t left, const float (&o)[4]) {
-    if (left >= 4) Vec<float>::store(p, o);
-    else
+template <typename T, bool TAIL> __device__ __forceinline__ void store_lane(T* p, int64_t left, const float (&o)[LANE]) {
+    constexpr int VN = Vec<T>::N;
+    if (TAIL && left < LANE) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < left) p[e] = o[e];
-}
-template <> __device__ __forceinline__ void store4<bf16_t>(bf16_t* p, int64_t left, const float (&o)[4]) {
-    if (left >= 4) *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
-    else
+        for (int e = 0; e < LANE; ++e)
+            if (e < left) {
+                if constexpr (VN == 8) p[e] = (T)pack_bf16x2(o[e], 0.f);
+                else p[e] = o[e];
+            }
+        return;
+    }
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < left) p[e] = (bf16_t)pack_bf16x2(o[e], 0.f);
+    for (int q = 0; q < LANE / VN; ++q) Vec<T>::store(p + q * VN, reinterpret_cast<const float (&)[VN]>(o[q * VN]));
 }
-// four e4m3 bytes
-__device__ __forceinline__ unsigned load4_q(const unsigned char* p, int64_t left) {
-    if (left >= 4) return *reinterpret_cast<const unsigned*>(p);
-    unsigned r = 0;
+// LANE e4m3 bytes
+template <bool TAIL> __device__ __forceinline__ uint2 load_bytes(const unsigned char* p, int64_t left) {
+    if (!TAIL || left >= LANE) return *reinterpret_cast<const uint2*>(p);
+    unsigned w[2] = {0u, 0u};
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (e < left) r |= (unsigned)p[e] << (8 * e);
-    return r;
+    for (int e = 0; e < LANE; ++e)
+        if (e < left) w[e / 4] |= (unsigned)p[e] << (8 * (e % 4));
+    return make_uint2(w[0], w[1]);
 }
-__device__ __forceinline__ void store4_q(unsigned char* p, int64_t left, unsigned q) {
-    if (left >= 4) { *reinterpret_cast<unsigned*>(p) = q; return; }
+template <bool TAIL> __device__ __forceinline__ void store_bytes(unsigned char* p, int64_t left, uint2 q) {
+    if (!TAIL || left >= LANE) { *reinterpret_cast<uint2*>(p) = q; return; }
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (e < left) p[e] = (unsigned char)(q >> (8 * e));
+    for (int e = 0; e < LANE; ++e)
+        if (e < left) p[e] = (unsigned char)((e < 4 ? q.x : q.y) >> (8 * (e % 4)));
 }
-__device__ __forceinline__ void from_q(unsigned q, float scale, float (&o)[4]) {
+__device__ __forceinline__ void from_q(uint2 q, float scale, float (&o)[LANE]) {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
-    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)q, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)q, true);
-    o[0] = rounded(a[0], scale); o[1] = rounded(a[1], scale); o[2] = rounded(b[0], scale); o[3] = rounded(b[1], scale);
-}
-__device__ __forceinline__ unsigned to_q(const float (&x)[4]) {
-    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false), true);
-}
-__device__ __forceinline__ float wave_max(float v) {
+    const unsigned w[2] = {q.x, q.y};
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    return v;
+    for (int i = 0; i < 2; ++i) {
+        const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
+        o[4 * i] = rounded(a[0], scale); o[4 * i + 1] = rounded(a[1], scale);
+        o[4 * i + 2] = rounded(b[0], scale); o[4 * i + 3] = rounded(b[1], scale);
+    }
 }
-// 20 bits of a hash of an element (the finaliser of MurmurHash3 over its number and the tensor's key) as a number in [0, 1)
-__device__ __forceinline__ float dither(uint32_t key, int64_t i) {
-    uint32_t h = (uint32_t)i * 0x9E3779B1u + (uint32_t)(i >> 32) * 0x27D4EB2Fu + key;
+__device__ __forceinline__ uint2 to_q(const float (&x)[LANE]) {
+    return make_uint2(__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false), true),
+                      __builtin_amdgcn_cvt_pk_fp8_f32(x[6], x[7], __builtin_amdgcn_cvt_pk_fp8_f32(x[4], x[5], 0, false), true));
+}
+// over the 32 lanes of a scale
+__device__ __forceinline__ float block_max(float v) {
+#pragma unroll
+    for (int o = QBLOCK / LANE / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    return fmaxf(v, 0x1p-100f);
+}
+// 20 bits of a hash of an element (the finaliser of MurmurHash3 over its number and the tensor's key)
+__device__ __forceinline__ uint32_t dither(uint32_t h) {
     h = (h ^ (h >> 16)) * 0x85EBCA6Bu;
     h = (h ^ (h >> 13)) * 0xC2B2AE35u;
-    return (float)((h ^ (h >> 16)) >> 12) * 0x1p-20f;
+    return (h ^ (h >> 16)) >> 12;
 }
-// r > 0 in units of the scale, rounded up to the next e4m3 value where what is cut off is 1 - u of a step or more; not to 0
-__device__ __forceinline__ float round_up_by(float r, float u) {
+// r in units of the scale, rounded up to the next e4m3 value where what is cut off and the dither make a step together; not to 0
+__device__ __forceinline__ float round_up_by(float r, uint32_t u) {
     const unsigned e = __float_as_uint(fmaxf(r, 0x1p-6f)) & 0x7F800000u;
     const float ulp = __uint_as_float(e - (3u << 23)), inv = __uint_as_float((257u << 23) - e);     // 2^(e-3) and its inverse
-    return r > 0.f ? fminf(fmaxf(floorf(r * inv + u) * ulp, 0x1p-9f), 448.f) : r;
+    const float q = floorf(fmaf((float)u, 0x1p-20f, r * inv)) * ulp;
+    return r > 0.f ? fminf(fmaxf(q, 0x1p-9f), 448.f) : r;
+}
+
+template <typename P, typename G, bool MASTER, int BITS, bool TAIL>
+__device__ __forceinline__ void adamw_block(const AdamArgs& a, const AdamTensor& t, const AdamStep& s, uint32_t key, int64_t i) {
+    const int64_t left = t.n - i;
+    if (TAIL && left <= -QBLOCK) return;            // the other lanes of a block of scales stay for its maximum
+    float g[LANE], w[LANE], m[LANE], v[LANE];
+    const int64_t blk = i / QBLOCK;
+    float ms = 0.f, vs = 0.f;
+    uint2 qm, qv;
+    load_lane<G, TAIL>((const G*)t.g + i, left, g);
+    if (MASTER) load_lane<float, TAIL>(t.master + i, left, w);
+    else load_lane<P, TAIL>((const P*)t.p + i, left, w);
+    if constexpr (BITS == 32) {
+        load_lane<float, TAIL>((const float*)t.m + i, left, m);
+        load_lane<float, TAIL>((const float*)t.v + i, left, v);
+    } else {
+        qm = load_bytes<TAIL>((const unsigned char*)t.m + i, left);
+        qv = load_bytes<TAIL>((const unsigned char*)t.v + i, left);
+        if (!TAIL || left > 0) { ms = t.ms[blk]; vs = t.vs[blk]; }
+        from_q(qm, ms, m);
+        from_q(qv, vs, v);
+    }
+    const float keep = 1.f - s.lr * t.wd;
+    float tm = 0.f, tv = 0.f;
+#pragma unroll
+    for (int e = 0; e < LANE; ++e) {
+        if (BITS == 8) v[e] = rounded(v[e], v[e]);
+        const float x = rounded(g[e], s.clip);
+        m[e] = rounded(a.b1, m[e]) + rounded(a.c1, x);
+        v[e] = rounded(a.b2, v[e]) + rounded(a.c2, rounded(x, x));
+        const float r = root(v[e]);
+        w[e] = fmaf(-s.size * m[e], __builtin_amdgcn_rcpf(fmaf(r, s.inv_root, a.eps)), w[e] * keep);
+        if (BITS == 8) {
+            v[e] = r;
+            tm = fmaxf(tm, fabsf(m[e]));            // of what does not exist: zeros
+            tv = fmaxf(tv, r);
+        }
+    }
+    if (MASTER) store_lane<float, TAIL>(t.master + i, left, w);
+    store_lane<P, TAIL>((P*)t.p + i, left, w);
+    if constexpr (BITS == 32) {
+        store_lane<float, TAIL>((float*)t.m + i, left, m);
+        store_lane<float, TAIL>((float*)t.v + i, left, v);
+    } else {
+        tm = block_max(tm);
+        tv = block_max(tv);
+        const float im = rounded(1.f / tm, 448.f), iv = rounded(1.f / tv, 448.f);
+        const uint32_t h = (uint32_t)i * 0x9E3779B1u + (uint32_t)(i >> 32) * 0x27D4EB2Fu + key;
+#pragma unroll
+        for (int e = 0; e < LANE; ++e) {
+            m[e] *= im;
+            v[e] = round_up_by(rounded(v[e], iv), dither(h + e * 0x9E3779B1u));
+        }
+        store_bytes<TAIL>((unsigned char*)t.m + i, left, to_q(m));
+        store_bytes<TAIL>((unsigned char*)t.v + i, left, to_q(v));
+        if (threadIdx.x % (QBLOCK / LANE) == 0 && (!TAIL || left > 0)) {
+            t.ms[blk] = tm * (1.f / 448.f);
+            t.vs[blk] = tv * (1.f / 448.f);
+        }
+    }
 }
 
 template <typename P, typename G, bool MASTER, int BITS>
@@ -162,63 +224,17 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
     AdamStep s;
     if (!adam_step(a, s)) return;
     int k = 0;
-    while ((int)blockIdx.x >= a.t[k].end) ++k;          // the grid has t[n_tensors - 1].end blocks
+#pragma unroll
+    for (int i = 0; i < ADAM_TENSORS; ++i) k += (int)blockIdx.x >= a.end[i];
     const AdamTensor& t = a.t[k];
-    const int64_t at = (int64_t)((int)blockIdx.x - (k > 0 ? a.t[k - 1].end : 0)) * CHUNK;
+    const int64_t at = (int64_t)((int)blockIdx.x - (k > 0 ? a.end[k - 1] : 0)) * CHUNK, i = at + threadIdx.x * LANE;
     const uint32_t key = a.seed + 0x85EBCA77u * (uint32_t)(a.first + k + 1) + 0xC2B2AE3Du * s.step;
-#pragma unroll
-    for (int r = 0; r < CHUNK / 1024; ++r) {
-        const int64_t i = at + r * 1024 + threadIdx.x * 4, left = t.n - i;      // a wave has 256 elements: one scale
-        float g[4], w[4], m[4], v[4];
-        load4<G>((const G*)t.g + i, left, g);
-        if (MASTER) load4<float>(t.master + i, left, w);
-        else load4<P>((const P*)t.p + i, left, w);
-        const int64_t blk = i / QBLOCK;
-        if constexpr (BITS == 32) {
-            load4<float>((const float*)t.m + i, left, m);
-            load4<float>((const float*)t.v + i, left, v);
-        } else {
-            const bool any = blk * QBLOCK < t.n;
-            from_q(load4_q((const unsigned char*)t.m + i, left), any ? t.ms[blk] : 0.f, m);
-            from_q(load4_q((const unsigned char*)t.v + i, left), any ? t.vs[blk] : 0.f, v);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = rounded(v[e], v[e]);
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) adam_one(a, s, t.wd, g[e], w[e], m[e], v[e]);
-        if (MASTER) store4<float>(t.master + i, left, w);
-        store4<P>((P*)t.p + i, left, w);
-        if constexpr (BITS == 32) {
-            store4<float>((float*)t.m + i, left, m);
-            store4<float>((float*)t.v + i, left, v);
-        } else {
-            float tm = 0.f, tv = 0.f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v[e] = sqrtf(v[e]);
-                tm = fmaxf(tm, e < left ? fabsf(m[e]) : 0.f);
-                tv = fmaxf(tv, e < left ? v[e] : 0.f);
-            }
-            tm = fmaxf(wave_max(tm), 0x1p-100f);
-            tv = fmaxf(wave_max(tv), 0x1p-100f);
-            const float im = rounded(1.f / tm, 448.f), iv = rounded(1.f / tv, 448.f);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                m[e] *= im;
-                v[e] = round_up_by(rounded(v[e], iv), dither(key, i + e));
-            }
-            store4_q((unsigned char*)t.m + i, left, to_q(m));
-            store4_q((unsigned char*)t.v + i, left, to_q(v));
-            if ((threadIdx.x & 63) == 0 && left > 0) {
-                t.ms[blk] = tm * (1.f / 448.f);
-                t.vs[blk] = tv * (1.f / 448.f);
-            }
-        }
-    }
+    if (at + CHUNK <= t.n) adamw_block<P, G, MASTER, BITS, false>(a, t, s, key, i);
+    else adamw_block<P, G, MASTER, BITS, true>(a, t, s, key, i);
 }
 
 // ---- global norm -----------------------------------------------------------
-constexpr int NORM_TENSORS = 160, NORM_BLOCKS = 2048, NORM_CHUNK = 8192;
+constexpr int NORM_TENSORS = 160, NORM_BLOCKS = 2048, NORM_CHUNK = 4 * CHUNK;
 struct NormArgs {
     const void* g[NORM_TENSORS];
     int64_t n[NORM_TENSORS];
@@ -234,26 +250,28 @@ __device__ __forceinline__ double wave_sum64(double v) {
 }
 
 // partial[block]: sum of the squares of the block's chunks, in fp64, where no square overflows
+template <typename G, bool TAIL> __device__ __forceinline__ void add_squares(const G* g, int64_t left, double (&s)[2]) {
+    float x[NORM_CHUNK / CHUNK][LANE];
+#pragma unroll
+    for (int r = 0; r < NORM_CHUNK / CHUNK; ++r) load_lane<G, TAIL>(g + r * CHUNK, left - r * CHUNK, x[r]);
+#pragma unroll
+    for (int r = 0; r < NORM_CHUNK / CHUNK; ++r)
+#pragma unroll
+        for (int e = 0; e < LANE; ++e) s[e & 1] = fma((double)x[r][e], (double)x[r][e], s[e & 1]);
+}
 template <typename G>
 __global__ __launch_bounds__(256) void grad_norm_kernel(NormArgs a, double* __restrict__ partial) {
     __shared__ double red[4];
-    double s = 0.;
+    double s[2] = {0., 0.};
     int k = 0;
     for (int c = blockIdx.x; c < a.end[a.n_tensors - 1]; c += gridDim.x) {
         while (c >= a.end[k]) ++k;
-        const G* g = (const G*)a.g[k];
-        const int64_t at = (int64_t)(c - (k > 0 ? a.end[k - 1] : 0)) * NORM_CHUNK;
-#pragma unroll
-        for (int r = 0; r < NORM_CHUNK / 1024; ++r) {
-            const int64_t i = at + r * 1024 + threadIdx.x * 4;
-            float x[4];
-            load4<G>(g + i, a.n[k] - i, x);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s += (double)x[e] * (double)x[e];
-        }
+        const int64_t at = (int64_t)(c - (k > 0 ? a.end[k - 1] : 0)) * NORM_CHUNK, i = at + threadIdx.x * LANE, n = a.n[k];
+        if (at + NORM_CHUNK <= n) add_squares<G, false>((const G*)a.g[k] + i, n - i, s);
+        else add_squares<G, true>((const G*)a.g[k] + i, n - i, s);
     }
-    s = wave_sum64(s);
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+    const double t = wave_sum64(s[0] + s[1]);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = t;
     __syncthreads();
     if (threadIdx.x == 0) partial[blockIdx.x] = red[0] + red[1] + red[2] + red[3];
 }
@@ -278,13 +296,13 @@ bool off(const void* p, size_t a) { return (uintptr_t)p % a != 0; }
 bool is_finite(double v) { return v - v == 0.; }
 
 template <typename P, typename G, bool MASTER, int BITS>
-void adamw_launch(const AdamArgs& a, hipStream_t st) {
-    adamw_kernel<P, G, MASTER, BITS><<<a.t[a.n_tensors - 1].end, 256, 0, st>>>(a);
+void adamw_launch(const AdamArgs& a, int grid, hipStream_t st) {
+    adamw_kernel<P, G, MASTER, BITS><<<grid, 256, 0, st>>>(a);
 }
 template <typename P, bool MASTER>
-void adamw_dispatch(const AdamArgs& a, bool g32, bool bits8, hipStream_t st) {
-    if (g32) bits8 ? adamw_launch<P, float, MASTER, 8>(a, st) : adamw_launch<P, float, MASTER, 32>(a, st);
-    else bits8 ? adamw_launch<P, bf16_t, MASTER, 8>(a, st) : adamw_launch<P, bf16_t, MASTER, 32>(a, st);
+void adamw_dispatch(const AdamArgs& a, int grid, bool g32, bool bits8, hipStream_t st) {
+    if (g32) bits8 ? adamw_launch<P, float, MASTER, 8>(a, grid, st) : adamw_launch<P, float, MASTER, 32>(a, grid, st);
+    else bits8 ? adamw_launch<P, bf16_t, MASTER, 8>(a, grid, st) : adamw_launch<P, bf16_t, MASTER, 32>(a, grid, st);
 }
 
 }  // namespace
@@ -317,26 +335,29 @@ cf_status cf_adamw_step(const cf_adamw_desc* d, const cf_adamw_tensor* tensors, 
     if (master && (plain || d->p_dtype == CF_F32)) return CF_ERR_SHAPE;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     AdamArgs a{};
-    a.beta1 = d->beta1; a.beta2 = d->beta2; a.lr = d->lr;
+    a.beta1 = d->beta1; a.beta2 = d->beta2; a.lr = (float)d->lr;
     a.b1 = (float)d->beta1; a.b2 = (float)d->beta2; a.c1 = (float)(1. - d->beta1); a.c2 = (float)(1. - d->beta2);
-    a.eps = (float)d->eps; a.step = d->step; a.seed = d->seed;
+    a.eps = (float)d->eps; a.step = d->step < 1 ? 1 : d->step; a.seed = d->seed;
+    adam_scalars(a.beta1, a.beta2, d->lr, a.step, a.size, a.inv_root);
     a.grad_scale = d->grad_scale; a.max_norm = d->max_norm;
     a.norm_dev = d->norm_dev; a.lr_dev = d->lr_dev; a.step_dev = d->step_dev;
     int k = 0;
     while (k < n_tensors) {
         // as many tensors as the arguments hold; of 2^35 elements at most each, their blocks are counted in 32 bits
-        a.first = k; a.n_tensors = 0;
+        a.first = k;
         int64_t blocks = 0;
-        for (; k < n_tensors && a.n_tensors < ADAM_TENSORS; ++k) {
-            const cf_adamw_tensor& t = tensors[k];
-            const int64_t b = (t.n + CHUNK - 1) / CHUNK;
-            blocks += b;
-            a.t[a.n_tensors++] = AdamTensor{t.p, t.master, t.g, t.m, t.v, t.m_scale, t.v_scale, t.n, t.weight_decay, (int32_t)blocks};
+        for (int i = 0; i < ADAM_TENSORS; ++i) {
+            a.end[i] = INT32_MAX;
+            if (k >= n_tensors) continue;
+            const cf_adamw_tensor& t = tensors[k++];
+            blocks += (t.n + CHUNK - 1) / CHUNK;
+            a.t[i] = AdamTensor{t.p, t.master, t.g, t.m, t.v, t.m_scale, t.v_scale, t.n, t.weight_decay};
+            a.end[i] = (int32_t)blocks;
         }
         if (blocks == 0) continue;
-        if (d->p_dtype == CF_F32) adamw_dispatch<float, false>(a, d->g_dtype == CF_F32, bits8, st);
-        else if (master) adamw_dispatch<bf16_t, true>(a, d->g_dtype == CF_F32, bits8, st);
-        else adamw_dispatch<bf16_t, false>(a, d->g_dtype == CF_F32, bits8, st);
+        if (d->p_dtype == CF_F32) adamw_dispatch<float, false>(a, (int)blocks, d->g_dtype == CF_F32, bits8, st);
+        else if (master) adamw_dispatch<bf16_t, true>(a, (int)blocks, d->g_dtype == CF_F32, bits8, st);
+        else adamw_dispatch<bf16_t, false>(a, (int)blocks, d->g_dtype == CF_F32, bits8, st);
         if (hipGetLastError() != hipSuccess) return CF_ERR_HIP;
     }
     return CF_OK;
