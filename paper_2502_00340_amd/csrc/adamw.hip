@@ -95,7 +95,10 @@ template <typename T, bool TAIL> __device__ __forceinline__ void load_lane(const
 #pragma unroll
     for (int q = 0; q < LANE / VN; ++q) Vec<T>::load(p + q * VN, reinterpret_cast<float (&)[VN]>(o[q * VN]));
 }
-template <typename T, bool TAIL> __device__ __forceinline__ void store_lane(T* p, int64_t left, const float (&o)[LANE]) {
+// AWAY: past the caches
+typedef float f32x4a __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2a __attribute__((ext_vector_type(2)));
+template <typename T, bool TAIL, bool AWAY = false> __device__ __forceinline__ void store_lane(T* p, int64_t left, const float (&o)[LANE]) {
     constexpr int VN = Vec<T>::N;
     if (TAIL && left < LANE) {
 #pragma unroll
@@ -107,7 +110,10 @@ template <typename T, bool TAIL> __device__ __forceinline__ void store_lane(T* p
         return;
     }
 #pragma unroll
-    for (int q = 0; q < LANE / VN; ++q) Vec<T>::store(p + q * VN, reinterpret_cast<const float (&)[VN]>(o[q * VN]));
+    for (int q = 0; q < LANE / VN; ++q) {
+        if constexpr (AWAY) __builtin_nontemporal_store(f32x4a{o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]}, reinterpret_cast<f32x4a*>(p) + q);
+        else Vec<T>::store(p + q * VN, reinterpret_cast<const float (&)[VN]>(o[q * VN]));
+    }
 }
 // LANE e4m3 bytes
 template <bool TAIL> __device__ __forceinline__ uint2 load_bytes(const unsigned char* p, int64_t left) {
@@ -119,7 +125,7 @@ template <bool TAIL> __device__ __forceinline__ uint2 load_bytes(const unsigned 
     return make_uint2(w[0], w[1]);
 }
 template <bool TAIL> __device__ __forceinline__ void store_bytes(unsigned char* p, int64_t left, uint2 q) {
-    if (!TAIL || left >= LANE) { *reinterpret_cast<uint2*>(p) = q; return; }
+    if (!TAIL || left >= LANE) { __builtin_nontemporal_store(u32x2a{q.x, q.y}, reinterpret_cast<u32x2a*>(p)); return; }
 #pragma unroll
     for (int e = 0; e < LANE; ++e)
         if (e < left) p[e] = (unsigned char)((e < 4 ? q.x : q.y) >> (8 * (e % 4)));
@@ -195,11 +201,11 @@ __device__ __forceinline__ void adamw_block(const AdamArgs& a, const AdamTensor&
             tv = fmaxf(tv, r);
         }
     }
-    if (MASTER) store_lane<float, TAIL>(t.master + i, left, w);
-    store_lane<P, TAIL>((P*)t.p + i, left, w);
+    if (MASTER) store_lane<float, TAIL, true>(t.master + i, left, w);
+    store_lane<P, TAIL, (Vec<P>::N == 4)>((P*)t.p + i, left, w);
     if constexpr (BITS == 32) {
-        store_lane<float, TAIL>((float*)t.m + i, left, m);
-        store_lane<float, TAIL>((float*)t.v + i, left, v);
+        store_lane<float, TAIL, true>((float*)t.m + i, left, m);
+        store_lane<float, TAIL, true>((float*)t.v + i, left, v);
     } else {
         tm = block_max(tm);
         tv = block_max(tv);
