@@ -517,52 +517,54 @@ def _need(ok, what: str):
         raise ValueError(what)
 
 
-def _on(device, **tensors):
-    """Every tensor given lies on `device`, which has to be the current one: the library launches on its current stream."""
-    _need(device.type == "cuda" and device.index == torch.cuda.current_device(), "tensors have to be on the current GPU, not on %s" % device)
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
+def _on(tensors):
+    """Every tensor given (None apart) lies on the current GPU: the library launches on its current stream.  Returns its number."""
+    now = torch.cuda.current_device() if torch.cuda.is_initialized() else -2
+    for t in tensors:
+        if t is not None and t.get_device() != now:
+            raise ValueError("a tensor is on %s, not on the current GPU" % t.device)
+    return now
 
 
-def _qk_rows(desc: LayerDesc, q, k, what: str, dtype):
-    """A cf_qk of q [n, Hq*d] and k [n, Hkv*d]: dense columns, any stride from row to row."""
-    for t, h in ((q, desc.Hq), (k, desc.Hkv)):
-        if not (t.dim() == 2 and t.shape[1] == h * desc.d and t.dtype == dtype and (t.stride(1) == 1 or t.numel() == 0)):
-            raise ValueError("%s: expected %s [rows, %d] with dense columns, got %s %s, strides %s" %
-                             (what, dtype, h * desc.d, t.dtype, tuple(t.shape), t.stride()))
-    n = q.shape[0]
-    _need(k.shape[0] == n, "%s: q has %d rows, k %d" % (what, n, k.shape[0]))
-    # the stride of a single row means nothing
-    return Qk(_ptr(q), _ptr(k), q.stride(0) if n > 1 else 0, k.stride(0) if n > 1 else 0)
+def _qk_rows(desc: LayerDesc, q, k, what: str, dtype, Nq: int, Nkv: int):
+    """A cf_qk of q [n, Nq] and k [n, Nkv]: dense columns, any stride from row to row."""
+    if q.dim() == 2 and k.dim() == 2:
+        (n, w), (m, x), a, b = q.shape, k.shape, q.stride(), k.stride()
+        if w == Nq and x == Nkv and n == m and q.dtype is dtype and k.dtype is dtype:
+            if n > 1 and a[1] == 1 and b[1] == 1 and a[0] >= w and b[0] >= x:
+                return n, Qk(q.data_ptr(), k.data_ptr(), a[0], b[0])
+            if n == 0 or n == 1 and a[1] == 1 and b[1] == 1:
+                return n, Qk(_ptr(q), _ptr(k), 0, 0)           # the stride of a single row means nothing
+    raise ValueError("%s: expected %s [rows, %d] and [rows, %d] with dense columns, got %s %s, strides %s, and %s %s, strides %s" %
+                     (what, dtype, Nq, Nkv, q.dtype, tuple(q.shape), q.stride(), k.dtype, tuple(k.shape), k.stride()))
 
 
-def _qk_norm(desc: LayerDesc, gq, gk, rope_cos, rope_sin, positions, rows: int, dtype):
+def _qk_norm(desc: LayerDesc, d: int, gq, gk, rope_cos, rope_sin, positions, rows: int, dtype):
     for g in (gq, gk):
-        _need(g.dtype == dtype and g.shape == (desc.d,) and g.is_contiguous(), "gains have to be %s [%d]" % (dtype, desc.d))
-    _need((rope_cos is None) == (rope_sin is None), "rope_cos and rope_sin: both or neither")
-    for t in (rope_cos, rope_sin):
-        _need(t is None or (t.dtype == torch.float32 and t.shape == (desc.S, desc.d // 2) and t.is_contiguous()),
-              "rotary tables have to be fp32 [%d, %d], contiguous" % (desc.S, desc.d // 2))
-    _need(positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() >= rows),
-          "positions have to be int32, contiguous, one per row")
+        if g.dtype is not dtype or g.dim() != 1 or g.shape[0] != d or not g.is_contiguous():
+            raise ValueError("gains have to be %s [%d]" % (dtype, d))
+    if rope_cos is not None or rope_sin is not None:
+        for t in (rope_cos, rope_sin):
+            if t is None or t.dtype is not torch.float32 or t.shape != (desc.S, d // 2) or not t.is_contiguous():
+                raise ValueError("rope_cos and rope_sin have to be fp32 [%d, %d], contiguous, both or neither" % (desc.S, d // 2))
+    if positions is not None and (positions.dtype is not torch.int32 or not positions.is_contiguous() or positions.numel() < rows):
+        raise ValueError("positions have to be int32, contiguous, one per row")
     return QkNorm(gq.data_ptr(), gk.data_ptr(), _addr(rope_cos), _addr(rope_sin), None if positions is None else _ptr(positions))
 
 
 def qk_norm_rope_fwd(desc: LayerDesc, q, k, gq, gk, rope_cos=None, rope_sin=None, positions=None, out=None):
     """Norm of every query and key head and its rotation at positions[row] (row mod S without positions).  q [n, Hq*d] and k [n, Hkv*d] may be columns
     of a longer row (a fused projection).  out: a pair to write to, q and k themselves for a pass in place."""
-    dt = torch_dtype(desc)
-    rows = _qk_rows(desc, q, k, "q, k", dt)
-    n = q.shape[0]
-    p = _qk_norm(desc, gq, gk, rope_cos, rope_sin, positions, n, dt)
-    dev = q.device
+    dt, d = torch_dtype(desc), desc.d
+    Nq, Nkv = desc.Hq * d, desc.Hkv * d
+    n, rows = _qk_rows(desc, q, k, "q, k", dt, Nq, Nkv)
+    p = _qk_norm(desc, d, gq, gk, rope_cos, rope_sin, positions, n, dt)
     if out is None:
-        out = (torch.empty((n, desc.Hq * desc.d), dtype=dt, device=dev), torch.empty((n, desc.Hkv * desc.d), dtype=dt, device=dev))
-    to = _qk_rows(desc, out[0], out[1], "out", dt)
-    _need(out[0].shape[0] == n, "out has %d rows, not %d" % (out[0].shape[0], n))
-    _on(dev, k=k, gq=gq, gk=gk, rope_cos=rope_cos, rope_sin=rope_sin, positions=positions, out_q=out[0], out_k=out[1])
-    _check((_lib or lib()).cf_qk_norm_rope_fwd(C.byref(desc), C.byref(p), C.byref(rows), n, C.byref(to), _stream()), "cf_qk_norm_rope_fwd")
+        out = torch.empty_like(q), torch.empty_like(k)
+    m, to = _qk_rows(desc, out[0], out[1], "out", dt, Nq, Nkv)
+    _need(m == n, "out has another number of rows")
+    device = _on((q, k, gq, gk, rope_cos, rope_sin, positions, *out))
+    _check((_lib or lib()).cf_qk_norm_rope_fwd(C.byref(desc), C.byref(p), C.byref(rows), n, C.byref(to), _stream(device)), "cf_qk_norm_rope_fwd")
     return out
 
 
@@ -572,33 +574,41 @@ def _kept_count(idx, n_kept_dev, rows: int, kept: int):
     _need(n_kept_dev is None or (n_kept_dev.dtype == torch.int32 and n_kept_dev.numel() == 1), "n_kept_dev has to be one int32")
 
 
+@functools.lru_cache(maxsize=1024)
+def _qk_ws_bytes(d, code, n):
+    return lib().cf_qk_norm_workspace_bytes(C.byref(LayerDesc(1, 1, 8, 1, 1, d, 8, code, 0.0, 0.0)), n)
+
+
 def qk_norm_rope_bwd(desc: LayerDesc, q, k, gq, gk, dq, dk, rope_cos=None, rope_sin=None, positions=None, idx=None, n_kept_dev=None,
                      need_gains: bool = True, main_grads=None, out=None):
     """Backward of qk_norm_rope_fwd for compact dq [n, Hq*d], dk [n, Hkv*d]; q and k are its inputs at full length.  Returns (dx of q, dx of k, dgq, dgk).
     n_kept_dev: only the first min(*n_kept_dev, n) rows.  main_grads: fp32 (dgq, dgk) that are added to.  out: as in the forward pass."""
-    dt = torch_dtype(desc)
-    x, dy = _qk_rows(desc, q, k, "q, k", dt), _qk_rows(desc, dq, dk, "dq, dk", dt)
-    n, dev = dq.shape[0], dq.device
-    _kept_count(idx, n_kept_dev, q.shape[0], n)
-    p = _qk_norm(desc, gq, gk, rope_cos, rope_sin, positions, q.shape[0], dt)
+    dt, d = torch_dtype(desc), desc.d
+    Nq, Nkv = desc.Hq * d, desc.Hkv * d
+    rows, x = _qk_rows(desc, q, k, "q, k", dt, Nq, Nkv)
+    n, dy = _qk_rows(desc, dq, dk, "dq, dk", dt, Nq, Nkv)
+    _kept_count(idx, n_kept_dev, rows, n)
+    p = _qk_norm(desc, d, gq, gk, rope_cos, rope_sin, positions, rows, dt)
     if out is None:
-        out = (torch.empty((n, desc.Hq * desc.d), dtype=dt, device=dev), torch.empty((n, desc.Hkv * desc.d), dtype=dt, device=dev))
-    dx = _qk_rows(desc, out[0], out[1], "out", dt)
-    _need(out[0].shape[0] == n, "out has %d rows, not %d" % (out[0].shape[0], n))
-    dg, wsb, ws = (None, None), 0, None
-    if main_grads is not None or need_gains:
-        dg = main_grads if main_grads is not None else tuple(torch.empty(desc.d, dtype=dt, device=dev) for _ in range(2))
-        for t in dg:
-            _need(t.dtype == (dt if main_grads is None else torch.float32) and t.shape == (desc.d,) and t.is_contiguous(),
-                  "main_grads have to be fp32 [%d]" % desc.d)
-        wsb = lib().cf_qk_norm_workspace_bytes(C.byref(desc), n)
-        ws = torch.empty(wsb, dtype=torch.uint8, device=dev)
-    _on(dev, q=q, k=k, dk=dk, gq=gq, gk=gk, rope_cos=rope_cos, rope_sin=rope_sin, positions=positions, idx=idx, n_kept_dev=n_kept_dev,
-        out_q=out[0], out_k=out[1], dgq=dg[0], dgk=dg[1])
+        out = torch.empty_like(dq), torch.empty_like(dk)
+    m, dx = _qk_rows(desc, out[0], out[1], "out", dt, Nq, Nkv)
+    _need(m == n, "out has another number of rows")
+    dgq = dgk = ws = None
+    wsb = 0
+    if main_grads is not None:
+        dgq, dgk = main_grads
+        for t in main_grads:
+            _need(t.dtype is torch.float32 and t.shape == (d,) and t.is_contiguous(), "main_grads have to be fp32 [%d]" % d)
+    elif need_gains:
+        dgq, dgk = torch.empty_like(gq), torch.empty_like(gk)
+    if dgq is not None:
+        wsb = _qk_ws_bytes(d, desc.dtype, n)
+        ws = torch.empty(wsb, dtype=torch.uint8, device=dq.device)
+    device = _on((q, k, gq, gk, dq, dk, rope_cos, rope_sin, positions, idx, n_kept_dev, dgq, dgk, *out))
     _check((_lib or lib()).cf_qk_norm_rope_bwd(C.byref(desc), C.byref(p), C.byref(x), C.byref(dy), None if idx is None else _ptr(idx),
-                                               _addr(n_kept_dev), n, C.byref(dx), _addr(dg[0]), _addr(dg[1]), int(main_grads is not None),
-                                               _addr(ws), wsb, _stream()), "cf_qk_norm_rope_bwd")
-    return out[0], out[1], dg[0], dg[1]
+                                               _addr(n_kept_dev), n, C.byref(dx), _addr(dgq), _addr(dgk), int(main_grads is not None),
+                                               _addr(ws), wsb, _stream(device)), "cf_qk_norm_rope_bwd")
+    return out[0], out[1], dgq, dgk
 
 
 def token_loss(logits, targets, old_logp=None, advantages=None, ref_logp=None, weights=None, clip=(0.2, 0.2), kl_coef: float = 0.0,
@@ -607,36 +617,35 @@ def token_loss(logits, targets, old_logp=None, advantages=None, ref_logp=None, w
     the clipped policy loss.  Per-row tensors are fp32 [rows] and read, like logits, at idx[j] (row j without idx).  Returns (stats [4]: loss, its first term, KL, clipped share;
     logp [max_kept]; dlogits [max_kept, V] or None).  max_kept: by default all of idx, or all rows.  out: dlogits to write to,
     logits itself for a gradient in place (without idx)."""
-    _need(logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] == 1), "logits have to be [rows, V] with dense columns")
-    rows, V = logits.shape
-    dev = logits.device
+    _need(logits.dim() == 2, "logits have to be [rows, V]")
+    (rows, V), (ls, dense) = logits.shape, logits.stride()
+    _need((dense == 1 or V == 1) and (ls >= V or rows < 2), "logits have to have dense columns, and rows that do not overlap")
     n = max_kept if max_kept is not None else rows if idx is None else idx.numel()
     _kept_count(idx, n_kept_dev, rows, n)
-    _need(targets.dtype == torch.int64 and targets.shape == (rows,) and targets.is_contiguous(), "targets have to be int64 [%d]" % rows)
+    _need(targets.dtype is torch.int64 and targets.shape == (rows,) and targets.is_contiguous(), "targets have to be int64 [%d]" % rows)
     policy = advantages is not None
     _need(policy or (old_logp is None and ref_logp is None), "old_logp and ref_logp belong to a loss with advantages")
-    per_row = dict(old_logp=old_logp, advantages=advantages, ref_logp=ref_logp, weights=weights)
-    for name, t in per_row.items():
-        if t is not None and not (t.dtype == torch.float32 and t.shape == (rows,) and t.is_contiguous()):
-            raise ValueError("%s has to be fp32 [%d]" % (name, rows))
+    for t in (old_logp, advantages, ref_logp, weights):
+        if t is not None and not (t.dtype is torch.float32 and t.shape == (rows,) and t.is_contiguous()):
+            raise ValueError("old_logp, advantages, ref_logp and weights have to be fp32 [%d]" % rows)
     code = _dtype_code(logits)
-    if out is None:
-        out = torch.empty((n, V), dtype=logits.dtype, device=dev) if need_grad else None
-    else:
-        _need(out.dim() == 2 and out.dtype == logits.dtype and out.shape[0] >= n and out.shape[1] == V and (out.stride(1) == 1 or V == 1),
+    ds, dev = 0, logits.device
+    if out is not None:
+        _need(out.dim() == 2 and out.dtype is logits.dtype and out.shape[0] >= n and out.shape[1] == V and (out.stride(1) == 1 or V == 1),
               "out has to be %s [%d, %d] with dense columns" % (logits.dtype, n, V))
-        _need(out.shape[0] < 2 or out.stride(0) >= V, "rows of out must not overlap")
-    _on(dev, targets=targets, idx=idx, n_kept_dev=n_kept_dev, out=out, **per_row)
+        ds = out.stride(0) if out.shape[0] > 1 else 0
+        _need(out.shape[0] < 2 or ds >= V, "rows of out must not overlap")
+    elif need_grad:
+        out = torch.empty((n, V), dtype=logits.dtype, device=dev)
+    device = _on((logits, targets, old_logp, advantages, ref_logp, weights, idx, n_kept_dev, out))
     logp = torch.empty(n, dtype=torch.float32, device=dev)
     stats = torch.empty(4, dtype=torch.float32, device=dev)
-    L = _lib or lib()
-    wsb = L.cf_token_loss_workspace_bytes(n)
-    ws = torch.empty(wsb, dtype=torch.uint8, device=dev)
+    ws = torch.empty((16 * n + 256) // 256 * 256, dtype=torch.uint8, device=dev)        # cf_token_loss_workspace_bytes(n) or more: the call compares
     d = LossDesc(CF_LOSS_POLICY if policy else CF_LOSS_NLL, V, code, logit_scale, clip[0], clip[1], kl_coef, norm)
-    stride = lambda t: t.stride(0) if t.shape[0] > 1 else 0
-    _check(L.cf_token_loss(C.byref(d), _ptr(logits), stride(logits), _ptr(targets), _addr(old_logp), _addr(ref_logp), _addr(advantages),
-                           _addr(weights), None if idx is None else _ptr(idx), _addr(n_kept_dev), n, None if out is None else _ptr(out),
-                           0 if out is None else stride(out), _ptr(logp), stats.data_ptr(), ws.data_ptr(), wsb, _stream()), "cf_token_loss")
+    _check((_lib or lib()).cf_token_loss(C.byref(d), _ptr(logits), ls if rows > 1 else 0, _ptr(targets), _addr(old_logp), _addr(ref_logp),
+                                         _addr(advantages), _addr(weights), None if idx is None else _ptr(idx), _addr(n_kept_dev), n,
+                                         None if out is None else _ptr(out), ds, _ptr(logp), stats.data_ptr(), ws.data_ptr(), ws.numel(),
+                                         _stream(device)), "cf_token_loss")
     return stats, logp, out
 
 
@@ -708,8 +717,7 @@ class AdamW:
 
     def step(self, lr: float | None = None, step: int | None = None) -> None:
         """One update.  step: its number, 1 for the first; by default one more than the last call's."""
-        _on(self.device)
-        L, st, d = _lib or lib(), _stream(), self._d
+        L, st, d = _lib or lib(), _stream(_on(self.params[:1])), self._d
         d.step = self.t + 1 if step is None else step
         if lr is not None:
             d.lr = lr

@@ -8,17 +8,38 @@
 
 namespace cf {
 
-// what a lane holds of a head: VN columns of the lower and VN of the upper half
+// what a lane holds of a head: VN columns of the lower and VN of the upper half, as they are stored and widened
 template <typename T> struct Half2 {
     static constexpr int VN = Vec<T>::N;
     float lo[VN], hi[VN];
-    __device__ __forceinline__ void load(const T* p, int half) {
-        Vec<T>::load(p, lo);
-        Vec<T>::load(p + half, hi);
-    }
     __device__ __forceinline__ void store(T* p, int half) const {
         Vec<T>::store(p, lo);
         Vec<T>::store(p + half, hi);
+    }
+};
+typedef unsigned u32x4q __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void widen16(const u32x4q& b, float (&o)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = __uint_as_float(b[i]);
+}
+__device__ __forceinline__ void widen16(const u32x4q& b, float (&o)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        o[2 * i] = __uint_as_float(b[i] << 16);
+        o[2 * i + 1] = __uint_as_float(b[i] & 0xFFFF0000u);
+    }
+}
+template <typename T> struct Raw2 {
+    u32x4q lo, hi;
+    __device__ __forceinline__ void load(const T* p, int half) {
+        lo = *reinterpret_cast<const u32x4q*>(p);
+        hi = *reinterpret_cast<const u32x4q*>(p + half);
+    }
+    __device__ __forceinline__ Half2<T> wide() const {
+        Half2<T> h;
+        widen16(lo, h.lo);
+        widen16(hi, h.hi);
+        return h;
     }
 };
 
@@ -42,19 +63,25 @@ template <typename T, int LANES> struct RowTables {
     static constexpr int VN = Vec<T>::N, HALF = VN * LANES;
     float c[VN], s[VN];
     __device__ __forceinline__ void load(const QkShape& sh, int64_t row, int part) {
-        if (sh.cos == nullptr) {
-#pragma unroll
-            for (int e = 0; e < VN; ++e) { c[e] = 1.f; s[e] = 0.f; }
-            return;
-        }
-        int pos = sh.positions != nullptr ? sh.positions[row] : (int)(row % sh.S);
-        pos = pos < 0 ? 0 : (pos < sh.S ? pos : sh.S - 1);
-        const int64_t at = (int64_t)pos * HALF + part * VN;
+        u32x4q a[VN / 4], b[VN / 4];
 #pragma unroll
         for (int q = 0; q < VN / 4; ++q) {
-            const float4 a = reinterpret_cast<const float4*>(sh.cos + at)[q], b = reinterpret_cast<const float4*>(sh.sin + at)[q];
-            c[4 * q] = a.x; c[4 * q + 1] = a.y; c[4 * q + 2] = a.z; c[4 * q + 3] = a.w;
-            s[4 * q] = b.x; s[4 * q + 1] = b.y; s[4 * q + 2] = b.z; s[4 * q + 3] = b.w;
+            a[q] = u32x4q{0x3F800000u, 0x3F800000u, 0x3F800000u, 0x3F800000u};      // no tables: no rotation
+            b[q] = u32x4q{0u, 0u, 0u, 0u};
+        }
+        if (sh.cos != nullptr) {
+            const int at = sh.positions != nullptr ? sh.positions[row] : (int)(row % sh.S), pos = min(max(at, 0), sh.S - 1);
+            const int64_t i = (int64_t)pos * HALF + part * VN;
+#pragma unroll
+            for (int q = 0; q < VN / 4; ++q) {
+                a[q] = reinterpret_cast<const u32x4q*>(sh.cos + i)[q];
+                b[q] = reinterpret_cast<const u32x4q*>(sh.sin + i)[q];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < VN; ++e) {
+            c[e] = __uint_as_float(a[e / 4][e % 4]);
+            s[e] = __uint_as_float(b[e / 4][e % 4]);
         }
     }
 };
@@ -62,10 +89,11 @@ template <typename T, int LANES> struct RowTables {
 template <typename T> struct QkPtr {
     T *q, *k;
     int64_t qs, ks;
-    __device__ __forceinline__ T* head(int64_t row, int h, int Hq, int d) const {
-        return h < Hq ? q + row * qs + (int64_t)h * d : k + row * ks + (int64_t)(h - Hq) * d;
-    }
 };
+
+// Heads h0, h0 + hp, ... of H, U at a time: all loads of U heads ahead of the arithmetic.  A lane group that has no head left does what the one
+// with the last head does, so that no access hangs on a branch; in place too, since the last head belongs to the last U.
+constexpr int QK_U = 4;
 
 template <typename T, int LANES>
 __global__ __launch_bounds__(256) void qk_norm_fwd_kernel(QkShape sh, QkPtr<const T> in, QkPtr<T> out, int n_rows) {
@@ -74,31 +102,45 @@ __global__ __launch_bounds__(256) void qk_norm_fwd_kernel(QkShape sh, QkPtr<cons
     const int h0 = group & (sh.hp - 1), rpw = GROUPS / sh.hp;
     const int64_t row = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * rpw + group / sh.hp;
     if (row >= n_rows) return;
-    const int heads = sh.Hq + sh.Hkv;
     RowTables<T, LANES> tab;
     tab.load(sh, row, part);
-    for (int h = h0; h < heads; h += sh.hp) {
-        Half2<T> x, g, y;
-        x.load(in.head(row, h, sh.Hq, D) + part * VN, HALF);
-        g.load((const T*)(h < sh.Hq ? sh.gq : sh.gk) + part * VN, HALF);
-        float ss = 0.f;
+    auto heads = [&](const T* src, T* dst, int H, const void* gain) __attribute__((always_inline)) {
+        Raw2<T> graw;
+        graw.load((const T*)gain + part * VN, HALF);
+        for (int hb = 0; hb < H; hb += QK_U * sh.hp) {
+            Raw2<T> x[QK_U];
 #pragma unroll
-        for (int e = 0; e < VN; ++e) ss += x.lo[e] * x.lo[e] + x.hi[e] * x.hi[e];
-        const float rstd = rsqrtf(lanes_sum<LANES>(ss) * (1.0f / D) + sh.eps);
+            for (int u = 0; u < QK_U; ++u) x[u].load(src + (int64_t)min(hb + u * sh.hp + h0, H - 1) * D + part * VN, HALF);
+            const Half2<T> g = graw.wide();
 #pragma unroll
-        for (int e = 0; e < VN; ++e) {
-            const float a = x.lo[e] * rstd * g.lo[e], b = x.hi[e] * rstd * g.hi[e];
-            y.lo[e] = a * tab.c[e] - b * tab.s[e];
-            y.hi[e] = b * tab.c[e] + a * tab.s[e];
+            for (int u = 0; u < QK_U; ++u) {
+                if (u > 0 && hb + u * sh.hp >= H) break;
+                const Half2<T> w = x[u].wide();
+                float ss = 0.f;
+#pragma unroll
+                for (int e = 0; e < VN; ++e) ss += w.lo[e] * w.lo[e] + w.hi[e] * w.hi[e];
+                const float rstd = rsqrtf(lanes_sum<LANES>(ss) * (1.0f / D) + sh.eps);
+                Half2<T> y;
+#pragma unroll
+                for (int e = 0; e < VN; ++e) {
+                    const float a = w.lo[e] * rstd * g.lo[e], b = w.hi[e] * rstd * g.hi[e];
+                    y.lo[e] = a * tab.c[e] - b * tab.s[e];
+                    y.hi[e] = b * tab.c[e] + a * tab.s[e];
+                }
+                y.store(dst + (int64_t)min(hb + u * sh.hp + h0, H - 1) * D + part * VN, HALF);
+                __builtin_amdgcn_sched_barrier(0);          // one head after the other: waves hide the latencies, and registers decide how many there are
+            }
         }
-        y.store(out.head(row, h, sh.Hq, D) + part * VN, HALF);
-    }
+    };
+    heads(in.q + row * in.qs, out.q + row * out.qs, sh.Hq, sh.gq);
+    heads(in.k + row * in.ks, out.k + row * out.ks, sh.Hkv, sh.gk);
 }
 
 // Blocks that the live rows are dealt out to, and so the partials of the gain gradients: a function of the live rows alone.
+constexpr int QK_BWD_BLOCKS = 768;
 __host__ __device__ inline int qk_bwd_nblk(int n_rows) {
     const int b = (n_rows + 3) / 4;
-    return b < 1024 ? b : 1024;
+    return b < QK_BWD_BLOCKS ? b : QK_BWD_BLOCKS;
 }
 
 // partial [nblk][2][D]: the block's sums of u*n over its rows, of the query heads and of the key heads (null: not wanted).
@@ -106,81 +148,110 @@ template <typename T, int LANES>
 __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(QkShape sh, QkPtr<const T> in, QkPtr<const T> dy, const int32_t* __restrict__ idx,
                                                           int n_max, const int32_t* __restrict__ n_dev, QkPtr<T> dx,
                                                           float* __restrict__ partial) {
-    constexpr int VN = Vec<T>::N, HALF = VN * LANES, D = 2 * HALF, GROUPS = 64 / LANES;
-    __shared__ float red[4][2 * D];
+    constexpr int VN = Vec<T>::N, HALF = VN * LANES, D = 2 * HALF, GROUPS = 64 / LANES, U = 2;
+    __shared__ float red[4 * GROUPS * D];
     const int n_rows = live_rows(n_max, n_dev), nblk = qk_bwd_nblk(n_rows);
     if ((int)blockIdx.x >= nblk) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane & (LANES - 1), group = lane / LANES;
     const int h0 = group & (sh.hp - 1), rpw = GROUPS / sh.hp;
-    const int heads = sh.Hq + sh.Hkv;
-    float acc[2][2][VN];
+    float acc[2][2 * VN];
 #pragma unroll
-    for (int i = 0; i < 4 * VN; ++i) (&acc[0][0][0])[i] = 0.f;
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 2 * VN; ++e) acc[k][e] = 0.f;
     for (int64_t j = ((int64_t)blockIdx.x * 4 + wave) * rpw + group / sh.hp; j < n_rows; j += (int64_t)nblk * 4 * rpw) {
         const int64_t row = idx != nullptr ? idx[j] : j;
         RowTables<T, LANES> tab;
         tab.load(sh, row, part);
-        for (int h = h0; h < heads; h += sh.hp) {
-            const bool is_q = h < sh.Hq;
-            Half2<T> x, y, g;
-            x.load(in.head(row, h, sh.Hq, D) + part * VN, HALF);
-            y.load(dy.head(j, h, sh.Hq, D) + part * VN, HALF);
-            g.load((const T*)(is_q ? sh.gq : sh.gk) + part * VN, HALF);
-            float ss = 0.f, sd = 0.f;
+        auto heads = [&](const T* xs, const T* ys, T* dst, int H, const void* gain, float (&ac)[2 * VN]) __attribute__((always_inline)) {
+            Raw2<T> graw;
+            graw.load((const T*)gain + part * VN, HALF);
+            for (int hb = 0; hb < H; hb += U * sh.hp) {
+                Raw2<T> x[U], y[U];
 #pragma unroll
-            for (int e = 0; e < VN; ++e) {      // u = R^T dy in place of dy
-                const float a = y.lo[e] * tab.c[e] + y.hi[e] * tab.s[e], b = y.hi[e] * tab.c[e] - y.lo[e] * tab.s[e];
-                y.lo[e] = a; y.hi[e] = b;
-                ss += x.lo[e] * x.lo[e] + x.hi[e] * x.hi[e];
-                sd += a * g.lo[e] * x.lo[e] + b * g.hi[e] * x.hi[e];
-            }
-            const float rstd = rsqrtf(lanes_sum<LANES>(ss) * (1.0f / D) + sh.eps);
-            const float c = lanes_sum<LANES>(sd) * rstd * (1.0f / D);      // mean(u*g*n)
+                for (int u = 0; u < U; ++u) {
+                    const int64_t at = (int64_t)min(hb + u * sh.hp + h0, H - 1) * D + part * VN;
+                    x[u].load(xs + at, HALF);
+                    y[u].load(ys + at, HALF);
+                }
+                const Half2<T> g = graw.wide();
 #pragma unroll
-            for (int e = 0; e < VN; ++e) {
-                const float nl = x.lo[e] * rstd, nh = x.hi[e] * rstd;
-                const float al = y.lo[e] * nl, ah = y.hi[e] * nh;
-                acc[0][0][e] += is_q ? al : 0.f; acc[0][1][e] += is_q ? ah : 0.f;
-                acc[1][0][e] += is_q ? 0.f : al; acc[1][1][e] += is_q ? 0.f : ah;
-                y.lo[e] = rstd * (y.lo[e] * g.lo[e] - nl * c);
-                y.hi[e] = rstd * (y.hi[e] * g.hi[e] - nh * c);
+                for (int u = 0; u < U; ++u) {
+                    if (u > 0 && hb + u * sh.hp >= H) break;
+                    const float mine = hb + u * sh.hp + h0 < H ? 1.f : 0.f;         // a head that is another group's does not count twice
+                    const Half2<T> w = x[u].wide();
+                    Half2<T> v = y[u].wide();
+                    float ss = 0.f, sd = 0.f;
+#pragma unroll
+                    for (int e = 0; e < VN; ++e) {      // u = R^T dy in place of dy
+                        const float a = v.lo[e] * tab.c[e] + v.hi[e] * tab.s[e], b = v.hi[e] * tab.c[e] - v.lo[e] * tab.s[e];
+                        v.lo[e] = a; v.hi[e] = b;
+                        ss += w.lo[e] * w.lo[e] + w.hi[e] * w.hi[e];
+                        sd += a * g.lo[e] * w.lo[e] + b * g.hi[e] * w.hi[e];
+                    }
+                    const float rstd = rsqrtf(lanes_sum<LANES>(ss) * (1.0f / D) + sh.eps);
+                    const float c = lanes_sum<LANES>(sd) * rstd * (1.0f / D);      // mean(u*g*n)
+                    const float rm = rstd * mine;
+#pragma unroll
+                    for (int e = 0; e < VN; ++e) {
+                        ac[e] += v.lo[e] * (w.lo[e] * rm);
+                        ac[VN + e] += v.hi[e] * (w.hi[e] * rm);
+                        v.lo[e] = rstd * (v.lo[e] * g.lo[e] - w.lo[e] * rstd * c);
+                        v.hi[e] = rstd * (v.hi[e] * g.hi[e] - w.hi[e] * rstd * c);
+                    }
+                    v.store(dst + (int64_t)min(hb + u * sh.hp + h0, H - 1) * D + part * VN, HALF);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
-            y.store(dx.head(j, h, sh.Hq, D) + part * VN, HALF);
-        }
+        };
+        heads(in.q + row * in.qs, dy.q + j * dy.qs, dx.q + j * dx.qs, sh.Hq, sh.gq, acc[0]);
+        heads(in.k + row * in.ks, dy.k + j * dy.ks, dx.k + j * dx.ks, sh.Hkv, sh.gk, acc[1]);
     }
     if (partial == nullptr) return;
+    // the lane groups' sums by way of LDS, the queries' and then the keys': all threads add up rows of it, then a thread a column their sums
+    constexpr int SUB = 256 / D;
+    const int col = threadIdx.x % D, sub = threadIdx.x / D;
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+    for (int k = 0; k < 2; ++k) {
+        if (k > 0) __syncthreads();
+        float* mine = red + (wave * GROUPS + group) * D;
 #pragma unroll
-        for (int p = 0; p < 2; ++p)
+        for (int e = 0; e < VN; ++e) {
+            mine[part * VN + e] = acc[k][e];
+            mine[HALF + part * VN + e] = acc[k][VN + e];
+        }
+        __syncthreads();
+        float s = 0.f;
 #pragma unroll
-            for (int e = 0; e < VN; ++e) {
-                float v = acc[k][p][e];
+        for (int r = 0; r < 4 * GROUPS / SUB; ++r) s += red[(sub + r * SUB) * D + col];
+        if (SUB > 1) {
+            __syncthreads();
+            red[threadIdx.x] = s;
+            __syncthreads();
+            s = 0.f;
 #pragma unroll
-                for (int o = LANES; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
-                if (group == 0) red[wave][k * D + p * HALF + part * VN + e] = v;
-            }
-    __syncthreads();
-    for (int c = threadIdx.x; c < 2 * D; c += 256)
-        partial[(int64_t)blockIdx.x * (2 * D) + c] = red[0][c] + red[1][c] + red[2][c] + red[3][c];
+            for (int r = 0; r < SUB; ++r) s += red[r * D + col];
+        }
+        if (threadIdx.x < D) partial[(int64_t)blockIdx.x * (2 * D) + k * D + col] = s;
+    }
 }
 
-// dg[c] (+)= sum over the blocks' partials: 8 columns a block, 32 row groups
+// dg[c] (+)= sum over the blocks' partials: 16 columns a block, 64 row groups, all of a thread's loads in flight at once
 template <typename T, bool ACC>
-__global__ __launch_bounds__(256) void qk_gain_kernel(const float* __restrict__ partial, int n_max, const int32_t* __restrict__ n_dev,
-                                                      int d, T* __restrict__ dgq, T* __restrict__ dgk) {
-    __shared__ float red[32][9];
+__global__ __launch_bounds__(1024) void qk_gain_kernel(const float* __restrict__ partial, int n_max, const int32_t* __restrict__ n_dev,
+                                                       int d, T* __restrict__ dgq, T* __restrict__ dgk) {
+    __shared__ float red[64][17];
     const int nblk = qk_bwd_nblk(live_rows(n_max, n_dev));
-    const int cl = threadIdx.x & 7, rg = threadIdx.x >> 3, c = blockIdx.x * 8 + cl;
+    const int cl = threadIdx.x & 15, rg = threadIdx.x >> 4, c = blockIdx.x * 16 + cl;
     float s = 0.f;
-#pragma unroll 8
-    for (int b = rg; b < nblk; b += 32) s += partial[(int64_t)b * (2 * d) + c];
+#pragma unroll
+    for (int i = 0; i < QK_BWD_BLOCKS / 64; ++i) s += rg + 64 * i < nblk ? partial[(int64_t)(rg + 64 * i) * (2 * d) + c] : 0.f;
     red[rg][cl] = s;
     __syncthreads();
-    if (threadIdx.x < 8) {
+    if (threadIdx.x < 16) {
         float t = 0.f;
 #pragma unroll
-        for (int r = 0; r < 32; ++r) t += red[r][threadIdx.x];
+        for (int r = 0; r < 64; ++r) t += red[r][threadIdx.x];
         T* out = c < d ? dgq + c : dgk + (c - d);
         if (ACC) *out += from_f32<T>(t);
         else *out = from_f32<T>(t);
@@ -239,10 +310,10 @@ hipError_t launch_qk_norm_bwd(const cf_layer_desc& L, const cf_qk_norm& p, const
         CF_QK_LANES(qk_bwd_t, L, p, in, dy, idx, rows, dx, into, st)
     }
     if (dgq) {      // no rows: no partials, zeros
-        const int grid = 2 * L.d / 8;
-        if (acc_f32) qk_gain_kernel<float, true><<<grid, 256, 0, st>>>(partial, rows.n, rows.dev, L.d, (float*)dgq, (float*)dgk);
-        else if (L.dtype == CF_F32) qk_gain_kernel<float, false><<<grid, 256, 0, st>>>(partial, rows.n, rows.dev, L.d, (float*)dgq, (float*)dgk);
-        else qk_gain_kernel<bf16_t, false><<<grid, 256, 0, st>>>(partial, rows.n, rows.dev, L.d, (bf16_t*)dgq, (bf16_t*)dgk);
+        const int grid = 2 * L.d / 16;
+        if (acc_f32) qk_gain_kernel<float, true><<<grid, 1024, 0, st>>>(partial, rows.n, rows.dev, L.d, (float*)dgq, (float*)dgk);
+        else if (L.dtype == CF_F32) qk_gain_kernel<float, false><<<grid, 1024, 0, st>>>(partial, rows.n, rows.dev, L.d, (float*)dgq, (float*)dgk);
+        else qk_gain_kernel<bf16_t, false><<<grid, 1024, 0, st>>>(partial, rows.n, rows.dev, L.d, (bf16_t*)dgq, (bf16_t*)dgk);
     }
     return hipGetLastError();
 }

@@ -287,7 +287,7 @@ def test_binding_refuses_what_the_library_cannot_see(L):
     d = _desc()
     q, k, g, idx = torch.zeros(6, 256, dtype=BF), torch.zeros(6, 128, dtype=BF), torch.ones(64, dtype=BF), torch.zeros(6, dtype=torch.int32)
     cos = torch.zeros(64, 32)
-    for a in ((q[:, :128], k, g, g), (q, k[:5], g, g), (q.float(), k, g, g), (q, k, g[:32], g), (q, k, g.float(), g), (q.t().contiguous().t(), k, g, g),
+    for a in ((q[:, :128], k, g, g), (q, k[:5], g, g), (q.float(), k, g, g), (q, k, g[:32], g), (q, k, g.float(), g), (q.t().contiguous().t(), k, g, g), (q[:1].expand(6, 256), k, g, g),
               (q, k, g, g, cos), (q, k, g, g, cos[:10], cos), (q, k, g, g, None, None, idx[:3]), (q, k, g, g, None, None, idx.long()), (q, k, g, g)):
         with pytest.raises(ValueError):
             Bn.qk_norm_rope_fwd(d, *a)
@@ -295,7 +295,7 @@ def test_binding_refuses_what_the_library_cannot_see(L):
         with pytest.raises(ValueError):
             Bn.qk_norm_rope_bwd(d, q, k, g, g, q, k, **kw)
     l, y, f = torch.zeros(6, 10), torch.zeros(6, dtype=torch.int64), torch.zeros(6)
-    for a, kw in (((l, y.int()), {}), ((l, y[:5]), {}), ((l.t(), y), {}), ((l, y), dict(old_logp=f)), ((l, y, f, f[:3]), {}), ((l, y, f, f.double()), {}),
+    for a, kw in (((l, y.int()), {}), ((l, y[:5]), {}), ((l.t(), y), {}), ((l[:1].expand(6, 10), y), {}), ((l, y), dict(out=l[:1].expand(6, 10))), ((l, y), dict(old_logp=f)), ((l, y, f, f[:3]), {}), ((l, y, f, f.double()), {}),
                   ((l, y), dict(max_kept=7)), ((l, y), dict(idx=idx[:2], max_kept=3)), ((l, y), dict(out=l[:3])), ((l, y), dict(out=l.to(BF))),
                   ((l, y), dict(weights=f[:2])), ((l, y), {})):
         with pytest.raises(ValueError):
@@ -1021,6 +1021,7 @@ def test_training_step_end_to_end(dtype):
     logits = out @ P["wh"]
     loss = torch.nn.functional.cross_entropy(logits, y)
     loss.backward()
+    loss = loss.detach()
     # the same through the library
     dsv, dW = _layer_qk_device(shape, W, sv, tabs)
     desc = Bn.make_desc(B, S, H, Hq, Hkv, d, shape.F, shape.dtype, rms_eps=EPS_N)
