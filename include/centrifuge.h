@@ -360,7 +360,8 @@ cf_status cf_layer_bwd_lora_qk(const cf_layer_desc* desc, const cf_saved* saved,
  *   logits   [rows,V], row stride logits_stride elements (0 = V); kept row j is row idx[j] (NULL: row j).  Any alignment of rows:
  *            pointers need their element's only, multiples of 16 bytes are faster
  *   targets, old_logp, ref_logp, advantages, weights   one per row of logits, read at the same idx[j].  weights NULL: 1
- *   dlogits  [max_kept,V], row stride dlogits_stride (nullable: not wanted).  May be logits itself (same stride) without idx
+ *   dlogits  [max_kept,V], row stride dlogits_stride (nullable: not wanted).  May be logits itself (same stride) without idx,
+ *            and must not overlap them otherwise
  *   logp     [max_kept] fp32 (nullable): lp.  For the same logits it has the same bits with and without dlogits, so that old_logp
  *            from a call without gradient makes r exactly 1
  *   stats    [4] fp32 (nullable): loss, its first term, the mean k, the share of clipped tokens (all weighted by w/norm)

@@ -80,8 +80,8 @@ __device__ __forceinline__ float rounded(float a, float b) {
 // The square root of a normal number to half a step: the hardware's, which is off by one, and what a fused residual says is missing.  A third of the
 // instructions of sqrtf, which an element of an 8-bit state has not the time for next to its 18 bytes.
 __device__ __forceinline__ float root(float v) {
-    const float s = __builtin_amdgcn_sqrtf(v);
-    return fmaf(fmaf(-s, s, v), 0.5f * __builtin_amdgcn_rcpf(fmaxf(s, 0x1p-70f)), s);
+    const float s = __builtin_amdgcn_sqrtf(v), r = fmaf(fmaf(-s, s, v), 0.5f * __builtin_amdgcn_rcpf(fmaxf(s, 0x1p-70f)), s);
+    return s < INFINITY ? r : s;            // a square beyond fp32 makes an update of 0
 }
 
 // LANE elements from i on, of which `left` exist: all of them, unless TAIL

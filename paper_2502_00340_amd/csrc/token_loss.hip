@@ -154,7 +154,8 @@ __device__ __forceinline__ RowEnd row_end(const LossArgs& a, const RowHead& r, i
 
 // A row read twice, with no bound on its length
 template <typename T, int NT> __device__ __forceinline__ void stream_row(const LossArgs& a, const RowHead& r, int j, float inv_norm, float (&red)[NT / 32]) {
-    constexpr int VN = Vec<T>::N, WAVES = NT / 64;
+    constexpr int VN = Vec<T>::N, WAVES = NT / 64, U = 4;          // vectors whose loads a thread has in flight
+    constexpr bool EXACT = VN == 4;
     const int tid = threadIdx.x, V = a.V, nv = V / VN;
     const T* l = (const T*)r.l;
     Expo ex{-3.402823466e38f, a.k, a.klo};
@@ -167,12 +168,19 @@ template <typename T, int NT> __device__ __forceinline__ void stream_row(const L
             s *= __builtin_amdgcn_exp2f((ex.m - t) * ex.k);
             ex.m = t;
 #pragma unroll
-            for (int e = 0; e < VN; ++e) s += expo<true>(ex, x[e]);
+            for (int e = 0; e < VN; ++e) s += expo<EXACT>(ex, x[e]);
         };
-        for (int v = tid; v < nv; v += NT) {
-            float x[VN];
-            widen<T>(reinterpret_cast<const Bytes16*>(l)[v], x);
-            take(x);
+        for (int v = tid; v < nv; v += U * NT) {
+            Bytes16 b[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) b[u] = reinterpret_cast<const Bytes16*>(l)[min(v + u * NT, nv - 1)];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (v + u * NT >= nv) break;
+                float x[VN];
+                widen<T>(b[u], x);
+                take(x);
+            }
         }
         if (int c = nv * VN + tid; c < V) {
             float x[VN];
@@ -186,15 +194,23 @@ template <typename T, int NT> __device__ __forceinline__ void stream_row(const L
     const RowEnd end = row_end(a, r, j, ex.m, s, inv_norm, threadIdx.x == 0);
     if (a.dlogits == nullptr) return;
     T* dl = (T*)a.dlogits + (int64_t)j * a.dstride;
-    for (int v = tid; v < nv; v += NT) {
-        float x[VN];
-        widen<T>(reinterpret_cast<const Bytes16*>(l)[v], x);
+    for (int v = tid; v < nv; v += U * NT) {
+        Bytes16 b[U];
 #pragma unroll
-        for (int e = 0; e < VN; ++e) x[e] = !r.live() ? 0.f : v * VN + e == r.y ? end.at_y : end.neg * expo<true>(ex, x[e]);
-        reinterpret_cast<Bytes16*>(dl)[v] = narrow<T>(x);
+        for (int u = 0; u < U; ++u) b[u] = reinterpret_cast<const Bytes16*>(l)[min(v + u * NT, nv - 1)];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int at = v + u * NT;
+            if (at >= nv) break;
+            float x[VN];
+            widen<T>(b[u], x);
+#pragma unroll
+            for (int e = 0; e < VN; ++e) x[e] = !r.live() ? 0.f : at * VN + e == r.y ? end.at_y : end.neg * expo<EXACT>(ex, x[e]);
+            __builtin_nontemporal_store(narrow<T>(x), reinterpret_cast<Bytes16*>(dl) + at);
+        }
     }
     if (int c = nv * VN + tid; c < V)
-        dl[c] = one_from_f32<T>(!r.live() ? 0.f : c == r.y ? end.at_y : end.neg * expo<true>(ex, to_f32<T>(l[c])));
+        dl[c] = one_from_f32<T>(!r.live() ? 0.f : c == r.y ? end.at_y : end.neg * expo<EXACT>(ex, to_f32<T>(l[c])));
 }
 
 template <typename T, int NT>
@@ -393,7 +409,7 @@ template <typename T, int NT, int NV> static void launch_rows(const LossArgs& a,
 // added up in the same order in every call.
 template <typename T> static void launch_token_loss(const LossArgs& a, hipStream_t st) {
     const int nv = a.V / Vec<T>::N;
-    if (nv < 1 || nv > 1024 * 20) token_loss_stream_kernel<T, 512><<<a.n_max, 512, 0, st>>>(a);
+    if (nv < 1 || nv > 1024 * 20) token_loss_stream_kernel<T, 1024><<<a.n_max, 1024, 0, st>>>(a);
     else if (nv <= 256 * 4) launch_rows<T, 256, 4>(a, st);
     else if (nv <= 256 * 8) launch_rows<T, 256, 8>(a, st);
     else if (nv <= 256 * 12) launch_rows<T, 256, 12>(a, st);
@@ -440,7 +456,13 @@ cf_status cf_token_loss(const cf_loss_desc* desc, const void* logits, int64_t lo
     for (const void* p : {(const void*)old_logp, (const void*)ref_logp, (const void*)advantages, (const void*)weights, (const void*)idx,
                           (const void*)n_kept_dev, (const void*)logp, (const void*)stats})
         if (off(p, 4)) return CF_ERR_SHAPE;
-    if (dlogits == logits && (idx || ls != ds)) return CF_ERR_SHAPE;     // a row would be written before another block has read it
+    // a row would be written before another block has read it
+    if (dlogits == logits && (idx || ls != ds)) return CF_ERR_SHAPE;
+    if (dlogits && dlogits != logits && !idx && max_kept > 0) {
+        const uintptr_t l0 = (uintptr_t)logits, d0 = (uintptr_t)dlogits;
+        const uint64_t ln = ((uint64_t)(max_kept - 1) * ls + desc->V) * e, dn = ((uint64_t)(max_kept - 1) * ds + desc->V) * e;
+        if (l0 < d0 + dn && d0 < l0 + ln) return CF_ERR_SHAPE;
+    }
     if (!ws || off(ws, 16) || ws_bytes < cf_token_loss_workspace_bytes(max_kept)) return CF_ERR_WORKSPACE;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     const double k = (double)scale * 1.4426950408889634;

@@ -249,7 +249,7 @@ def test_token_loss_refusals(L):
                      (dict(desc=D(hi=-0.1)), 2), (dict(desc=D(hi=nan)), 2), (dict(desc=D(kl=nan)), 2), (dict(desc=D(norm=nan)), 2), (dict(ref=None), 2),
                      (dict(n=-1), 2), (dict(ls=99), 2), (dict(ds=99), 2), (dict(ls=-100), 2), (dict(logits=FAKE + 1), 2), (dict(dl=FAKE + 1), 2), (dict(y=FAKE + 4), 2),
                      (dict(w=FAKE + 2), 2), (dict(idx=FAKE + 2), 2), (dict(nd=FAKE + 1), 2), (dict(lp=FAKE + 2), 2), (dict(st=FAKE + 2), 2),
-                     (dict(dl=FAKE, idx=FAKE), 2), (dict(dl=FAKE, ds=200), 2), (dict(ws=None), 4), (dict(ws=FAKE + 8), 4), (dict(wsb=100), 4)):
+                     (dict(dl=FAKE, idx=FAKE), 2), (dict(dl=FAKE, ds=200), 2), (dict(dl=FAKE + 200), 2), (dict(dl=FAKE - 1998), 2), (dict(ws=None), 4), (dict(ws=FAKE + 8), 4), (dict(wsb=100), 4)):
         assert call(**kw) == code, kw
     assert L.cf_token_loss_workspace_bytes(-1) == 0 and L.cf_token_loss_workspace_bytes(0) > 0
 
@@ -823,6 +823,21 @@ def test_global_norm_and_clipping(g_dtype):
     opt = Bn.AdamW([q], big, lr=LR, max_norm=1.0, state=([m1], [v1]))
     opt.step()
     assert abs(float(opt.grad_norm) / (1e30 * math.sqrt(5000.0)) - 1.0) < 4 * U and bool(q.isfinite().all())
+
+
+@gpu
+def test_adamw_with_squares_beyond_fp32_and_below():
+    """Without clipping: a second moment that overflows makes an update of 0 (m / inf), gradients of 1e-25 underflow to a moment of 0 and are left to eps."""
+    say("adamw extremes")
+    g = torch.tensor([1e30, -1e30, 1e-25, 0.0, 1.0], device=DEV)
+    p = torch.arange(5, device=DEV, dtype=F32)
+    opt = Bn.AdamW([p], [g], lr=LR, betas=(B1, B2), eps=AEPS)
+    opt.step()
+    want = torch.arange(5, dtype=F64)
+    want[4] -= LR
+    close(p, want, 4 * U * want + 64 * U * LR + LR * 1e-25 / AEPS, "parameter")
+    opt.step()
+    assert bool(p.isfinite().all())
 
 
 @gpu
