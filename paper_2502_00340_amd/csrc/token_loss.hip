@@ -230,6 +230,9 @@ __global__ __launch_bounds__(NT) void token_loss_stream_kernel(LossArgs a) {
 // twice it took 601.  4096 rows of 32000 102 us (126), 701 of 50257 fp32 logits 59 us (87).  Arithmetic does not bound it: with its exponentials left out it takes 402.
 // The gradient is written past the caches: 406 against 417 us, 102 against 110; with the two products of a [V, 2048] head behind it, 64 to 2048 rows
 // of 32000 take 0.97 to 1.00 of the time, 1024 of 128256 0.995, and 4096 of 32000, which just fit the last cache, 1.03.
+// Four vectors a thread leave registers for eight waves a SIMD: 8192 rows of 8000 56 -> 49 us, 16384 of 1000 fp32 42 -> 36; eight vectors do not
+// (8192 rows of 16000 105 -> 115).  Rows that start on odd elements cost 1.1 (4096 x 50257 and 50264: 190 and 171 us, without gradient 102 and 79); loads of
+// aligned vectors would make the order of a row's sums, and logp's last bits, depend on where the row lies.
 // Keeps a vector as it is stored, and the arithmetic where it stands: widened values of one pass are not to be kept for the next one.
 __device__ __forceinline__ void hold(Bytes16& b) { asm volatile("" : "+v"(b)); }
 __device__ __forceinline__ void hold(float& a, float& b) { asm volatile("" : "+v"(a), "+v"(b)); }
@@ -242,7 +245,7 @@ __device__ __forceinline__ Bytes16* vector_at(const void* base, unsigned offset)
 }
 
 template <typename T, int NT, int NV, bool GRAD>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void token_loss_kernel(LossArgs a) {
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NV <= 4 ? 8 : 4, 8))) void token_loss_kernel(LossArgs a) {
     constexpr int VN = Vec<T>::N, WAVES = NT / 64;
     // The launch takes this kernel for rows of more than FULL * NT vectors: up to there every lane has one.  Behind, a vector that no lane has is skipped,
     // and lanes behind the last one do what its owner does.  No access is conditional but for that: what is in flight is counted, and
@@ -400,7 +403,7 @@ __global__ __launch_bounds__(1024) void loss_stats_kernel(const float4* __restri
 }
 
 template <typename T, int NT, int NV> static void launch_rows(const LossArgs& a, hipStream_t st) {
-    const int resident = compute_units() * (1024 / NT), grid = a.n_max < resident ? a.n_max : resident;
+    const int resident = compute_units() * (1024 / NT) * (NV <= 4 ? 2 : 1), grid = a.n_max < resident ? a.n_max : resident;
     if (a.dlogits != nullptr) token_loss_kernel<T, NT, NV, true><<<grid, NT, 0, st>>>(a);
     else token_loss_kernel<T, NT, NV, false><<<grid, NT, 0, st>>>(a);
 }
