@@ -262,17 +262,22 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NV <= 4 ? 8 
     auto at = [&](int i) __attribute__((always_inline)) { return (unsigned)(i < FULL ? tid : min(tid, nv - 1 - i * NT)) * 16u; };
     auto load = [&](const void* l, int i) __attribute__((always_inline)) { return *vector_at((const char*)l + i * NT * 16, at(i)); };
     const int tail_at = min(ct, V - 1);         // the row's last elements, one a thread, as they are stored
+    // the next row's; behind the last row all lanes ask for its first 16 bytes, over and over
+    unsigned far = ~0u;
+    auto load_next = [&](const void* l, int i) __attribute__((always_inline)) {
+        return *vector_at((const char*)l + (far & (unsigned)(i * NT * 16)), at(i) & far);
+    };
     RowHead r, rn;
     T xt;
     Expo ex{0.f, a.k, a.klo};
     float s, tail;
-    // What the row needs apart from its vectors, and where the next one is (behind the last row its own vectors are asked for again); the threads'
-    // maximum and sum
+    // What the row needs apart from its vectors, and where the next one is; the threads' maximum and sum
     auto begin = [&]() __attribute__((always_inline)) {
         load_head<T>(a, r);
         rn = r;
         jn = j + (int)gridDim.x;
         if (jn < n_rows) find_row<T>(a, jn, rn);
+        far = jn < n_rows ? ~0u : 0u;
         ex.m = -3.402823466e38f;
         s = 0.f;
         auto take = [&](const auto& o) __attribute__((always_inline)) {
@@ -297,7 +302,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NV <= 4 ? 8 
                 for (int e = 0; e < VN; ++e) o[e] = tid < nv - i * NT ? o[e] : -INFINITY;
             }
             take(o);
-            if (!GRAD) x[i] = load(rn.l, i);
+            if (!GRAD) x[i] = load_next(rn.l, i);
             __builtin_amdgcn_sched_barrier(0);
         }
         tail = ct < V ? to_f32<T>(xt) : -INFINITY;
@@ -363,7 +368,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NV <= 4 ? 8 
                     hold(g);
                 }
                 __builtin_nontemporal_store(g, vector_at(dl + i * NT * 16, at(i)));
-                x[i] = load(rn.l, i);
+                x[i] = load_next(rn.l, i);
                 __builtin_amdgcn_sched_barrier(0);
             }
             xt = ((const T*)rn.l)[tail_at];
