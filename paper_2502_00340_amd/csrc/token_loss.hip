@@ -225,9 +225,10 @@ __global__ __launch_bounds__(NT) void token_loss_stream_kernel(LossArgs a) {
 }
 
 // A row in a block's registers, NV vectors of 16 bytes a thread, so that it is read once.  The block walks through rows, and each vector of the next
-// row is asked for as soon as its register has given its part of the gradient (or of the sum, without a gradient): reads, arithmetic
-// and writes of neighbouring rows overlap.  4096 of 8192 rows of 128256 bf16 logits: 2.1 GB in 406 us, 5.2 TB/s where a copy of 1 GiB reaches 6.2; read
-// twice it took 601.  4096 rows of 32000 102 us (126), 701 of 50257 fp32 logits 59 us (87).  Arithmetic does not bound it: with its exponentials left out it takes 402.
+// row is asked for as soon as its register has given its part of the gradient (or of the sum, without a gradient), or BURST of them together: reads, arithmetic
+// and writes of neighbouring rows overlap.  4096 of 8192 rows of 128256 bf16 logits: 2.1 GB in 382 us, 5.5 TB/s where a copy of 1 GiB reaches 6.2; read
+// twice it took 601.  4096 rows of 32000 102 us (126), 701 of 50257 fp32 logits 56 us (87).  Arithmetic does not bound it: with its exponentials left out
+// it took 402 of 405 before the bursts.
 // The gradient is written past the caches: 406 against 417 us, 102 against 110; with the two products of a [V, 2048] head behind it, 64 to 2048 rows
 // of 32000 take 0.97 to 1.00 of the time, 1024 of 128256 0.995, and 4096 of 32000, which just fit the last cache, 1.03.
 // Four vectors a thread leave registers for eight waves a SIMD: 8192 rows of 8000 56 -> 49 us, 16384 of 1000 fp32 42 -> 36; eight vectors do not
@@ -244,7 +245,7 @@ __device__ __forceinline__ Bytes16* vector_at(const void* base, unsigned offset)
     return (Bytes16*)((__attribute__((address_space(1))) char*)p + offset);
 }
 
-template <typename T, int NT, int NV, bool GRAD>
+template <typename T, int NT, int NV, int BURST, bool GRAD>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NV <= 4 ? 8 : 4, 8))) void token_loss_kernel(LossArgs a) {
     constexpr int VN = Vec<T>::N, WAVES = NT / 64;
     // The launch takes this kernel for rows of more than FULL * NT vectors: up to there every lane has one.  Behind, a vector that no lane has is skipped,
@@ -349,27 +350,37 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NV <= 4 ? 8 
             if (ct < V) ((T*)dl)[ct] = one_from_f32<T>(!r.live() ? 0.f : ct == r.y ? at_y : grad(tail));
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                if (i >= FULL && i * NT >= nv) continue;
-                Bytes16 g;
-                hold(x[i]);
-                if (r.live()) {
-                    float o[VN];
-                    widen<T>(x[i], o);
+                if (i < FULL || i * NT < nv) {
+                    Bytes16 g;
+                    hold(x[i]);
+                    if (r.live()) {
+                        float o[VN];
+                        widen<T>(x[i], o);
 #pragma unroll
-                    for (int e = 0; e < VN; ++e) o[e] = grad(o[e]);
-                    if (at(i) == yv - i * NT * 16) {
+                        for (int e = 0; e < VN; ++e) o[e] = grad(o[e]);
+                        if (at(i) == yv - i * NT * 16) {
 #pragma unroll
-                        for (int e = 0; e < VN; ++e) o[e] = e == ye ? at_y : o[e];
+                            for (int e = 0; e < VN; ++e) o[e] = e == ye ? at_y : o[e];
+                        }
+                        g = narrow<T>(o);
+                        hold(g);
+                    } else {
+                        g = Bytes16{0u, 0u, 0u, 0u};
+                        hold(g);
                     }
-                    g = narrow<T>(o);
-                    hold(g);
-                } else {
-                    g = Bytes16{0u, 0u, 0u, 0u};
-                    hold(g);
+                    x[i] = g;
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                __builtin_nontemporal_store(g, vector_at(dl + i * NT * 16, at(i)));
-                x[i] = load_next(rn.l, i);
-                __builtin_amdgcn_sched_barrier(0);
+                if (i % BURST == BURST - 1 || i == NV - 1) {
+#pragma unroll
+                    for (int z = i / BURST * BURST; z <= i; ++z)
+                        if (z < FULL || z * NT < nv) __builtin_nontemporal_store(x[z], vector_at(dl + z * NT * 16, at(z)));
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int z = i / BURST * BURST; z <= i; ++z)
+                        if (z < FULL || z * NT < nv) x[z] = load_next(rn.l, z);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
             xt = ((const T*)rn.l)[tail_at];
         }
@@ -409,8 +420,18 @@ __global__ __launch_bounds__(1024) void loss_stats_kernel(const float4* __restri
 
 template <typename T, int NT, int NV> static void launch_rows(const LossArgs& a, hipStream_t st) {
     const int resident = compute_units() * (1024 / NT) * (NV <= 4 ? 2 : 1), grid = a.n_max < resident ? a.n_max : resident;
-    if (a.dlogits != nullptr) token_loss_kernel<T, NT, NV, true><<<grid, NT, 0, st>>>(a);
-    else token_loss_kernel<T, NT, NV, false><<<grid, NT, 0, st>>>(a);
+    if (a.dlogits == nullptr) { token_loss_kernel<T, NT, NV, 1, false><<<grid, NT, 0, st>>>(a); return; }
+    if constexpr (NT == 1024) {
+        // Whole rows at once: a block that has a CU to itself computes a row's gradient into its registers, writes all of it and asks for all of the next
+        // row.  What is open in memory at one time then lies closer together: 4096 x 128256 bf16 403 -> 383 us, x 151936 485 -> 452, 2048 x 50257 fp32 176
+        // -> 169.  Not where rows lie between dwords, whose parts of a line the caches would have to hold longer (2048 x 128257 244 -> 256), and not for
+        // less than three rows a block (512 x 128256 50.7 -> 51.8).
+        if ((uintptr_t)a.dlogits % 4 == 0 && (a.dstride * sizeof(T)) % 4 == 0 && (int64_t)a.n_max > 2 * (int64_t)grid) {
+            token_loss_kernel<T, NT, NV, NV, true><<<grid, NT, 0, st>>>(a);
+            return;
+        }
+    }
+    token_loss_kernel<T, NT, NV, 1, true><<<grid, NT, 0, st>>>(a);
 }
 
 // The smallest block whose registers hold a row.  A function of the vocabulary and the type alone: a row's sums, and its logp, are

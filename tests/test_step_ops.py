@@ -637,6 +637,31 @@ def test_token_loss(dtype, rows, V, policy):
 
 
 @gpu
+@pytest.mark.parametrize("dtype,rows,V", [(BF, 2300, 1003), (F32, 2300, 3001), (BF, 1200, 18000), (BF, 1100, 30001), (BF, 560, 50264), (BF, 560, 50257), (BF, 780, 70004), (BF, 780, 70001),
+                                          (F32, 800, 40003), (BF, 530, 140002), (BF, 300, 170001)])
+def test_token_loss_of_more_rows_than_blocks(dtype, rows, V):
+    """Blocks that walk through several rows, each asked for while the one before is written: into rows of another stride through an index, and in place."""
+    say("loss many rows", dtype, rows, V)
+    g0, l, y = _loss_case(rows, dtype, rows, V)
+    y[torch.rand(rows, generator=g0).to(DEV) < 0.1] = -100
+    w = torch.rand(rows, generator=g0).to(DEV) + 0.5
+    idx = torch.randperm(rows, generator=g0)[:rows - 7].sort().values.int().to(DEV)
+    n = rows - 7
+    out = torch.full((n, V + 6), 7.0, dtype=dtype, device=DEV)
+    got = Bn.token_loss(l, y, weights=w, idx=idx, out=out[:, :V])
+    at = idx.long()
+    want = loss_ref(l[at], y[at], None, w[at])
+    _check_loss(got, want, l[at], y[at], dtype, 1.0, w[at].to(F64) / n, False)
+    assert bool((out[:, V:] == 7.0).all())
+    del want
+    again = Bn.token_loss(l, y, weights=w, norm=float(n))
+    kept = again[2][at]
+    assert torch.equal(again[1][at], got[1]) and torch.equal(kept, out[:, :V])
+    Bn.token_loss(l, y, weights=w, norm=float(n), out=l)
+    assert torch.equal(l, again[2])
+
+
+@gpu
 @pytest.mark.parametrize("dtype,V", [(BF, 1003), (F32, 1003), (BF, 40960)])
 def test_token_loss_on_kept_rows(dtype, V):
     """Through an index, with a bound above the live rows, ignored targets, weights of zero: what is left out may hold anything."""
