@@ -635,6 +635,9 @@ def token_loss(logits, targets, old_logp=None, advantages=None, ref_logp=None, w
               "out has to be %s [%d, %d] with dense columns" % (logits.dtype, n, V))
         ds = out.stride(0) if out.shape[0] > 1 else 0
         _need(out.shape[0] < 2 or ds >= V, "rows of out must not overlap")
+        if idx is not None and n:
+            a, b, e = logits.data_ptr(), out.data_ptr(), logits.element_size()
+            _need(a >= b + ((n - 1) * ds + V) * e or b >= a + ((rows - 1) * ls + V) * e, "with idx, out must not overlap logits")
     elif need_grad:
         out = torch.empty((n, V), dtype=logits.dtype, device=dev)
     device = _on((logits, targets, old_logp, advantages, ref_logp, weights, idx, n_kept_dev, out))
@@ -700,6 +703,8 @@ class AdamW:
         if bits == 8:
             for ts, what in ((self.m_scale, "m_scale"), (self.v_scale, "v_scale")):
                 check(ts, what, torch.float32, lambda i: -(-size[i] // STATE_BLOCK))
+        used = [t.data_ptr() for ts in (self.params, self.master or (), self.m, self.v) for t in ts if t.numel()]
+        _need(len(set(used)) == len(used), "a tensor that is updated may be listed once only")
         for t, dt in ((step_dev, torch.int32), (lr_dev, torch.float32)):
             _need(t is None or (t.dtype == dt and t.numel() == 1 and t.device == dev), "step_dev: one int32, lr_dev: one fp32, on %s" % dev)
         self.step_dev, self.lr_dev = step_dev, lr_dev
@@ -716,7 +721,8 @@ class AdamW:
                             grad_scale, 0.0 if max_norm is None else max_norm, _addr(self.grad_norm), _addr(step_dev), _addr(lr_dev))
 
     def step(self, lr: float | None = None, step: int | None = None) -> None:
-        """One update.  step: its number, 1 for the first; by default one more than the last call's."""
+        """One update.  step: its number, 1 for the first; by default one more than the last call's (one that the norm left out counts).
+        lr: from this call on."""
         L, st, d = _lib or lib(), _stream(_on(self.params[:1])), self._d
         d.step = self.t + 1 if step is None else step
         if lr is not None:

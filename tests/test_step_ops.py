@@ -297,7 +297,7 @@ def test_binding_refuses_what_the_library_cannot_see(L):
     l, y, f = torch.zeros(6, 10), torch.zeros(6, dtype=torch.int64), torch.zeros(6)
     for a, kw in (((l, y.int()), {}), ((l, y[:5]), {}), ((l.t(), y), {}), ((l[:1].expand(6, 10), y), {}), ((l, y), dict(out=l[:1].expand(6, 10))), ((l, y), dict(old_logp=f)), ((l, y, f, f[:3]), {}), ((l, y, f, f.double()), {}),
                   ((l, y), dict(max_kept=7)), ((l, y), dict(idx=idx[:2], max_kept=3)), ((l, y), dict(out=l[:3])), ((l, y), dict(out=l.to(BF))),
-                  ((l, y), dict(weights=f[:2])), ((l, y), {})):
+                  ((l, y), dict(weights=f[:2])), ((l, y), dict(idx=idx, out=l)), ((l, y), dict(idx=idx[:2], out=l[1:3])), ((l, y), {})):
         with pytest.raises(ValueError):
             Bn.token_loss(*a, **kw)
     with pytest.raises(TypeError):
@@ -305,7 +305,7 @@ def test_binding_refuses_what_the_library_cannot_see(L):
     p = [torch.zeros(8, 8)]
     for a, kw in (((p, []), {}), (([], []), {}), ((p, [torch.zeros(8)]), {}), ((p, [torch.zeros(8, 8).t()[::2].repeat(2, 1).t()]), {}), ((p, p), dict(state_bits=16)),
                   ((p, p), dict(weight_decay=[0.1, 0.2])), ((p, p), dict(state=(p, [p[0].to(BF)]))), ((p, p), dict(step_dev=torch.zeros(1))),
-                  ((p + [p[0].to(BF)], p + p), {})):
+                  ((p + [p[0].to(BF)], p + p), {}), ((p + p, p + p), {}), ((p, p), dict(state=(p, p)))):
         with pytest.raises(ValueError):
             Bn.AdamW(*a, lr=1e-3, **kw)
     with pytest.raises(ValueError):
