@@ -386,7 +386,7 @@ cf_status cf_token_loss(const cf_loss_desc* desc, const void* logits, int64_t lo
                         int64_t dlogits_stride, float* logp, float* stats, void* ws, size_t ws_bytes, cf_stream stream);
 
 /* ---- AdamW over many tensors ---------------------------------------------------------------
- * What takes cf_grads (and cf_lora_grads): one launch per 40 tensors, of any sizes,
+ * What takes cf_grads (and cf_lora_grads): one launch per 40 tensors of any sizes (or per 2^31 elements),
  *   g' = grad_scale * g * min(1, max_norm / (norm + 1e-6))
  *   m = beta1*m + (1-beta1)*g',  v = beta2*v + (1-beta2)*g'^2
  *   p = p - lr*weight_decay*p - lr * (m / (1-beta1^step)) / (sqrt(v / (1-beta2^step)) + eps)
@@ -405,7 +405,7 @@ typedef struct {
     const void* g;
     void *m, *v;
     float *m_scale, *v_scale;      /* state_bits 8                              */
-    int64_t n;                     /* elements, 0 to 2^35                       */
+    int64_t n;                     /* elements, 0 to 2^34                       */
     float weight_decay;
 } cf_adamw_tensor;
 

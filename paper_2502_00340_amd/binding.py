@@ -392,7 +392,12 @@ class LayerBackward:
             _check(getattr(lib(), "cf_" + name)(C.byref(self.desc), C.byref(sv), C.byref(w), *args), "cf_" + name)
             return
         name = {"layer_bwd_compact_dev": "layer_bwd_compact"}.get(name, name) + "_qk"
-        qk = LayerQk(*[t.data_ptr() for t in (saved["q_pre"], saved["k_pre"], weights["gq"], weights["gk"])], self.qk_norm_eps,
+        D, dt = self.desc, torch_dtype(self.desc)
+        ts = saved["q_pre"], saved["k_pre"], weights["gq"], weights["gk"]
+        for t, n in zip(ts, (D.B * D.S * D.Hq * D.d, D.B * D.S * D.Hkv * D.d, D.d, D.d)):
+            if t.dtype is not dt or t.numel() != n or not t.is_contiguous():
+                raise ValueError("q_pre, k_pre, gq and gk have to be contiguous and %s, like what the layer's call reads beside them" % dt)
+        qk = LayerQk(*[t.data_ptr() for t in ts], self.qk_norm_eps,
                      _addr(self.grads.get("dgq")), _addr(self.grads.get("dgk")))
         _check(getattr(lib(), "cf_" + name)(C.byref(self.desc), C.byref(sv), C.byref(w), C.byref(qk), *args), "cf_" + name)
 
@@ -571,6 +576,7 @@ def qk_norm_rope_fwd(desc: LayerDesc, q, k, gq, gk, rope_cos=None, rope_sin=None
 def _kept_count(idx, n_kept_dev, rows: int, kept: int):
     _need(idx is None or (idx.dtype == torch.int32 and idx.is_contiguous() and idx.numel() >= kept), "idx has to be int32, one per kept row")
     _need(idx is not None or kept <= rows, "without idx there are at most %d rows" % rows)
+    _need(kept == 0 or rows > 0, "kept rows of an empty tensor")
     _need(n_kept_dev is None or (n_kept_dev.dtype == torch.int32 and n_kept_dev.numel() == 1), "n_kept_dev has to be one int32")
 
 

@@ -95,6 +95,9 @@ static inline hipError_t allow_dynamic_lds(const void* kernel, int bytes, std::a
 }
 
 static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+// Blocks of one launch, at most: a launch counts its threads in 32 bits.
+constexpr int MAX_GRID = 1 << 20;
+
 static inline int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 static inline size_t dtype_size(int dtype) { return dtype == CF_F32 ? 4 : 2; }
 

@@ -40,6 +40,7 @@ struct LossArgs {
     const float *old_logp, *ref_logp, *adv, *weights;
     const int32_t *idx, *n_dev;
     int n_max, V;
+    int first;              // row of the launch's first block
     float scale, k, klo;        // of the logits; times log2(e), and what rounding that left
     bool policy;
     float lo, hi, kl_coef;      // bounds of the ratio
@@ -216,7 +217,7 @@ template <typename T, int NT> __device__ __forceinline__ void stream_row(const L
 template <typename T, int NT>
 __global__ __launch_bounds__(NT) void token_loss_stream_kernel(LossArgs a) {
     __shared__ float red[NT / 32];
-    const int n_rows = live_rows(a.n_max, a.n_dev), j = blockIdx.x;
+    const int n_rows = live_rows(a.n_max, a.n_dev), j = a.first + (int)blockIdx.x;
     if (j >= n_rows) return;
     RowHead r;
     find_row<T>(a, j, r);
@@ -436,10 +437,12 @@ template <typename T, int NT, int NV> static void launch_rows(const LossArgs& a,
 
 // The smallest block whose registers hold a row.  A function of the vocabulary and the type alone: a row's sums, and its logp, are
 // added up in the same order in every call.
-template <typename T> static void launch_token_loss(const LossArgs& a, hipStream_t st) {
+template <typename T> static void launch_token_loss(LossArgs& a, hipStream_t st) {
     const int nv = a.V / Vec<T>::N;
-    if (nv < 1 || nv > 1024 * 20) token_loss_stream_kernel<T, 1024><<<a.n_max, 1024, 0, st>>>(a);
-    else if (nv <= 256 * 4) launch_rows<T, 256, 4>(a, st);
+    if (nv < 1 || nv > 1024 * 20) {
+        for (; a.first < a.n_max; a.first += MAX_GRID)
+            token_loss_stream_kernel<T, 1024><<<a.n_max - a.first < MAX_GRID ? a.n_max - a.first : MAX_GRID, 1024, 0, st>>>(a);
+    } else if (nv <= 256 * 4) launch_rows<T, 256, 4>(a, st);
     else if (nv <= 256 * 8) launch_rows<T, 256, 8>(a, st);
     else if (nv <= 256 * 12) launch_rows<T, 256, 12>(a, st);
     else if (nv <= 256 * 16) launch_rows<T, 256, 16>(a, st);
@@ -495,7 +498,7 @@ cf_status cf_token_loss(const cf_loss_desc* desc, const void* logits, int64_t lo
     if (!ws || off(ws, 16) || ws_bytes < cf_token_loss_workspace_bytes(max_kept)) return CF_ERR_WORKSPACE;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     const double k = (double)scale * 1.4426950408889634;
-    LossArgs a{logits, ls, targets, old_logp, ref_logp, advantages, weights, idx, n_kept_dev, max_kept, desc->V, scale, (float)k, (float)(k - (float)k), policy,
+    LossArgs a{logits, ls, targets, old_logp, ref_logp, advantages, weights, idx, n_kept_dev, max_kept, desc->V, 0, scale, (float)k, (float)(k - (float)k), policy,
                1.f - desc->clip_lo, 1.f + desc->clip_hi, policy ? desc->kl_coef : 0.f, desc->norm, dlogits, ds, logp, (float4*)ws};
     if (max_kept > 0) desc->dtype == CF_F32 ? launch_token_loss<float>(a, st) : launch_token_loss<bf16_t>(a, st);
     if (stats) loss_stats_kernel<<<1, 1024, 0, st>>>((const float4*)ws, max_kept, n_kept_dev, desc->norm, stats);

@@ -291,13 +291,15 @@ def test_binding_refuses_what_the_library_cannot_see(L):
               (q, k, g, g, cos), (q, k, g, g, cos[:10], cos), (q, k, g, g, None, None, idx[:3]), (q, k, g, g, None, None, idx.long()), (q, k, g, g)):
         with pytest.raises(ValueError):
             Bn.qk_norm_rope_fwd(d, *a)
+    with pytest.raises(ValueError):
+        Bn.qk_norm_rope_bwd(d, q[:0], k[:0], g, g, q, k, idx=idx)
     for kw in (dict(idx=idx.long()), dict(idx=idx[:2]), dict(n_kept_dev=idx), dict(main_grads=(g, g)), dict(out=(q[:2], k[:2])), {}):
         with pytest.raises(ValueError):
             Bn.qk_norm_rope_bwd(d, q, k, g, g, q, k, **kw)
     l, y, f = torch.zeros(6, 10), torch.zeros(6, dtype=torch.int64), torch.zeros(6)
     for a, kw in (((l, y.int()), {}), ((l, y[:5]), {}), ((l.t(), y), {}), ((l[:1].expand(6, 10), y), {}), ((l, y), dict(out=l[:1].expand(6, 10))), ((l, y), dict(old_logp=f)), ((l, y, f, f[:3]), {}), ((l, y, f, f.double()), {}),
                   ((l, y), dict(max_kept=7)), ((l, y), dict(idx=idx[:2], max_kept=3)), ((l, y), dict(out=l[:3])), ((l, y), dict(out=l.to(BF))),
-                  ((l, y), dict(weights=f[:2])), ((l, y), dict(idx=idx, out=l)), ((l, y), dict(idx=idx[:2], out=l[1:3])), ((l, y), {})):
+                  ((l, y), dict(weights=f[:2])), ((l, y), dict(idx=idx, out=l)), ((l, y), dict(idx=idx[:2], out=l[1:3])), ((l[:0], y[:0]), dict(idx=idx)), ((l, y), {})):
         with pytest.raises(ValueError):
             Bn.token_loss(*a, **kw)
     with pytest.raises(TypeError):
@@ -407,6 +409,21 @@ def test_qk_norm_positions_outside_the_tables_and_zero_rows():
     assert out[0].shape == (0, 256) and out[1].shape == (0, 128)
     got = Bn.qk_norm_rope_bwd(desc, q, k, gq, gk, q[:0], k[:0], cos, sin)
     assert not bool(got[2].any()) and not bool(got[3].any())
+
+
+@gpu
+def test_qk_norm_of_more_rows_than_one_launch_takes():
+    """33 heads, so that a row takes a wave: 4.2 million rows are more than 2^20 blocks of four."""
+    say("qk many rows")
+    S, times = 1000, 4200
+    g0, q, k, gq, gk, cos, sin = _qk_case(17, BF, S, 31, 2, 16, S)
+    desc = Bn.make_desc(1, S, 256, 31, 2, 16, 256, BF, rms_eps=EPS_N)
+    want = Bn.qk_norm_rope_fwd(desc, q, k, gq, gk, cos, sin)
+    x = [t.repeat(times, 1) for t in (q, k)]
+    Bn.qk_norm_rope_fwd(desc, *x, gq, gk, cos, sin, out=x)
+    for t, w in zip(x, want):
+        for part in t.view(times, S, -1).split(600):
+            assert bool((part == w).all())
 
 
 @gpu
@@ -531,6 +548,22 @@ def test_layer_calls_with_query_key_norm(dtype, rope, main):
     none.compact(dsv, dW, kept, plan.idx, plan.cu_kept, 0)
     for k in names[:-1]:
         assert bool((none.grads[k] == (3.0 if main else 0.0)).all()), k
+
+
+@gpu
+def test_layer_binding_refuses_projections_that_are_views():
+    """Columns of a fused projection, another type, other sizes: the library would read them as dense rows."""
+    shape, W, sv, tabs, _ = _layer_qk_problem(BF)
+    dsv, dW = _layer_qk_device(shape, W, sv, tabs)
+    plan = Bn.LayerBackward(Bn.make_desc(shape.B, shape.S, shape.H, shape.Hq, shape.Hkv, shape.d, shape.F, shape.dtype), qk_norm_eps=EPS_N)
+    dy = torch.zeros((shape.T, shape.H), dtype=BF, device=DEV)
+    fused = torch.cat((dsv["q_pre"], dsv["k_pre"]), 1)
+    for bad in (dict(q_pre=fused[:, :shape.Hq * shape.d]), dict(k_pre=dsv["k_pre"].float()), dict(q_pre=dsv["q_pre"][1:]), dict(k_pre=dsv["q_pre"])):
+        with pytest.raises(ValueError):
+            plan.dense({**dsv, **bad}, dW, dy)
+    for bad in (dict(gq=dW["gq"].float()), dict(gk=dW["gk"][:32])):
+        with pytest.raises(ValueError):
+            plan.dense(dsv, {**dW, **bad}, dy)
 
 
 @gpu
@@ -659,6 +692,21 @@ def test_token_loss_of_more_rows_than_blocks(dtype, rows, V):
     assert torch.equal(again[1][at], got[1]) and torch.equal(kept, out[:, :V])
     Bn.token_loss(l, y, weights=w, norm=float(n), out=l)
     assert torch.equal(l, again[2])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_token_loss_of_more_rows_than_one_launch_takes(dtype):
+    """Rows too short for a vector, many more than 2^20 of them by way of an index with repetitions."""
+    say("loss 2^20 rows", dtype)
+    rows, V, n = 50, 3, (1 << 20) + 77
+    g0, l, y = _loss_case(23, dtype, rows, V)
+    idx = torch.randint(0, rows, (n,), generator=g0, dtype=torch.int32).to(DEV)
+    one = Bn.token_loss(l, y, norm=100.0)
+    got = Bn.token_loss(l, y, norm=100.0, idx=idx)
+    assert torch.equal(got[1], one[1][idx.long()]) and torch.equal(got[2], one[2][idx.long()])
+    want = -one[1][idx.long()].to(F64).sum() / 100
+    close(got[0][0], want, 2 * U * abs(float(want)), "sum")        # fp64 sums of the same fp32 terms, rounded once
 
 
 @gpu
@@ -824,6 +872,24 @@ def test_adamw_first_step_from_zero_states_and_many_tensors():
         opt.step()
         for x, o, d in zip(p, old, g):
             close(x, o.to(F64) - LR * d.to(F64).sign(), 64 * U * LR + 2 * U * o.abs().to(F64) + 1e-12 / d.abs().to(F64) * LR, "first step")
+
+
+@gpu
+def test_adamw_of_more_elements_than_one_launch_takes():
+    """2^31 elements a launch: the third of these tensors is another one's.  From equal values all move alike, and m, rounded to nearest, as well."""
+    say("adamw 3 * 2^30")
+    n = 1 << 30
+    g = torch.empty(n, dtype=BF, device=DEV).normal_(generator=torch.Generator(DEV).manual_seed(3))
+    p = [torch.zeros(k, dtype=BF, device=DEV) for k in (n, n, n, 5000)]
+    opt = Bn.AdamW(p, [g, g, g, g[:5000]], lr=LR, state_bits=8)
+    opt.step()
+    assert torch.equal(p[0] == 0, g == 0)                         # a step of lr, and none without a gradient
+    for i in (1, 2, 3):
+        k = p[i].numel()
+        assert torch.equal(p[i], p[0][:k]), i
+        whole = k - k % 256                                       # scales of what ends inside a block are its own
+        assert torch.equal(opt.m[i][:whole].view(torch.uint8), opt.m[0][:whole].view(torch.uint8)), i
+        assert torch.equal(opt.v_scale[i][:whole // 256], opt.v_scale[0][:whole // 256]), i
 
 
 @gpu
