@@ -95,10 +95,10 @@ template <typename T, bool TAIL> __device__ __forceinline__ void load_lane(const
 #pragma unroll
     for (int q = 0; q < LANE / VN; ++q) Vec<T>::load(p + q * VN, reinterpret_cast<float (&)[VN]>(o[q * VN]));
 }
-// AWAY: past the caches
-typedef float f32x4a __attribute__((ext_vector_type(4)));
+// Past the caches, as all that a step writes.  For bf16 parameters 739 -> 733 us (8 bits, 218 M elements), and 192 -> 187 for the norm that comes next.
+typedef unsigned u32x4a __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2a __attribute__((ext_vector_type(2)));
-template <typename T, bool TAIL, bool AWAY = false> __device__ __forceinline__ void store_lane(T* p, int64_t left, const float (&o)[LANE]) {
+template <typename T, bool TAIL> __device__ __forceinline__ void store_lane(T* p, int64_t left, const float (&o)[LANE]) {
     constexpr int VN = Vec<T>::N;
     if (TAIL && left < LANE) {
 #pragma unroll
@@ -111,8 +111,12 @@ template <typename T, bool TAIL, bool AWAY = false> __device__ __forceinline__ v
     }
 #pragma unroll
     for (int q = 0; q < LANE / VN; ++q) {
-        if constexpr (AWAY) __builtin_nontemporal_store(f32x4a{o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]}, reinterpret_cast<f32x4a*>(p) + q);
-        else Vec<T>::store(p + q * VN, reinterpret_cast<const float (&)[VN]>(o[q * VN]));
+        u32x4a b;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if constexpr (VN == 8) b[e] = pack_bf16x2(o[2 * e], o[2 * e + 1]);
+            else b[e] = __float_as_uint(o[4 * q + e]);
+        __builtin_nontemporal_store(b, reinterpret_cast<u32x4a*>(p) + q);
     }
 }
 // LANE e4m3 bytes
@@ -201,11 +205,11 @@ __device__ __forceinline__ void adamw_block(const AdamArgs& a, const AdamTensor&
             tv = fmaxf(tv, r);
         }
     }
-    if (MASTER) store_lane<float, TAIL, true>(t.master + i, left, w);
-    store_lane<P, TAIL, (Vec<P>::N == 4)>((P*)t.p + i, left, w);
+    if (MASTER) store_lane<float, TAIL>(t.master + i, left, w);
+    store_lane<P, TAIL>((P*)t.p + i, left, w);
     if constexpr (BITS == 32) {
-        store_lane<float, TAIL, true>((float*)t.m + i, left, m);
-        store_lane<float, TAIL, true>((float*)t.v + i, left, v);
+        store_lane<float, TAIL>((float*)t.m + i, left, m);
+        store_lane<float, TAIL>((float*)t.v + i, left, v);
     } else {
         tm = block_max(tm);
         tv = block_max(tv);
@@ -218,15 +222,29 @@ __device__ __forceinline__ void adamw_block(const AdamArgs& a, const AdamTensor&
         }
         store_bytes<TAIL>((unsigned char*)t.m + i, left, to_q(m));
         store_bytes<TAIL>((unsigned char*)t.v + i, left, to_q(v));
-        if (threadIdx.x % (QBLOCK / LANE) == 0 && (!TAIL || left > 0)) {
-            t.ms[blk] = tm * (1.f / 448.f);
-            t.vs[blk] = tv * (1.f / 448.f);
+        if constexpr (TAIL) {
+            if (threadIdx.x % (QBLOCK / LANE) == 0 && left > 0) {
+                t.ms[blk] = tm * (1.f / 448.f);
+                t.vs[blk] = tv * (1.f / 448.f);
+            }
+        } else {
+            __shared__ float sc[2][CHUNK / QBLOCK];         // a block's scales are written together: 739 -> 732 us for 218 M elements
+            if (threadIdx.x % (QBLOCK / LANE) == 0) {
+                sc[0][threadIdx.x / (QBLOCK / LANE)] = tm * (1.f / 448.f);
+                sc[1][threadIdx.x / (QBLOCK / LANE)] = tv * (1.f / 448.f);
+            }
+            __syncthreads();
+            if (threadIdx.x < CHUNK / QBLOCK) {
+                const int64_t b0 = i / CHUNK * (CHUNK / QBLOCK) + threadIdx.x;
+                t.ms[b0] = sc[0][threadIdx.x];
+                t.vs[b0] = sc[1][threadIdx.x];
+            }
         }
     }
 }
 
-// bf16 with fp32 copies and gradients, 32-bit states: 44 M elements, 1.3 GB in 214 us (6.2 TB/s, a large copy's rate).  8-bit states: 218 M elements,
-// 3.9 GB in 672 us (5.9 TB/s).  Four elements a lane with conditions took 236 and 756; eight, and conditions only in a tensor's last block, 223 and 713; copies
+// bf16 with fp32 copies and gradients, 32-bit states: 44 M elements, 1.3 GB in 221 us (6.0 TB/s; a copy of 1 GiB reaches 6.2).  8-bit states: 218 M elements,
+// 3.9 GB in 699 us (5.6 TB/s).  Four elements a lane with conditions took 236 and 756; eight, and conditions only in a tensor's last block, 223 and 713; copies
 // and states past the caches the rest.  A block takes CHUNK elements and ends: with 2, 4, 8 and 16 times as many, 218 (of then) became 233, 240, 252 and 275.
 template <typename P, typename G, bool MASTER, int BITS>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
