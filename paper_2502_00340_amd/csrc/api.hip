@@ -496,6 +496,14 @@ cf_status check_qk_rows(const cf_layer_desc& L, const cf_qk* r) {
     return CF_OK;
 }
 
+// rows written in place have to be those that are read
+bool qk_in_place(const cf_layer_desc& L, const cf_qk& from, const cf_qk& to, int n_rows) {
+    const int64_t nq = (int64_t)L.Hq * L.d, nk = (int64_t)L.Hkv * L.d;
+    const auto stride = [](int64_t s, int64_t dense) { return s ? s : dense; };
+    return n_rows < 2 || ((to.q != from.q || stride(to.q_stride, nq) == stride(from.q_stride, nq)) &&
+                          (to.k != from.k || stride(to.k_stride, nk) == stride(from.k_stride, nk)));
+}
+
 cf_status check_layer_qk(const cf_layer_desc* L, const cf_layer_qk* qk, bool lora) {
     if (!qk || !qk->q_pre || !qk->k_pre || !qk->gq || !qk->gk || (qk->dgq == nullptr) != (qk->dgk == nullptr)) return CF_ERR_NULL;
     cf_layer_desc D = *L;
@@ -940,7 +948,7 @@ cf_status cf_qk_norm_rope_fwd(const cf_layer_desc* desc, const cf_qk_norm* p, co
     if (s == CF_OK) s = check_qk_rows(*desc, in);
     if (s == CF_OK) s = check_qk_rows(*desc, out);
     if (s != CF_OK) return s;
-    if (n_rows < 0 || n_rows > 1 << 30) return CF_ERR_SHAPE;
+    if (n_rows < 0 || n_rows > 1 << 30 || !qk_in_place(*desc, *in, *out, n_rows)) return CF_ERR_SHAPE;
     CF_HIP(launch_qk_norm_fwd(*desc, *p, *in, n_rows, *out, as_stream(stream)));
     return CF_OK;
 }
@@ -955,6 +963,7 @@ cf_status cf_qk_norm_rope_bwd(const cf_layer_desc* desc, const cf_qk_norm* p, co
     if (s != CF_OK) return s;
     if ((dgq == nullptr) != (dgk == nullptr)) return CF_ERR_NULL;
     if (max_kept < 0 || max_kept > 1 << 30 || (main_grad != 0 && main_grad != 1)) return CF_ERR_SHAPE;
+    if (!qk_in_place(*desc, *dy_kept, *dx_kept, max_kept)) return CF_ERR_SHAPE;
     if (misaligned(idx, 4) || misaligned(n_kept_dev, 4) || misaligned(dgq, 4) || misaligned(dgk, 4)) return CF_ERR_SHAPE;
     if (dgq && (!ws || misaligned(ws, 256) || ws_bytes < qk_norm_partial_bytes(desc->d, max_kept))) return CF_ERR_WORKSPACE;
     CF_HIP(launch_qk_norm_bwd(*desc, *p, *in, *dy_kept, idx, RowCount{max_kept, n_kept_dev}, *dx_kept, dgq, dgk, main_grad != 0,

@@ -184,6 +184,7 @@ def test_qk_norm_refusals(L):
             (dict(p=Bn.QkNorm(FAKE, FAKE, None, None, FAKE + 2)), 2),
             (dict(x=Bn.Qk(None, FAKE, 0, 0)), 1), (dict(x=Bn.Qk(FAKE, FAKE + 2, 0, 0)), 2), (dict(x=Bn.Qk(FAKE, FAKE, 260, 0)), 2),
             (dict(x=Bn.Qk(FAKE, FAKE, 248, 0)), 2), (dict(y=Bn.Qk(FAKE, FAKE, 0, 120)), 2), (dict(y=Bn.Qk(FAKE, FAKE, 0, -128)), 2),
+            (dict(y=Bn.Qk(FAKE, FAKE, 264, 0)), 2), (dict(x=Bn.Qk(FAKE, FAKE, 0, 136)), 2),
             (dict(desc=_desc(d=80)), 5), (dict(desc=_desc(d=512)), 5), (dict(desc=_desc(d=8)), 5), (dict(desc=_desc(d=60)), 2),
             (dict(desc=_desc(d=4, dtype="f32")), 2), (dict(desc=_desc(d=512, dtype="f32")), 2), (dict(desc=_desc(rms_eps=-1.0)), 2),
             (dict(desc=_desc(rms_eps=float("nan"))), 2), (dict(desc=_desc(S=0)), 2), (dict(desc=_desc(Hkv=0)), 2)):
@@ -196,11 +197,11 @@ def test_qk_norm_refusals(L):
     assert 0 < need < L.cf_qk_norm_workspace_bytes(C.byref(d), 100000) and L.cf_qk_norm_workspace_bytes(C.byref(d), -1) == 0
     assert L.cf_qk_norm_workspace_bytes(C.byref(_desc(d=80)), 100) == 0
 
-    def bwd(idx=FAKE, nd=None, n=100, dgq=FAKE, dgk=FAKE, main=0, ws=FAKE, wsb=need):
-        return L.cf_qk_norm_rope_bwd(C.byref(d), C.byref(p), C.byref(x), C.byref(x), idx, nd, n, C.byref(x), dgq, dgk, main, ws, wsb, None)
+    def bwd(idx=FAKE, nd=None, n=100, dgq=FAKE, dgk=FAKE, main=0, ws=FAKE, wsb=need, dx=x):
+        return L.cf_qk_norm_rope_bwd(C.byref(d), C.byref(p), C.byref(x), C.byref(x), idx, nd, n, C.byref(dx), dgq, dgk, main, ws, wsb, None)
 
     for kw, code in ((dict(dgk=None), 1), (dict(dgq=None), 1), (dict(n=-1), 2), (dict(main=2), 2), (dict(idx=FAKE + 1), 2), (dict(nd=FAKE + 2), 2),
-                     (dict(dgq=FAKE + 1), 2), (dict(ws=None), 4), (dict(ws=FAKE + 16), 4), (dict(wsb=need - 512), 4)):
+                     (dict(dgq=FAKE + 1), 2), (dict(dx=Bn.Qk(FAKE, FAKE, 264, 0)), 2), (dict(ws=None), 4), (dict(ws=FAKE + 16), 4), (dict(wsb=need - 512), 4)):
         assert bwd(**kw) == code, kw
 
 
@@ -548,6 +549,46 @@ def test_layer_calls_with_query_key_norm(dtype, rope, main):
     none.compact(dsv, dW, kept, plan.idx, plan.cu_kept, 0)
     for k in names[:-1]:
         assert bool((none.grads[k] == (3.0 if main else 0.0)).all()), k
+
+
+@gpu
+@pytest.mark.parametrize("main", [False, True])
+def test_layer_call_with_query_key_norm_in_a_graph(main):
+    """Replays with other counts, none and all among them, against eager calls of another plan between them."""
+    say("layer qk graph", main)
+    shape, W, sv, tabs, rng = _layer_qk_problem(BF)
+    dsv, dW = _layer_qk_device(shape, W, sv, tabs)
+    dy = Hn.to_dev(Hn.quantize(rng.standard_normal((shape.T, shape.H)), shape.dtype), shape.dtype)
+    desc = Bn.make_desc(shape.B, shape.S, shape.H, shape.Hq, shape.Hkv, shape.d, shape.F, shape.dtype)
+    plan, other = (Bn.LayerBackward(desc, main_grad=main, qk_norm_eps=EPS_N) for _ in range(2))
+    mask = torch.from_numpy(WL.mask_topk(rng, shape.B, shape.S, 0.6)).to(DEV)
+
+    def call(p):
+        idx, cu, nd, _ = Bn.build_keep_index(mask, sync=False)
+        p.compact_dev(dsv, dW, dy, idx, cu, nd)
+        return nd
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        call(plan)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            call(plan)
+    torch.cuda.synchronize()
+    for rho in (0.3, 1.0, 0.0, 0.7):
+        mask.copy_((torch.rand((shape.B, shape.S), generator=gen(int(10 * rho))) < rho).to(torch.uint8))
+        for p in (plan, other):
+            for g in p.grads.values():
+                g.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        n = int(call(other))
+        torch.cuda.synchronize()
+        assert n == int(mask.sum())
+        for k, g in plan.grads.items():
+            assert torch.equal(g[:n], other.grads[k][:n]) if k == "dx" else torch.equal(g, other.grads[k]), (rho, k)
 
 
 @gpu
