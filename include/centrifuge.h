@@ -394,10 +394,12 @@ cf_status cf_token_loss(const cf_loss_desc* desc, const void* logits, int64_t lo
  * step_dev, lr_dev (device, nullable) replace step and lr, for a call captured into a graph.
  *   p        CF_F32 parameters, or CF_BF16 ones with (master) or without an fp32 master copy; p is the rounded master
  *   m, v     state_bits 32: fp32.  state_bits 8: e4m3 bytes that stand for m / m_scale and sqrt(v) / v_scale, with a scale for every
- *            256 elements (ceil(n/256) of them): the block's largest absolute value / 448.  m is rounded to nearest.  sqrt(v) is rounded up with the
+ *            256 elements (ceil(n/256) of them): the block's largest absolute value / 448.  sqrt(v) is rounded up with the
  *            probability of what is cut off, by 20 bits of a hash of (seed, step, tensor's number in the call, element): to nearest, an average over
  *            1/(1-beta2) steps would stand still, since a step changes it by less than half a step of 8 bits; and never
- *            to 0 unless it is 0, which a later division by eps would blow up.
+ *            to 0 unless it is 0, which a later division by eps would blow up.  m is rounded to nearest, but in the same way (by 12 other bits of the hash, to
+ *            0 too) where |g'| is at most 3/8 of |m| and |m| falls by less than half a step: an m whose gradient has ended would stand still beside
+ *            a root that goes on falling.
  * All pointers 16-byte aligned (scales: 4); no overlap.  The tensors array is read on the host during the call. */
 typedef struct {
     void* p;

@@ -149,23 +149,44 @@ __device__ __forceinline__ uint2 to_q(const float (&x)[LANE]) {
                       __builtin_amdgcn_cvt_pk_fp8_f32(x[6], x[7], __builtin_amdgcn_cvt_pk_fp8_f32(x[4], x[5], 0, false), true));
 }
 // over the 32 lanes of a scale
+constexpr float TOP_MIN = 0x1p-100f;
 __device__ __forceinline__ float block_max(float v) {
 #pragma unroll
     for (int o = QBLOCK / LANE / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    return fmaxf(v, 0x1p-100f);
+    return fmaxf(v, TOP_MIN);
 }
-// 20 bits of a hash of an element: two multiplications with shifts around them over its number and the tensor's key
+// A hash of an element: two multiplications with shifts around them over its number and the tensor's key.  Its upper 20 bits round v, the
+// lower 12 m.
 __device__ __forceinline__ uint32_t dither(uint32_t h) {
     h = (h ^ (h >> 16)) * 0x85EBCA6Bu;
     h = (h ^ (h >> 13)) * 0xC2B2AE35u;
-    return (h ^ (h >> 16)) >> 12;
+    return h ^ (h >> 16);
+}
+// The distance of the e4m3 values from r (not negative, in units of the scale) on, and its inverse
+__device__ __forceinline__ void e4m3_step(float r, float& ulp, float& inv) {
+    const unsigned e = __float_as_uint(fmaxf(r, 0x1p-6f)) & 0x7F800000u;
+    ulp = __uint_as_float(e - (3u << 23)), inv = __uint_as_float((257u << 23) - e);     // 2^(e-3)
 }
 // r in units of the scale, rounded up to the next e4m3 value where what is cut off and the dither make a step together; not to 0
 __device__ __forceinline__ float round_up_by(float r, uint32_t u) {
-    const unsigned e = __float_as_uint(fmaxf(r, 0x1p-6f)) & 0x7F800000u;
-    const float ulp = __uint_as_float(e - (3u << 23)), inv = __uint_as_float((257u << 23) - e);     // 2^(e-3) and its inverse
+    float ulp, inv;
+    e4m3_step(r, ulp, inv);
     const float q = floorf(fmaf((float)u, 0x1p-20f, r * inv)) * ulp;
     return r > 0.f ? fminf(fmaxf(q, 0x1p-9f), 448.f) : r;
+}
+// What m may be of its old value, in gradients, to fall by itself.  With beta1 = 0.9 such an m falls by 1/16 or more, which is half of e4m3's largest step:
+// only below the normal values does nearest keep it then.
+constexpr float FALLS = 0.375f;
+// m (new) in units of the scale (im: its inverse), of which the old value was `old`: rounded to nearest by the conversion behind, unless it falls by itself and by
+// less than half a step.  There nearest would keep it, for good where the gradient has ended, while the root of v falls on: such an m is rounded down
+// or up by 12 random bits, without bias.
+__device__ __forceinline__ float let_fall(float m, float old, float b1, float c1, float im, uint32_t u) {
+    const float r = fabsf(m) * im, r0 = fabsf(old) * im;
+    float ulp, inv;
+    e4m3_step(r, ulp, inv);
+    const bool alone = fabsf(m - b1 * old) <= FALLS * c1 * fabsf(old);
+    const float q = fminf(floorf(fmaf((float)u, 0x1p-12f, r * inv)) * ulp, 448.f);
+    return copysignf(alone && r0 - r < 0.5f * ulp ? q : r, m);
 }
 
 template <typename P, typename G, bool MASTER, int BITS, bool TAIL>
@@ -190,12 +211,15 @@ __device__ __forceinline__ void adamw_block(const AdamArgs& a, const AdamTensor&
         from_q(qv, vs, v);
     }
     const float keep = 1.f - s.lr * t.wd;
-    float tm = 0.f, tv = 0.f;
+    float tm = 0.f, tv = 0.f, fall = -INFINITY;
 #pragma unroll
     for (int e = 0; e < LANE; ++e) {
         if (BITS == 8) v[e] = rounded(v[e], v[e]);
-        const float x = rounded(g[e], s.clip);
+        const float x = rounded(g[e], s.clip), old = fabsf(m[e]);
         m[e] = rounded(a.b1, m[e]) + rounded(a.c1, x);
+        // above -(half of the smallest step): let_fall may have something to do
+        if (BITS == 8) fall = fmaxf(fall, fminf(fmaf(1.0625f, fabsf(m[e]), -old), fmaf(FALLS, old, -fabsf(x))));
+        if (BITS == 8) asm("" : "+v"(fall));
         v[e] = rounded(a.b2, v[e]) + rounded(a.c2, rounded(x, x));
         const float r = root(v[e]);
         w[e] = fmaf(-s.size * m[e], __builtin_amdgcn_rcpf(fmaf(r, s.inv_root, a.eps)), w[e] * keep);
@@ -216,12 +240,22 @@ __device__ __forceinline__ void adamw_block(const AdamArgs& a, const AdamTensor&
         const float im = rounded(1.f / tm, 448.f), iv = rounded(1.f / tv, 448.f);
         const uint32_t h = (uint32_t)i * 0x9E3779B1u + (uint32_t)(i >> 32) * 0x27D4EB2Fu + key;
 #pragma unroll
-        for (int e = 0; e < LANE; ++e) {
-            m[e] *= im;
-            v[e] = round_up_by(rounded(v[e], iv), dither(h + e * 0x9E3779B1u));
+        for (int e = 0; e < LANE; ++e) v[e] = round_up_by(rounded(v[e], iv), dither(h + e * 0x9E3779B1u) >> 12);
+        store_bytes<TAIL>((unsigned char*)t.v + i, left, to_q(v));
+        if (fall >= tm * (-0x1p-10f / 448.f) && tm > TOP_MIN) {
+            from_q(qm, ms, v);          // the old ones
+            uint32_t again = h;         // the hashes are made again, rather than held in eight registers
+            asm("" : "+v"(again));
+#pragma unroll
+            for (int e = 0; e < LANE; ++e) {
+                m[e] = let_fall(m[e], v[e], a.b1, a.c1, im, dither(again + e * 0x9E3779B1u) & 0xFFFu);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < LANE; ++e) m[e] *= im;
         }
         store_bytes<TAIL>((unsigned char*)t.m + i, left, to_q(m));
-        store_bytes<TAIL>((unsigned char*)t.v + i, left, to_q(v));
         if constexpr (TAIL) {
             if (threadIdx.x % (QBLOCK / LANE) == 0 && left > 0) {
                 t.ms[blk] = tm * (1.f / 448.f);

@@ -1,0 +1,81 @@
+"""Edges of the operators around the layer calls: states that outlive their gradients, values beyond a type, sizes at the ends of an index,
+overlapping tensors.  Plain forms and tolerances as in test_step_ops."""
+import ctypes as C
+import math
+
+import pytest
+import torch
+
+from paper_2502_00340_amd import binding as Bn
+from tests import harness as Hn
+from tests import test_step_ops as ops
+from tests.test_step_ops import AEPS, B1, B2, BF, DEV, EPS_N, F32, F64, LR, U, close, gen, gpu, randn, say
+
+
+# ---- AdamW: 8-bit states -----------------------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("b1,b2", [(0.9, 0.95), (0.9, 0.999), (0.95, 0.95), (0.95, 0.999)])
+def test_adamw_8_bit_states_come_to_rest_without_a_gradient(b1, b2):
+    """Half of the elements of every block lose their gradient after 100 steps, the others keep the scales up.  m is unbiased while it falls: n steps on, the
+    mean code of what was at most 448 * 2^9 smallest codes is b1^n times that, 1e-7 of one after the n below (an m is at rest with all but 1e-7 of
+    probability, one of 8192 but for 1e-3): then the parameter stands still.  Until then it moves as far as with 32-bit states: an m and a root are off by a step of
+    2^-3 at most, their quotient by (1 + 2^-3) / (1 - 2^-3) - 1 < 0.3, and so is the mean of what the elements moved."""
+    say("adamw8 rest", b1, b2)
+    n, live = 16384, 100
+    rest = int(math.log(448 * 512 * 1e7) / -math.log(b1))
+    dead = torch.arange(n, device=DEV) % 2 == 1
+    g0 = torch.Generator(DEV).manual_seed(11)
+    g = torch.empty(n, device=DEV)
+    opts = [Bn.AdamW([torch.zeros(n, device=DEV)], [g], lr=1.0, betas=(b1, b2), eps=1e-12, state_bits=bits, seed=5) for bits in (32, 8)]
+    at = []
+    for step in range(live + rest + 300):
+        g.normal_(std=1e-2, generator=g0)
+        if step >= live:
+            g.masked_fill_(dead, 0.0)
+        for o in opts:
+            o.step()
+        if step + 1 in (live, live + rest):
+            at.append([o.params[0].clone() for o in opts])
+    assert not bool(opts[1].m[0].float()[dead].any()), "the average of a gradient that ended"
+    assert torch.equal(opts[1].params[0][dead], at[1][1][dead]), "a parameter without a gradient"
+    far = [float((o.params[0] - a)[dead].double().abs().mean()) for o, a in zip(opts, at[0])]
+    assert abs(far[1] / far[0] - 1.0) < 0.3, far
+    assert bool((opts[1].v[0].float()[dead] > 0).all())
+
+
+@gpu
+@pytest.mark.parametrize("b1", [0.95, 0.99, 0.999])
+def test_adamw_8_bit_averages_fall_without_bias(b1):
+    """One step from all kinds of codes, without a gradient but for the one that keeps a block's scale: an m that falls by less than half a step is off by less than
+    a step, and by nothing on average.  A step s of e4m3, n elements, errors between -s and s with a variance of at most s^2/4: the mean is within
+    6 * s / (2 sqrt(n)), and 2^-12 steps below for the 12 bits that decide.  Those that fall by more are rounded to nearest."""
+    say("adamw8 falls", b1)
+    n = 1 << 18
+    g0 = gen(31)
+    q = (torch.randn(n, generator=g0) * torch.exp2(-16 * torch.rand(n, generator=g0)) * 120).clamp(-448, 448)
+    q[::256] = 448.0
+    q = q.to(torch.float8_e4m3fn).to(DEV)
+    scale = torch.full((n // 256,), 2.0 ** -12, device=DEV)
+    m0 = q.double() * 2.0 ** -12
+    g = torch.zeros(n, device=DEV)
+    g[::256] = 448.0 * 2.0 ** -12
+    opt = Bn.AdamW([torch.zeros(n, device=DEV)], [g], lr=1e-3, betas=(b1, 0.999), seed=3,
+                   state=([q], [torch.full((n,), 448.0, device=DEV).to(torch.float8_e4m3fn)], [scale], [scale.clone()]))
+    opt.step(step=50)
+    close(opt.m_scale[0], torch.full((n // 256,), 2.0 ** -12), 8 * U * 2.0 ** -12, "scale")
+    y = m0.abs() * b1 * 4096.0
+    step = torch.exp2(torch.floor(torch.log2(y.clamp(min=2.0 ** -6))) - 3.0)
+    off = (opt.m[0].double() * m0.sign() - y) / step
+    free = (g == 0) & (m0 != 0)
+    slow = free & ((m0.abs() * 4096.0 - y) < (0.5 - 1e-4) * step)
+    assert int(slow.sum()) > n // 10 and float(off[slow].abs().max()) <= 1.0 + 1e-4
+    for k in (slow, slow & (y < 2.0 ** -6), slow & (y >= 2.0 ** -6)):
+        mean, lim = float(off[k].mean()), 6 * 0.5 / math.sqrt(int(k.sum()))
+        assert int(k.sum()) > 1000 and -lim - 2.0 ** -12 < mean < lim, (mean, lim, int(k.sum()))
+    fast = free & ((m0.abs() * 4096.0 - y) > (0.5 + 1e-4) * step)
+    assert not bool(fast.any()) or float(off[fast].abs().max()) <= 0.5 + 1e-4
+    assert not bool(opt.m[0].float()[m0 == 0].any())
+
+
+L = ops.L
