@@ -399,7 +399,8 @@ cf_status cf_token_loss(const cf_loss_desc* desc, const void* logits, int64_t lo
  *            1/(1-beta2) steps would stand still, since a step changes it by less than half a step of 8 bits; and never
  *            to 0 unless it is 0, which a later division by eps would blow up.  m is rounded to nearest, but in the same way (by 12 other bits of the hash, to
  *            0 too) where |g'| is at most 3/8 of |m| and |m| falls by less than half a step: an m whose gradient has ended would stand still beside
- *            a root that goes on falling.
+ *            a root that goes on falling.  An element whose new v is beyond fp32 keeps its moments (its update is 0, and NaN for an infinite g', as
+ *            with 32 bits); NaN counts for no scale.  A finite value far above its block's others takes their resolution.
  * All pointers 16-byte aligned (scales: 4); no overlap.  The tensors array is read on the host during the call. */
 typedef struct {
     void* p;

@@ -78,4 +78,40 @@ def test_adamw_8_bit_averages_fall_without_bias(b1):
     assert not bool(opt.m[0].float()[m0 == 0].any())
 
 
+@gpu
+@pytest.mark.parametrize("bad", [1e30, -1e30, float("inf"), float("-inf"), float("nan")])
+def test_adamw_8_bit_block_outlives_a_value_beyond_fp32(bad):
+    """Without clipping: what one element does to itself, as with 32-bit states, its block's others do not see."""
+    say("adamw8 poison", bad)
+    n, at = 700, [5, 300, 699]
+    g0 = gen(33)
+    first, then = randn(g0, n, std=1e-2), randn(g0, n, std=1e-2)
+    ends = []
+    for with_bad in (False, True):
+        g = first.clone()
+        g[at] = bad if with_bad else 0.0
+        opt = Bn.AdamW([torch.zeros(n, device=DEV)], [g], lr=LR, betas=(B1, B2), eps=AEPS, state_bits=8, seed=7)
+        opt.step()
+        moved = opt.params[0].clone()
+        g.copy_(then)
+        for _ in range(3):
+            opt.step()
+        ends.append((moved, opt.params[0], opt.m[0].float(), opt.v[0].float(), opt.m_scale[0], opt.v_scale[0]))
+    others = torch.ones(n, dtype=torch.bool, device=DEV)
+    others[at] = False
+    if math.isnan(bad):         # it stays, and takes no part in the scales
+        for a, b in zip(ends[0][:4], ends[1][:4]):
+            assert bool(b[at].isnan().all()) and bool(a[others].isfinite().all()) and bool(b[others].isfinite().all())
+        return
+    for a, b in zip(ends[0][:1] + ends[0][2:4], ends[1][:1] + ends[1][2:4]):
+        assert torch.equal(a[others], b[others])
+    for a, b in zip(ends[0][4:], ends[1][4:]):
+        assert torch.equal(a, b)
+    assert torch.equal(ends[0][1][others], ends[1][1][others])
+    if math.isfinite(bad):      # an update of 0, moments as they were
+        assert not bool(ends[1][0][at].any()) and torch.equal(ends[0][1], ends[1][1])
+    else:
+        assert bool(ends[1][0][at].isnan().all())
+
+
 L = ops.L
