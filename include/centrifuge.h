@@ -354,8 +354,8 @@ cf_status cf_layer_bwd_lora_qk(const cf_layer_desc* desc, const cf_saved* saved,
  *   CF_LOSS_POLICY  L = -min(r*A, clip(r, 1-clip_lo, 1+clip_hi)*A) + kl_coef*k,  r = exp(lp - old_logp),
  *                   k = exp(ref_logp - lp) - (ref_logp - lp) - 1   (ref_logp NULL: k = 0)
  *   loss = sum_j w_j*L_j / norm,   dlogits[j,c] = w_j/norm * dL/dlp * s * ([c == y] - exp(s*l_c - logsumexp)),
- * with dL/dlp of the first term 0 where the clipped product is the smaller one and -r*A elsewhere.  norm 0 stands for the
- * number of live rows.  A row whose target lies outside [0,V) or whose weight is 0 is left out whatever it holds (infinities
+ * with dL/dlp of the first term 0 where the clipped product is the smaller one and -r*A elsewhere.  r*A is 0 where A is, and a KL term with kl_coef 0 is in
+ * stats alone, also where r or k is beyond fp32.  norm 0 stands for the number of live rows.  A row whose target lies outside [0,V) or whose weight is 0 is left out whatever it holds (infinities
  * and NaN included): its logp and its gradient are 0; it counts in the number of live rows.  A logit of -inf has probability 0.
  *   logits   [rows,V], row stride logits_stride elements (0 = V); kept row j is row idx[j] (NULL: row j).  Any alignment of rows:
  *            pointers need their element's only, multiples of 16 bytes are faster

@@ -93,17 +93,21 @@ template <typename T> __device__ __forceinline__ void load_head(const LossArgs& 
 __device__ __forceinline__ RowLoss row_loss(const LossArgs& a, const RowHead& h, float lp, float inv_norm) {
     const float w = h.w;
     if (!a.policy) return RowLoss{make_float4(-w * lp, -w * lp, 0.f, 0.f), -w * inv_norm};
-    const float A = h.adv, r = expf(lp - h.old);
+    // A ratio beyond fp32 counts for nothing without an advantage, and a divergence beyond it for nothing without a coefficient: neither makes 0 * inf
+    const float A = h.adv, r = expf(lp - h.old), rA = A == 0.f && r == r ? 0.f : r * A;
     const float rc = fminf(fmaxf(r, a.lo), a.hi);
-    const bool clipped = r * A > rc * A;
-    const float first = clipped ? -rc * A : -r * A;
-    float d = clipped ? 0.f : -r * A, k = 0.f;
+    const bool clipped = rA > rc * A;
+    const float first = clipped ? -rc * A : -rA;
+    float d = clipped ? 0.f : -rA, k = 0.f, kl = 0.f;
     if (a.ref_logp != nullptr) {
         const float q = h.ref - lp, e = expm1f(q);          // exp(q) - 1 as such: k is the small rest of it
-        k = e - q;
-        d -= a.kl_coef * e;
+        k = e < INFINITY ? e - q : e;
+        if (a.kl_coef != 0.f) {
+            kl = a.kl_coef * k;
+            d -= a.kl_coef * e;
+        }
     }
-    return RowLoss{make_float4(w * (first + a.kl_coef * k), w * first, w * k, clipped ? w : 0.f), w * inv_norm * d};
+    return RowLoss{make_float4(w * (first + kl), w * first, w * k, clipped ? w : 0.f), w * inv_norm * d};
 }
 
 // One exponential of a softmax, 2^(k*(x - m)).  For fp32 logits (EXACT) the roundings of k*(x - m) and of k itself, up to 2^-19 of a small

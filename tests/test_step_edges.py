@@ -114,4 +114,55 @@ def test_adamw_8_bit_block_outlives_a_value_beyond_fp32(bad):
         assert bool(ends[1][0][at].isnan().all())
 
 
+# ---- losses ------------------------------------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_policy_loss_is_finite_where_it_is_defined(dtype):
+    """A KL term that is only watched, of a target that a mask has taken away since; no advantage at a ratio beyond fp32; both at once, and next to rows
+    that hold neither."""
+    say("policy finite", dtype)
+    V, rows = 300, 6
+    g0 = gen(41)
+    l = randn(g0, rows, V, std=2.0, dtype=dtype)
+    y = torch.randint(0, V, (rows,), generator=g0).to(DEV)
+    at = torch.arange(rows, device=DEV)
+    l[0, y[0]] = -200.0                     # lp about -206: exp(ref - lp) beyond fp32
+    l[2, y[2]] = -torch.inf
+    lp = torch.log_softmax(l.double(), 1)[at, y]
+    ref = (lp + 0.1).float()
+    ref[0], ref[2] = -3.0, -2.0
+    old = (lp - 0.05).float()
+    old[0], old[1], old[2], old[4] = -190.0, float(lp[1]) - 150.0, -1.0, float(lp[4]) - 100.0
+    adv = torch.tensor([1.5, 0.0, -1.0, 0.7, -0.0, 0.0], device=DEV)
+    kw = dict(old_logp=old, advantages=adv, clip=(0.2, 0.3), norm=float(rows))
+    stats, got, dl = Bn.token_loss(l, y, ref_logp=ref, kl_coef=0.0, **kw)
+    plain = Bn.token_loss(l, y, **kw)
+    for a, b in ((stats[:2], plain[0][:2]), (got, plain[1]), (dl, plain[2])):
+        assert torch.equal(a, b), "a KL term that does not count"
+    assert math.isinf(float(stats[2])), "it is reported all the same"
+    # row by row: ratios exp(lp - old), clipped where the clipped product is smaller, nothing where there is no advantage
+    r = (lp - old.double()).exp().clamp(max=1e30)
+    a = adv.double()
+    slope = torch.where(torch.minimum(r * a, r.clamp(0.8, 1.3) * a) < r * a, 0.0, -r * a)
+    first = -torch.minimum(r * a, r.clamp(0.8, 1.3) * a)
+    p = torch.softmax(l.double(), 1)
+    p.neg_()[at, y] += 1.0
+    want = p * (slope / rows)[:, None]
+    tol = (ops.EPS[dtype] + 2.0 ** -12) * want.abs() + 2.0 ** -12 * (slope.abs() / rows)[:, None] * 1e-3      # exp of lp - old: an lp of 206 is off by 2^-13 at most
+    close(dl, want, tol, "dlogits")
+    close(stats[0], first.sum() / rows, 2.0 ** -12 * first.abs().sum() / rows, "loss")
+    # with a KL term that counts, the rows without an advantage have that term alone
+    some = torch.tensor([1, 3, 4, 5], dtype=torch.int32, device=DEV)
+    stats, _, dl = Bn.token_loss(l, y, ref_logp=ref, kl_coef=0.1, idx=some, **kw)
+    i = some.long()
+    q = ref.double()[i] - lp[i]
+    want = p[i] * ((slope[i] + 0.1 * (1.0 - q.exp())) / rows)[:, None]
+    close(dl, want, ops.EPS[dtype] * want.abs() + 2.0 ** -12 * ((slope[i].abs() + 0.1) / rows)[:, None] * (p[i].abs() + 1e-3), "dlogits with KL")
+    close(stats[0], (first[i] + 0.1 * (q.exp() - 1.0 - q)).sum() / rows, 2.0 ** -12 * (first[i].abs() + 0.1).sum() / rows, "loss with KL")
+    for bad in (float("nan"), float("inf")):        # what is not defined does not become so: a row of NaN keeps its NaN
+        l[5, 7] = bad
+        assert bool(Bn.token_loss(l, y, ref_logp=ref, kl_coef=0.0, **kw)[2][5].isnan().all())
+
+
 L = ops.L
