@@ -310,9 +310,9 @@ cf_status layer_core(const cf_layer_desc& L, const cf_saved& sv, const cf_weight
                                  w.dk, w.dv, w.attn_ws, st, idx ? sv.attn_out : nullptr, idx ? sv.q : nullptr, sv.rope_cos,
                                  sv.rope_sin, parts);
     if (as != CF_OK) return as;
-    if (qk) CF_HIP(qk_norm_back(L, *qk, w, idx, rows, mg, st));
     dw(a_rows, w.dr, G.dwo, Nq, H);                  // dWo = a^T * dr      [Nq,H]
     if (!late_dwo) CF_HIP(dw_launch(&dws[--n_dw], 1));
+    if (qk) CF_HIP(qk_norm_back(L, *qk, w, idx, rows, mg, st));      // behind it: the heads' gains are outputs, too
 
     void* dh1 = w.bufHb;
     {   // dh1 = dq*Wq^T + dk*Wk^T + dv*Wv^T

@@ -165,4 +165,31 @@ def test_policy_loss_is_finite_where_it_is_defined(dtype):
         assert bool(Bn.token_loss(l, y, ref_logp=ref, kl_coef=0.0, **kw)[2][5].isnan().all())
 
 
+# ---- query/key norm ----------------------------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("main", [False, True])
+def test_dense_layer_call_whose_gains_lie_over_the_attention_output(dtype, main):
+    """Outputs may lie over the attention output of a dense call; the gains' gradients come out earlier than most."""
+    say("gains over attn_out", dtype, main)
+    shape, W, sv, tabs, rng = ops._layer_qk_problem(dtype)
+    dsv, dW = ops._layer_qk_device(shape, W, sv, tabs)
+    dy = Hn.to_dev(Hn.quantize(rng.standard_normal((shape.T, shape.H)), shape.dtype), shape.dtype)
+    desc = Bn.make_desc(shape.B, shape.S, shape.H, shape.Hq, shape.Hkv, shape.d, shape.F, shape.dtype)
+    apart, over = (Bn.LayerBackward(desc, main_grad=main, qk_norm_eps=EPS_N) for _ in range(2))
+    apart.dense(dsv, dW, dy)
+    a = dsv["attn_out"].clone()
+    flat = a.view(-1).view(F32) if main else a.view(-1)
+    spots = [flat[k * 1024:k * 1024 + shape.d] for k in (1, 2)]
+    if main:        # what lies there is added to: read the fp32 values as they are
+        before = [t.clone() for t in spots]
+    over.grads.update(dgq=spots[0], dgk=spots[1])
+    over.dense({**dsv, "attn_out": a}, dW, dy)
+    for k, g in apart.grads.items():
+        if k in ("dgq", "dgk") and main:
+            g = g + before[k == "dgk"]
+        assert torch.equal(g, over.grads[k]), k
+
+
 L = ops.L
