@@ -390,7 +390,7 @@ cf_status cf_token_loss(const cf_loss_desc* desc, const void* logits, int64_t lo
  *   g' = grad_scale * g * min(1, max_norm / (norm + 1e-6))
  *   m = beta1*m + (1-beta1)*g',  v = beta2*v + (1-beta2)*g'^2
  *   p = p - lr*weight_decay*p - lr * (m / (1-beta1^step)) / (sqrt(v / (1-beta2^step)) + eps)
- * in fp32.  norm_dev (device, nullable: no clipping) is what cf_grad_norm left; where it is not finite the call changes nothing.
+ * in fp32; with 32-bit states a sqrt(v) that fp32 has no normal square of counts as a value between itself and 2^-63, 2^-64 at least.  norm_dev (device, nullable: no clipping) is what cf_grad_norm left; where it is not finite the call changes nothing.
  * step_dev, lr_dev (device, nullable) replace step and lr, for a call captured into a graph.
  *   p        CF_F32 parameters, or CF_BF16 ones with (master) or without an fp32 master copy; p is the rounded master
  *   m, v     state_bits 32: fp32.  state_bits 8: e4m3 bytes that stand for m / m_scale and sqrt(v) / v_scale, with a scale for every

@@ -5,6 +5,7 @@
 // a launch covers up to 40 tensors, a block CHUNK elements of one of them, a lane 8 of these.  8-bit states have a scale for every 256
 // elements of a tensor, the ones of half a wave.
 #include <initializer_list>
+#include <type_traits>
 
 #include "common.h"
 
@@ -77,11 +78,22 @@ __device__ __forceinline__ float rounded(float a, float b) {
     return p;
 }
 
-// The square root of a normal number to half a step: the hardware's, which is off by one, and what a fused residual says is missing.  A third of the
-// instructions of sqrtf, which an element of an 8-bit state has not the time for next to its 18 bytes.
+// Whether any lane of the wave has it: a branch of the whole wave, out of the way (900 -> 889 us for 218 M elements, where a branch of single lanes costs 8)
+__device__ __forceinline__ bool seldom(bool c) { return __builtin_expect(__any(c), 0); }
+
+// The square root to half a step: the hardware's, which is off by one and takes what is below the normal numbers for 0, and what a fused residual says is missing; a
+// third of the instructions of sqrtf.  Below the normal numbers it comes out between 2^-64 and 2^-63, not below the root itself: what such a v has lost to fp32 does not
+// divide a step.
 __device__ __forceinline__ float root(float v) {
-    const float s = __builtin_amdgcn_sqrtf(v), r = fmaf(fmaf(-s, s, v), 0.5f * __builtin_amdgcn_rcpf(fmaxf(s, 0x1p-70f)), s);
+    const float s = fmaxf(__builtin_amdgcn_sqrtf(v), 0x1p-63f), r = fmaf(fmaf(-s, s, v), 0.5f * __builtin_amdgcn_rcpf(s), s);
     return s < INFINITY ? r : s;            // a square beyond fp32 makes an update of 0
+}
+// The root that an 8-bit state keeps: 0 of 0.  TINY: of any number, scaled up where it is small, else of normal ones.
+template <bool TINY> __device__ __forceinline__ float kept_root(float v) {
+    const int up = TINY && v < 0x1p-96f ? 32 : 0;
+    const float x = TINY ? ldexpf(v, 2 * up) : v, s = __builtin_amdgcn_sqrtf(x);
+    const float r = fmaf(fmaf(-s, s, x), 0.5f * __builtin_amdgcn_rcpf(fmaxf(s, 0x1p-70f)), s);
+    return s < INFINITY ? TINY ? ldexpf(r, -up) : r : s;
 }
 
 // LANE elements from i on, of which `left` exist: all of them, unless TAIL
@@ -160,8 +172,6 @@ __device__ __forceinline__ float block_max(float v) {
     for (int o = QBLOCK / LANE / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
     return fmaxf(v, TOP_MIN);
 }
-// Whether any lane of the wave has it: a branch of the whole wave, out of the way (900 -> 889 us for 218 M elements, where a branch of single lanes costs 8)
-__device__ __forceinline__ bool seldom(bool c) { return __builtin_expect(__any(c), 0); }
 // A hash of an element: two multiplications with shifts around them over its number and the tensor's key.  Its upper 20 bits round v, the
 // lower 12 m.
 __device__ __forceinline__ uint32_t dither(uint32_t h) {
@@ -219,6 +229,10 @@ __device__ __forceinline__ void adamw_block(const AdamArgs& a, const AdamTensor&
     }
     const float keep = 1.f - s.lr * t.wd;
     float tm = 0.f, tv = 0.f, fall = -INFINITY;
+    unsigned low = ~0u;
+    auto moved = [&](float p, float mean, float r) __attribute__((always_inline)) {
+        return fmaf(-s.size * mean, __builtin_amdgcn_rcpf(fmaf(r, s.inv_root, a.eps)), p * keep);
+    };
 #pragma unroll
     for (int e = 0; e < LANE; ++e) {
         if (BITS == 8) v[e] = rounded(v[e], v[e]);
@@ -228,13 +242,21 @@ __device__ __forceinline__ void adamw_block(const AdamArgs& a, const AdamTensor&
         if (BITS == 8) fall = fmaxf(fall, fminf(fmaf(1.0625f, fabsf(m[e]), -old), fmaf(FALLS, old, -fabsf(x))));
         if (BITS == 8) asm("" : "+v"(fall));
         v[e] = rounded(a.b2, v[e]) + rounded(a.c2, rounded(x, x));
-        const float r = root(v[e]);
-        w[e] = fmaf(-s.size * m[e], __builtin_amdgcn_rcpf(fmaf(r, s.inv_root, a.eps)), w[e] * keep);
-        if (BITS == 8) {
-            v[e] = r;
-            tm = fmaxf(tm, fabsf(m[e]));            // of what does not exist: zeros
-            tv = fmaxf(tv, r);
-        }
+        if (BITS == 32) w[e] = moved(w[e], m[e], root(v[e]));
+        else low = min(low, __float_as_uint(v[e]) - 1u);
+    }
+    if constexpr (BITS == 8) {
+        auto update = [&](auto tiny) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = 0; e < LANE; ++e) {
+                v[e] = kept_root<tiny.value>(v[e]);
+                w[e] = moved(w[e], m[e], v[e]);
+                tm = fmaxf(tm, fabsf(m[e]));            // of what does not exist: zeros
+                tv = fmaxf(tv, v[e]);
+            }
+        };
+        if (seldom(low < 0x7FFFFFu)) update(std::true_type{});         // a v below the normal numbers, and not 0
+        else update(std::false_type{});
     }
     if (MASTER) store_lane<float, TAIL>(t.master + i, left, w);
     store_lane<P, TAIL>((P*)t.p + i, left, w);

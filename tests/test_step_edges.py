@@ -114,6 +114,52 @@ def test_adamw_8_bit_block_outlives_a_value_beyond_fp32(bad):
         assert bool(ends[1][0][at].isnan().all())
 
 
+# ---- AdamW: the ends of fp32 -------------------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_root_of_second_moments_below_the_normal_numbers(bits):
+    """v from 2^-110 down to 2^-146 with an eps that hides nothing.  A v below the normal numbers is rounded to multiples of 2^-149: three times, of the square, the
+    product and the sum, by 2^-150 each.  With 32 bits its root counts as something between itself (2^-64 at least) and 2^-63."""
+    say("adamw root", bits)
+    e = torch.arange(110, 147, dtype=F64)
+    root = torch.exp2(-e / 2)
+    n = root.numel()
+    p = torch.zeros(n, device=DEV)
+    m = (root * 0.5).float().to(DEV)
+    if bits == 8:       # a root each of its own block, so that the code is exact: 1.5 times its scale
+        root = root.float().double()
+        size = n * 256
+        q = torch.zeros(size)
+        q[::256] = 448.0
+        p, g = torch.zeros(size, device=DEV), torch.zeros(size, device=DEV)
+        q = q.to(torch.float8_e4m3fn).to(DEV)
+        scale = (root / 448).float().to(DEV)
+        ms = (root / 896).float().to(DEV)
+        state = ([q.clone()], [q.clone()], [ms.clone()], [scale.clone()])
+        v0, m0 = (scale.double() * 448).cpu() ** 2, (ms.double() * 448).cpu()
+    else:
+        g = torch.zeros(n, device=DEV)
+        v = torch.exp2(-e).float().to(DEV)
+        state = ([m], [v])
+        v0, m0 = v.double().cpu(), m.double().cpu()
+    opt = Bn.AdamW([p], [g], lr=LR, betas=(0.9, 0.99), eps=1e-30, state=state)
+    opt.step(step=5000)
+    got = (opt.params[0][::256] if bits == 8 else opt.params[0]).double().cpu()
+    v1 = 0.99 * v0
+    want = -LR * 0.9 * m0 / (v1.sqrt() + 1e-30)
+    off = (1.0 - 3 * 2.0 ** -150 / v1) ** -0.5 - 1.0         # of a quotient by the root of a v that much too small
+    far = (32 * U + off) * want.abs()
+    if bits == 32:
+        few = v1 < 2.0 ** -126
+        least, most = (LR * 0.9 * m0 / (r + 1e-30) for r in (torch.full_like(v1, 2.0 ** -63), v1.sqrt().clamp(min=2.0 ** -64)))
+        assert bool((-got[few] >= (least - far)[few]).all()) and bool((-got[few] <= (most + far)[few]).all())
+        got, want, far = got[~few], want[~few], far[~few]
+    close(got, want, far, "parameter")
+    if bits == 8:
+        close(opt.v_scale[0], v1.sqrt() / 448, (16 * U + off) * v1.sqrt() / 448, "scale")
+
+
 # ---- losses ------------------------------------------------------------------------------------------------
 
 @gpu
