@@ -413,7 +413,7 @@ typedef struct {
 } cf_adamw_tensor;
 
 typedef struct {
-    double lr, beta1, beta2, eps;
+    double lr, beta1, beta2, eps;  /* eps >= 2^-126: its reciprocal is finite */
     int32_t step;                  /* 1 for the first                           */
     int32_t p_dtype, g_dtype;      /* cf_dtype of all parameters, of all gradients */
     int32_t state_bits;            /* 32 or 8                                   */

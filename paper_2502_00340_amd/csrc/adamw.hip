@@ -422,7 +422,7 @@ cf_status cf_adamw_step(const cf_adamw_desc* d, const cf_adamw_tensor* tensors, 
     for (int dt : {d->p_dtype, d->g_dtype})
         if (dt != CF_BF16 && dt != CF_F32) return CF_ERR_DTYPE;
     if (n_tensors < 0 || (d->state_bits != 8 && d->state_bits != 32)) return CF_ERR_SHAPE;
-    if (!(d->lr >= 0.) || !is_finite(d->lr) || !(d->beta1 >= 0. && d->beta1 < 1.) || !(d->beta2 >= 0. && d->beta2 < 1.) || !((float)d->eps > 0.f) ||
+    if (!(d->lr >= 0.) || !is_finite(d->lr) || !(d->beta1 >= 0. && d->beta1 < 1.) || !(d->beta2 >= 0. && d->beta2 < 1.) || !((float)d->eps >= 0x1p-126f) ||
         !is_finite(d->eps) || !is_finite(d->grad_scale) || (!d->step_dev && d->step < 1))
         return CF_ERR_SHAPE;
     if (d->norm_dev && !(d->max_norm > 0.f)) return CF_ERR_SHAPE;

@@ -160,6 +160,13 @@ def test_adamw_root_of_second_moments_below_the_normal_numbers(bits):
         close(opt.v_scale[0], v1.sqrt() / 448, (16 * U + off) * v1.sqrt() / 448, "scale")
 
 
+def test_adamw_refuses_an_eps_below_the_normal_numbers(L):
+    """Its reciprocal is infinite: an element without moments would be 0 times that."""
+    t = Bn.AdamwTensor(ops.FAKE, None, ops.FAKE, ops.FAKE, ops.FAKE, None, None, 8, 0.0)
+    call = lambda eps: L.cf_adamw_step(C.byref(Bn.AdamwDesc(1e-3, 0.9, 0.99, eps, 1, 1, 1, 32, 0, 1.0, 0.0, None, None, None)), C.byref(t), 0, None)
+    assert call(1e-39) == 2 and call(2.0 ** -127) == 2 and call(2.0 ** -126) == 0 and call(1e-8) == 0        # of no tensors: nothing is launched
+
+
 # ---- losses ------------------------------------------------------------------------------------------------
 
 @gpu
