@@ -371,7 +371,7 @@ typedef enum { CF_LOSS_NLL = 0, CF_LOSS_POLICY = 1 } cf_loss_kind;
 
 typedef struct {
     int32_t kind;                  /* cf_loss_kind                              */
-    int32_t V;                     /* vocabulary                                */
+    int32_t V;                     /* vocabulary, at most 2^30                  */
     int32_t dtype;                 /* cf_dtype of logits and dlogits            */
     float logit_scale;             /* 0 => 1 (one over a sampling temperature)  */
     float clip_lo, clip_hi;        /* policy: 0 <= clip_lo <= 1, clip_hi >= 0   */

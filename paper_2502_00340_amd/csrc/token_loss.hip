@@ -479,7 +479,7 @@ cf_status cf_token_loss(const cf_loss_desc* desc, const void* logits, int64_t lo
     if (policy && (!old_logp || !advantages)) return CF_ERR_NULL;
     const float scale = desc->logit_scale == 0.f ? 1.f : desc->logit_scale;
     const auto finite = [](float v) { return v - v == 0.f; };
-    if (desc->V <= 0 || max_kept < 0 || max_kept > (1 << 30)) return CF_ERR_SHAPE;
+    if (desc->V <= 0 || desc->V > (1 << 30) || max_kept < 0 || max_kept > (1 << 30)) return CF_ERR_SHAPE;
     if (!(scale > 0.f) || !finite(scale) || !finite(desc->norm)) return CF_ERR_SHAPE;
     if (policy && (!(desc->clip_lo >= 0.f && desc->clip_lo <= 1.f) || !(desc->clip_hi >= 0.f) || !finite(desc->kl_coef) ||
                    (!ref_logp && desc->kl_coef != 0.f)))

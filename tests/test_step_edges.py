@@ -218,6 +218,17 @@ def test_policy_loss_is_finite_where_it_is_defined(dtype):
         assert bool(Bn.token_loss(l, y, ref_logp=ref, kl_coef=0.0, **kw)[2][5].isnan().all())
 
 
+def _loss_without_workspace(L, V, scale=0.0):
+    """4, the workspace's refusal, where nothing before it is refused"""
+    d = Bn.LossDesc(0, V, 0, scale, 0.0, 0.0, 0.0, 1.0)
+    return L.cf_token_loss(C.byref(d), ops.FAKE, 0, ops.FAKE, None, None, None, None, None, None, 0, None, 0, ops.FAKE, None, None, 0, None)
+
+
+def test_token_loss_refuses_a_vocabulary_that_its_index_does_not_hold(L):
+    """Columns are counted in 32 bits, by a block's threads beyond the last one too."""
+    assert [_loss_without_workspace(L, V) for V in (2 ** 31 - 1, 2 ** 30 + 1, 2 ** 30)] == [2, 2, 4]
+
+
 # ---- query/key norm ----------------------------------------------------------------------------------------
 
 @gpu
