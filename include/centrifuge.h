@@ -373,7 +373,7 @@ typedef struct {
     int32_t kind;                  /* cf_loss_kind                              */
     int32_t V;                     /* vocabulary, at most 2^30                  */
     int32_t dtype;                 /* cf_dtype of logits and dlogits            */
-    float logit_scale;             /* 0 => 1 (one over a sampling temperature)  */
+    float logit_scale;             /* 0 => 1 (one over a sampling temperature); times log2(e) it has to be finite */
     float clip_lo, clip_hi;        /* policy: 0 <= clip_lo <= 1, clip_hi >= 0   */
     float kl_coef;                 /* policy; 0 without ref_logp                */
     float norm;                    /* 0 => the number of live rows              */

@@ -480,7 +480,8 @@ cf_status cf_token_loss(const cf_loss_desc* desc, const void* logits, int64_t lo
     const float scale = desc->logit_scale == 0.f ? 1.f : desc->logit_scale;
     const auto finite = [](float v) { return v - v == 0.f; };
     if (desc->V <= 0 || desc->V > (1 << 30) || max_kept < 0 || max_kept > (1 << 30)) return CF_ERR_SHAPE;
-    if (!(scale > 0.f) || !finite(scale) || !finite(desc->norm)) return CF_ERR_SHAPE;
+    const double k = (double)scale * 1.4426950408889634;
+    if (!(scale > 0.f) || !finite((float)k) || !finite(desc->norm)) return CF_ERR_SHAPE;
     if (policy && (!(desc->clip_lo >= 0.f && desc->clip_lo <= 1.f) || !(desc->clip_hi >= 0.f) || !finite(desc->kl_coef) ||
                    (!ref_logp && desc->kl_coef != 0.f)))
         return CF_ERR_SHAPE;
@@ -501,7 +502,6 @@ cf_status cf_token_loss(const cf_loss_desc* desc, const void* logits, int64_t lo
     }
     if (!ws || off(ws, 16) || ws_bytes < cf_token_loss_workspace_bytes(max_kept)) return CF_ERR_WORKSPACE;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    const double k = (double)scale * 1.4426950408889634;
     LossArgs a{logits, ls, targets, old_logp, ref_logp, advantages, weights, idx, n_kept_dev, max_kept, desc->V, 0, scale, (float)k, (float)(k - (float)k), policy,
                1.f - desc->clip_lo, 1.f + desc->clip_hi, policy ? desc->kl_coef : 0.f, desc->norm, dlogits, ds, logp, (float4*)ws};
     if (max_kept > 0) desc->dtype == CF_F32 ? launch_token_loss<float>(a, st) : launch_token_loss<bf16_t>(a, st);

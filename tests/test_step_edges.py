@@ -229,6 +229,11 @@ def test_token_loss_refuses_a_vocabulary_that_its_index_does_not_hold(L):
     assert [_loss_without_workspace(L, V) for V in (2 ** 31 - 1, 2 ** 30 + 1, 2 ** 30)] == [2, 2, 4]
 
 
+def test_token_loss_refuses_a_scale_that_fp32_does_not_hold(L):
+    """Logits are scaled by logit_scale * log2(e): infinite, it would be multiplied by the 0 of a row's maximum."""
+    assert [_loss_without_workspace(L, 10, s) for s in (3e38, 2.4e38, 2.3e38, 1e-30)] == [2, 2, 4, 4]
+
+
 # ---- query/key norm ----------------------------------------------------------------------------------------
 
 @gpu
