@@ -541,6 +541,9 @@ bool linear_in_parts(int n, int in, int out) {
     return pairs - std::max<int64_t>(per, w_steps) >= (one_round ? GROUP_GAIN : 28);
 }
 
+// What a layer call's max_kept stands for where its workspace is asked for: 0 is every token, as in the calls; a bound above that asks for more.
+int row_bound(const cf_layer_desc& L, int max_kept) { return max_kept > 0 ? max_kept : L.B * L.S; }
+
 // The gains' partials of the query/key norm lie behind a call's other scratch, `used` bytes of it; false: the workspace is too small.
 bool take_qk_partial(const cf_layer_desc& L, const cf_layer_qk* qk, int max_kept, size_t used, void* ws, size_t ws_bytes, float*& partial) {
     if (qk) partial = reinterpret_cast<float*>(static_cast<unsigned char*>(ws) + used);
@@ -836,6 +839,7 @@ cf_status cf_attn_bwd_filtered(const cf_layer_desc* desc, const void* q_kept, co
 
 size_t cf_layer_workspace_bytes(const cf_layer_desc* desc, int32_t max_kept) {
     if (check_layer_desc(desc) != CF_OK || max_kept < 0) return 0;
+    max_kept = row_bound(*desc, max_kept);
     return carve_layer(*desc, max_kept, nullptr).total + attn_ws_spare(*desc, max_kept);
 }
 
@@ -905,6 +909,7 @@ cf_status cf_layer_bwd_dense_qk(const cf_layer_desc* desc, const cf_saved* saved
 
 size_t cf_lora_workspace_bytes(const cf_layer_desc* desc, int32_t rank, int32_t max_kept) {
     if (check_layer_desc(desc) != CF_OK || max_kept < 0 || rank <= 0) return 0;
+    max_kept = row_bound(*desc, max_kept);
     return carve_lora(*desc, rank, max_kept, nullptr).total + attn_ws_spare(*desc, max_kept);
 }
 
@@ -919,12 +924,12 @@ cf_status cf_layer_bwd_lora(const cf_layer_desc* desc, const cf_saved* saved, co
 
 size_t cf_layer_qk_workspace_bytes(const cf_layer_desc* desc, int32_t max_kept) {
     const size_t n = cf_layer_workspace_bytes(desc, max_kept);
-    return n && check_qk_heads(desc) == CF_OK ? n + qk_norm_partial_bytes(desc->d, max_kept) : 0;
+    return n && check_qk_heads(desc) == CF_OK ? n + qk_norm_partial_bytes(desc->d, row_bound(*desc, max_kept)) : 0;
 }
 
 size_t cf_lora_qk_workspace_bytes(const cf_layer_desc* desc, int32_t rank, int32_t max_kept) {
     const size_t n = cf_lora_workspace_bytes(desc, rank, max_kept);
-    return n && check_qk_heads(desc) == CF_OK ? n + qk_norm_partial_bytes(desc->d, max_kept) : 0;
+    return n && check_qk_heads(desc) == CF_OK ? n + qk_norm_partial_bytes(desc->d, row_bound(*desc, max_kept)) : 0;
 }
 
 cf_status cf_layer_bwd_lora_qk(const cf_layer_desc* desc, const cf_saved* saved, const cf_weights* w, const cf_layer_qk* qk,

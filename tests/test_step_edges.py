@@ -236,6 +236,14 @@ def test_token_loss_refuses_a_scale_that_fp32_does_not_hold(L):
 
 # ---- query/key norm ----------------------------------------------------------------------------------------
 
+def test_layer_workspaces_for_a_bound_of_zero(L):
+    """0 stands for every token in the calls, so it does where their workspace is asked for."""
+    for dtype in ("bf16", "f32"):
+        d = Bn.make_desc(B=2, S=640, H=256, Hq=4, Hkv=2, d=64, F=512, dtype=dtype)
+        for f in (L.cf_layer_workspace_bytes, L.cf_layer_qk_workspace_bytes, lambda d, n: L.cf_lora_workspace_bytes(d, 8, n), lambda d, n: L.cf_lora_qk_workspace_bytes(d, 8, n)):
+            assert f(C.byref(d), 0) == f(C.byref(d), 1280) > f(C.byref(d), 640) > f(C.byref(d), 1) > 0
+
+
 @gpu
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("main", [False, True])
