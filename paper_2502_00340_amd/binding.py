@@ -709,10 +709,17 @@ class AdamW:
         if bits == 8:
             for ts, what in ((self.m_scale, "m_scale"), (self.v_scale, "v_scale")):
                 check(ts, what, torch.float32, lambda i: -(-size[i] // STATE_BLOCK))
-        used = [t.data_ptr() for ts in (self.params, self.master or (), self.m, self.v) for t in ts if t.numel()]
-        _need(len(set(used)) == len(used), "a tensor that is updated may be listed once only")
         for t, dt in ((step_dev, torch.int32), (lr_dev, torch.float32)):
             _need(t is None or (t.dtype == dt and t.numel() == 1 and t.device == dev), "step_dev: one int32, lr_dev: one fp32, on %s" % dev)
+        # what a step writes overlaps nothing; what it reads may overlap what it reads
+        written = (self.params, self.master, self.m, self.v, self.m_scale, self.v_scale)
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), w) for ts, w in
+                       [(ts, True) for ts in written if ts is not None] + [(self.grads_list, False), ([t for t in (step_dev, lr_dev) if t is not None], False)]
+                       for t in ts if t.numel())
+        end = {True: 0, False: 0}           # of the ranges so far, written ones and read ones
+        for a, b, w in spans:
+            _need(a >= end[True] and not (w and a < end[False]), "a tensor that a step writes may be listed once only, and overlap no other")
+            end[w] = max(end[w], b)
         self.step_dev, self.lr_dev = step_dev, lr_dev
         at = lambda ts, i: ts[i].data_ptr() if ts is not None else None
         self._t = (AdamwTensor * n)(*[AdamwTensor(at(self.params, i), at(self.master, i), at(self.grads_list, i), at(self.m, i), at(self.v, i),

@@ -167,6 +167,21 @@ def test_adamw_refuses_an_eps_below_the_normal_numbers(L):
     assert call(1e-39) == 2 and call(2.0 ** -127) == 2 and call(2.0 ** -126) == 0 and call(1e-8) == 0        # of no tensors: nothing is launched
 
 
+def test_adamw_refuses_tensors_that_overlap_what_it_writes(L):
+    """Scales among what is written, views that start elsewhere, gradients that a step would write over."""
+    f = torch.zeros(4096)
+    p, g, m, v = f[:512], torch.zeros(512), torch.zeros(512), torch.zeros(512)
+    q, r = torch.zeros(512).to(torch.float8_e4m3fn), torch.zeros(512).to(torch.float8_e4m3fn)
+    sc = torch.zeros(8)
+    make = lambda p=[p], g=[g], **kw: Bn.AdamW(p, g, lr=1e-3, **kw)
+    make(), make(state=([m], [v])), make(state=([q], [r], [sc[:2]], [sc[2:4]])), make(p=[p, f[512:1024]], g=[g, g])
+    for bad in (dict(state=([q], [r], [sc[:2]], [sc[:2]])), dict(state=([q], [r], [sc[:2]], [sc[1:3]])), dict(state=([m], [f[100:612]])), dict(g=[p]), dict(g=[f[511:1023]]),
+                dict(p=[p, f[508:1020]], g=[g, g]), dict(state=([m], [v]), g=[v]), dict(p=[p.view(torch.bfloat16)[:512]], g=[g], master=[f[:512]]),
+                dict(state=([q], [q.view(torch.uint8).view(torch.float8_e4m3fn)], [sc[:2]], [sc[2:4]])), dict(step_dev=p.view(torch.int32)[7:8]), dict(lr_dev=m[3:4], state=([m], [v]))):
+        with pytest.raises(ValueError):
+            make(**bad)
+
+
 # ---- losses ------------------------------------------------------------------------------------------------
 
 @gpu
