@@ -251,6 +251,15 @@ def test_token_loss_refuses_a_scale_that_fp32_does_not_hold(L):
 
 # ---- query/key norm ----------------------------------------------------------------------------------------
 
+@gpu
+@pytest.mark.parametrize("n,Hq,Hkv", [(1, 1, 1), (301, 5, 2), (70, 64, 8), (2100, 3, 1)])
+def test_qk_norm_of_the_smallest_heads(n, Hq, Hkv):
+    """d = 8 in fp32: one lane a head, and one block sums the gains of both kinds."""
+    ops.test_qk_norm_forward(F32, n, Hq, Hkv, 8, 64)
+    for main in (False, True):
+        ops.test_qk_norm_backward(F32, n, Hq, Hkv, 8, 64, main)
+
+
 def test_layer_workspaces_for_a_bound_of_zero(L):
     """0 stands for every token in the calls, so it does where their workspace is asked for."""
     for dtype in ("bf16", "f32"):
