@@ -293,4 +293,30 @@ def test_dense_layer_call_whose_gains_lie_over_the_attention_output(dtype, main)
         assert torch.equal(g, over.grads[k]), k
 
 
+@gpu
+def test_two_training_steps_with_cleared_gradients():
+    """Main gradients are added to: a step clears them before the next backward pass, which then gives what a new plan gives."""
+    say("two steps")
+    shape, W, sv, tabs, rng = ops._layer_qk_problem(BF)
+    dsv, dW = ops._layer_qk_device(shape, W, sv, tabs)
+    desc = Bn.make_desc(shape.B, shape.S, shape.H, shape.Hq, shape.Hkv, shape.d, shape.F, shape.dtype)
+    names = ("wq", "wk", "wv", "wo", "wg", "wu", "wd", "g1", "g2", "gq", "gk")
+    mask = torch.ones((shape.B, shape.S), dtype=torch.uint8, device=DEV)
+    plan = Bn.LayerBackward(desc, main_grad=True, qk_norm_eps=EPS_N)
+    grads = [plan.grads["d" + n] for n in names]
+    opt = Bn.AdamW([dW[n] for n in names], grads, lr=1e-3, max_norm=1.0, master=True, state_bits=8)
+    for _ in range(2):
+        dy = Hn.to_dev(Hn.quantize(rng.standard_normal((shape.T, shape.H)), shape.dtype), shape.dtype)
+        other = Bn.LayerBackward(desc, main_grad=True, qk_norm_eps=EPS_N)
+        for p in (plan, other):
+            p.filtered(dsv, dW, dy, mask)
+        for n in names:
+            assert torch.equal(plan.grads["d" + n], other.grads["d" + n]), n
+        opt.step()
+        norm = math.sqrt(sum(float(other.grads["d" + n].double().square().sum()) for n in names))
+        assert abs(float(opt.grad_norm) - norm) <= 2 * U * norm
+        for g in grads:
+            g.zero_()
+
+
 L = ops.L
