@@ -622,7 +622,8 @@ def token_loss(logits, targets, old_logp=None, advantages=None, ref_logp=None, w
     """Loss of the kept rows of logits [rows, V] (dense columns, any stride) and its gradient: the mean NLL of targets [rows] int64, or with advantages
     the clipped policy loss.  Per-row tensors are fp32 [rows] and read, like logits, at idx[j] (row j without idx).  Returns (stats [4]: loss, its first term, KL, clipped share;
     logp [max_kept]; dlogits [max_kept, V] or None).  max_kept: by default all of idx, or all rows.  out: dlogits to write to,
-    logits itself for a gradient in place (without idx)."""
+    logits itself for a gradient in place (without idx).  n_kept_dev: only the first min(*n_kept_dev, max_kept) rows are written; the others hold what they
+    held, so a product over all max_kept rows wants a cleared out."""
     _need(logits.dim() == 2, "logits have to be [rows, V]")
     (rows, V), (ls, dense) = logits.shape, logits.stride()
     _need((dense == 1 or V == 1) and (ls >= V or rows < 2), "logits have to have dense columns, and rows that do not overlap")

@@ -319,4 +319,42 @@ def test_two_training_steps_with_cleared_gradients():
             g.zero_()
 
 
+@gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("on_host", [True, False])
+def test_head_gradients_of_a_partly_kept_batch(dtype, on_host):
+    """Index, loss and head one after the other with the count on the host, and on the device with cleared operands, over memory that held NaN."""
+    say("head", dtype, on_host)
+    B, S, H, V = 2, 100, 64, 264
+    g0 = gen(51)
+    x, w = randn(g0, B * S, H, dtype=dtype), randn(g0, H, V, std=0.1, dtype=dtype)
+    y = torch.randint(0, V, (B * S,), generator=g0).to(DEV)
+    mask = (torch.rand((B, S), generator=g0) < 0.45).to(torch.uint8).to(DEV)
+    logits = (x.float() @ w.float()).to(dtype)
+    junk = [torch.full((B * S, V), float("nan"), dtype=dtype, device=DEV) for _ in range(4)]
+    del junk
+    if on_host:
+        idx, _, _, n = Bn.build_keep_index(mask)
+        stats, _, dl = Bn.token_loss(logits, y, idx=idx[:n])
+        kept = Bn.gather_rows(x, idx, n)
+    else:
+        idx, _, nd, _ = Bn.build_keep_index(mask, sync=False)
+        stats, _, dl = Bn.token_loss(logits, y, idx=idx, n_kept_dev=nd, out=torch.zeros((B * S, V), dtype=dtype, device=DEV))
+        kept = Bn.gather_rows(x, idx, B * S, out=torch.zeros_like(x), n_kept_dev=nd)
+        n = int(nd)
+    dy, dw = Bn.linear_bwd_reduced(kept, dl, w)
+    at = mask.view(-1).nonzero().squeeze(1)
+    assert n == at.numel()
+    p = torch.softmax(logits[at].double(), 1)
+    p[torch.arange(n, device=DEV), y[at]] -= 1.0
+    p /= n
+    # dlogits are off by a rounding of their type (and 2^-18 of the largest in fp32), the products by one of theirs and fp32 sums
+    e = ops.EPS[dtype] + 2.0 ** -18
+    want = p @ w.double().t()
+    close(dy[:n], want, e * want.abs() + (e + (V + 8) * U) * (p.abs() @ w.double().abs().t()) + 2.0 ** -18 / n, "dy")
+    want = x[at].double().t() @ p
+    close(dw, want, e * want.abs() + (e + (n + 8) * U) * (x[at].double().abs().t() @ p.abs()) + 2.0 ** -18 / n, "dw")
+    assert on_host or not bool(dy[n:].any())
+
+
 L = ops.L
