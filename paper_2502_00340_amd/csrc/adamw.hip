@@ -172,8 +172,8 @@ __device__ __forceinline__ float block_max(float v) {
     for (int o = QBLOCK / LANE / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
     return fmaxf(v, TOP_MIN);
 }
-// A hash of an element: two multiplications with shifts around them over its number and the tensor's key.  Its upper 20 bits round v, the
-// lower 12 m.
+// A hash of an element: the published finishing steps of MurmurHash3 (two multiplications with shifts around them) over its number and the tensor's key.  Its
+// upper 20 bits round v, the lower 12 m.
 __device__ __forceinline__ uint32_t dither(uint32_t h) {
     h = (h ^ (h >> 16)) * 0x85EBCA6Bu;
     h = (h ^ (h >> 13)) * 0xC2B2AE35u;
