@@ -309,7 +309,7 @@ cf_status cf_qk_norm_rope_fwd(const cf_layer_desc* desc, const cf_qk_norm* p, co
                               const cf_qk* out, cf_stream stream);
 
 /* The backward pass on kept rows.  in: the tensors before the norm, full length, read through idx (NULL: row j is row j); dy,
- * dx: compact, one row per kept token; dx may be dy itself (same pointers and strides), no other overlap.  n_kept_dev and max_kept as for
+ * dx: compact, one row per kept token; dx may be dy itself (same pointers and strides), without idx in itself too, no other overlap.  n_kept_dev and max_kept as for
  * cf_gather_rows.  dgq, dgk [d] (both or neither NULL: frozen gains): gain gradients, overwritten in the storage dtype, or
  * (main_grad 1) fp32 buffers that the call adds to; zero rows give zero gradients.  The sums' order depends on the sizes alone.
  * ws is needed for the gain gradients only. */

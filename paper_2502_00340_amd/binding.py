@@ -585,10 +585,17 @@ def _qk_ws_bytes(d, code, n):
     return lib().cf_qk_norm_workspace_bytes(C.byref(LayerDesc(1, 1, 8, 1, 1, d, 8, code, 0.0, 0.0)), n)
 
 
+def _ranges_meet(a, b) -> bool:
+    """Whether the addresses from the first to the last element of two tensors meet."""
+    end = lambda t: t.data_ptr() + (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))) * t.element_size()
+    return a.numel() > 0 and b.numel() > 0 and a.data_ptr() < end(b) and b.data_ptr() < end(a)
+
+
 def qk_norm_rope_bwd(desc: LayerDesc, q, k, gq, gk, dq, dk, rope_cos=None, rope_sin=None, positions=None, idx=None, n_kept_dev=None,
                      need_gains: bool = True, main_grads=None, out=None):
     """Backward of qk_norm_rope_fwd for compact dq [n, Hq*d], dk [n, Hkv*d]; q and k are its inputs at full length.  Returns (dx of q, dx of k, dgq, dgk).
-    n_kept_dev: only the first min(*n_kept_dev, n) rows.  main_grads: fp32 (dgq, dgk) that are added to.  out: as in the forward pass."""
+    n_kept_dev: only the first min(*n_kept_dev, n) rows.  main_grads: fp32 (dgq, dgk) that are added to.  out: a pair to write to, dq and dk themselves for a
+    pass in place."""
     dt, d = torch_dtype(desc), desc.d
     Nq, Nkv = desc.Hq * d, desc.Hkv * d
     rows, x = _qk_rows(desc, q, k, "q, k", dt, Nq, Nkv)
@@ -597,6 +604,9 @@ def qk_norm_rope_bwd(desc: LayerDesc, q, k, gq, gk, dq, dk, rope_cos=None, rope_
     p = _qk_norm(desc, d, gq, gk, rope_cos, rope_sin, positions, rows, dt)
     if out is None:
         out = torch.empty_like(dq), torch.empty_like(dk)
+    elif idx is not None:
+        for t in out:
+            _need(not any(_ranges_meet(t, x) for x in (q, k)), "with idx, out must not overlap q and k")
     m, dx = _qk_rows(desc, out[0], out[1], "out", dt, Nq, Nkv)
     _need(m == n, "out has another number of rows")
     dgq = dgk = ws = None

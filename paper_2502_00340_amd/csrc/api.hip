@@ -496,12 +496,31 @@ cf_status check_qk_rows(const cf_layer_desc& L, const cf_qk* r) {
     return CF_OK;
 }
 
-// rows written in place have to be those that are read
-bool qk_in_place(const cf_layer_desc& L, const cf_qk& from, const cf_qk& to, int n_rows) {
-    const int64_t nq = (int64_t)L.Hq * L.d, nk = (int64_t)L.Hkv * L.d;
-    const auto stride = [](int64_t s, int64_t dense) { return s ? s : dense; };
-    return n_rows < 2 || ((to.q != from.q || stride(to.q_stride, nq) == stride(from.q_stride, nq)) &&
-                          (to.k != from.k || stride(to.k_stride, nk) == stride(from.k_stride, nk)));
+// One kind of a cf_qk: rows of `width` bytes, `stride` bytes apart
+struct QkRows {
+    uintptr_t at;
+    uint64_t stride, width;
+};
+QkRows qk_rows(const cf_layer_desc& L, const cf_qk& t, bool keys) {
+    const uint64_t e = dtype_size(L.dtype), width = (uint64_t)(keys ? L.Hkv : L.Hq) * L.d * e, s = (keys ? t.k_stride : t.q_stride) * e;
+    return QkRows{(uintptr_t)(keys ? t.k : t.q), s ? s : width, width};
+}
+// Whether n rows of each share an address.  Columns of one longer row, which equal strides tell, lie apart though their ranges do not.
+bool rows_meet(const QkRows& a, const QkRows& b, int n) {
+    if (n <= 0 || !overlap((const void*)a.at, (n - 1) * a.stride + a.width, (const void*)b.at, (n - 1) * b.stride + b.width)) return false;
+    if (n == 1 || a.stride != b.stride) return true;
+    const uint64_t off = b.at >= a.at ? (b.at - a.at) % a.stride : (a.stride - (a.at - b.at) % a.stride) % a.stride;
+    return off < a.width || a.stride - off < b.width;
+}
+// `to` may be `from` itself (in_place), queries and keys each for itself, and shares no address with it otherwise
+bool qk_apart(const cf_layer_desc& L, const cf_qk& from, const cf_qk& to, int n, bool in_place = true) {
+    const QkRows f[2] = {qk_rows(L, from, false), qk_rows(L, from, true)}, t[2] = {qk_rows(L, to, false), qk_rows(L, to, true)};
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2; ++j) {
+            const bool same = in_place && i == j && f[i].at == t[j].at && (n < 2 || f[i].stride == t[j].stride);
+            if (!same && rows_meet(f[i], t[j], n)) return false;
+        }
+    return !rows_meet(t[0], t[1], n);
 }
 
 cf_status check_layer_qk(const cf_layer_desc* L, const cf_layer_qk* qk, bool lora) {
@@ -953,7 +972,7 @@ cf_status cf_qk_norm_rope_fwd(const cf_layer_desc* desc, const cf_qk_norm* p, co
     if (s == CF_OK) s = check_qk_rows(*desc, in);
     if (s == CF_OK) s = check_qk_rows(*desc, out);
     if (s != CF_OK) return s;
-    if (n_rows < 0 || n_rows > 1 << 30 || !qk_in_place(*desc, *in, *out, n_rows)) return CF_ERR_SHAPE;
+    if (n_rows < 0 || n_rows > 1 << 30 || !qk_apart(*desc, *in, *out, n_rows)) return CF_ERR_SHAPE;
     CF_HIP(launch_qk_norm_fwd(*desc, *p, *in, n_rows, *out, as_stream(stream)));
     return CF_OK;
 }
@@ -968,9 +987,9 @@ cf_status cf_qk_norm_rope_bwd(const cf_layer_desc* desc, const cf_qk_norm* p, co
     if (s != CF_OK) return s;
     if ((dgq == nullptr) != (dgk == nullptr)) return CF_ERR_NULL;
     if (max_kept < 0 || max_kept > 1 << 30 || (main_grad != 0 && main_grad != 1)) return CF_ERR_SHAPE;
-    if (!qk_in_place(*desc, *dy_kept, *dx_kept, max_kept)) return CF_ERR_SHAPE;
     if (misaligned(idx, 4) || misaligned(n_kept_dev, 4) || misaligned(dgq, 4) || misaligned(dgk, 4)) return CF_ERR_SHAPE;
     if (dgq && (!ws || misaligned(ws, 256) || ws_bytes < qk_norm_partial_bytes(desc->d, max_kept))) return CF_ERR_WORKSPACE;
+    if (!qk_apart(*desc, *dy_kept, *dx_kept, max_kept) || !qk_apart(*desc, *in, *dx_kept, max_kept, idx == nullptr)) return CF_ERR_SHAPE;
     CF_HIP(launch_qk_norm_bwd(*desc, *p, *in, *dy_kept, idx, RowCount{max_kept, n_kept_dev}, *dx_kept, dgq, dgk, main_grad != 0,
                               static_cast<float*>(ws), as_stream(stream)));
     return CF_OK;

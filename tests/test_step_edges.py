@@ -260,6 +260,60 @@ def test_qk_norm_of_the_smallest_heads(n, Hq, Hkv):
         ops.test_qk_norm_backward(F32, n, Hq, Hkv, 8, 64, main)
 
 
+def test_qk_norm_refuses_outputs_that_lie_over_other_rows(L):
+    """In place is row by row, queries over queries and keys over keys; anything else would be written before another wave has read it."""
+    d = Bn.make_desc(B=2, S=64, H=256, Hq=4, Hkv=2, d=64, F=512, dtype="bf16")
+    p = Bn.QkNorm(ops.FAKE, ops.FAKE, None, None, None)
+    Q, K = 1 << 20, 1 << 21                # ten rows: 5120 and 2560 bytes of bf16
+
+    def fwd(x, y, n=10):
+        return L.cf_qk_norm_rope_fwd(C.byref(d), C.byref(p), C.byref(Bn.Qk(*x)), n, C.byref(Bn.Qk(*y)), None)
+
+    def bwd(x, dy, dx, idx=None, n=10):
+        return L.cf_qk_norm_rope_bwd(C.byref(d), C.byref(p), C.byref(Bn.Qk(*x)), C.byref(Bn.Qk(*dy)), idx, None, n, C.byref(Bn.Qk(*dx)), None, None, 0, None, 0, None)
+    far = (1 << 22, 1 << 23, 0, 0)
+    x = (Q, K, 0, 0)
+    for y in ((Q + 512, K, 0, 0), (Q, K + 256, 0, 0), (Q + 16, 1 << 24, 0, 0), (1 << 24, Q + 512, 0, 0), (K, 1 << 24, 0, 0), (Q, K, 264, 0), (1 << 24, (1 << 24) + 256, 0, 0),
+              (Q - 5104, 1 << 24, 0, 0), (1 << 24, K + 2544, 0, 0)):
+        assert fwd(x, y) == 2 and bwd(far, x, y) == 2 and bwd(x, far, y) == 2 and bwd(x, far, y, idx=ops.FAKE) == 2, y
+    assert bwd(x, far, x, idx=ops.FAKE) == 2           # compact rows over those that are read through the index
+    # columns of one row: of equal strides, and not those of the other kind
+    row = lambda q, k: (Q + 2 * q, Q + 2 * k, 512, 512)
+    assert fwd(row(0, 256), row(256, 0)) == 2 and fwd(row(0, 256), row(0, 320)) == 2 and fwd(row(0, 256), row(8, 384)) == 2
+
+
+def test_qk_norm_binding_refuses_compact_rows_over_full_ones(L):
+    d = Bn.make_desc(B=2, S=64, H=256, Hq=4, Hkv=2, d=64, F=512, dtype="bf16")
+    q, k, g, idx = torch.zeros(6, 256, dtype=BF), torch.zeros(6, 128, dtype=BF), torch.ones(64, dtype=BF), torch.arange(3, dtype=torch.int32)
+    dq, dk = torch.zeros(3, 256, dtype=BF), torch.zeros(3, 128, dtype=BF)
+    for out in ((q[:3], dk), (dq, k[3:]), (q[3:], k[3:])):
+        with pytest.raises(ValueError, match="overlap"):
+            Bn.qk_norm_rope_bwd(d, q, k, g, g, dq, dk, idx=idx, out=out)
+
+
+@gpu
+def test_qk_norm_over_columns_of_one_row():
+    """Queries and keys side by side in one buffer, in place and into other columns of it, forward and backward."""
+    say("qk columns")
+    n, Hq, Hkv, d = 37, 4, 2, 64
+    g0, q, k, gq, gk, cos, sin = ops._qk_case(61, BF, n, Hq, Hkv, d, 50)
+    desc = Bn.make_desc(1, 50, 256, Hq, Hkv, d, 256, BF, rms_eps=EPS_N)
+    dq, dk = randn(g0, n, Hq * d, dtype=BF), randn(g0, n, Hkv * d, dtype=BF)
+    calls = (lambda a, b, **kw: Bn.qk_norm_rope_fwd(desc, a, b, gq, gk, cos, sin, **kw), lambda a, b, **kw: Bn.qk_norm_rope_bwd(desc, q, k, gq, gk, a, b, cos, sin, **kw),
+             lambda a, b, **kw: Bn.qk_norm_rope_bwd(desc, a, b, gq, gk, dq, dk, cos, sin, **kw))
+    for f in calls:
+        a, b = (q, k) if f is not calls[1] else (dq, dk)
+        want = f(a, b)
+        wide = torch.full((n, 1000), 7.0, dtype=BF, device=DEV)
+        fq, fk, oq, ok = wide[:, 8:264], wide[:, 264:392], wide[:, 400:656], wide[:, 656:784]
+        fq.copy_(a), fk.copy_(b)
+        f(fq, fk, out=(oq, ok))
+        assert torch.equal(fq, a) and torch.equal(fk, b) and torch.equal(oq, want[0]) and torch.equal(ok, want[1])
+        f(fq, fk, out=(fq, fk))
+        assert torch.equal(fq, want[0]) and torch.equal(fk, want[1])
+        assert all(bool((t == 7.0).all()) for t in (wide[:, :8], wide[:, 392:400], wide[:, 784:]))
+
+
 def test_layer_workspaces_for_a_bound_of_zero(L):
     """0 stands for every token in the calls, so it does where their workspace is asked for."""
     for dtype in ("bf16", "f32"):
