@@ -323,8 +323,8 @@ __device__ __forceinline__ void adamw_block(const AdamArgs& a, const AdamTensor&
     }
 }
 
-// bf16 with fp32 copies and gradients, 32-bit states: 44 M elements, 1.3 GB in 221 us (6.0 TB/s; a copy of 1 GiB reaches 6.2).  8-bit states: 218 M elements,
-// 3.9 GB in 699 us (5.6 TB/s).  Four elements a lane with conditions took 236 and 756; eight, and conditions only in a tensor's last block, 223 and 713; copies
+// bf16 with fp32 copies and gradients, 32-bit states: 44 M elements, 1.3 GB in 213 to 225 us by box (5.9 to 6.2 TB/s; a copy of 1 GiB reaches 6.2).  8-bit states: 218 M
+// elements, 3.9 GB in 704 us (5.6 TB/s).  Four elements a lane with conditions took 236 and 756; eight, and conditions only in a tensor's last block, 223 and 713; copies
 // and states past the caches the rest.  A block takes CHUNK elements and ends: with 2, 4, 8 and 16 times as many, 218 (of then) became 233, 240, 252 and 275.
 template <typename P, typename G, bool MASTER, int BITS>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {

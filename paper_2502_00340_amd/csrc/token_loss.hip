@@ -237,8 +237,8 @@ __global__ __launch_bounds__(NT) void token_loss_stream_kernel(LossArgs a) {
 // The gradient is written past the caches: 406 against 417 us, 102 against 110; with the two products of a [V, 2048] head behind it, 64 to 2048 rows
 // of 32000 take 0.97 to 1.00 of the time, 1024 of 128256 0.995, and 4096 of 32000, which just fit the last cache, 1.03.
 // Four vectors a thread leave registers for eight waves a SIMD: 8192 rows of 8000 56 -> 49 us, 16384 of 1000 fp32 42 -> 36; eight vectors do not
-// (8192 rows of 16000 105 -> 115).  Rows that start on odd elements cost 1.1 (4096 x 50257 and 50264: 190 and 171 us, without gradient 102 and 79); loads of
-// aligned vectors would make the order of a row's sums, and logp's last bits, depend on where the row lies.
+// (8192 rows of 16000 105 -> 115).  Rows that start on odd elements cost 1.1 (4096 x 50257 and 50264: 190 and 171 us, without gradient 102 and 79): their
+// 16-byte loads lie between dwords.
 // Keeps a vector as it is stored, and the arithmetic where it stands: widened values of one pass are not to be kept for the next one.
 __device__ __forceinline__ void hold(Bytes16& b) { asm volatile("" : "+v"(b)); }
 __device__ __forceinline__ void hold(float& a, float& b) { asm volatile("" : "+v"(a), "+v"(b)); }
