@@ -385,6 +385,54 @@ cf_status cf_token_loss(const cf_loss_desc* desc, const void* logits, int64_t lo
                         const int32_t* idx, const int32_t* n_kept_dev, int32_t max_kept, void* dlogits,
                         int64_t dlogits_stride, float* logp, float* stats, void* ws, size_t ws_bytes, cf_stream stream);
 
+/* ---- the ends of the stack of layers --------------------------------------------------------
+ * Token embeddings, the norm of rows and the loss straight from the head's input: what a training step does below the lowest layer and above the
+ * highest one.  n_kept_dev and max_kept as for cf_gather_rows; idx may be NULL (row j is row j); rows behind the live ones are left as they were.  H is
+ * a multiple of 8 in CF_BF16 and of 4 in CF_F32; tensors of elements are dense and 16-byte aligned; workspaces 256-byte aligned.
+ *
+ * cf_embed_fwd: out[t,:] = scale * table[tokens[t],:], table [V,H], out [n,H]; 0 for a token outside [0,V).  out must not overlap table.
+ * cf_embed_bwd: dtable[c,:] = scale * sum of the rows j of dx_kept [max_kept,H] with tokens[idx[j]] == c, in ascending order of j with fp32 sums: a function
+ *   of the inputs alone, with no atomics.  main_grad 0: all of dtable [V,H] is written in the storage dtype, zeros where no row has the token.  main_grad 1:
+ *   dtable is fp32 and is added to; rows without a token are not touched.  dx rows whose token lies outside [0,V) count for nothing, whatever they hold. */
+cf_status cf_embed_fwd(const void* table, int32_t V, int32_t H, int32_t dtype, const int64_t* tokens, int64_t n, float scale, void* out,
+                       cf_stream stream);
+size_t cf_embed_bwd_workspace_bytes(int32_t H, int32_t max_kept);
+cf_status cf_embed_bwd(const int64_t* tokens, const void* dx_kept, int32_t V, int32_t H, int32_t dtype, const int32_t* idx,
+                       const int32_t* n_kept_dev, int32_t max_kept, float scale, void* dtable, int32_t main_grad, void* ws, size_t ws_bytes,
+                       cf_stream stream);
+
+/* cf_norm_fwd: y[j,:] = n * g + b of row idx[j] of x, n = (x - mu) * rstd, rstd = (mean((x - mu)^2) + eps)^(-1/2); mu is the row's mean (layer 1) or 0
+ *   (layer 0: root mean square norm).  b (layer 1 only, nullable): biases.  y [max_kept,H] may be x itself without idx; no other overlap.
+ * cf_norm_bwd: with u = dy * g,  dx = rstd * (u - [layer 1] mean(u) - n * mean(u * n)),  dg = sum over rows of dy * n,  db = sum of dy (layer 1).
+ *   The statistics are made again from x.  dx_kept [max_kept,H] may be dy_kept itself, without idx x itself; no other overlap.  dg, db [H] (nullable; db
+ *   with dg only): in the storage dtype, overwritten, or (main_grad 1) fp32 and added to.  The sums' order depends on the sizes alone.  ws is needed for dg and db only.
+ * H at most 32768 in CF_BF16 and 16384 in CF_F32 (CF_ERR_UNSUPPORTED above). */
+typedef struct {
+    int32_t H, dtype, layer;
+    float eps;
+} cf_norm_desc;
+
+cf_status cf_norm_fwd(const cf_norm_desc* desc, const void* x, const void* g, const void* b, const int32_t* idx, const int32_t* n_kept_dev,
+                      int32_t max_kept, void* y, cf_stream stream);
+size_t cf_norm_bwd_workspace_bytes(const cf_norm_desc* desc, int32_t max_kept);
+cf_status cf_norm_bwd(const cf_norm_desc* desc, const void* x, const void* g, const void* dy_kept, const int32_t* idx, const int32_t* n_kept_dev,
+                      int32_t max_kept, void* dx_kept, void* dg, void* db, int32_t main_grad, void* ws, size_t ws_bytes, cf_stream stream);
+
+/* cf_head_loss: the losses of cf_token_loss (same description, per-row inputs, terms and rules for rows that are left out) for the logits
+ * l = x_kept * table^T, x_kept [max_kept,H] compact, table [V,H] as for the embeddings, and their gradients towards both operands:
+ *   dx_kept = dlogits * table [max_kept,H] (nullable; may be x_kept itself),  dtable = dlogits^T * x_kept [V,H] (nullable; main_grad as for cf_embed_bwd,
+ *   so that a tied table's two gradients share one buffer).
+ * The logits are fp32 values that are never stored.  What is kept of them for the gradients is bounded by the workspace: exponentials, in the storage
+ * dtype, of as many columns as it has room for; those of the others are computed again, piece by piece.  A larger workspace is faster; logp and stats do not
+ * depend on it, gradients by the order of fp32 sums.  For the same rows logp has the same bits with and without gradients.
+ *   cf_head_loss_workspace_bytes: what to provide for a call with (need_dx, need_dtable): as much as is of use, at most `limit`, or the least that will do
+ *   where that is more.  0 for sizes that are refused. */
+size_t cf_head_loss_workspace_bytes(const cf_loss_desc* desc, int32_t H, int32_t max_kept, int32_t need_dx, int32_t need_dtable, size_t limit);
+cf_status cf_head_loss(const cf_loss_desc* desc, int32_t H, const void* x_kept, const void* table, const int64_t* targets, const float* old_logp,
+                       const float* ref_logp, const float* advantages, const float* weights, const int32_t* idx, const int32_t* n_kept_dev,
+                       int32_t max_kept, void* dx_kept, void* dtable, int32_t main_grad, float* logp, float* stats, void* ws, size_t ws_bytes,
+                       cf_stream stream);
+
 /* ---- AdamW over many tensors ---------------------------------------------------------------
  * What takes cf_grads (and cf_lora_grads): one launch per 40 tensors of any sizes (or per 2^31 elements),
  *   g' = grad_scale * g * min(1, max_norm / (norm + 1e-6))

@@ -32,6 +32,8 @@ EXPORTS = (
     "cf_qk_norm_rope_fwd", "cf_qk_norm_workspace_bytes", "cf_qk_norm_rope_bwd", "cf_layer_qk_workspace_bytes",
     "cf_lora_qk_workspace_bytes", "cf_layer_bwd_filtered_qk", "cf_layer_bwd_compact_qk", "cf_layer_bwd_dense_qk", "cf_layer_bwd_lora_qk",
     "cf_token_loss_workspace_bytes", "cf_token_loss", "cf_adamw_step", "cf_grad_norm_workspace_bytes", "cf_grad_norm",
+    "cf_embed_fwd", "cf_embed_bwd_workspace_bytes", "cf_embed_bwd", "cf_norm_fwd", "cf_norm_bwd_workspace_bytes", "cf_norm_bwd",
+    "cf_head_loss_workspace_bytes", "cf_head_loss",
 )
 
 
@@ -90,6 +92,10 @@ class LayerQk(C.Structure):
 class LossDesc(C.Structure):
     _fields_ = [("kind", C.c_int32), ("V", C.c_int32), ("dtype", C.c_int32)] + \
                [(n, C.c_float) for n in ("logit_scale", "clip_lo", "clip_hi", "kl_coef", "norm")]
+
+
+class NormDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("H", "dtype", "layer")] + [("eps", C.c_float)]
 
 
 class AdamwTensor(C.Structure):
@@ -178,6 +184,14 @@ def lib() -> C.CDLL:
                                                        vp, sz, vp]),
             ("cf_token_loss_workspace_bytes", sz, [i32]),
             ("cf_token_loss", C.c_int, [C.POINTER(LossDesc), vp, i64, vp, vp, vp, vp, vp, vp, vp, i32, vp, i64, vp, vp, vp, sz, vp]),
+            ("cf_embed_fwd", C.c_int, [vp, i32, i32, i32, vp, i64, f32, vp, vp]),
+            ("cf_embed_bwd_workspace_bytes", sz, [i32, i32]),
+            ("cf_embed_bwd", C.c_int, [vp, vp, i32, i32, i32, vp, vp, i32, f32, vp, i32, vp, sz, vp]),
+            ("cf_norm_fwd", C.c_int, [C.POINTER(NormDesc), vp, vp, vp, vp, vp, i32, vp, vp]),
+            ("cf_norm_bwd_workspace_bytes", sz, [C.POINTER(NormDesc), i32]),
+            ("cf_norm_bwd", C.c_int, [C.POINTER(NormDesc), vp, vp, vp, vp, vp, i32, vp, vp, vp, i32, vp, sz, vp]),
+            ("cf_head_loss_workspace_bytes", sz, [C.POINTER(LossDesc), i32, i32, i32, i32, sz]),
+            ("cf_head_loss", C.c_int, [C.POINTER(LossDesc), i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, i32, vp, vp, vp, sz, vp]),
             ("cf_adamw_step", C.c_int, [C.POINTER(AdamwDesc), C.POINTER(AdamwTensor), i32, vp]),
             ("cf_grad_norm_workspace_bytes", sz, [i32]),
             ("cf_grad_norm", C.c_int, [C.POINTER(vp), C.POINTER(i64), i32, i32, f32, vp, vp, sz, vp])):
@@ -667,6 +681,182 @@ def token_loss(logits, targets, old_logp=None, advantages=None, ref_logp=None, w
                                          None if out is None else _ptr(out), ds, _ptr(logp), stats.data_ptr(), ws.data_ptr(), ws.numel(),
                                          _stream(device)), "cf_token_loss")
     return stats, logp, out
+
+
+# --------------------------------------------------------------------------
+# the ends of the stack of layers: embeddings, the norm of rows, the loss from the head's input
+# --------------------------------------------------------------------------
+
+def _dense(t, dtype, shape, what: str):
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s has to be %s %s, contiguous, not %s %s" % (what, dtype, list(shape), t.dtype, list(t.shape)))
+
+
+def _ws(nbytes: int, device):
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def embed_fwd(table, tokens, scale: float = 1.0, out=None):
+    """scale * table[tokens] for tokens (int64, contiguous, any shape); 0 for tokens outside [0, V).  out: to write to."""
+    _need(table.dim() == 2 and table.is_contiguous(), "table has to be [V, H], contiguous")
+    _need(tokens.dtype is torch.int64 and tokens.is_contiguous(), "tokens have to be int64, contiguous")
+    V, H = table.shape
+    shape = (*tokens.shape, H)
+    if out is None:
+        out = torch.empty(shape, dtype=table.dtype, device=table.device)
+    else:
+        _dense(out, table.dtype, shape, "out")
+        _need(not _ranges_meet(out, table), "out must not overlap table")
+    device = _on((table, tokens, out))
+    _check((_lib or lib()).cf_embed_fwd(_ptr(table), V, H, _dtype_code(table), _ptr(tokens), tokens.numel(), scale, _ptr(out), _stream(device)),
+           "cf_embed_fwd")
+    return out
+
+
+@functools.lru_cache(maxsize=1024)
+def _embed_ws_bytes(H, n):
+    return lib().cf_embed_bwd_workspace_bytes(H, n)
+
+
+def embed_bwd(tokens, dx, V: int, scale: float = 1.0, idx=None, n_kept_dev=None, main_grad=None, out=None):
+    """Gradient [V, H] of embed_fwd's table for compact dx [n, H]: row j has token tokens[idx[j]] (tokens[j] without idx).  main_grad: fp32 [V, H] that is
+    added to and returned; otherwise all of the gradient is written in dx's type (to out).  n_kept_dev: only the first min(*n_kept_dev, n) rows.  Reproducible."""
+    _need(dx.dim() == 2 and dx.is_contiguous(), "dx has to be [n, H], contiguous")
+    _need(tokens.dtype is torch.int64 and tokens.is_contiguous(), "tokens have to be int64, contiguous")
+    n, H = dx.shape
+    _kept_count(idx, n_kept_dev, tokens.numel(), n)
+    if main_grad is not None:
+        _need(out is None, "main_grad is added to: there is no other out")
+        _dense(main_grad, torch.float32, (V, H), "main_grad")
+        out = main_grad
+    elif out is None:
+        out = torch.empty((V, H), dtype=dx.dtype, device=dx.device)
+    else:
+        _dense(out, dx.dtype, (V, H), "out")
+    _need(not _ranges_meet(out, dx), "the gradient must not overlap dx")
+    device = _on((tokens, dx, idx, n_kept_dev, out))
+    wsb = _embed_ws_bytes(H, n)
+    ws = _ws(wsb, dx.device)
+    _check((_lib or lib()).cf_embed_bwd(_ptr(tokens), _ptr(dx), V, H, _dtype_code(dx), None if idx is None else _ptr(idx), _addr(n_kept_dev), n,
+                                        scale, _ptr(out), int(main_grad is not None), ws.data_ptr(), wsb, _stream(device)), "cf_embed_bwd")
+    return out
+
+
+def _norm_args(x, g, b, layer: bool):
+    _need(x.dim() == 2 and x.is_contiguous(), "x has to be [rows, H], contiguous")
+    _dense(g, x.dtype, (x.shape[1],), "g")
+    if b is not None:
+        _need(layer, "biases belong to a layer norm")
+        _dense(b, x.dtype, (x.shape[1],), "b")
+
+
+def norm_fwd(x, g, b=None, eps: float = 1e-5, layer: bool = False, idx=None, n_kept_dev=None, max_kept: int | None = None, out=None):
+    """Root mean square norm, or layer norm, of the rows idx of x [rows, H] (all without idx), times g, plus b (layer norm only).  Returns [max_kept, H], by
+    default as many rows as idx has.  out: to write to, without idx x itself too.  n_kept_dev: only the first min(*n_kept_dev, max_kept) rows."""
+    _norm_args(x, g, b, layer)
+    rows, H = x.shape
+    n = max_kept if max_kept is not None else rows if idx is None else idx.numel()
+    _kept_count(idx, n_kept_dev, rows, n)
+    if out is None:
+        out = torch.empty((n, H), dtype=x.dtype, device=x.device)
+    else:
+        _dense(out, x.dtype, (n, H), "out")
+        _need(not _ranges_meet(out, x) or (idx is None and out.data_ptr() == x.data_ptr()), "out must not overlap x, or be x without idx")
+    device = _on((x, g, b, idx, n_kept_dev, out))
+    d = NormDesc(H, _dtype_code(x), int(layer), eps)
+    _check((_lib or lib()).cf_norm_fwd(C.byref(d), _ptr(x), g.data_ptr(), _addr(b), None if idx is None else _ptr(idx), _addr(n_kept_dev), n, _ptr(out),
+                                       _stream(device)), "cf_norm_fwd")
+    return out
+
+
+@functools.lru_cache(maxsize=1024)
+def _norm_ws_bytes(H, code, layer, n):
+    return lib().cf_norm_bwd_workspace_bytes(C.byref(NormDesc(H, code, layer, 0.0)), n)
+
+
+def norm_bwd(x, g, dy, eps: float = 1e-5, layer: bool = False, idx=None, n_kept_dev=None, need_gains: bool = True, main_grads=None, out=None):
+    """Backward of norm_fwd for compact dy [n, H]; x is its input at full length.  Returns (dx [n, H], dg, db); db is None without layer, both without
+    need_gains.  main_grads: fp32 (dg, db) that are added to.  out: dx to write to, dy itself too.  n_kept_dev: only the first min(*n_kept_dev, n) rows."""
+    _norm_args(x, g, None, layer)
+    rows, H = x.shape
+    _need(dy.dim() == 2, "dy has to be [n, H]")
+    n = dy.shape[0]
+    _dense(dy, x.dtype, (n, H), "dy")
+    _kept_count(idx, n_kept_dev, rows, n)
+    if out is None:
+        out = torch.empty_like(dy)
+    else:
+        _dense(out, x.dtype, (n, H), "out")
+        _need(not _ranges_meet(out, dy) or out.data_ptr() == dy.data_ptr(), "out must not overlap dy, or be dy")
+        _need(not _ranges_meet(out, x) or (idx is None and out.data_ptr() == x.data_ptr()), "out must not overlap x, or be x without idx")
+    dg = db = ws = None
+    wsb = 0
+    if main_grads is not None:
+        dg, db = main_grads if isinstance(main_grads, (tuple, list)) else (main_grads, None)
+        _dense(dg, torch.float32, (H,), "main_grads[0]")
+        if db is not None:
+            _need(layer, "biases belong to a layer norm")
+            _dense(db, torch.float32, (H,), "main_grads[1]")
+    elif need_gains:
+        dg, db = torch.empty_like(g), torch.empty_like(g) if layer else None
+    code = _dtype_code(x)
+    if dg is not None:
+        wsb = _norm_ws_bytes(H, code, int(layer), n)
+        ws = _ws(wsb, x.device)
+    device = _on((x, g, dy, idx, n_kept_dev, out, dg, db))
+    d = NormDesc(H, code, int(layer), eps)
+    _check((_lib or lib()).cf_norm_bwd(C.byref(d), _ptr(x), g.data_ptr(), _ptr(dy), None if idx is None else _ptr(idx), _addr(n_kept_dev), n,
+                                       _ptr(out), _addr(dg), _addr(db), int(main_grads is not None), _addr(ws), wsb, _stream(device)), "cf_norm_bwd")
+    return out, dg, db
+
+
+@functools.lru_cache(maxsize=1024)
+def _head_ws_bytes(V, code, H, n, dx, dt, limit, device):
+    """A function of the sizes and of the current device, whose compute units the library asks for."""
+    return lib().cf_head_loss_workspace_bytes(C.byref(LossDesc(CF_LOSS_NLL, V, code, 0.0, 0.0, 0.0, 0.0, 0.0)), H, n, dx, dt, limit)
+
+
+def head_loss(x, table, targets, old_logp=None, advantages=None, ref_logp=None, weights=None, clip=(0.2, 0.2), kl_coef: float = 0.0,
+              logit_scale: float = 1.0, norm: float = 0.0, idx=None, n_kept_dev=None, need_dx: bool = True, need_dtable: bool = True, main_grad=None,
+              dx_out=None, ws_limit: int = 2 << 30):
+    """The losses of token_loss straight from the head's input x [n, H] (compact: row j belongs to targets[idx[j]], and so on) and its table [V, H], with no
+    logits in memory.  Returns (stats [4], logp [n], dx [n, H] or None, dtable [V, H] or None).  main_grad: fp32 [V, H] that the table's gradient is added to.
+    dx_out: to write dx to, x itself too.  n_kept_dev: only the first min(*n_kept_dev, n) rows.  ws_limit: bytes of scratch that the call may
+    allocate; exponentials of logits that do not fit are computed twice."""
+    _need(x.dim() == 2 and x.is_contiguous() and table.dim() == 2 and table.is_contiguous(), "x has to be [n, H] and table [V, H], contiguous")
+    (n, H), V = x.shape, table.shape[0]
+    _dense(table, x.dtype, (V, H), "table")
+    rows = targets.numel()
+    _need(targets.dtype is torch.int64 and targets.dim() == 1 and targets.is_contiguous(), "targets have to be int64 [rows], contiguous")
+    _kept_count(idx, n_kept_dev, rows, n)
+    policy = advantages is not None
+    _need(policy or (old_logp is None and ref_logp is None), "old_logp and ref_logp belong to a loss with advantages")
+    for t in (old_logp, advantages, ref_logp, weights):
+        if t is not None and not (t.dtype is torch.float32 and t.shape == (rows,) and t.is_contiguous()):
+            raise ValueError("old_logp, advantages, ref_logp and weights have to be fp32 [%d]" % rows)
+    code, dev = _dtype_code(x), x.device
+    dx = dt = None
+    if dx_out is not None:
+        _dense(dx_out, x.dtype, (n, H), "dx_out")
+        dx = dx_out
+    elif need_dx:
+        dx = torch.empty_like(x)
+    if main_grad is not None:
+        _dense(main_grad, torch.float32, (V, H), "main_grad")
+        dt = main_grad
+    elif need_dtable:
+        dt = torch.empty_like(table)
+    device = _on((x, table, targets, old_logp, advantages, ref_logp, weights, idx, n_kept_dev, dx, dt))
+    logp = torch.empty(n, dtype=torch.float32, device=dev)
+    stats = torch.empty(4, dtype=torch.float32, device=dev)
+    wsb = _head_ws_bytes(V, code, H, n, int(dx is not None), int(dt is not None), ws_limit, device)
+    ws = _ws(wsb, dev)
+    d = LossDesc(CF_LOSS_POLICY if policy else CF_LOSS_NLL, V, code, logit_scale, clip[0], clip[1], kl_coef, norm)
+    at = lambda t: None if t is None else _ptr(t)
+    _check((_lib or lib()).cf_head_loss(C.byref(d), H, _ptr(x), _ptr(table), _ptr(targets), at(old_logp), at(ref_logp), at(advantages), at(weights), at(idx),
+                                        _addr(n_kept_dev), n, at(dx), at(dt), int(main_grad is not None), _ptr(logp), stats.data_ptr(), _ptr(ws), wsb,
+                                        _stream(device)), "cf_head_loss")
+    return stats, logp, dx, dt
 
 
 STATE_BLOCK = 256       # elements that share a scale of an 8-bit state

@@ -74,6 +74,11 @@ template <typename T> __device__ __forceinline__ T from_f32(float v);
 template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
 template <> __device__ __forceinline__ bf16_t from_f32<bf16_t>(float v) { return f32_to_bf16(v); }
 
+// one value, rounded; NaN stays NaN
+template <typename T> __device__ __forceinline__ T narrow_one(float v);
+template <> __device__ __forceinline__ float narrow_one<float>(float v) { return v; }
+template <> __device__ __forceinline__ bf16_t narrow_one<bf16_t>(float v) { return (bf16_t)pack_bf16x2(v, 0.f); }
+
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);

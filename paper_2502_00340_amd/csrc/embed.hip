@@ -1,0 +1,461 @@
+// Token embeddings and their gradient.  y_t = s * E[tok_t] is a gather: HBM-bound, rows in and rows out.  The gradient dE[c] (+)= s * sum of the dx rows
+// whose token is c is a sum over equal tokens: the rows are put in the order (token, row), so that a token's rows stand together and are added
+// up in ascending order, whatever the launch does.  It reads the rows once and touches, in a main gradient, no other row of the table.
+#include "common.h"
+#include "mfma_util.h"
+
+namespace cf {
+
+// ---- forward -------------------------------------------------------------------------------------------------
+
+template <typename T>
+__global__ __launch_bounds__(256) void embed_fwd_kernel(const T* __restrict__ table, const int64_t* __restrict__ tokens, int64_t n, int V, int vpr,
+                                                        int lanes, int rpb, float scale, T* __restrict__ y) {
+    constexpr int VN = Vec<T>::N;
+    const int r = threadIdx.x / lanes, c0 = threadIdx.x % lanes;
+    if (r >= rpb) return;
+    for (int64_t j = (int64_t)blockIdx.x * rpb + r; j < n; j += (int64_t)gridDim.x * rpb) {
+        const int64_t t = tokens[j];
+        const bool live = t >= 0 && t < V;
+        const T* src = table + (live ? t : 0) * vpr * VN;
+        T* dst = y + j * vpr * VN;
+        for (int c = c0; c < vpr; c += lanes) {
+            u32x4_t w = {0u, 0u, 0u, 0u};
+            if (live) {
+                w = *reinterpret_cast<const u32x4_t*>(src + c * VN);
+                if (scale != 1.f) {
+                    float o[VN];
+                    Vec<T>::load(src + c * VN, o);
+#pragma unroll
+                    for (int e = 0; e < VN; ++e) o[e] *= scale;
+                    Vec<T>::store(dst + c * VN, o);
+                    continue;
+                }
+            }
+            *reinterpret_cast<u32x4_t*>(dst + c * VN) = w;
+        }
+    }
+}
+
+template <typename T>
+static void launch_embed_fwd(const void* table, const int64_t* tokens, int64_t n, int V, int H, float scale, void* y, hipStream_t st) {
+    const int vpr = H / Vec<T>::N;
+    int lanes = 256;
+    while (lanes > 1 && lanes / 2 >= vpr) lanes /= 2;
+    const int rpb = 256 / lanes;
+    const int64_t blocks = (n + rpb - 1) / rpb;
+    embed_fwd_kernel<T><<<(int)(blocks < MAX_GRID ? blocks : MAX_GRID), 256, 0, st>>>((const T*)table, tokens, n, V, vpr, lanes, rpb, scale, (T*)y);
+}
+
+// ---- the rows in the order (token, row) ----------------------------------------------------------------------
+// A block sorts a span of up to 8192 rows in LDS: passes of nine bits, lowest first, each keeping the order of what is equal.  A wave takes a
+// contiguous part of the span, 64 rows at a time; rows of one wave and round that share a digit find each other by nine ballots.  Two passes do for
+// 2^18 tokens.  Spans are merged by rank: a row's place is its place in its span and, for each other span, the number of rows there that go ahead of it.
+
+constexpr int SPAN = 8192, DIGIT_BITS = 9, DIGITS = 1 << DIGIT_BITS, SORT_WAVES = 16, SORT_THREADS = 64 * SORT_WAVES, PER_THREAD = SPAN / SORT_THREADS;
+constexpr int SORT_LDS = SPAN * 4 + SPAN * 2 + SORT_WAVES * DIGITS * 2 + 64;
+
+struct SortArgs {
+    const int64_t* tokens;
+    const int32_t *idx, *n_dev;
+    int n_max, V, passes;
+    int32_t *tok, *row;     // out: sorted, span by span
+    int spans;
+    u32x4_t* zero;          // nullable: the blocks behind those of the spans clear zero[0 .. n_zero)
+    int64_t n_zero;
+};
+
+__global__ __launch_bounds__(SORT_THREADS) void embed_sort_kernel(SortArgs a) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if ((int)blockIdx.x >= a.spans) {
+        const int64_t stride = (int64_t)((int)gridDim.x - a.spans) * SORT_THREADS;
+        for (int64_t i = (int64_t)((int)blockIdx.x - a.spans) * SORT_THREADS + tid; i < a.n_zero; i += stride)
+            __builtin_nontemporal_store(u32x4_t{0u, 0u, 0u, 0u}, a.zero + i);
+        return;
+    }
+    extern __shared__ __align__(16) unsigned char smem[];
+    unsigned* skey = reinterpret_cast<unsigned*>(smem);
+    uint16_t* sval = reinterpret_cast<uint16_t*>(smem + SPAN * 4);
+    uint16_t* cnt = sval + SPAN;                        // [wave][digit]
+    int* tot = reinterpret_cast<int*>(cnt + SORT_WAVES * DIGITS);
+    const int n_rows = live_rows(a.n_max, a.n_dev), first = (int)blockIdx.x * SPAN, m = min(n_rows - first, SPAN);
+    if (m <= 0) return;
+    const int rounds = (m + SORT_THREADS - 1) / SORT_THREADS;          // of 64 rows, for each wave
+    const int at0 = wave * rounds * 64 + lane;
+    unsigned key[PER_THREAD];
+    int val[PER_THREAD];
+#pragma unroll
+    for (int r = 0; r < PER_THREAD; ++r) {
+        const int i = at0 + r * 64;
+        key[r] = 0;
+        val[r] = i;
+        if (r < rounds && i < m) {
+            const int j = first + i;
+            const int64_t t = a.tokens[a.idx != nullptr ? a.idx[j] : j];
+            key[r] = t >= 0 && t < a.V ? (unsigned)t : (unsigned)a.V;      // what is no token goes last
+        }
+    }
+    for (int pass = 0; pass < a.passes; ++pass) {
+        const int shift = pass * DIGIT_BITS;
+        for (int i = tid; i < SORT_WAVES * DIGITS / 2; i += SORT_THREADS) reinterpret_cast<unsigned*>(cnt)[i] = 0u;
+        __syncthreads();
+        volatile uint16_t* mine = cnt + wave * DIGITS;
+        int rank[PER_THREAD];
+#pragma unroll
+        for (int r = 0; r < PER_THREAD; ++r) {
+            rank[r] = 0;
+            if (r < rounds) {                           // the same for all threads
+                const bool valid = at0 + r * 64 < m;
+                const unsigned d = (key[r] >> shift) & (DIGITS - 1);
+                uint64_t same = __ballot(valid);
+#pragma unroll
+                for (int b = 0; b < DIGIT_BITS; ++b) {
+                    const uint64_t bal = __ballot((d >> b) & 1u);
+                    same &= (d >> b) & 1u ? bal : ~bal;
+                }
+                if (valid) {
+                    const int before = mine[d];         // read by all, then written by the first lane: a wave's LDS accesses keep their order
+                    const int below = __popcll(same & ((1ull << lane) - 1ull));
+                    rank[r] = before + below;
+                    __builtin_amdgcn_wave_barrier();
+                    if (below == 0) mine[d] = (uint16_t)(before + __popcll(same));
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+        __syncthreads();
+        // a digit's rows of wave w start behind all rows of smaller digits and those of the waves ahead of it
+        int total = 0;
+        if (tid < DIGITS) {
+#pragma unroll
+            for (int w = 0; w < SORT_WAVES; ++w) {
+                const int c = cnt[w * DIGITS + tid];
+                cnt[w * DIGITS + tid] = (uint16_t)total;
+                total += c;
+            }
+        }
+        int incl = total;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(incl, o, 64);
+            if (lane >= o) incl += v;
+        }
+        if (tid < DIGITS && lane == 63) tot[wave] = incl;
+        __syncthreads();
+        if (tid < DIGITS) {
+            int base = incl - total;
+#pragma unroll
+            for (int w = 0; w < DIGITS / 64; ++w) base += w < wave ? tot[w] : 0;
+#pragma unroll
+            for (int w = 0; w < SORT_WAVES; ++w) cnt[w * DIGITS + tid] = (uint16_t)(cnt[w * DIGITS + tid] + base);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < PER_THREAD; ++r) {
+            if (r < rounds && at0 + r * 64 < m) {
+                const int to = cnt[wave * DIGITS + ((key[r] >> shift) & (DIGITS - 1))] + rank[r];
+                skey[to] = key[r];
+                sval[to] = (uint16_t)val[r];
+            }
+        }
+        __syncthreads();
+        if (pass + 1 == a.passes) break;
+#pragma unroll
+        for (int r = 0; r < PER_THREAD; ++r) {
+            if (r < rounds && at0 + r * 64 < m) {
+                key[r] = skey[at0 + r * 64];
+                val[r] = sval[at0 + r * 64];
+            }
+        }
+    }
+    for (int i = tid; i < m; i += SORT_THREADS) {
+        a.tok[first + i] = (int32_t)skey[i];
+        a.row[first + i] = first + (int)sval[i];
+    }
+}
+
+// rows of s[0 .. m) with a token below t, or up to it
+__device__ __forceinline__ int rank_in(const int32_t* __restrict__ s, int m, int t, bool equal_too) {
+    int lo = 0, hi = m;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        const bool ahead = equal_too ? s[mid] <= t : s[mid] < t;
+        lo = ahead ? mid + 1 : lo;
+        hi = ahead ? hi : mid;
+    }
+    return lo;
+}
+
+__global__ __launch_bounds__(256) void embed_merge_kernel(const int32_t* __restrict__ tok, const int32_t* __restrict__ row, int n_max,
+                                                          const int32_t* __restrict__ n_dev, int32_t* __restrict__ tok_out,
+                                                          int32_t* __restrict__ row_out) {
+    const int n_rows = live_rows(n_max, n_dev);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n_rows; i += (int64_t)gridDim.x * 256) {
+        const int span = (int)(i / SPAN), t = tok[i];
+        int64_t to = i % SPAN;
+        for (int s = 0; (int64_t)s * SPAN < n_rows; ++s)
+            if (s != span) to += rank_in(tok + (int64_t)s * SPAN, min(SPAN, n_rows - s * SPAN), t, s < span);
+        tok_out[to] = t;
+        row_out[to] = row[i];
+    }
+}
+
+// ---- sums ----------------------------------------------------------------------------------------------------
+// A block takes CH rows of that order, and TILE columns.  All its loads are asked for at once (rows, and the main gradient's old values); then the
+// rows are added up one by one, and a token's sum leaves where its last row has been added.  A token whose rows reach over the border of a block leaves parts: [chunk][0]
+// of one that began ahead of the chunk, [chunk][1] of one that begins here and goes on.  embed_join_kernel adds these up in order.
+constexpr int CH = 8;
+
+struct SumArgs {
+    const int32_t *tok, *row, *n_dev;
+    int n_max, V, H;
+    const void* dx;
+    float scale;
+    void* out;
+    float* part;
+};
+
+template <typename T, bool MAIN>
+__device__ __forceinline__ void embed_out(const SumArgs& a, int t, int c, const float (&s)[Vec<T>::N], const float (&old)[Vec<T>::N]) {
+    constexpr int VN = Vec<T>::N;
+    float o[VN];
+#pragma unroll
+    for (int e = 0; e < VN; ++e) o[e] = MAIN ? fmaf(a.scale, s[e], old[e]) : a.scale * s[e];
+    if constexpr (MAIN) {
+        float* p = (float*)a.out + (int64_t)t * a.H + c;
+#pragma unroll
+        for (int q = 0; q < VN / 4; ++q) reinterpret_cast<float4*>(p)[q] = make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+    } else {
+        Vec<T>::store((T*)a.out + (int64_t)t * a.H + c, o);
+    }
+}
+
+template <typename T, int NT, bool MAIN>
+__global__ __launch_bounds__(NT) void embed_sum_kernel(SumArgs a) {
+    constexpr int VN = Vec<T>::N;
+    const int n_rows = live_rows(a.n_max, a.n_dev), vpr = a.H / VN, tiles = (vpr + NT - 1) / NT;
+    const int64_t units = (int64_t)((n_rows + CH - 1) / CH) * tiles;
+    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+        const int chunk = (int)(u / tiles), p0 = chunk * CH, v = (int)(u % tiles) * NT + threadIdx.x;
+        int t[CH + 2];              // tokens of rows p0 - 1 .. p0 + CH; V: none
+#pragma unroll
+        for (int i = 0; i < CH + 2; ++i) {
+            const int p = p0 + i - 1;
+            t[i] = p >= 0 && p < n_rows ? a.tok[p] : a.V;
+        }
+        if (t[1] >= a.V) break;     // what is no token stands last
+        const bool mine = v < vpr;
+        const int c = (mine ? v : 0) * VN;
+        u32x4_t x[CH];
+        float old[CH][MAIN ? VN : 1];
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+            if (t[i + 1] < a.V) x[i] = *reinterpret_cast<const u32x4_t*>((const T*)a.dx + (int64_t)a.row[p0 + i] * a.H + c);
+        if constexpr (MAIN) {
+            bool whole = t[0] != t[1];          // the token of row i began in this chunk
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const bool ends = t[i + 2] != t[i + 1];
+                if (whole && ends && t[i + 1] < a.V) {
+                    const float4* p = reinterpret_cast<const float4*>((const float*)a.out + (int64_t)t[i + 1] * a.H + c);
+#pragma unroll
+                    for (int q = 0; q < VN / 4; ++q) {
+                        const float4 w = p[q];
+                        old[i][4 * q] = w.x; old[i][4 * q + 1] = w.y; old[i][4 * q + 2] = w.z; old[i][4 * q + 3] = w.w;
+                    }
+                }
+                whole |= ends;
+            }
+        }
+        if (!mine) continue;
+        float s[VN];
+#pragma unroll
+        for (int e = 0; e < VN; ++e) s[e] = 0.f;
+        bool whole = t[0] != t[1];
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            if (t[i + 1] >= a.V) break;
+            const bool ends = t[i + 2] != t[i + 1];
+            float o[VN];
+            Vec<T>::load(reinterpret_cast<const T*>(&x[i]), o);
+#pragma unroll
+            for (int e = 0; e < VN; ++e) s[e] += o[e];
+            if (ends || i == CH - 1) {
+                if (whole && ends) {
+                    if constexpr (MAIN) embed_out<T, true>(a, t[i + 1], c, s, old[i]);
+                    else embed_out<T, false>(a, t[i + 1], c, s, s);
+                } else {
+                    float* p = a.part + ((int64_t)chunk * 2 + (whole ? 1 : 0)) * a.H + c;
+#pragma unroll
+                    for (int q = 0; q < VN / 4; ++q)
+                        reinterpret_cast<float4*>(p)[q] = make_float4(s[4 * q], s[4 * q + 1], s[4 * q + 2], s[4 * q + 3]);
+                }
+#pragma unroll
+                for (int e = 0; e < VN; ++e) s[e] = 0.f;
+                whole = true;
+            }
+        }
+    }
+}
+
+// The tokens whose rows reach over chunks.  An item is a chunk and 256 columns; it is live where a token begins in the chunk that goes on in the next one.
+// 16 waves take every 16th part each, in order, and are added up in order.
+template <typename T, bool MAIN>
+__global__ __launch_bounds__(1024) void embed_join_kernel(SumArgs a) {
+    __shared__ float red[16][256];
+    __shared__ int list[1024];
+    __shared__ int n_list;
+    const int n_rows = live_rows(a.n_max, a.n_dev), chunks = (n_rows + CH - 1) / CH, tiles = (a.H + 255) / 256;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t items = (int64_t)(chunks - 1) * tiles;            // nothing goes on behind the last chunk
+    for (int64_t i0 = 0; (int64_t)blockIdx.x + i0 * gridDim.x < items; i0 += 1024) {
+        if (tid == 0) n_list = 0;
+        __syncthreads();
+        const int64_t it = (int64_t)blockIdx.x + (i0 + tid) * gridDim.x;
+        if (it < items) {
+            const int p1 = (int)(it / tiles) * CH + CH, t = a.tok[p1 - 1];
+            const bool live = t < a.V && t == a.tok[p1] && (p1 == CH || a.tok[p1 - CH - 1] != t);
+            if (live) list[atomicAdd(&n_list, 1)] = tid;            // their order does not matter: each is on its own
+        }
+        __syncthreads();
+        const int n = n_list;
+        for (int l = 0; l < n; ++l) {
+            const int64_t item = (int64_t)blockIdx.x + (i0 + list[l]) * gridDim.x;
+            const int chunk = (int)(item / tiles), c = (int)(item % tiles) * 256 + lane * 4, t = a.tok[chunk * CH + CH - 1];
+            int parts = 1;                                          // this chunk's and those of the chunks that begin with the token
+            for (int k0 = chunk + 1;; k0 += 1024) {
+                const int here = __syncthreads_count((int64_t)(k0 + tid) < chunks && a.tok[(k0 + tid) * CH] == t);
+                parts += here;
+                if (here < 1024) break;
+            }
+            float s[4] = {0.f, 0.f, 0.f, 0.f};
+            if (c < a.H) {
+#pragma unroll 4
+                for (int k = wave; k < parts; k += 16) {
+                    const float4 w = *reinterpret_cast<const float4*>(a.part + ((int64_t)(chunk + k) * 2 + (k == 0 ? 1 : 0)) * a.H + c);
+                    s[0] += w.x; s[1] += w.y; s[2] += w.z; s[3] += w.w;
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) red[wave][lane * 4 + e] = s[e];
+            __syncthreads();
+            if (tid < 256 && (c & ~255) + tid < a.H) {
+                const int col = (int)(item % tiles) * 256 + tid;
+                float sum = 0.f;
+#pragma unroll
+                for (int w = 0; w < 16; ++w) sum += red[w][tid];
+                const int64_t at = (int64_t)t * a.H + col;
+                if constexpr (MAIN) ((float*)a.out)[at] = fmaf(a.scale, sum, ((float*)a.out)[at]);
+                else ((T*)a.out)[at] = narrow_one<T>(a.scale * sum);
+            }
+            __syncthreads();
+        }
+        __syncthreads();
+    }
+}
+
+// workspace: the order (twice where spans have to be merged), then the parts
+struct EmbedWs {
+    size_t order, part, total;
+    EmbedWs(int H, int n) {
+        n = n > 0 ? n : 1;
+        order = align_up((size_t)n * 4, 256);
+        part = order * (n > SPAN ? 4 : 2);
+        total = part + align_up((size_t)ceil_div(n, CH) * 2 * H * 4, 256);
+    }
+};
+
+template <typename T, bool MAIN>
+static hipError_t launch_embed_bwd(SumArgs a, SortArgs so, unsigned char* ws, hipStream_t st) {
+    const EmbedWs L(a.H, a.n_max);
+    const int n = a.n_max;
+    so.tok = (int32_t*)ws;
+    so.row = (int32_t*)(ws + L.order);
+    so.spans = ceil_div(n, SPAN);
+    if (!MAIN) {
+        so.zero = (u32x4_t*)a.out;
+        so.n_zero = (int64_t)a.V * a.H * (int64_t)sizeof(T) / 16;
+    }
+    static std::atomic<uint64_t> lds_ok{0};
+    const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&embed_sort_kernel), SORT_LDS, lds_ok);
+    if (e != hipSuccess) return e;
+    const int64_t fill = MAIN ? 0 : (so.n_zero + 4 * SORT_THREADS - 1) / (4 * SORT_THREADS);
+    const int grid = so.spans + (int)(fill < 8 * compute_units() ? fill : 8 * compute_units());
+    if (grid > 0) embed_sort_kernel<<<grid, SORT_THREADS, SORT_LDS, st>>>(so);
+    if (n == 0) return hipGetLastError();
+    a.tok = so.tok;
+    a.row = so.row;
+    if (so.spans > 1) {
+        int32_t *tok = (int32_t*)(ws + 2 * L.order), *row = (int32_t*)(ws + 3 * L.order);
+        embed_merge_kernel<<<ceil_div(n, 256) < MAX_GRID ? ceil_div(n, 256) : MAX_GRID, 256, 0, st>>>(a.tok, a.row, n, a.n_dev, tok, row);
+        a.tok = tok;
+        a.row = row;
+    }
+    a.part = (float*)(ws + L.part);
+    const int vpr = a.H / Vec<T>::N, chunks = ceil_div(n, CH);
+    const auto blocks = [&](int nt) { const int64_t u = (int64_t)chunks * ((vpr + nt - 1) / nt); return (int)(u < MAX_GRID ? u : MAX_GRID); };
+    if (vpr <= 64) embed_sum_kernel<T, 64, MAIN><<<blocks(64), 64, 0, st>>>(a);
+    else if (vpr <= 128) embed_sum_kernel<T, 128, MAIN><<<blocks(128), 128, 0, st>>>(a);
+    else embed_sum_kernel<T, 256, MAIN><<<blocks(256), 256, 0, st>>>(a);
+    if (chunks > 1) {
+        const int64_t items = (int64_t)(chunks - 1) * ((a.H + 255) / 256);
+        embed_join_kernel<T, MAIN><<<(int)(items < 2 * compute_units() ? items : 2 * compute_units()), 1024, 0, st>>>(a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace cf
+
+using namespace cf;
+
+static bool off16(const void* p) { return (uintptr_t)p % 16 != 0; }
+
+static cf_status embed_sizes(int32_t V, int32_t H, int32_t dtype) {
+    if (dtype != CF_BF16 && dtype != CF_F32) return CF_ERR_DTYPE;
+    if (V <= 0 || V > (1 << 30) || H <= 0 || H > (1 << 20) || H % (dtype == CF_F32 ? 4 : 8) != 0) return CF_ERR_SHAPE;
+    return CF_OK;
+}
+
+extern "C" {
+
+cf_status cf_embed_fwd(const void* table, int32_t V, int32_t H, int32_t dtype, const int64_t* tokens, int64_t n, float scale, void* out,
+                       cf_stream stream) {
+    if (!table || !tokens || !out) return CF_ERR_NULL;
+    const cf_status ok = embed_sizes(V, H, dtype);
+    if (ok != CF_OK) return ok;
+    if (n < 0 || n > ((int64_t)1 << 40) / H || !(scale - scale == 0.f)) return CF_ERR_SHAPE;
+    if (off16(table) || off16(out) || (uintptr_t)tokens % 8 != 0) return CF_ERR_SHAPE;
+    if (n == 0) return CF_OK;
+    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    if (dtype == CF_F32) launch_embed_fwd<float>(table, tokens, n, V, H, scale, out, st);
+    else launch_embed_fwd<bf16_t>(table, tokens, n, V, H, scale, out, st);
+    return hipGetLastError() == hipSuccess ? CF_OK : CF_ERR_HIP;
+}
+
+size_t cf_embed_bwd_workspace_bytes(int32_t H, int32_t max_kept) {
+    if (H <= 0 || H > (1 << 20) || max_kept < 0 || max_kept > (1 << 30)) return 0;
+    return EmbedWs(H, max_kept).total;
+}
+
+cf_status cf_embed_bwd(const int64_t* tokens, const void* dx_kept, int32_t V, int32_t H, int32_t dtype, const int32_t* idx,
+                       const int32_t* n_kept_dev, int32_t max_kept, float scale, void* dtable, int32_t main_grad, void* ws, size_t ws_bytes,
+                       cf_stream stream) {
+    if (!tokens || !dx_kept || !dtable) return CF_ERR_NULL;
+    const cf_status ok = embed_sizes(V, H, dtype);
+    if (ok != CF_OK) return ok;
+    if (max_kept < 0 || max_kept > (1 << 30) || (main_grad != 0 && main_grad != 1) || !(scale - scale == 0.f)) return CF_ERR_SHAPE;
+    if (off16(dx_kept) || off16(dtable) || (uintptr_t)tokens % 8 != 0 || (uintptr_t)idx % 4 != 0 || (uintptr_t)n_kept_dev % 4 != 0) return CF_ERR_SHAPE;
+    if (!ws || (uintptr_t)ws % 256 != 0 || ws_bytes < cf_embed_bwd_workspace_bytes(H, max_kept)) return CF_ERR_WORKSPACE;
+    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    int passes = 0;
+    for (int64_t v = V; v > 0; v >>= DIGIT_BITS) ++passes;
+    SumArgs a{nullptr, nullptr, n_kept_dev, max_kept, V, H, dx_kept, scale, dtable, nullptr};
+    SortArgs so{tokens, idx, n_kept_dev, max_kept, V, passes, nullptr, nullptr, 0, nullptr, 0};
+    unsigned char* w = (unsigned char*)ws;
+    hipError_t e;
+    if (dtype == CF_F32) e = main_grad ? launch_embed_bwd<float, true>(a, so, w, st) : launch_embed_bwd<float, false>(a, so, w, st);
+    else e = main_grad ? launch_embed_bwd<bf16_t, true>(a, so, w, st) : launch_embed_bwd<bf16_t, false>(a, so, w, st);
+    return e == hipSuccess ? CF_OK : CF_ERR_HIP;
+}
+
+}  // extern "C"

@@ -1,0 +1,877 @@
+// Loss of kept tokens straight from the head's input x [n, H] and the table E [V, H], with the gradients towards both: the logits s * x E^T are made tile by
+// tile in the matrix cores' accumulators and never leave them.  What leaves is bounded by the caller's workspace:
+//
+//   1. head_rows      the target's logit of every row, a dot product: ref = s*log2(e) * x.E_y
+//   2. head_logits    tiles of x E^T; with t = s*log2(e)*l - ref, strips of 64 columns leave sum(2^t), and, for the first columns (as many as the
+//                     workspace has room for), e = 2^t in the storage type
+//   3. head_finish    per row lp = -log(sum over c of 2^t), the loss and its slope; a = -w/norm * dL/dlp * s * exp(lp) is the row's factor: the gradient of logit c is
+//                     a * e_c, and a * e'_y with e'_y = expm1(lp) / exp(lp) at the target.  x' = a * x for the table's gradient
+//   4. for each piece of the columns (the first one is there already, the others are made again by head_logits):
+//      head_dx        slots (+)= e E, fp32          head_dtable   dE (+)= e^T x'
+//   5. head_dx_sum    dx = a * sum of the slots
+//
+// Taking the target's logit as the reference (not the row's maximum, which is not known ahead of the product) makes e a number that needs no second scaling:
+// 2^t is at most exp(-lp), so that nothing leaves fp32's or bf16's range unless the target has a probability below exp(-40).  A strip whose sum says so raises its
+// row tile's flag; head_logits then goes over the flagged tiles again with strips' maxima, and the row's log-sum-exp becomes its reference.
+//
+// Roundings: logits, sums, lp and both gradients' sums are fp32; e, and x' = a*x, are rounded to the storage type once each (2^-8 relative in bf16), dx and
+// the table's gradient once where they are stored.
+#include <math.h>
+
+#include <algorithm>
+
+#include "common.h"
+#include "gemm_tiles.h"
+#include "loss_row.h"
+#include "mfma_util.h"
+
+namespace cf {
+
+constexpr int STRIP = 64;                       // columns that share a sum
+constexpr float FLAG_ABOVE = 288230376151711744.f;      // 2^58 = exp(40): a strip's sum beyond it asks for another reference
+
+struct HeadArgs {
+    const void *x, *table;
+    int H, V, n_max;
+    const int32_t* n_dev;
+    float k;                // logit scale * log2(e)
+    int ldn;                // rows of the strips' array
+    float *ref, *sums;      // [n_max]; [strips][ldn]
+    float *a, *ey;          // [n_max]: the row's factor; e at the target
+    int32_t *y, *flags;     // target or -1; flags[0]: any, flags[1 + i]: rows 256 i ..
+    void* e;                // [n_max, lde]: columns c0 .. c0 + lde - 1
+    int lde, c0, c1;        // the launch's columns: c0 .. c1 - 1
+    int store_end;          // columns below it are stored
+    bool flagged_only;
+};
+enum HeadKind { SUMS = 0, MAXIMA = 1, VALUES = 2 };
+
+// ---- 1. targets --------------------------------------------------------------------------------------------
+
+template <typename T>
+__global__ __launch_bounds__(256) void head_rows_kernel(HeadArgs a, LossArgs l) {
+    constexpr int VN = Vec<T>::N;
+    const int n_rows = live_rows(a.n_max, a.n_dev), lane = threadIdx.x & 63;
+    const int n_flags = (a.n_max + 255) / 256 + 1;
+    if (blockIdx.x == 0)
+        for (int i = threadIdx.x; i < n_flags; i += 256) a.flags[i] = 0;
+    for (int64_t j = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); j < n_rows; j += (int64_t)gridDim.x * 4) {
+        const int64_t row = l.idx != nullptr ? l.idx[j] : j, t = l.targets[row];
+        const bool live = t >= 0 && t < a.V && (l.weights == nullptr || l.weights[row] != 0.f);
+        float s = 0.f;
+        if (live) {
+            const T *x = (const T*)a.x + j * a.H, *w = (const T*)a.table + t * a.H;
+            for (int c = lane * VN; c < a.H; c += 64 * VN) {
+                float p[VN], q[VN];
+                Vec<T>::load(x + c, p);
+                Vec<T>::load(w + c, q);
+#pragma unroll
+                for (int e = 0; e < VN; ++e) s = fmaf(p[e], q[e], s);
+            }
+        }
+        s = wave_sum(s);
+        if (lane == 0) {
+            // +inf stands for a row that is left out: its 2^t is 0 whatever t; a live row whose logit is +inf has no finite probability at all
+            const float r = s * a.k;
+            a.ref[j] = live ? (r == INFINITY ? NAN : r) : INFINITY;
+            a.ey[j] = fmaf(s, a.k, -r);         // what rounding left, for head_finish
+            a.y[j] = live ? (int32_t)t : -1;
+        }
+    }
+}
+
+// ---- 2. tiles of logits ------------------------------------------------------------------------------------
+
+template <int KIND> struct LeaveLogits {
+    static constexpr bool OWN = true, LDA = false;
+    HeadArgs a;
+    int rows;
+    template <int TM, int TN>
+    __device__ __forceinline__ void operator()(f32x4_t (&acc)[2 * TM][2 * TN], const TileRef& t, unsigned char* smem, int wm, int wn) const {
+        constexpr int FM = 2 * TM, FN = 2 * TN, NS = FN / 4;
+        int ln = threadIdx.x & 63;
+        asm volatile("" : "+v"(ln));            // rebuilt for each tile, not carried through the products
+        const int l16 = ln & 15, g4 = ln >> 4;
+        const int n0 = t.n0 + wn * (32 * TN), mw = t.m0 + wm * (32 * TM);
+        if (t.n0 + 64 * TN > a.V) {             // columns behind the last: the product's zeros become probabilities of 0
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        if (n0 + j * 16 + 4 * g4 + v >= a.V) acc[i][j][v] = -INFINITY;
+        }
+        const bool store = KIND != MAXIMA && t.n0 < a.store_end;
+        constexpr int RBY = 64 * TN, CPR = RBY / 16, RPP = 64 / CPR, NP = 32 / RPP, NV = CPR / RPP;     // as in the products' own write-out
+        unsigned char* stg = smem + GEMM_RING + ((wm * 2 + wn) * 8192);
+        const int c = ln % CPR, rl = ln / CPR, col = n0 + c * 8;
+        const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(
+            (bf16_t*)a.e + (int64_t)mw * a.lde, 0, max(0, min(rows - mw, 32 * TM)) * a.lde * 2, 0x00020000);
+        const unsigned voff = col - a.c0 < a.lde ? (unsigned)(rl * a.lde + (col - a.c0)) * 2u : 0x80000000u;
+        const unsigned char* rd[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) rd[v] = stg + rl * RBY + ((c ^ ((rl + RPP * v) & (CPR - 1))) << 4);
+        unsigned char* const wr = stg + l16 * RBY + (g4 & 1) * 8;
+        const int wsw = l16 & (CPR - 1), wch = g4 >> 1;
+#pragma unroll
+        for (int i2 = 0; i2 < TM; ++i2) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int i = 2 * i2 + h, m = mw + i * 16 + l16;
+                const float ref = m < rows ? a.ref[m] : INFINITY;
+                const bool dead = ref == INFINITY;
+                int yrel = -1;
+                float ey = 0.f;
+                if (KIND == VALUES && m < rows) {
+                    yrel = a.y[m] - n0 - 4 * g4;
+                    ey = a.ey[m];
+                }
+                const unsigned mask = dead ? 0u : ~0u;          // whatever such a row holds, NaN included
+#pragma unroll
+                for (int z = 0; z < NS; ++z) {
+                    float s = 0.f, mx = -INFINITY;
+                    if (KIND == MAXIMA) {
+#pragma unroll
+                        for (int j = 4 * z; j < 4 * z + 4; ++j)
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) mx = fmaxf(mx, acc[i][j][v]);
+                        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+                        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+                        mx *= a.k;
+                    }
+                    const float r = KIND == MAXIMA ? (mx == -INFINITY ? 0.f : mx) : ref;
+#pragma unroll
+                    for (int j = 4 * z; j < 4 * z + 4; ++j) {
+                        float e[4];
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) {
+                            e[v] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][v], a.k, -r));
+                            if (KIND != VALUES) s += e[v];
+                            else e[v] = yrel == j * 16 + v ? ey : e[v];
+                        }
+                        if (store) {
+                            uint2 o;
+                            o.x = pack_bf16x2(e[0], e[1]) & mask;
+                            o.y = pack_bf16x2(e[2], e[3]) & mask;
+                            *reinterpret_cast<uint2*>(wr + h * 16 * RBY + (((2 * j + wch) ^ wsw) << 4)) = o;
+                        }
+                    }
+                    if (KIND != VALUES) {
+                        s += __shfl_xor(s, 16, 64);
+                        s += __shfl_xor(s, 32, 64);
+                        if (g4 == 0 && m < rows && n0 + z * STRIP < a.V) {
+                            a.sums[(int64_t)(n0 / STRIP + z) * a.ldn + m] = KIND == MAXIMA ? mx + log2f(s) : s;
+                            if (KIND == SUMS && !dead && !(s <= FLAG_ABOVE)) a.flags[0] = a.flags[1 + (m >> 8)] = 1;
+                        }
+                    }
+                }
+            }
+            if (store) {
+                u32x4_t val[NP];
+#pragma unroll
+                for (int q = 0; q < NP; ++q) val[q] = *reinterpret_cast<const u32x4_t*>(rd[q % NV] + q * RPP * RBY);
+#pragma unroll
+                for (int q = 0; q < NP; ++q)
+                    __builtin_amdgcn_raw_buffer_store_b128(val[q], rc, voff + (unsigned)((i2 * 32 + q * RPP) * a.lde) * 2u, 0, 0);
+            }
+        }
+    }
+};
+
+// The tiles of x E^T over the launch's columns, as a product's: whole 256x256 ones that fill rounds of the CUs, then the rest in smaller ones.
+template <int KIND> __global__ __launch_bounds__(256) void head_logits_kernel(HeadArgs a) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    if (a.flagged_only && __builtin_amdgcn_readfirstlane(a.flags[0]) == 0) return;
+    const int rows = __builtin_amdgcn_readfirstlane(live_rows(a.n_max, a.n_dev)), width = a.c1 - a.c0;
+    const int tiles_m = (rows + 255) / 256, tiles_n = (width + 255) / 256, tiles = tiles_m * tiles_n;
+    int n_full, sub;
+    plan_tiles(tiles, (int)gridDim.x, n_full, sub);
+    if (rows <= 128) { n_full = 0; sub = 4; }           // half of a whole tile's rows would not exist
+    n_full = __builtin_amdgcn_readfirstlane(n_full);
+    sub = __builtin_amdgcn_readfirstlane(sub);
+    const int n_items = n_full + (tiles - n_full) * sub, stride = (int)gridDim.x;
+    GemmArgs g;
+    g.A[0] = a.x; g.B[0] = a.table; g.K[0] = a.H; g.nseg = 1; g.C = nullptr; g.M = rows; g.N = a.c1; g.alpha = 1.f; g.beta = 0.f;
+    g.a_idx = nullptr; g.a_rows = 0; g.n_dev = nullptr; g.lda = a.H;
+    auto decode = [&](int w, TileRef& t) __attribute__((always_inline)) {
+        int bm, bn, m0, n0;
+        if (w < n_full) {
+            tile_coords(xcd_order(w, n_full), tiles_m, tiles_n, bm, bn);
+            m0 = bm * 256;
+            n0 = bn * 256;
+        } else {
+            const int j = xcd_order(w - n_full, n_items - n_full), part = j % sub;
+            tile_coords(n_full + j / sub, tiles_m, tiles_n, bm, bn);
+            m0 = bm * 256 + (sub == 4 ? (part >> 1) * 128 : 0);
+            n0 = bn * 256 + (sub == 4 ? (part & 1) * 128 : (sub == 2 ? part * 128 : 0));
+            if (m0 >= rows || n0 >= width) return false;
+        }
+        if (a.flagged_only && __builtin_amdgcn_readfirstlane(a.flags[1 + bm]) == 0) return false;
+        n0 += a.c0;
+        t.m0 = __builtin_amdgcn_readfirstlane(m0);
+        t.n0 = __builtin_amdgcn_readfirstlane(n0);
+        t.M = rows;
+        t.N = __builtin_amdgcn_readfirstlane(min(a.c1, n0 + 256));      // the descriptor of a tile's rows of the table spans these rows alone
+        t.A0 = uniform_ptr(a.x);
+        t.B0 = uniform_ptr(a.table);
+        t.C = nullptr;
+        return true;
+    };
+    const LeaveLogits<KIND> leave{a, rows};
+    int w = (int)blockIdx.x;
+    TileRef t;
+    auto seek = [&](int end) __attribute__((always_inline)) {       // this block's first live item from w on
+        for (; w < end; w += stride)
+            if (decode(w, t)) return true;
+        return false;
+    };
+    auto next_in = [&](int end) {
+        return [&, end](TileRef& nx) __attribute__((always_inline)) {
+            w += stride;
+            if (!seek(end)) return false;
+            nx = t;
+            return true;
+        };
+    };
+    if (seek(n_full)) gemm_tiles<0, 4, 4, false, false>(g, a.H, t, next_in(n_full), smem, 0, 0, nullptr, leave);
+    if (!seek(n_items)) return;
+    if (sub == 1) gemm_tiles<0, 4, 4, false, false>(g, a.H, t, next_in(n_items), smem, 0, 0, nullptr, leave);
+    else if (sub == 2) gemm_tiles<0, 4, 2, false, false>(g, a.H, t, next_in(n_items), smem, 0, 0, nullptr, leave);
+    else gemm_tiles<0, 2, 2, false, false>(g, a.H, t, next_in(n_items), smem, 0, 0, nullptr, leave);
+}
+
+// ---- 3. the rows' ends -------------------------------------------------------------------------------------
+// A block takes 16 rows: 64 groups of 16 lanes add their strips up, one lane a row ends it, and the block scales the rows of x.
+template <typename T>
+__global__ __launch_bounds__(1024) void head_finish_kernel(HeadArgs a, LossArgs l, void* xs) {
+    constexpr int VN = Vec<T>::N;
+    __shared__ float red[2][16][16];
+    __shared__ float fac[16];
+    const int n_rows = live_rows(a.n_max, a.n_dev), j0 = blockIdx.x * 16, tid = threadIdx.x, r = tid & 15, grp = tid >> 4, j = j0 + r;
+    if (j0 >= n_rows) return;
+    const int strips = (a.V + STRIP - 1) / STRIP;
+    const bool flagged = a.flags[1 + (j0 >> 8)] != 0;           // the same for the 16 rows
+    float m = 0.f, s = 0.f;
+    if (!flagged) {
+        if (j < n_rows) {
+#pragma unroll 8
+            for (int i = grp; i < strips; i += 64) s += a.sums[(int64_t)i * a.ldn + j];
+        }
+    } else {
+        m = -INFINITY;
+        if (j < n_rows)
+            for (int i = grp; i < strips; i += 64) {            // log2 of each strip's sum
+                const float t = a.sums[(int64_t)i * a.ldn + j], n = fmaxf(m, t);
+                if (t == -INFINITY) continue;
+                s = s * __builtin_amdgcn_exp2f(m - n) + __builtin_amdgcn_exp2f(t - n);
+                m = n;
+            }
+#pragma unroll
+        for (int o = 16; o < 64; o <<= 1) {
+            const float mo = __shfl_xor(m, o, 64), so = __shfl_xor(s, o, 64), n = fmaxf(m, mo);
+            if (n != -INFINITY) s = s * __builtin_amdgcn_exp2f(m - n) + so * __builtin_amdgcn_exp2f(mo - n);
+            m = n;
+        }
+    }
+    if (!flagged) {
+        s += __shfl_xor(s, 16, 64);
+        s += __shfl_xor(s, 32, 64);
+    }
+    if ((tid & 63) < 16) { red[0][tid >> 6][r] = m; red[1][tid >> 6][r] = s; }
+    __syncthreads();
+    if (tid < 16 && j < n_rows) {
+        m = red[0][0][r];
+#pragma unroll
+        for (int w = 1; w < 16; ++w) m = fmaxf(m, red[0][w][r]);
+        s = 0.f;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) {
+            const float t = red[1][w][r];
+            s += !flagged ? t : t == 0.f ? 0.f : t * __builtin_amdgcn_exp2f(red[0][w][r] - m);
+        }
+        const int y = a.y[j];
+        float lp = 0.f, fy = 0.f;
+        RowLoss rl{make_float4(0.f, 0.f, 0.f, 0.f), 0.f};
+        if (y >= 0) {
+            // lp = ln(2) * (target - log2(sum)), with the sum relative to ref or, flagged, to m
+            const float ref = a.ref[j], ln2 = 0.6931471805599453f, rest = ln2 * a.ey[j];
+            if (!flagged) {
+                lp = rest - logf(s);
+            } else {
+                lp = ln2 * (ref - m) + (rest - logf(s));
+                const float lse = m + log2f(s);
+                a.ref[j] = lse == INFINITY ? NAN : lse;
+            }
+            lp = lp > 0.f ? 0.f : lp;           // the target's logit comes from another order of sums than the strips'
+            RowHead h;
+            h.row = l.idx != nullptr ? l.idx[j] : j;
+            h.y = y;
+            h.w = l.weights != nullptr ? l.weights[h.row] : 1.f;
+            h.old = h.ref = h.adv = 0.f;
+            if (l.policy) {
+                h.old = l.old_logp[h.row];
+                h.adv = l.adv[h.row];
+                if (l.ref_logp != nullptr) h.ref = l.ref_logp[h.row];
+            }
+            rl = row_loss(l, h, lp, 1.f / (l.norm != 0.f ? l.norm : (float)n_rows));
+            // e of the other columns is relative to exp(lp) (flagged: to 1)
+            const float by = flagged ? 1.f : s;
+            fy = -rl.coef * l.scale / by;
+            const float ey = expm1f(lp) * by;
+            a.ey[j] = ey;
+            if (a.e != nullptr && !flagged && y < a.store_end) ((T*)a.e)[(int64_t)j * a.lde + y] = narrow_one<T>(ey);
+        }
+        a.a[j] = fy;
+        fac[r] = fy;
+        if (l.logp != nullptr) l.logp[j] = lp;
+        l.terms[j] = rl.terms;
+    }
+    if (xs == nullptr) return;
+    __syncthreads();
+    const int vpr = a.H / VN, rows = min(16, n_rows - j0);
+    for (int v = tid; v < rows * vpr; v += 1024) {
+        const int q = v / vpr;
+        const int64_t at = (int64_t)(j0 + q) * a.H + (v - q * vpr) * VN;
+        float o[VN];
+        Vec<T>::load((const T*)a.x + at, o);
+#pragma unroll
+        for (int e = 0; e < VN; ++e) o[e] = a.y[j0 + q] < 0 ? 0.f : o[e] * fac[q];
+        Vec<T>::store((T*)xs + at, o);
+    }
+}
+
+// ---- 4. products of a piece --------------------------------------------------------------------------------
+
+// dx: e [n, K] times the piece's rows of the table [K, H], in `parts` parts of the contraction, each into a slot [n, H] of its own, which the first piece writes
+// and the others add to.
+struct LeaveSlots {
+    static constexpr bool OWN = true, LDA = true;
+    float* slot;
+    bool first;
+    template <int TM, int TN>
+    __device__ __forceinline__ void operator()(f32x4_t (&acc)[2 * TM][2 * TN], const TileRef& t, unsigned char*, int wm, int wn) const {
+        constexpr int FM = 2 * TM, FN = 2 * TN;
+        int ln = threadIdx.x & 63;
+        asm volatile("" : "+v"(ln));
+        const int mw = t.m0 + wm * (32 * TM), n = t.n0 + wn * (32 * TN) + 4 * (ln >> 4);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int m = mw + i * 16 + (ln & 15);
+            if (m >= t.M) continue;
+            float* p = slot + (int64_t)m * t.N + n;
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                if (n + j * 16 >= t.N) continue;
+                float4 o = make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
+                if (!first) {
+                    const float4 b = *reinterpret_cast<const float4*>(p + j * 16);
+                    o.x += b.x; o.y += b.y; o.z += b.z; o.w += b.w;
+                }
+                *reinterpret_cast<float4*>(p + j * 16) = o;
+            }
+        }
+    }
+};
+struct DxArgs {
+    const void *e, *table;      // the piece's rows of the table
+    int lde, K, H, n_max;
+    const int32_t* n_dev;
+    float* slots;
+    int parts, tile;            // 256 or 128
+    bool first;
+};
+__global__ __launch_bounds__(256) void head_dx_kernel(DxArgs a) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int rows = __builtin_amdgcn_readfirstlane(live_rows(a.n_max, a.n_dev));
+    const int tm = (rows + a.tile - 1) / a.tile, tn = (a.H + a.tile - 1) / a.tile, tiles = tm * tn, items = tiles * a.parts;
+    const int pairs = (a.K + 63) / 64, per = (pairs + a.parts - 1) / a.parts;
+    GemmArgs g;
+    g.A[0] = a.e; g.B[0] = a.table; g.K[0] = a.K; g.nseg = 1; g.C = nullptr; g.M = rows; g.N = a.H; g.alpha = 1.f; g.beta = 0.f;
+    g.a_idx = nullptr; g.a_rows = 0; g.n_dev = nullptr; g.lda = a.lde;
+    auto none = [](TileRef&) { return false; };
+    for (int w = blockIdx.x; w < items; w += gridDim.x) {
+        const int l = xcd_order(w, items);
+        const int part = __builtin_amdgcn_readfirstlane(l / tiles);
+        int bm, bn;
+        tile_coords(l - part * tiles, tm, tn, bm, bn);
+        TileRef t{__builtin_amdgcn_readfirstlane(bm * a.tile), __builtin_amdgcn_readfirstlane(bn * a.tile), rows, a.H, uniform_ptr(a.e),
+                  uniform_ptr(a.table), nullptr};
+        const LeaveSlots leave{a.slots + (int64_t)part * a.n_max * a.H, a.first};
+        const int pbeg = min(pairs, part * per), pend = min(pairs, pbeg + per);
+        if (a.tile == 256) gemm_tiles<2, 4, 4, true, false>(g, a.K, t, none, smem, pbeg, pend, nullptr, leave);
+        else gemm_tiles<2, 2, 2, true, false>(g, a.K, t, none, smem, pbeg, pend, nullptr, leave);
+        wait_vmcnt<0>();
+        lds_barrier();
+    }
+}
+
+// the table's gradient: e^T x' over the live rows, bf16 written or fp32 added to
+struct WideA : Product {
+    static constexpr bool LDA = true;
+};
+struct DtableArgs {
+    const void *e, *xs;
+    void* out;                  // the piece's rows of the gradient
+    int lde, K, H, n_max;       // K: the piece's rows
+    const int32_t* n_dev;
+    int n_full, sub;
+};
+template <bool CF32> __global__ __launch_bounds__(256) void head_dtable_kernel(DtableArgs a) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int rows = __builtin_amdgcn_readfirstlane(live_rows(a.n_max, a.n_dev));
+    const int tm = (a.K + 255) / 256, tn = (a.H + 255) / 256;
+    GemmArgs g;
+    g.A[0] = a.e; g.B[0] = a.xs; g.K[0] = rows; g.nseg = 1; g.C = a.out; g.M = a.K; g.N = a.H; g.alpha = 1.f; g.beta = 0.f;
+    g.a_idx = nullptr; g.a_rows = 0; g.n_dev = nullptr; g.lda = a.lde;
+    gemm_items<1, CF32, WideA>(g, rows, tm * tn, a.n_full, a.sub, (int)gridDim.x, [&](int l, TileRef& t, int& bm, int& bn) __attribute__((always_inline)) {
+        t = TileRef{0, 0, a.K, a.H, a.e, a.xs, a.out};
+        tile_coords(l, tm, tn, bm, bn);
+    }, smem);
+}
+
+// ---- 5. dx -------------------------------------------------------------------------------------------------
+
+template <typename T>
+__global__ __launch_bounds__(256) void head_dx_sum_kernel(const float* __restrict__ slots, int parts, const float* __restrict__ fac,
+                                                          const int32_t* __restrict__ y, int n_max, const int32_t* __restrict__ n_dev, int H,
+                                                          T* __restrict__ dx) {
+    constexpr int VN = Vec<T>::N;
+    const int n_rows = live_rows(n_max, n_dev), vpr = H / VN;
+    const int64_t total = (int64_t)n_rows * vpr, slot = (int64_t)n_max * H;
+    for (int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x; v < total; v += (int64_t)gridDim.x * 256) {
+        const int j = (int)(v / vpr);
+        const float* p = slots + v * VN;
+        float s[VN];
+#pragma unroll
+        for (int e = 0; e < VN; ++e) s[e] = 0.f;
+        for (int k = 0; k < parts; ++k, p += slot) {
+#pragma unroll
+            for (int q = 0; q < VN / 4; ++q) {
+                const float4 w = reinterpret_cast<const float4*>(p)[q];
+                s[4 * q] += w.x; s[4 * q + 1] += w.y; s[4 * q + 2] += w.z; s[4 * q + 3] += w.w;
+            }
+        }
+        const float f = fac[j];
+        const bool live = y[j] >= 0;
+#pragma unroll
+        for (int e = 0; e < VN; ++e) s[e] = live ? f * s[e] : 0.f;
+        Vec<T>::store(dx + v * VN, s);
+    }
+}
+
+// ---- fp32 --------------------------------------------------------------------------------------------------
+// The same steps with the fp32 matrix instruction (32x32x2, 256 flop a cycle and CU): 128x128 tiles, four waves of 64x64, steps of 16 through two LDS stages laid
+// out [k][row], the next step's operands on their way in registers.  Operands as for the bf16 products: MODE 0 A and B with k contiguous, 1 both k-major,
+// 2 A contiguous, B k-major.  D = B-frag x A-frag: lane l holds row l % 32 and, in register v, column 8 * (v / 4) + 4 * (l / 32) + v % 4 of a fragment.
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16_t;
+constexpr int F32_STEP = 16, F32_LD = 132;
+
+struct F32Tile {
+    const float *A, *B;
+    int64_t lda, ldb;
+    int M, N;               // rows and columns that exist (MODE 1: of A's and B's columns)
+    int k0, k1;             // the contraction's range
+    int m0, n0;
+};
+template <int MODE>
+__device__ __forceinline__ void f32_tile(const F32Tile& t, float (&As)[2][F32_STEP][F32_LD], float (&Bs)[2][F32_STEP][F32_LD], f32x16_t (&acc)[2][2]) {
+    constexpr bool AK = MODE != 1, BK = MODE == 0;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
+    float4 ra[2], rb[2];
+    // rows (k contiguous): two of 64 rows apart, four k each; k-major: two of 8 k apart, four columns each
+    auto fetch = [&](float4 (&r)[2], const float* p, int64_t ld, int base, int lim, int k, bool kc) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            r[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (kc) {
+                const int row = base + (tid >> 2) + 64 * i, kk = k + (tid & 3) * 4;
+                if (row < lim && kk < t.k1) r[i] = *reinterpret_cast<const float4*>(p + (int64_t)row * ld + kk);
+            } else {
+                const int kk = k + (tid >> 5) + 8 * i, col = base + (tid & 31) * 4;
+                if (col < lim && kk < t.k1) r[i] = *reinterpret_cast<const float4*>(p + (int64_t)kk * ld + col);
+            }
+        }
+    };
+    auto put = [&](const float4 (&r)[2], float (&s)[F32_STEP][F32_LD], bool kc) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (kc) {
+                const int row = (tid >> 2) + 64 * i, kk = (tid & 3) * 4;
+                s[kk][row] = r[i].x; s[kk + 1][row] = r[i].y; s[kk + 2][row] = r[i].z; s[kk + 3][row] = r[i].w;
+            } else {
+                *reinterpret_cast<float4*>(&s[(tid >> 5) + 8 * i][(tid & 31) * 4]) = r[i];
+            }
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+    if (t.k0 >= t.k1) return;
+    fetch(ra, t.A, t.lda, t.m0, t.M, t.k0, AK);
+    fetch(rb, t.B, t.ldb, t.n0, t.N, t.k0, BK);
+    int st = 0;
+    put(ra, As[0], AK);
+    put(rb, Bs[0], BK);
+    __syncthreads();
+    for (int k = t.k0; k < t.k1; k += F32_STEP, st ^= 1) {
+        const bool more = k + F32_STEP < t.k1;
+        if (more) {
+            fetch(ra, t.A, t.lda, t.m0, t.M, k + F32_STEP, AK);
+            fetch(rb, t.B, t.ldb, t.n0, t.N, k + F32_STEP, BK);
+        }
+#pragma unroll
+        for (int kk = 0; kk < F32_STEP; kk += 2) {
+            float fa[2], fb[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                fa[i] = As[st][kk + (lane >> 5)][wm * 64 + i * 32 + (lane & 31)];
+                fb[i] = Bs[st][kk + (lane >> 5)][wn * 64 + i * 32 + (lane & 31)];
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(fb[j], fa[i], acc[i][j], 0, 0, 0);
+        }
+        if (more) {
+            put(ra, As[st ^ 1], AK);
+            put(rb, Bs[st ^ 1], BK);
+        }
+        __syncthreads();
+    }
+}
+
+template <int KIND> __global__ __launch_bounds__(256) void head_logits_f32_kernel(HeadArgs a) {
+    __shared__ __align__(16) float As[2][F32_STEP][F32_LD], Bs[2][F32_STEP][F32_LD];
+    if (a.flagged_only && a.flags[0] == 0) return;
+    const int rows = live_rows(a.n_max, a.n_dev), tm = (rows + 127) / 128, tn = (a.c1 - a.c0 + 127) / 128;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, hi = lane >> 5;
+    for (int64_t w = blockIdx.x; w < (int64_t)tm * tn; w += gridDim.x) {
+        const int bm = (int)(w % tm), m0 = bm * 128, n0 = a.c0 + (int)(w / tm) * 128;
+        if (a.flagged_only && a.flags[1 + (m0 >> 8)] == 0) continue;
+        const F32Tile t{(const float*)a.x, (const float*)a.table, a.H, a.H, rows, min(a.c1, a.V), 0, a.H, m0, n0};
+        f32x16_t acc[2][2];
+        f32_tile<0>(t, As, Bs, acc);
+        const int c = n0 + wn * 64;             // a strip
+        const bool store = KIND != MAXIMA && n0 < a.store_end;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int m = m0 + wm * 64 + i * 32 + (lane & 31);
+            const float ref = m < rows ? a.ref[m] : INFINITY;
+            const bool dead = ref == INFINITY;
+            float s = 0.f, mx = -INFINITY, ey = 0.f;
+            int y = -1;
+            if (KIND == VALUES && m < rows) { y = a.y[m]; ey = a.ey[m]; }
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    if (c + j * 32 + 8 * (v >> 2) + 4 * hi + (v & 3) >= a.V) acc[i][j][v] = -INFINITY;
+                    mx = fmaxf(mx, acc[i][j][v]);
+                }
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * a.k;
+            const float r = KIND == MAXIMA ? (mx == -INFINITY ? 0.f : mx) : ref;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int col = c + j * 32 + 8 * q + 4 * hi;
+                    float e[4];
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        e[v] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][4 * q + v], a.k, -r));
+                        s += e[v];
+                        if (KIND == VALUES && col + v == y) e[v] = ey;
+                        if (dead) e[v] = 0.f;
+                    }
+                    if (store && m < rows && col - a.c0 < a.lde)
+                        *reinterpret_cast<float4*>((float*)a.e + (int64_t)m * a.lde + (col - a.c0)) = make_float4(e[0], e[1], e[2], e[3]);
+                }
+            if (KIND != VALUES) {
+                s += __shfl_xor(s, 32, 64);
+                if (hi == 0 && m < rows && c < a.V) {
+                    a.sums[(int64_t)(c / STRIP) * a.ldn + m] = KIND == MAXIMA ? mx + log2f(s) : s;
+                    if (KIND == SUMS && !dead && !(s <= FLAG_ABOVE)) a.flags[0] = a.flags[1 + (m >> 8)] = 1;
+                }
+            }
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void head_dx_f32_kernel(DxArgs a) {
+    __shared__ __align__(16) float As[2][F32_STEP][F32_LD], Bs[2][F32_STEP][F32_LD];
+    const int rows = live_rows(a.n_max, a.n_dev), tm = (rows + 127) / 128, tn = (a.H + 127) / 128, tiles = tm * tn, items = tiles * a.parts;
+    const int steps = (a.K + F32_STEP - 1) / F32_STEP, per = (steps + a.parts - 1) / a.parts;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
+    for (int w = blockIdx.x; w < items; w += gridDim.x) {
+        const int part = w / tiles, l = w - part * tiles, m0 = (l % tm) * 128, n0 = (l / tm) * 128;
+        const F32Tile t{(const float*)a.e, (const float*)a.table, a.lde, a.H, rows, a.H, min(steps, part * per) * F32_STEP,
+                        min(a.K, min(steps, part * per + per) * F32_STEP), m0, n0};
+        f32x16_t acc[2][2];
+        f32_tile<2>(t, As, Bs, acc);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int m = m0 + wm * 64 + i * 32 + (lane & 31);
+            if (m >= rows) continue;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int n = n0 + wn * 64 + j * 32 + 8 * q + 4 * (lane >> 5);
+                    if (n >= a.H) continue;
+                    float4* p = reinterpret_cast<float4*>(a.slots + ((int64_t)part * a.n_max + m) * a.H + n);
+                    float4 o = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+                    if (!a.first) {
+                        const float4 b = *p;
+                        o.x += b.x; o.y += b.y; o.z += b.z; o.w += b.w;
+                    }
+                    *p = o;
+                }
+        }
+    }
+}
+
+template <bool MAIN> __global__ __launch_bounds__(256) void head_dtable_f32_kernel(DtableArgs a) {
+    __shared__ __align__(16) float As[2][F32_STEP][F32_LD], Bs[2][F32_STEP][F32_LD];
+    const int rows = live_rows(a.n_max, a.n_dev), tm = (a.K + 127) / 128, tn = (a.H + 127) / 128;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
+    for (int64_t w = blockIdx.x; w < (int64_t)tm * tn; w += gridDim.x) {
+        const int m0 = (int)(w / tn) * 128, n0 = (int)(w % tn) * 128;
+        const F32Tile t{(const float*)a.e, (const float*)a.xs, a.lde, a.H, a.lde, a.H, 0, rows, m0, n0};
+        f32x16_t acc[2][2];
+        f32_tile<1>(t, As, Bs, acc);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int m = m0 + wm * 64 + i * 32 + (lane & 31);
+            if (m >= a.K) continue;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int n = n0 + wn * 64 + j * 32 + 8 * q + 4 * (lane >> 5);
+                    if (n >= a.H) continue;
+                    float4* p = reinterpret_cast<float4*>((float*)a.out + (int64_t)m * a.H + n);
+                    float4 o = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+                    if (MAIN) {
+                        const float4 b = *p;
+                        o.x += b.x; o.y += b.y; o.z += b.z; o.w += b.w;
+                    }
+                    *p = o;
+                }
+        }
+    }
+}
+
+// ---- workspace and launches --------------------------------------------------------------------------------
+
+// Parts of dx's contraction over the vocabulary: the fewest rounds of the CUs per part, a part and its slot costing a hundredth of a whole contraction.
+static int dx_parts(int64_t tiles, int V, int n_cu) {
+    int best = 1;
+    double least = 1e30;
+    for (int s = 1; s <= 16 && (s == 1 || (int64_t)V >= (int64_t)s * 512); ++s) {
+        const double cost = (double)((tiles * s + n_cu - 1) / n_cu) / s + 0.01 * s;
+        if (cost < least - 1e-9) { least = cost; best = s; }
+    }
+    return best;
+}
+
+struct HeadWs {
+    int strips, ldn, tile, parts, cap;          // cap: columns of e (0: too little room, or no gradient)
+    size_t ref, a, ey, y, terms, flags, sums, xs, slots, e, total;
+    HeadWs(int V, int H, int n_rows, int dtype, bool need_dx, bool need_dt, size_t bytes) {
+        const int n = n_rows > 0 ? n_rows : 1;
+        const size_t es = dtype_size(dtype);
+        strips = ceil_div(V, STRIP);
+        ldn = (int)align_up((size_t)n, 16);
+        size_t at = 0;
+        auto take = [&](size_t b) { const size_t p = at; at += align_up(b, 256); return p; };
+        ref = take((size_t)n * 4);
+        a = take((size_t)n * 4);
+        ey = take((size_t)n * 4);
+        y = take((size_t)n * 4);
+        terms = take((size_t)n * 16);
+        flags = take((size_t)(ceil_div(n, 256) + 1) * 4);
+        sums = take((size_t)strips * ldn * 4);
+        xs = take(need_dt ? (size_t)n * H * es : 0);
+        tile = dtype == CF_F32 || n <= 128 ? 128 : 256;
+        parts = need_dx ? dx_parts((int64_t)ceil_div(n, tile) * ceil_div(H, tile), V, compute_units()) : 0;
+        slots = take((size_t)parts * n * H * 4);
+        e = at;
+        cap = 0;
+        total = at;
+        if (!need_dx && !need_dt) return;
+        int64_t whole = (int64_t)align_up((size_t)V, 256), least = std::min<int64_t>(whole, 2048), most = whole;
+        if (dtype == CF_BF16) {     // matrices below 2 GiB: 32-bit offsets
+            const int64_t lim = ((int64_t)1 << 31) - 1;
+            most = std::min({most, lim / (2 * std::max<int64_t>(n, 256)) / 256 * 256, (lim / (2 * (int64_t)H) - 256) / 256 * 256});
+            least = std::min(least, most);
+        }
+        if (most < 256) { cap = -1; return; }
+        int64_t c = bytes > at ? (int64_t)((bytes - at) / ((size_t)n * es)) / 256 * 256 : 0;
+        cap = (int)std::max(least, std::min(most, c));
+        total = at + align_up((size_t)n * cap * es, 256);
+    }
+};
+
+template <typename T> struct HeadLaunch;
+template <> struct HeadLaunch<bf16_t> {
+    template <int KIND> static hipError_t logits(const HeadArgs& a, hipStream_t st) {
+        static std::atomic<uint64_t> lds_ok{0};
+        const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&head_logits_kernel<KIND>), GEMM_SMEM, lds_ok);
+        if (e != hipSuccess) return e;
+        head_logits_kernel<KIND><<<compute_units(), 256, GEMM_SMEM, st>>>(a);
+        return hipGetLastError();
+    }
+    static hipError_t dx(const DxArgs& a, hipStream_t st) {
+        static std::atomic<uint64_t> lds_ok{0};
+        const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&head_dx_kernel), GEMM_SMEM, lds_ok);
+        if (e != hipSuccess) return e;
+        const int64_t items = (int64_t)ceil_div(a.n_max, a.tile) * ceil_div(a.H, a.tile) * a.parts;
+        head_dx_kernel<<<(int)std::min<int64_t>(items, compute_units()), 256, GEMM_SMEM, st>>>(a);
+        return hipGetLastError();
+    }
+    static hipError_t dtable(DtableArgs a, bool main, hipStream_t st) {
+        static std::atomic<uint64_t> lds_ok[2];
+        void (*const kernel)(DtableArgs) = main ? head_dtable_kernel<true> : head_dtable_kernel<false>;
+        const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), GEMM_SMEM, lds_ok[main]);
+        if (e != hipSuccess) return e;
+        const int tiles = ceil_div(a.K, 256) * ceil_div(a.H, 256);
+        plan_tiles(tiles, compute_units(), a.n_full, a.sub);
+        kernel<<<std::min(a.n_full + (tiles - a.n_full) * a.sub, compute_units()), 256, GEMM_SMEM, st>>>(a);
+        return hipGetLastError();
+    }
+};
+template <> struct HeadLaunch<float> {
+    static int grid(int64_t items) { return (int)std::min<int64_t>(items, 2 * compute_units()); }
+    template <int KIND> static hipError_t logits(const HeadArgs& a, hipStream_t st) {
+        head_logits_f32_kernel<KIND><<<grid((int64_t)ceil_div(a.n_max, 128) * ceil_div(a.c1 - a.c0, 128)), 256, 0, st>>>(a);
+        return hipGetLastError();
+    }
+    static hipError_t dx(const DxArgs& a, hipStream_t st) {
+        head_dx_f32_kernel<<<grid((int64_t)ceil_div(a.n_max, 128) * ceil_div(a.H, 128) * a.parts), 256, 0, st>>>(a);
+        return hipGetLastError();
+    }
+    static hipError_t dtable(const DtableArgs& a, bool main, hipStream_t st) {
+        const int g = grid((int64_t)ceil_div(a.K, 128) * ceil_div(a.H, 128));
+        if (main) head_dtable_f32_kernel<true><<<g, 256, 0, st>>>(a);
+        else head_dtable_f32_kernel<false><<<g, 256, 0, st>>>(a);
+        return hipGetLastError();
+    }
+};
+
+#define CF_TRY(call)                            \
+    do {                                        \
+        const hipError_t e_ = (call);           \
+        if (e_ != hipSuccess) return e_;        \
+    } while (0)
+
+template <typename T>
+static hipError_t launch_head(HeadArgs a, LossArgs l, const HeadWs& L, unsigned char* ws, void* dx, void* dtable, bool main, float* stats, hipStream_t st) {
+    const int n = a.n_max, V = a.V, H = a.H;
+    if (n > 0) {
+        const bool grads = dx != nullptr || dtable != nullptr;
+        a.ref = (float*)(ws + L.ref);
+        a.a = (float*)(ws + L.a);
+        a.ey = (float*)(ws + L.ey);
+        a.y = (int32_t*)(ws + L.y);
+        a.flags = (int32_t*)(ws + L.flags);
+        a.sums = (float*)(ws + L.sums);
+        a.ldn = L.ldn;
+        l.terms = (float4*)(ws + L.terms);
+        void* xs = dtable != nullptr ? ws + L.xs : nullptr;
+        const int first = std::min(V, L.cap);           // columns whose exponentials are kept
+        a.c0 = 0; a.c1 = V; a.lde = (int)align_up((size_t)first, 8); a.store_end = grads ? first : 0; a.e = grads ? ws + L.e : nullptr;
+        a.flagged_only = false;
+        const int blocks = ceil_div(n, 4);
+        head_rows_kernel<T><<<std::min(blocks, 8 * compute_units()), 256, 0, st>>>(a, l);
+        CF_TRY(hipGetLastError());
+        CF_TRY(HeadLaunch<T>::template logits<SUMS>(a, st));
+        a.flagged_only = true;
+        CF_TRY(HeadLaunch<T>::template logits<MAXIMA>(a, st));
+        head_finish_kernel<T><<<ceil_div(n, 16), 1024, 0, st>>>(a, l, xs);
+        CF_TRY(hipGetLastError());
+        for (int c = 0; grads && c < V; c += L.cap) {
+            const int w = std::min(L.cap, V - c);
+            a.c0 = c; a.c1 = c + w; a.lde = (int)align_up((size_t)w, 8); a.store_end = c + w; a.flagged_only = c == 0;
+            CF_TRY(HeadLaunch<T>::template logits<VALUES>(a, st));
+            if (dx != nullptr)
+                CF_TRY(HeadLaunch<T>::dx(DxArgs{a.e, (const T*)a.table + (int64_t)c * H, a.lde, w, H, n, a.n_dev, (float*)(ws + L.slots), L.parts, L.tile, c == 0}, st));
+            if (dtable != nullptr)
+                CF_TRY(HeadLaunch<T>::dtable(DtableArgs{a.e, xs, (char*)dtable + (int64_t)c * H * (main ? 4 : (int)sizeof(T)), a.lde, w, H, n, a.n_dev, 0, 1}, main, st));
+        }
+        if (dx != nullptr) {
+            const int64_t vecs = (int64_t)n * (H / Vec<T>::N);
+            head_dx_sum_kernel<T><<<(int)std::min<int64_t>((vecs + 255) / 256, 32 * compute_units()), 256, 0, st>>>(
+                (const float*)(ws + L.slots), L.parts, a.a, a.y, n, a.n_dev, H, (T*)dx);
+            CF_TRY(hipGetLastError());
+        }
+    } else if (dtable != nullptr && !main) {
+        CF_TRY(launch_fill_zero(dtable, (size_t)V * H * sizeof(T), st));
+    }
+    if (stats != nullptr) launch_loss_stats((const float4*)(ws + L.terms), n, a.n_dev, l.norm, stats, st);
+    return hipGetLastError();
+}
+
+}  // namespace cf
+
+using namespace cf;
+
+static cf_status head_sizes(const cf_loss_desc* d, int32_t H, int32_t max_kept) {
+    if (!d) return CF_ERR_NULL;
+    if (d->dtype != CF_BF16 && d->dtype != CF_F32) return CF_ERR_DTYPE;
+    if (d->V <= 0 || d->V > (1 << 30) || H <= 0 || H % (d->dtype == CF_F32 ? 4 : 8) != 0 || max_kept < 0 || max_kept > (1 << 30)) return CF_ERR_SHAPE;
+    if (H > (1 << 20)) return CF_ERR_UNSUPPORTED;
+    if (d->dtype == CF_BF16 && (int64_t)max_kept * H * 2 >= ((int64_t)1 << 31)) return CF_ERR_UNSUPPORTED;
+    return CF_OK;
+}
+
+static bool ranges_meet(const void* a, uint64_t an, const void* b, uint64_t bn) {
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return a && b && an && bn && x < y + bn && y < x + an;
+}
+
+extern "C" {
+
+size_t cf_head_loss_workspace_bytes(const cf_loss_desc* desc, int32_t H, int32_t max_kept, int32_t need_dx, int32_t need_dtable, size_t limit) {
+    if (head_sizes(desc, H, max_kept) != CF_OK) return 0;
+    const HeadWs L(desc->V, H, max_kept, desc->dtype, need_dx != 0, need_dtable != 0, limit);
+    return L.cap < 0 ? 0 : L.total;
+}
+
+cf_status cf_head_loss(const cf_loss_desc* desc, int32_t H, const void* x_kept, const void* table, const int64_t* targets, const float* old_logp,
+                       const float* ref_logp, const float* advantages, const float* weights, const int32_t* idx, const int32_t* n_kept_dev,
+                       int32_t max_kept, void* dx_kept, void* dtable, int32_t main_grad, float* logp, float* stats, void* ws, size_t ws_bytes,
+                       cf_stream stream) {
+    if (!desc || !x_kept || !table || !targets) return CF_ERR_NULL;
+    if (!dx_kept && !dtable && !logp && !stats) return CF_ERR_NULL;
+    cf_status ok = loss_desc_check(desc, old_logp, ref_logp, advantages, max_kept);
+    if (ok == CF_OK) ok = head_sizes(desc, H, max_kept);
+    if (ok != CF_OK) return ok;
+    if (main_grad != 0 && main_grad != 1) return CF_ERR_SHAPE;
+    const auto off = [](const void* p, size_t a) { return (uintptr_t)p % a != 0; };
+    if (off(x_kept, 16) || off(table, 16) || off(dx_kept, 16) || off(dtable, 16) || off(targets, 8)) return CF_ERR_SHAPE;
+    for (const void* p : {(const void*)old_logp, (const void*)ref_logp, (const void*)advantages, (const void*)weights, (const void*)idx,
+                          (const void*)n_kept_dev, (const void*)logp, (const void*)stats})
+        if (off(p, 4)) return CF_ERR_SHAPE;
+    const uint64_t es = dtype_size(desc->dtype), xb = (uint64_t)max_kept * H * es, tb = (uint64_t)desc->V * H * es;
+    const uint64_t db = (uint64_t)desc->V * H * (main_grad ? 4 : es);
+    if ((dx_kept != x_kept && ranges_meet(dx_kept, xb, x_kept, xb)) || ranges_meet(dx_kept, xb, table, tb) || ranges_meet(dtable, db, table, tb) ||
+        ranges_meet(dtable, db, x_kept, xb) || ranges_meet(dtable, db, dx_kept, xb))
+        return CF_ERR_SHAPE;
+    const HeadWs L(desc->V, H, max_kept, desc->dtype, dx_kept != nullptr, dtable != nullptr, ws_bytes);
+    if (L.cap < 0) return CF_ERR_UNSUPPORTED;
+    if (!ws || off(ws, 256) || ws_bytes < L.total) return CF_ERR_WORKSPACE;
+    const LossArgs l = loss_args(desc, targets, old_logp, ref_logp, advantages, weights, idx, n_kept_dev, max_kept, logp);
+    HeadArgs a{};
+    a.x = x_kept; a.table = table; a.H = H; a.V = desc->V; a.n_max = max_kept; a.n_dev = n_kept_dev; a.k = l.k;
+    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    unsigned char* w = (unsigned char*)ws;
+    const hipError_t e = desc->dtype == CF_F32 ? launch_head<float>(a, l, L, w, dx_kept, dtable, main_grad != 0, stats, st)
+                                               : launch_head<bf16_t>(a, l, L, w, dx_kept, dtable, main_grad != 0, stats, st);
+    return e == hipSuccess ? CF_OK : CF_ERR_HIP;
+}
+
+}  // extern "C"

@@ -4,6 +4,7 @@
 #include <math.h>
 
 #include "common.h"
+#include "loss_row.h"
 
 namespace cf {
 
@@ -33,29 +34,6 @@ template <typename T> __device__ __forceinline__ T one_from_f32(float v);
 template <> __device__ __forceinline__ float one_from_f32<float>(float v) { return v; }
 template <> __device__ __forceinline__ bf16_t one_from_f32<bf16_t>(float v) { return (bf16_t)pack_bf16x2(v, 0.f); }     // NaN stays NaN
 
-struct LossArgs {
-    const void* logits;
-    int64_t stride;
-    const int64_t* targets;
-    const float *old_logp, *ref_logp, *adv, *weights;
-    const int32_t *idx, *n_dev;
-    int n_max, V;
-    int first;              // row of the launch's first block
-    float scale, k, klo;        // of the logits; times log2(e), and what rounding that left
-    bool policy;
-    float lo, hi, kl_coef;      // bounds of the ratio
-    float norm;                 // 0: the number of live rows
-    void* dlogits;
-    int64_t dstride;
-    float *logp;
-    float4* terms;              // per live row, times its weight: loss, its first term, k, clipped or not
-};
-
-// What a row's log probability gives: the terms, and w/norm * dL/dlp
-struct RowLoss {
-    float4 terms;
-    float coef;
-};
 // What a block knows of a row apart from its logits.  The same for all its threads, which the compiler cannot know of what it loads:
 // these go through the scalar path, apart from the vectors in flight (nothing in them is written during the kernel before it is read).
 template <typename U> __device__ __forceinline__ U scalar_load(const U* p) {
@@ -68,12 +46,6 @@ template <> __device__ __forceinline__ float scalar_load_f32<bf16_t>(const void*
     const unsigned u = scalar_load((const unsigned*)(at & ~(uintptr_t)3));
     return __uint_as_float((at & 2) ? u & 0xFFFF0000u : u << 16);
 }
-struct RowHead {
-    int row, y;             // y: -1 for a row that is left out
-    const void* l;
-    float w, ly, old, ref, adv;
-    __device__ __forceinline__ bool live() const { return y >= 0; }
-};
 template <typename T> __device__ __forceinline__ void find_row(const LossArgs& a, int j, RowHead& r) {
     r.row = a.idx != nullptr ? scalar_load(a.idx + j) : j;
     r.l = (const T*)a.logits + (int64_t)r.row * a.stride;
@@ -90,26 +62,6 @@ template <typename T> __device__ __forceinline__ void load_head(const LossArgs& 
     r.y = y >= 0 && y < a.V && r.w != 0.f ? (int)y : -1;
     r.ly = scalar_load_f32<T>(r.l, r.y < 0 ? 0 : r.y);
 }
-__device__ __forceinline__ RowLoss row_loss(const LossArgs& a, const RowHead& h, float lp, float inv_norm) {
-    const float w = h.w;
-    if (!a.policy) return RowLoss{make_float4(-w * lp, -w * lp, 0.f, 0.f), -w * inv_norm};
-    // A ratio beyond fp32 counts for nothing without an advantage, and a divergence beyond it for nothing without a coefficient: neither makes 0 * inf
-    const float A = h.adv, r = expf(lp - h.old), rA = A == 0.f && r == r ? 0.f : r * A;
-    const float rc = fminf(fmaxf(r, a.lo), a.hi);
-    const bool clipped = rA > rc * A;
-    const float first = clipped ? -rc * A : -rA;
-    float d = clipped ? 0.f : -rA, k = 0.f, kl = 0.f;
-    if (a.ref_logp != nullptr) {
-        const float q = h.ref - lp, e = expm1f(q);          // exp(q) - 1 as such: k is the small rest of it
-        k = e < INFINITY ? e - q : e;
-        if (a.kl_coef != 0.f) {
-            kl = a.kl_coef * k;
-            d -= a.kl_coef * e;
-        }
-    }
-    return RowLoss{make_float4(w * (first + kl), w * first, w * k, clipped ? w : 0.f), w * inv_norm * d};
-}
-
 // One exponential of a softmax, 2^(k*(x - m)).  For fp32 logits (EXACT) the roundings of k*(x - m) and of k itself, up to 2^-19 of a small
 // probability, are carried along and multiplied in; a bf16 gradient has 2^-8.
 struct Expo {
@@ -423,6 +375,10 @@ __global__ __launch_bounds__(1024) void loss_stats_kernel(const float4* __restri
     }
 }
 
+void launch_loss_stats(const float4* terms, int n_max, const int32_t* n_dev, float norm, float* stats, hipStream_t st) {
+    loss_stats_kernel<<<1, 1024, 0, st>>>(terms, n_max, n_dev, norm, stats);
+}
+
 template <typename T, int NT, int NV> static void launch_rows(const LossArgs& a, hipStream_t st) {
     const int resident = compute_units() * (1024 / NT) * (NV <= 4 ? 2 : 1), grid = a.n_max < resident ? a.n_max : resident;
     if (a.dlogits == nullptr) { token_loss_kernel<T, NT, NV, 1, false><<<grid, NT, 0, st>>>(a); return; }
@@ -473,18 +429,8 @@ cf_status cf_token_loss(const cf_loss_desc* desc, const void* logits, int64_t lo
                         float* logp, float* stats, void* ws, size_t ws_bytes, cf_stream stream) {
     if (!desc || !logits || !targets) return CF_ERR_NULL;
     if (!dlogits && !logp && !stats) return CF_ERR_NULL;
-    if (desc->dtype != CF_BF16 && desc->dtype != CF_F32) return CF_ERR_DTYPE;
-    const bool policy = desc->kind == CF_LOSS_POLICY;
-    if (!policy && desc->kind != CF_LOSS_NLL) return CF_ERR_SHAPE;
-    if (policy && (!old_logp || !advantages)) return CF_ERR_NULL;
-    const float scale = desc->logit_scale == 0.f ? 1.f : desc->logit_scale;
-    const auto finite = [](float v) { return v - v == 0.f; };
-    if (desc->V <= 0 || desc->V > (1 << 30) || max_kept < 0 || max_kept > (1 << 30)) return CF_ERR_SHAPE;
-    const double k = (double)scale * 1.4426950408889634;
-    if (!(scale > 0.f) || !finite((float)k) || !finite(desc->norm)) return CF_ERR_SHAPE;
-    if (policy && (!(desc->clip_lo >= 0.f && desc->clip_lo <= 1.f) || !(desc->clip_hi >= 0.f) || !finite(desc->kl_coef) ||
-                   (!ref_logp && desc->kl_coef != 0.f)))
-        return CF_ERR_SHAPE;
+    const cf_status ok = loss_desc_check(desc, old_logp, ref_logp, advantages, max_kept);
+    if (ok != CF_OK) return ok;
     const int64_t ls = logits_stride ? logits_stride : desc->V, ds = dlogits_stride ? dlogits_stride : desc->V;
     if (ls < desc->V || (dlogits && ds < desc->V)) return CF_ERR_SHAPE;
     const size_t e = dtype_size(desc->dtype);
@@ -502,10 +448,12 @@ cf_status cf_token_loss(const cf_loss_desc* desc, const void* logits, int64_t lo
     }
     if (!ws || off(ws, 16) || ws_bytes < cf_token_loss_workspace_bytes(max_kept)) return CF_ERR_WORKSPACE;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    LossArgs a{logits, ls, targets, old_logp, ref_logp, advantages, weights, idx, n_kept_dev, max_kept, desc->V, 0, scale, (float)k, (float)(k - (float)k), policy,
-               1.f - desc->clip_lo, 1.f + desc->clip_hi, policy ? desc->kl_coef : 0.f, desc->norm, dlogits, ds, logp, (float4*)ws};
+    LossArgs a = loss_args(desc, targets, old_logp, ref_logp, advantages, weights, idx, n_kept_dev, max_kept, logp);
+    a.logits = logits; a.stride = ls;
+    a.dlogits = dlogits; a.dstride = ds;
+    a.terms = (float4*)ws;
     if (max_kept > 0) desc->dtype == CF_F32 ? launch_token_loss<float>(a, st) : launch_token_loss<bf16_t>(a, st);
-    if (stats) loss_stats_kernel<<<1, 1024, 0, st>>>((const float4*)ws, max_kept, n_kept_dev, desc->norm, stats);
+    if (stats) launch_loss_stats((const float4*)ws, max_kept, n_kept_dev, desc->norm, stats, st);
     return hipGetLastError() == hipSuccess ? CF_OK : CF_ERR_HIP;
 }
 
