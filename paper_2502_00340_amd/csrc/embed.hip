@@ -65,12 +65,16 @@ struct SortArgs {
     int64_t n_zero;
 };
 
+// block of blocks, of `threads`; as a rule a vector a thread: 8 tables of 169 MB in turn 29 us each, with loops over 4 vectors 32 (past the caches the same)
+__device__ __forceinline__ void clear_table(const SortArgs& a, int block, int blocks, int threads) {
+    const int64_t stride = (int64_t)blocks * threads;
+    for (int64_t i = (int64_t)block * threads + threadIdx.x; i < a.n_zero; i += stride) a.zero[i] = u32x4_t{0u, 0u, 0u, 0u};
+}
+
 __global__ __launch_bounds__(SORT_THREADS) void embed_sort_kernel(SortArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     if ((int)blockIdx.x >= a.spans) {
-        const int64_t stride = (int64_t)((int)gridDim.x - a.spans) * SORT_THREADS;
-        for (int64_t i = (int64_t)((int)blockIdx.x - a.spans) * SORT_THREADS + tid; i < a.n_zero; i += stride)
-            __builtin_nontemporal_store(u32x4_t{0u, 0u, 0u, 0u}, a.zero + i);
+        clear_table(a, (int)blockIdx.x - a.spans, (int)gridDim.x - a.spans, SORT_THREADS);
         return;
     }
     extern __shared__ __align__(16) unsigned char smem[];
@@ -171,6 +175,62 @@ __global__ __launch_bounds__(SORT_THREADS) void embed_sort_kernel(SortArgs a) {
     for (int i = tid; i < m; i += SORT_THREADS) {
         a.tok[first + i] = (int32_t)skey[i];
         a.row[first + i] = first + (int)sval[i];
+    }
+}
+
+// Up to a span the rows are put in order by counting instead, on all CUs in one launch: a row's place is the number of rows with a smaller token and of rows
+// ahead of it with the same one.  n^2 comparisons of keys in LDS; a wave takes a row.
+constexpr int RANK_ROWS = 16, RANK_THREADS = 64 * RANK_ROWS;
+
+__global__ __launch_bounds__(RANK_THREADS) void embed_rank_kernel(SortArgs a, int rank_blocks) {
+    __shared__ __align__(16) int key[SPAN];
+    const int tid = threadIdx.x;
+    if ((int)blockIdx.x >= rank_blocks) {
+        clear_table(a, (int)blockIdx.x - rank_blocks, (int)gridDim.x - rank_blocks, RANK_THREADS);
+        return;
+    }
+    const int n_rows = live_rows(a.n_max, a.n_dev), j0 = blockIdx.x * RANK_ROWS;
+    if (j0 >= n_rows) return;
+    const int padded = (n_rows + 255) & ~255;           // keys of rows that do not exist are larger than every token
+    constexpr int U = 4;
+    for (int i0 = tid; i0 < padded; i0 += U * RANK_THREADS) {
+        int at[U];
+        int64_t t[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = min(i0 + u * RANK_THREADS, n_rows - 1);
+            at[u] = a.idx != nullptr ? a.idx[i] : i;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) t[u] = a.tokens[at[u]];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * RANK_THREADS;
+            if (i < padded) key[i] = i >= n_rows ? INT32_MAX : t[u] >= 0 && t[u] < a.V ? (int)t[u] : a.V;
+        }
+    }
+    __syncthreads();
+    const int j = __builtin_amdgcn_readfirstlane(j0 + (tid >> 6)), lane = tid & 63;
+    if (j >= n_rows) return;
+    const int k = key[j], border = j & ~255;            // keys ahead of row j count up to k, those behind it below k
+    int rank = 0;
+    auto count = [&](int from, int to, int below) __attribute__((always_inline)) {
+#pragma unroll 4
+        for (int i = from + lane * 4; i < to; i += 256) {
+            const int4 v = *reinterpret_cast<const int4*>(&key[i]);
+            rank += (v.x < below) + (v.y < below) + (v.z < below) + (v.w < below);
+        }
+    };
+    count(0, border, k + 1);
+    count(border + 256, padded, k);
+    const int i = border + lane * 4;
+    const int4 v = *reinterpret_cast<const int4*>(&key[i]);
+    rank += (v.x < k + (i < j)) + (v.y < k + (i + 1 < j)) + (v.z < k + (i + 2 < j)) + (v.w < k + (i + 3 < j));
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) rank += __shfl_xor(rank, o, 64);
+    if (lane == 0) {
+        a.tok[rank] = k;
+        a.row[rank] = j;
     }
 }
 
@@ -298,59 +358,49 @@ __global__ __launch_bounds__(NT) void embed_sum_kernel(SumArgs a) {
     }
 }
 
-// The tokens whose rows reach over chunks.  An item is a chunk and 256 columns; it is live where a token begins in the chunk that goes on in the next one.
-// 16 waves take every 16th part each, in order, and are added up in order.
+// The tokens whose rows reach over chunks.  A wave takes a chunk and 256 columns; it has work where a token begins in the chunk that goes on in the next one.
+// Parts are added in order, 16 of them in flight.
 template <typename T, bool MAIN>
-__global__ __launch_bounds__(1024) void embed_join_kernel(SumArgs a) {
-    __shared__ float red[16][256];
-    __shared__ int list[1024];
-    __shared__ int n_list;
-    const int n_rows = live_rows(a.n_max, a.n_dev), chunks = (n_rows + CH - 1) / CH, tiles = (a.H + 255) / 256;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t items = (int64_t)(chunks - 1) * tiles;            // nothing goes on behind the last chunk
-    for (int64_t i0 = 0; (int64_t)blockIdx.x + i0 * gridDim.x < items; i0 += 1024) {
-        if (tid == 0) n_list = 0;
-        __syncthreads();
-        const int64_t it = (int64_t)blockIdx.x + (i0 + tid) * gridDim.x;
-        if (it < items) {
-            const int p1 = (int)(it / tiles) * CH + CH, t = a.tok[p1 - 1];
-            const bool live = t < a.V && t == a.tok[p1] && (p1 == CH || a.tok[p1 - CH - 1] != t);
-            if (live) list[atomicAdd(&n_list, 1)] = tid;            // their order does not matter: each is on its own
+__global__ __launch_bounds__(256) void embed_join_kernel(SumArgs a) {
+    const int n_rows = live_rows(a.n_max, a.n_dev), chunks = (n_rows + CH - 1) / CH, tiles = (a.H + 255) / 256, lane = threadIdx.x & 63;
+    const int64_t items = (int64_t)(chunks - 1) * tiles, stride = (int64_t)gridDim.x * 4;          // nothing goes on behind the last chunk
+    for (int64_t it = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); it < items; it += stride) {
+        const int chunk = (int)(it / tiles), p1 = chunk * CH + CH, c = (int)(it % tiles) * 256 + lane * 4;
+        // one load for what tells whether there is work, and, with the first 64 chunks behind this one, how much
+        const int t = a.tok[p1 - 1], before = a.tok[chunk > 0 ? p1 - CH - 1 : 0];
+        const int k0 = chunk + 1 + lane, ahead = a.tok[(k0 < chunks ? k0 : chunk + 1) * CH];
+        if (t >= a.V || (chunk > 0 && before == t)) continue;
+        uint64_t same = __ballot(k0 < chunks && ahead == t);
+        if ((same & 1) == 0) continue;
+        int parts = 1 + __popcll(same);                            // this chunk's and those of the chunks that begin with the token
+        for (int k = chunk + 65; same == ~0ull; k += 64) {
+            same = __ballot(k + lane < chunks && a.tok[(k + lane < chunks ? k + lane : 0) * CH] == t);
+            parts += __popcll(same);
         }
-        __syncthreads();
-        const int n = n_list;
-        for (int l = 0; l < n; ++l) {
-            const int64_t item = (int64_t)blockIdx.x + (i0 + list[l]) * gridDim.x;
-            const int chunk = (int)(item / tiles), c = (int)(item % tiles) * 256 + lane * 4, t = a.tok[chunk * CH + CH - 1];
-            int parts = 1;                                          // this chunk's and those of the chunks that begin with the token
-            for (int k0 = chunk + 1;; k0 += 1024) {
-                const int here = __syncthreads_count((int64_t)(k0 + tid) < chunks && a.tok[(k0 + tid) * CH] == t);
-                parts += here;
-                if (here < 1024) break;
-            }
-            float s[4] = {0.f, 0.f, 0.f, 0.f};
-            if (c < a.H) {
-#pragma unroll 4
-                for (int k = wave; k < parts; k += 16) {
-                    const float4 w = *reinterpret_cast<const float4*>(a.part + ((int64_t)(chunk + k) * 2 + (k == 0 ? 1 : 0)) * a.H + c);
-                    s[0] += w.x; s[1] += w.y; s[2] += w.z; s[3] += w.w;
-                }
-            }
+        if (c >= a.H) continue;
+        const int64_t at = (int64_t)t * a.H + c;
+        float4 old = make_float4(0.f, 0.f, 0.f, 0.f);
+        if constexpr (MAIN) old = *reinterpret_cast<const float4*>((const float*)a.out + at);
+        const float* p = a.part + (int64_t)chunk * 2 * a.H + c;
+        float4 s = *reinterpret_cast<const float4*>(p + a.H);
+        for (int k = 1; k < parts; k += 16) {
+            float4 w[16];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) red[wave][lane * 4 + e] = s[e];
-            __syncthreads();
-            if (tid < 256 && (c & ~255) + tid < a.H) {
-                const int col = (int)(item % tiles) * 256 + tid;
-                float sum = 0.f;
+            for (int u = 0; u < 16; ++u) w[u] = *reinterpret_cast<const float4*>(p + (int64_t)min(k + u, parts - 1) * 2 * a.H);
 #pragma unroll
-                for (int w = 0; w < 16; ++w) sum += red[w][tid];
-                const int64_t at = (int64_t)t * a.H + col;
-                if constexpr (MAIN) ((float*)a.out)[at] = fmaf(a.scale, sum, ((float*)a.out)[at]);
-                else ((T*)a.out)[at] = narrow_one<T>(a.scale * sum);
+            for (int u = 0; u < 16; ++u) {
+                const bool have = k + u < parts;
+                s.x += have ? w[u].x : 0.f; s.y += have ? w[u].y : 0.f; s.z += have ? w[u].z : 0.f; s.w += have ? w[u].w : 0.f;
             }
-            __syncthreads();
         }
-        __syncthreads();
+        if constexpr (MAIN) {
+            *reinterpret_cast<float4*>((float*)a.out + at) =
+                make_float4(fmaf(a.scale, s.x, old.x), fmaf(a.scale, s.y, old.y), fmaf(a.scale, s.z, old.z), fmaf(a.scale, s.w, old.w));
+        } else {
+            T* o = (T*)a.out + at;
+            o[0] = narrow_one<T>(a.scale * s.x); o[1] = narrow_one<T>(a.scale * s.y);
+            o[2] = narrow_one<T>(a.scale * s.z); o[3] = narrow_one<T>(a.scale * s.w);
+        }
     }
 }
 
@@ -376,12 +426,19 @@ static hipError_t launch_embed_bwd(SumArgs a, SortArgs so, unsigned char* ws, hi
         so.zero = (u32x4_t*)a.out;
         so.n_zero = (int64_t)a.V * a.H * (int64_t)sizeof(T) / 16;
     }
-    static std::atomic<uint64_t> lds_ok{0};
-    const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&embed_sort_kernel), SORT_LDS, lds_ok);
-    if (e != hipSuccess) return e;
-    const int64_t fill = MAIN ? 0 : (so.n_zero + 4 * SORT_THREADS - 1) / (4 * SORT_THREADS);
-    const int grid = so.spans + (int)(fill < 8 * compute_units() ? fill : 8 * compute_units());
-    if (grid > 0) embed_sort_kernel<<<grid, SORT_THREADS, SORT_LDS, st>>>(so);
+    const auto fill = [&](int threads) {        // blocks that clear the table beside those that put the rows in order
+        const int64_t blocks = MAIN ? 0 : (so.n_zero + threads - 1) / threads;
+        return (int)(blocks < MAX_GRID / 2 ? blocks : MAX_GRID / 2);
+    };
+    if (n <= SPAN) {
+        const int rank_blocks = ceil_div(n, RANK_ROWS), grid = rank_blocks + fill(RANK_THREADS);
+        if (grid > 0) embed_rank_kernel<<<grid, RANK_THREADS, 0, st>>>(so, rank_blocks);
+    } else {
+        static std::atomic<uint64_t> lds_ok{0};
+        const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&embed_sort_kernel), SORT_LDS, lds_ok);
+        if (e != hipSuccess) return e;
+        embed_sort_kernel<<<so.spans + fill(SORT_THREADS), SORT_THREADS, SORT_LDS, st>>>(so);
+    }
     if (n == 0) return hipGetLastError();
     a.tok = so.tok;
     a.row = so.row;
@@ -398,8 +455,8 @@ static hipError_t launch_embed_bwd(SumArgs a, SortArgs so, unsigned char* ws, hi
     else if (vpr <= 128) embed_sum_kernel<T, 128, MAIN><<<blocks(128), 128, 0, st>>>(a);
     else embed_sum_kernel<T, 256, MAIN><<<blocks(256), 256, 0, st>>>(a);
     if (chunks > 1) {
-        const int64_t items = (int64_t)(chunks - 1) * ((a.H + 255) / 256);
-        embed_join_kernel<T, MAIN><<<(int)(items < 2 * compute_units() ? items : 2 * compute_units()), 1024, 0, st>>>(a);
+        const int64_t waves = (int64_t)(chunks - 1) * ((a.H + 255) / 256), blocks = (waves + 3) / 4, most = 16 * compute_units();
+        embed_join_kernel<T, MAIN><<<(int)(blocks < most ? blocks : most), 256, 0, st>>>(a);
     }
     return hipGetLastError();
 }

@@ -55,15 +55,13 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_fwd_kernel(NormArgs 
     int64_t j = (int64_t)blockIdx.x * RPB + threadIdx.x / NT;
     u32x4_t x[NV];
     auto fetch = [&](int64_t j) __attribute__((always_inline)) {
+        j = j < n_rows ? j : n_rows - 1;
         const T* row = (const T*)a.x + (a.idx != nullptr ? (int64_t)a.idx[j] : j) * H;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int v = tid + i * NT;
-            x[i] = u32x4_t{0u, 0u, 0u, 0u};
-            if (v < vpr) x[i] = *reinterpret_cast<const u32x4_t*>(row + v * VN);
-        }
+        for (int i = 0; i < NV; ++i) x[i] = *reinterpret_cast<const u32x4_t*>(row + min(tid + i * NT, vpr - 1) * VN);
     };
-    if (j < n_rows) fetch(j);
+    if (n_rows == 0) return;
+    fetch(j);
     // gains and biases: once a thread
     u32x4_t gv[NV], bv[NV];
 #pragma unroll
@@ -78,8 +76,8 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_fwd_kernel(NormArgs 
     for (; j < n_rows; j += step) {
         float xf[NV][VN], mu = 0.f;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) unpack<T>(x[i], xf[i]);
-        if (j + step < n_rows) fetch(j + step);
+        for (int i = 0; i < NV; ++i) unpack<T>(tid + i * NT < vpr ? x[i] : u32x4_t{0u, 0u, 0u, 0u}, xf[i]);
+        fetch(j + step);
         if (LAYER) {
             float s[1] = {0.f};
 #pragma unroll
@@ -132,23 +130,24 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_bwd_kernel(NormArgs 
     if ((int)blockIdx.x >= used) return;
     const float inv_h = 1.f / (float)H;
     const int64_t step = (int64_t)used * RPB;
-    u32x4_t x[NV], dy[NV], gv[NV];
+    // rows whose loads are in flight beside the one in work; behind the last one it is read again: no load is conditional, or the one waited for would be the last
+    constexpr int AHEAD = NV <= 2 ? 2 : 1;
+    u32x4_t x[AHEAD][NV], dy[AHEAD][NV], gv[NV];
     float sg[NV][VN], sb[LAYER ? NV : 1][VN];
-    auto fetch = [&](int64_t j) __attribute__((always_inline)) {
+    auto fetch = [&](u32x4_t (&xr)[NV], u32x4_t (&dr)[NV], int64_t j) __attribute__((always_inline)) {
+        j = j < n_rows ? j : n_rows - 1;
         const T* row = (const T*)a.x + (a.idx != nullptr ? (int64_t)a.idx[j] : j) * H;
         const T* drow = (const T*)a.dy + j * H;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int v = tid + i * NT;
-            x[i] = dy[i] = u32x4_t{0u, 0u, 0u, 0u};
-            if (v < vpr) {
-                x[i] = *reinterpret_cast<const u32x4_t*>(row + v * VN);
-                dy[i] = *reinterpret_cast<const u32x4_t*>(drow + v * VN);
-            }
+            const int v = min(tid + i * NT, vpr - 1);
+            xr[i] = *reinterpret_cast<const u32x4_t*>(row + v * VN);
+            dr[i] = *reinterpret_cast<const u32x4_t*>(drow + v * VN);
         }
     };
-    int64_t j = (int64_t)blockIdx.x * RPB + threadIdx.x / NT;
-    if (j < n_rows) fetch(j);
+    const int64_t first = (int64_t)blockIdx.x * RPB + threadIdx.x / NT;
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) fetch(x[k], dy[k], first + k * step);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int v = tid + i * NT;
@@ -160,14 +159,15 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_bwd_kernel(NormArgs 
             if (LAYER) sb[i][e] = 0.f;
         }
     }
-    for (; j < n_rows; j += step) {
+    auto take = [&](u32x4_t (&xr)[NV], u32x4_t (&dr)[NV], int64_t j) __attribute__((always_inline)) {
         float xf[NV][VN], df[NV][VN], mu = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            unpack<T>(x[i], xf[i]);
-            unpack<T>(dy[i], df[i]);
+            const bool have = tid + i * NT < vpr;
+            unpack<T>(have ? xr[i] : u32x4_t{0u, 0u, 0u, 0u}, xf[i]);
+            unpack<T>(have ? dr[i] : u32x4_t{0u, 0u, 0u, 0u}, df[i]);
         }
-        if (j + step < n_rows) fetch(j + step);
+        fetch(xr, dr, j + AHEAD * step);
         if (LAYER) {
             float s[1] = {0.f};
 #pragma unroll
@@ -212,6 +212,11 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_bwd_kernel(NormArgs 
             if (v < vpr) Vec<T>::store(dx + v * VN, o);
         }
         if (NT > 64 && !LAYER) __syncthreads();
+    };
+    for (int64_t j = first; j < n_rows; j += AHEAD * step) {
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (j + k * step < n_rows) take(x[k], dy[k], j + k * step);
     }
     if (a.pg == nullptr) return;
     if constexpr (RPB == 1) {
@@ -230,27 +235,30 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_bwd_kernel(NormArgs 
             }
         }
     } else {
-        // the block's four waves, one after the other, a vector at a time
-        __shared__ float part[RPB][64 * VN];
-        auto leave = [&](const float (&s)[VN], int i, float* out) __attribute__((always_inline)) {
+        // the block's four waves, in order
+        __shared__ __align__(16) float part[RPB][NV * 64 * VN];
+        auto leave = [&](const auto& s, float* out) __attribute__((always_inline)) {
             __syncthreads();
 #pragma unroll
-            for (int e = 0; e < VN; ++e) part[threadIdx.x / NT][tid * VN + e] = s[e];
-            __syncthreads();
-            for (int c = threadIdx.x; c < 64 * VN; c += BT) {
-                if (i * 64 * VN + c >= H) break;
-                float t = 0.f;
+            for (int i = 0; i < NV; ++i)
 #pragma unroll
-                for (int r = 0; r < RPB; ++r) t += part[r][c];
-                out[(int64_t)blockIdx.x * H + i * 64 * VN + c] = t;
+                for (int q = 0; q < VN / 4; ++q)
+                    *reinterpret_cast<float4*>(&part[threadIdx.x / NT][(tid + i * NT) * VN + 4 * q]) =
+                        make_float4(s[i][4 * q], s[i][4 * q + 1], s[i][4 * q + 2], s[i][4 * q + 3]);
+            __syncthreads();
+            for (int c = threadIdx.x * 4; c < H; c += BT * 4) {
+                float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int r = 0; r < RPB; ++r) {
+                    const float4 w = *reinterpret_cast<const float4*>(&part[r][c]);
+                    t.x += w.x; t.y += w.y; t.z += w.z; t.w += w.w;
+                }
+                *reinterpret_cast<float4*>(out + (int64_t)blockIdx.x * H + c) = t;
             }
         };
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            leave(sg[i], i, a.pg);
-            if constexpr (LAYER) {
-                if (a.pb != nullptr) leave(sb[i], i, a.pb);
-            }
+        leave(sg, a.pg);
+        if constexpr (LAYER) {
+            if (a.pb != nullptr) leave(sb, a.pb);
         }
     }
 }
