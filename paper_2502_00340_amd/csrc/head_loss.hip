@@ -35,7 +35,7 @@ struct HeadArgs {
     int H, V, n_max;
     const int32_t* n_dev;
     float k;                // logit scale * log2(e)
-    int ldn;                // rows of the strips' array
+    int ldn, strips;        // rows of the strips' array; sums that a row has where its tile is not flagged
     float *ref, *sums;      // [n_max]; [strips][ldn]
     float *a, *ey;          // [n_max]: the row's factor; e at the target
     int32_t *y, *flags;     // target or -1; flags[0]: any, flags[1 + i]: rows 256 i ..
@@ -241,6 +241,143 @@ template <int KIND> __global__ __launch_bounds__(256) void head_logits_kernel(He
     else gemm_tiles<0, 2, 2, false, false>(g, a.H, t, next_in(n_items), smem, 0, 0, nullptr, leave);
 }
 
+// Few rows: the table's traffic counts, not the products.  A block of eight waves walks through tiles of 128 rows of the table, which go from memory
+// straight into the registers that the MFMAs take them from, P steps of 64 k ahead; x, 16 * NF rows of 64 k a step, lies in a ring in LDS that all waves
+// fill and read.  Each wave keeps the sums of its columns over all its tiles: one value a row and block leaves.  The loads never stop, between tiles neither.
+// Blocks begin a row's k at different places: rows of the table are a power of two apart as a rule, and blocks that all read the same part of theirs meet in
+// the same memory channels (64 rows of x, [128256, 4096]: 217 us, and 176 so, 6.0 TB/s; tiles of 256 rows 241 and 180; 128x128 product tiles 289).
+template <int NF, int P> __global__ __launch_bounds__(512) void head_few_kernel(HeadArgs a) {
+    constexpr int R = P + 1, ROWS = 16 * NF, SLOT = ROWS * 128, XL = NF > 4 ? NF / 4 : 1, NB = 2;            // XL, NB: loads of a wave and step
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ float red[8][ROWS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
+    const int rows = __builtin_amdgcn_readfirstlane(live_rows(a.n_max, a.n_dev)), H = a.H, steps = (H + 63) / 64;
+    if (rows == 0) return;
+    constexpr int TILE = 128;
+    const int tiles = (a.V + TILE - 1) / TILE;
+    const i32x4_t rx = make_rsrc(a.x, (int64_t)rows * H * 2);
+    constexpr unsigned OOB = 0x80000000u;
+    unsigned xoff[XL];
+    int xk[XL];
+    unsigned xdst[XL];
+#pragma unroll
+    for (int u = 0; u < XL; ++u) {
+        const int part = (wave + 8 * u) % (2 * NF), row = part * 8 + (lane >> 3);       // of the slot; with few rows several waves load the same part
+        xk[u] = ((lane & 7) ^ nt_swz(row)) * 8;
+        xoff[u] = (unsigned)row * (unsigned)H * 2u + xk[u] * 2u;
+        xdst[u] = __builtin_amdgcn_readfirstlane(lds_addr_of(smem) + part * 1024);
+    }
+    // (tile, step) that the next loads fetch
+    const int rot = (int)(blockIdx.x * 37u) % steps;
+    int lt = blockIdx.x, ls = 0, slot_in = 0;
+    __amdgpu_buffer_rsrc_t rb;
+    auto open = [&]() __attribute__((always_inline)) {
+        const int64_t v0 = (int64_t)lt * TILE;
+        const int64_t have = lt < tiles ? min((int64_t)TILE, a.V - v0) : 0;
+        rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>((const bf16_t*)a.table + (lt < tiles ? v0 : 0) * H), 0, (int)(have * H * 2), 0x00020000);
+    };
+    open();
+    const unsigned boff = (unsigned)(wave * 16 + l16) * (unsigned)H * 2u + g4 * 16u;
+    u32x4_t b[P][NB];
+    auto fetch = [&](u32x4_t (&to)[NB]) __attribute__((always_inline)) {
+        const int k0 = (ls + rot >= steps ? ls + rot - steps : ls + rot) * 64;
+#pragma unroll
+        for (int u = 0; u < XL; ++u)
+            dma16s(xdst[u] + slot_in * SLOT, rx, k0 + xk[u] < H ? xoff[u] : OOB, (unsigned)k0 * 2u);
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+            to[ks] = __builtin_amdgcn_raw_buffer_load_b128(rb, k0 + ks * 32 + g4 * 8 < H ? boff : OOB, (k0 + ks * 32) * 2, 0);
+        CF_SCHED_FENCE();
+        slot_in = slot_in + 1 == R ? 0 : slot_in + 1;
+        if (++ls == steps) {
+            ls = 0;
+            lt += (int)gridDim.x;
+            open();
+        }
+    };
+    float ref[NF], sum[NF];
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+        const int m = i * 16 + l16;
+        ref[i] = m < rows ? a.ref[m] : INFINITY;
+        sum[i] = 0.f;
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p) fetch(b[p]);
+    f32x4_t acc[NF];
+#pragma unroll
+    for (int i = 0; i < NF; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    int tile = blockIdx.x, s = 0, slot = 0;
+    auto leave = [&]() __attribute__((always_inline)) {
+        const int c = tile * TILE + wave * 16 + 4 * g4;
+#pragma unroll
+        for (int i = 0; i < NF; ++i) {
+            float e[4];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                e[v] = __builtin_amdgcn_exp2f(fmaf(acc[i][v], a.k, -ref[i]));
+                e[v] = c + v < a.V ? e[v] : 0.f;
+                sum[i] += e[v];
+            }
+            const int m = i * 16 + l16;
+            if (a.store_end > 0 && m < rows && c < a.lde) {         // zeros behind the last column, too
+                const bool dead = ref[i] == INFINITY;
+                uint2 o;
+                o.x = dead ? 0u : pack_bf16x2(e[0], e[1]);
+                o.y = dead ? 0u : pack_bf16x2(e[2], e[3]);
+                *reinterpret_cast<uint2*>((bf16_t*)a.e + (int64_t)m * a.lde + c) = o;
+            }
+        }
+    };
+    const int frag = l16 * 128, ch0 = (g4 ^ nt_swz(l16)) << 4, ch1 = ((4 + g4) ^ nt_swz(l16)) << 4;
+    // Whole rounds of P steps (the steps behind the last tile's run on zeros, and nothing takes what they give): a way out in the middle would have the compiler wait for
+    // the youngest load at the loop's head
+    const int mine = (tiles - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
+    for (int64_t left = (int64_t)mine * steps; left > 0; left -= P) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            wait_vmcnt<(P - 1) * (XL + NB)>();
+            lds_barrier();              // the step's rows of x are there, and every wave is done with the step before
+            const unsigned char* xs = smem + slot * SLOT + frag;
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+                for (int i = 0; i < NF; ++i) {
+                    const bf16x8_t fa = *reinterpret_cast<const bf16x8_t*>(xs + i * 2048 + (ks ? ch1 : ch0));
+                    acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, b[p][ks]), fa, acc[i], 0, 0, 0);
+                }
+            CF_SCHED_FENCE();
+            fetch(b[p]);
+            slot = slot + 1 == R ? 0 : slot + 1;
+            if (++s == steps) {
+                if (tile < tiles) leave();
+#pragma unroll
+                for (int i = 0; i < NF; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                s = 0;
+                tile += (int)gridDim.x;
+            }
+        }
+    }
+    wait_vmcnt<0>();            // loads into LDS must not outlive the block
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+        sum[i] += __shfl_xor(sum[i], 16, 64);
+        sum[i] += __shfl_xor(sum[i], 32, 64);
+        if (g4 == 0) red[wave][i * 16 + l16] = sum[i];
+    }
+    __syncthreads();
+    for (int m = threadIdx.x; m < rows; m += 512) {
+        float t = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) t += red[w][m];
+        a.sums[(int64_t)blockIdx.x * a.ldn + m] = t;
+        if (a.ref[m] != INFINITY && !(t <= FLAG_ABOVE)) a.flags[0] = a.flags[1] = 1;
+    }
+}
+
+static int few_blocks(int V, int n_cu) { return std::min(ceil_div(V, 128), n_cu); }
+constexpr int FEW_ROWS = 128;
+
 // ---- 3. the rows' ends -------------------------------------------------------------------------------------
 // A block takes 16 rows: 64 groups of 16 lanes add their strips up, one lane a row ends it, and the block scales the rows of x.
 template <typename T>
@@ -250,8 +387,8 @@ __global__ __launch_bounds__(1024) void head_finish_kernel(HeadArgs a, LossArgs 
     __shared__ float fac[16];
     const int n_rows = live_rows(a.n_max, a.n_dev), j0 = blockIdx.x * 16, tid = threadIdx.x, r = tid & 15, grp = tid >> 4, j = j0 + r;
     if (j0 >= n_rows) return;
-    const int strips = (a.V + STRIP - 1) / STRIP;
     const bool flagged = a.flags[1 + (j0 >> 8)] != 0;           // the same for the 16 rows
+    const int strips = flagged ? (a.V + STRIP - 1) / STRIP : a.strips;
     float m = 0.f, s = 0.f;
     if (!flagged) {
         if (j < n_rows) {
@@ -671,7 +808,7 @@ template <bool MAIN> __global__ __launch_bounds__(256) void head_dtable_f32_kern
 static int dx_parts(int64_t tiles, int V, int n_cu) {
     int best = 1;
     double least = 1e30;
-    for (int s = 1; s <= 16 && (s == 1 || (int64_t)V >= (int64_t)s * 512); ++s) {
+    for (int s = 1; s <= 64 && (s == 1 || (int64_t)V >= (int64_t)s * 512); ++s) {
         const double cost = (double)((tiles * s + n_cu - 1) / n_cu) / s + 0.01 * s;
         if (cost < least - 1e-9) { least = cost; best = s; }
     }
@@ -694,7 +831,7 @@ struct HeadWs {
         y = take((size_t)n * 4);
         terms = take((size_t)n * 16);
         flags = take((size_t)(ceil_div(n, 256) + 1) * 4);
-        sums = take((size_t)strips * ldn * 4);
+        sums = take((size_t)(n <= FEW_ROWS ? std::max(strips, compute_units()) : strips) * ldn * 4);
         xs = take(need_dt ? (size_t)n * H * es : 0);
         tile = dtype == CF_F32 || n <= 128 ? 128 : 256;
         parts = need_dx ? dx_parts((int64_t)ceil_div(n, tile) * ceil_div(H, tile), V, compute_units()) : 0;
@@ -725,6 +862,20 @@ template <> struct HeadLaunch<bf16_t> {
         head_logits_kernel<KIND><<<compute_units(), 256, GEMM_SMEM, st>>>(a);
         return hipGetLastError();
     }
+    template <int NF> static hipError_t few(const HeadArgs& a, hipStream_t st) {
+        static std::atomic<uint64_t> lds_ok{0};
+        constexpr int P = 8, lds = (P + 1) * NF * 16 * 128;
+        const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&head_few_kernel<NF, P>), lds, lds_ok);
+        if (e != hipSuccess) return e;
+        head_few_kernel<NF, P><<<a.strips, 512, lds, st>>>(a);
+        return hipGetLastError();
+    }
+    // sums of the whole vocabulary; sets the number of sums a row has
+    static hipError_t sums(HeadArgs& a, hipStream_t st) {
+        if (a.n_max > FEW_ROWS) return logits<SUMS>(a, st);
+        a.strips = few_blocks(a.V, compute_units());
+        return a.n_max <= 16 ? few<1>(a, st) : a.n_max <= 32 ? few<2>(a, st) : a.n_max <= 64 ? few<4>(a, st) : few<8>(a, st);
+    }
     static hipError_t dx(const DxArgs& a, hipStream_t st) {
         static std::atomic<uint64_t> lds_ok{0};
         const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&head_dx_kernel), GEMM_SMEM, lds_ok);
@@ -750,6 +901,7 @@ template <> struct HeadLaunch<float> {
         head_logits_f32_kernel<KIND><<<grid((int64_t)ceil_div(a.n_max, 128) * ceil_div(a.c1 - a.c0, 128)), 256, 0, st>>>(a);
         return hipGetLastError();
     }
+    static hipError_t sums(HeadArgs& a, hipStream_t st) { return logits<SUMS>(a, st); }
     static hipError_t dx(const DxArgs& a, hipStream_t st) {
         head_dx_f32_kernel<<<grid((int64_t)ceil_div(a.n_max, 128) * ceil_div(a.H, 128) * a.parts), 256, 0, st>>>(a);
         return hipGetLastError();
@@ -780,6 +932,7 @@ static hipError_t launch_head(HeadArgs a, LossArgs l, const HeadWs& L, unsigned 
         a.flags = (int32_t*)(ws + L.flags);
         a.sums = (float*)(ws + L.sums);
         a.ldn = L.ldn;
+        a.strips = L.strips;
         l.terms = (float4*)(ws + L.terms);
         void* xs = dtable != nullptr ? ws + L.xs : nullptr;
         const int first = std::min(V, L.cap);           // columns whose exponentials are kept
@@ -788,7 +941,7 @@ static hipError_t launch_head(HeadArgs a, LossArgs l, const HeadWs& L, unsigned 
         const int blocks = ceil_div(n, 4);
         head_rows_kernel<T><<<std::min(blocks, 8 * compute_units()), 256, 0, st>>>(a, l);
         CF_TRY(hipGetLastError());
-        CF_TRY(HeadLaunch<T>::template logits<SUMS>(a, st));
+        CF_TRY(HeadLaunch<T>::sums(a, st));
         a.flagged_only = true;
         CF_TRY(HeadLaunch<T>::template logits<MAXIMA>(a, st));
         head_finish_kernel<T><<<ceil_div(n, 16), 1024, 0, st>>>(a, l, xs);
