@@ -598,11 +598,14 @@ __global__ __launch_bounds__(256) void head_dx_sum_kernel(const float* __restric
 }
 
 // ---- fp32 --------------------------------------------------------------------------------------------------
-// The same steps with the fp32 matrix instruction (32x32x2, 256 flop a cycle and CU): 128x128 tiles, four waves of 64x64, steps of 16 through two LDS stages laid
-// out [k][row], the next step's operands on their way in registers.  Operands as for the bf16 products: MODE 0 A and B with k contiguous, 1 both k-major,
-// 2 A contiguous, B k-major.  D = B-frag x A-frag: lane l holds row l % 32 and, in register v, column 8 * (v / 4) + 4 * (l / 32) + v % 4 of a fragment.
-typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16_t;
-constexpr int F32_STEP = 16, F32_LD = 132;
+// The same steps with fp32 operands on the bf16 matrix cores: a value is the sum of three bf16 numbers, each the rounded rest of what is ahead of it, x = x1 + x2 + x3
+// but for 2^-27 of x, and a product the sum of the six of the nine partial ones that are not below 2^-26 of it: x1 y1 + x1 y2 + x2 y1 + x2 y2 + x1 y3 + x3 y1, all in
+// one fp32 accumulator.  That is fp32 accuracy at a sixth of the bf16 rate, 2.7 times that of the fp32 matrix instruction (values beyond 3.39e38 round to infinity).
+// Tiles of 128x128, four waves of 64x64, steps of 32 k: operands go from memory to registers, a step ahead, and from there, split, to three planes in LDS; two
+// blocks a CU cover each other's barriers.  MODE 0: A and B with k contiguous, 1: both k-major, 2: A contiguous, B k-major.  Planes of a k-contiguous operand are
+// [row][32 k], 16-byte chunks XOR-ed with a function of the row that keeps the 16 lanes of one pass of a ds_read_b128 apart; of a k-major one [k][row], read
+// transposed.  D = B-frag x A-frag: lane l holds row l % 16 and columns 4 * (l / 16) .. +3 of a fragment, as in the bf16 products.
+constexpr int F32_STEP = 32, F32_PLANE = 128 * F32_STEP * 2, F32_SMEM = 6 * F32_PLANE;
 
 struct F32Tile {
     const float *A, *B;
@@ -611,125 +614,157 @@ struct F32Tile {
     int k0, k1;             // the contraction's range
     int m0, n0;
 };
-template <int MODE>
-__device__ __forceinline__ void f32_tile(const F32Tile& t, float (&As)[2][F32_STEP][F32_LD], float (&Bs)[2][F32_STEP][F32_LD], f32x16_t (&acc)[2][2]) {
+
+// two values -> the rounded first, second and third parts of both
+__device__ __forceinline__ void split2(float a, float b, unsigned& p1, unsigned& p2, unsigned& p3) {
+    p1 = pack_bf16x2(a, b);
+    a -= __uint_as_float(p1 << 16);
+    b -= __uint_as_float(p1 & 0xFFFF0000u);
+    p2 = pack_bf16x2(a, b);
+    a -= __uint_as_float(p2 << 16);
+    b -= __uint_as_float(p2 & 0xFFFF0000u);
+    p3 = pack_bf16x2(a, b);
+}
+
+__device__ __forceinline__ int f32_swz(int row) { return -(row >> 2) & 3; }
+
+template <int MODE> __device__ __forceinline__ void f32_tile(const F32Tile& t, unsigned char* smem, f32x4_t (&acc)[4][4]) {
     constexpr bool AK = MODE != 1, BK = MODE == 0;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
-    float4 ra[2], rb[2];
-    // rows (k contiguous): two of 64 rows apart, four k each; k-major: two of 8 k apart, four columns each
-    auto fetch = [&](float4 (&r)[2], const float* p, int64_t ld, int base, int lim, int k, bool kc) __attribute__((always_inline)) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1, l16 = lane & 15, g4 = lane >> 4;
+    float4 ra[4], rb[4];
+    // k contiguous: eight lanes a row of 32 k, rows 32 apart; k-major: 32 lanes a row of 128 columns, k 8 apart.  What does not exist lies outside a descriptor's
+    // range: of the tile's rows, or of the step's k, which the scalar part of an address goes along
+    constexpr unsigned OOB = 0x80000000u;
+    auto lane_offset = [&](int base, int lim, int64_t ld, bool kc) __attribute__((always_inline)) {
+        if (kc) return (unsigned)(tid >> 3) * (unsigned)ld * 4u + (tid & 7) * 16u;
+        return base + (tid & 31) * 4 < lim ? (unsigned)(tid >> 5) * (unsigned)ld * 4u + (tid & 31) * 16u : OOB;
+    };
+    auto fetch = [&](float4 (&r)[4], const float* p, int64_t ld, int base, int lim, unsigned voff, int k, bool kc) __attribute__((always_inline)) {
+        const int64_t at = kc ? (int64_t)base * ld : (int64_t)k * ld + base, have = kc ? min(lim - base, 128) * ld : (int64_t)max(0, min(t.k1 - k, F32_STEP)) * ld - base;
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(p) + at, 0, (int)(have > 0 ? have * 4 : 0), 0x00020000);
+        if (kc && k + (tid & 7) * 4 >= t.k1) voff = OOB;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            r[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i = 0; i < 4; ++i)
+            r[i] = __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(rs, voff + i * (kc ? 32u : 8u) * (unsigned)ld * 4u, kc ? k * 4 : 0, 0));
+    };
+    auto put = [&](const float4 (&r)[4], unsigned char* s, bool kc) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint2 p[3];
+            split2(r[i].x, r[i].y, p[0].x, p[1].x, p[2].x);
+            split2(r[i].z, r[i].w, p[0].y, p[1].y, p[2].y);
+            int at;
             if (kc) {
-                const int row = base + (tid >> 2) + 64 * i, kk = k + (tid & 3) * 4;
-                if (row < lim && kk < t.k1) r[i] = *reinterpret_cast<const float4*>(p + (int64_t)row * ld + kk);
+                const int row = (tid >> 3) + 32 * i, ch = (tid & 7) >> 1;
+                at = row * 64 + ((ch ^ f32_swz(row)) << 4) + (tid & 1) * 8;
             } else {
-                const int kk = k + (tid >> 5) + 8 * i, col = base + (tid & 31) * 4;
-                if (col < lim && kk < t.k1) r[i] = *reinterpret_cast<const float4*>(p + (int64_t)kk * ld + col);
+                const int k = (tid >> 5) + 8 * i, ch = (tid & 31) >> 1;
+                at = k * 256 + ((ch ^ ((k & 3) << 2)) << 4) + (tid & 1) * 8;
             }
+#pragma unroll
+            for (int q = 0; q < 3; ++q) *reinterpret_cast<uint2*>(s + q * F32_PLANE + at) = p[q];
         }
     };
-    auto put = [&](const float4 (&r)[2], float (&s)[F32_STEP][F32_LD], bool kc) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if (kc) {
-                const int row = (tid >> 2) + 64 * i, kk = (tid & 3) * 4;
-                s[kk][row] = r[i].x; s[kk + 1][row] = r[i].y; s[kk + 2][row] = r[i].z; s[kk + 3][row] = r[i].w;
-            } else {
-                *reinterpret_cast<float4*>(&s[(tid >> 5) + 8 * i][(tid & 31) * 4]) = r[i];
-            }
+    // fragment f of the wave's 64 rows, plane q
+    auto frag = [&](unsigned char* s, int w, int f, int q, bool kc) __attribute__((always_inline)) {
+        s += q * F32_PLANE;
+        if (kc) {
+            const int row = w * 64 + f * 16 + l16;
+            return *reinterpret_cast<const bf16x8_t*>(s + row * 64 + ((g4 ^ f32_swz(row)) << 4));
         }
+        const int kl = 8 * g4 + (l16 >> 2), lc = (w * 64 + (f >> 1) * 32) / 8 + ((lane & 3) >> 1);
+        unsigned char* p = s + kl * 256 + ((lc ^ ((kl & 3) << 2)) << 4) + (lane & 1) * 8 + (f & 1) * 32;
+        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(__attribute__((address_space(3))) unsigned char*)p);
+        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(__attribute__((address_space(3))) unsigned char*)(p + 4 * 256));
+        return __builtin_bit_cast(bf16x8_t, (s16x8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     if (t.k0 >= t.k1) return;
-    fetch(ra, t.A, t.lda, t.m0, t.M, t.k0, AK);
-    fetch(rb, t.B, t.ldb, t.n0, t.N, t.k0, BK);
-    int st = 0;
-    put(ra, As[0], AK);
-    put(rb, Bs[0], BK);
-    __syncthreads();
-    for (int k = t.k0; k < t.k1; k += F32_STEP, st ^= 1) {
-        const bool more = k + F32_STEP < t.k1;
-        if (more) {
-            fetch(ra, t.A, t.lda, t.m0, t.M, k + F32_STEP, AK);
-            fetch(rb, t.B, t.ldb, t.n0, t.N, k + F32_STEP, BK);
+    unsigned char *sa = smem, *sb = smem + 3 * F32_PLANE;
+    const unsigned va = lane_offset(t.m0, t.M, t.lda, AK), vb = lane_offset(t.n0, t.N, t.ldb, BK);
+    fetch(ra, t.A, t.lda, t.m0, t.M, va, t.k0, AK);
+    fetch(rb, t.B, t.ldb, t.n0, t.N, vb, t.k0, BK);
+    for (int k = t.k0; k < t.k1; k += F32_STEP) {
+        lds_barrier();              // the step before has been read
+        put(ra, sa, AK);
+        put(rb, sb, BK);
+        lds_barrier();
+        // Nothing behind the last step.  One step ahead is enough with two blocks a CU (two: 284 and 277 us for 225 and 201, in 236 registers)
+        fetch(ra, t.A, t.lda, t.m0, t.M, va, k + F32_STEP, AK);
+        fetch(rb, t.B, t.ldb, t.n0, t.N, vb, k + F32_STEP, BK);
+        CF_SCHED_FENCE();
+        bf16x8_t fb[4][3];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int q = 0; q < 3; ++q) fb[j][q] = frag(sb, wn, j, q, BK);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            bf16x8_t fa[3];
+#pragma unroll
+            for (int q = 0; q < 3; ++q) fa[q] = frag(sa, wm, i, q, AK);
+            // the smallest first; four accumulators in turn
+            constexpr int PA[6] = {2, 0, 1, 1, 0, 0}, PB[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+            for (int z = 0; z < 6; ++z)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j][PB[z]], fa[PA[z]], acc[i][j], 0, 0, 0);
         }
-#pragma unroll
-        for (int kk = 0; kk < F32_STEP; kk += 2) {
-            float fa[2], fb[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                fa[i] = As[st][kk + (lane >> 5)][wm * 64 + i * 32 + (lane & 31)];
-                fb[i] = Bs[st][kk + (lane >> 5)][wn * 64 + i * 32 + (lane & 31)];
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(fb[j], fa[i], acc[i][j], 0, 0, 0);
-        }
-        if (more) {
-            put(ra, As[st ^ 1], AK);
-            put(rb, Bs[st ^ 1], BK);
-        }
-        __syncthreads();
     }
 }
 
 template <int KIND> __global__ __launch_bounds__(256) void head_logits_f32_kernel(HeadArgs a) {
-    __shared__ __align__(16) float As[2][F32_STEP][F32_LD], Bs[2][F32_STEP][F32_LD];
+    __shared__ __align__(16) unsigned char smem[F32_SMEM];
     if (a.flagged_only && a.flags[0] == 0) return;
     const int rows = live_rows(a.n_max, a.n_dev), tm = (rows + 127) / 128, tn = (a.c1 - a.c0 + 127) / 128;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, hi = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, l16 = lane & 15, g4 = lane >> 4;
     for (int64_t w = blockIdx.x; w < (int64_t)tm * tn; w += gridDim.x) {
         const int bm = (int)(w % tm), m0 = bm * 128, n0 = a.c0 + (int)(w / tm) * 128;
         if (a.flagged_only && a.flags[1 + (m0 >> 8)] == 0) continue;
         const F32Tile t{(const float*)a.x, (const float*)a.table, a.H, a.H, rows, min(a.c1, a.V), 0, a.H, m0, n0};
-        f32x16_t acc[2][2];
-        f32_tile<0>(t, As, Bs, acc);
+        f32x4_t acc[4][4];
+        f32_tile<0>(t, smem, acc);
         const int c = n0 + wn * 64;             // a strip
         const bool store = KIND != MAXIMA && n0 < a.store_end;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int m = m0 + wm * 64 + i * 32 + (lane & 31);
+        for (int i = 0; i < 4; ++i) {
+            const int m = m0 + wm * 64 + i * 16 + l16;
             const float ref = m < rows ? a.ref[m] : INFINITY;
             const bool dead = ref == INFINITY;
             float s = 0.f, mx = -INFINITY, ey = 0.f;
             int y = -1;
             if (KIND == VALUES && m < rows) { y = a.y[m]; ey = a.ey[m]; }
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    if (c + j * 32 + 8 * (v >> 2) + 4 * hi + (v & 3) >= a.V) acc[i][j][v] = -INFINITY;
+                for (int v = 0; v < 4; ++v) {
+                    if (c + j * 16 + 4 * g4 + v >= a.V) acc[i][j][v] = -INFINITY;
                     mx = fmaxf(mx, acc[i][j][v]);
                 }
+            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * a.k;
             const float r = KIND == MAXIMA ? (mx == -INFINITY ? 0.f : mx) : ref;
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < 4; ++j) {
+                const int col = c + j * 16 + 4 * g4;
+                float e[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int col = c + j * 32 + 8 * q + 4 * hi;
-                    float e[4];
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        e[v] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][4 * q + v], a.k, -r));
-                        s += e[v];
-                        if (KIND == VALUES && col + v == y) e[v] = ey;
-                        if (dead) e[v] = 0.f;
-                    }
-                    if (store && m < rows && col - a.c0 < a.lde)
-                        *reinterpret_cast<float4*>((float*)a.e + (int64_t)m * a.lde + (col - a.c0)) = make_float4(e[0], e[1], e[2], e[3]);
+                for (int v = 0; v < 4; ++v) {
+                    e[v] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][v], a.k, -r));
+                    s += e[v];
+                    if (KIND == VALUES && col + v == y) e[v] = ey;
+                    if (dead) e[v] = 0.f;
                 }
+                if (store && m < rows && col - a.c0 < a.lde)
+                    *reinterpret_cast<float4*>((float*)a.e + (int64_t)m * a.lde + (col - a.c0)) = make_float4(e[0], e[1], e[2], e[3]);
+            }
             if (KIND != VALUES) {
+                s += __shfl_xor(s, 16, 64);
                 s += __shfl_xor(s, 32, 64);
-                if (hi == 0 && m < rows && c < a.V) {
+                if (g4 == 0 && m < rows && c < a.V) {
                     a.sums[(int64_t)(c / STRIP) * a.ldn + m] = KIND == MAXIMA ? mx + log2f(s) : s;
                     if (KIND == SUMS && !dead && !(s <= FLAG_ABOVE)) a.flags[0] = a.flags[1 + (m >> 8)] = 1;
                 }
@@ -739,7 +774,7 @@ template <int KIND> __global__ __launch_bounds__(256) void head_logits_f32_kerne
 }
 
 __global__ __launch_bounds__(256) void head_dx_f32_kernel(DxArgs a) {
-    __shared__ __align__(16) float As[2][F32_STEP][F32_LD], Bs[2][F32_STEP][F32_LD];
+    __shared__ __align__(16) unsigned char smem[F32_SMEM];
     const int rows = live_rows(a.n_max, a.n_dev), tm = (rows + 127) / 128, tn = (a.H + 127) / 128, tiles = tm * tn, items = tiles * a.parts;
     const int steps = (a.K + F32_STEP - 1) / F32_STEP, per = (steps + a.parts - 1) / a.parts;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
@@ -747,69 +782,68 @@ __global__ __launch_bounds__(256) void head_dx_f32_kernel(DxArgs a) {
         const int part = w / tiles, l = w - part * tiles, m0 = (l % tm) * 128, n0 = (l / tm) * 128;
         const F32Tile t{(const float*)a.e, (const float*)a.table, a.lde, a.H, rows, a.H, min(steps, part * per) * F32_STEP,
                         min(a.K, min(steps, part * per + per) * F32_STEP), m0, n0};
-        f32x16_t acc[2][2];
-        f32_tile<2>(t, As, Bs, acc);
+        f32x4_t acc[4][4];
+        f32_tile<2>(t, smem, acc);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int m = m0 + wm * 64 + i * 32 + (lane & 31);
+        for (int i = 0; i < 4; ++i) {
+            const int m = m0 + wm * 64 + i * 16 + (lane & 15);
             if (m >= rows) continue;
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int n = n0 + wn * 64 + j * 32 + 8 * q + 4 * (lane >> 5);
-                    if (n >= a.H) continue;
-                    float4* p = reinterpret_cast<float4*>(a.slots + ((int64_t)part * a.n_max + m) * a.H + n);
-                    float4 o = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-                    if (!a.first) {
-                        const float4 b = *p;
-                        o.x += b.x; o.y += b.y; o.z += b.z; o.w += b.w;
-                    }
-                    *p = o;
+            for (int j = 0; j < 4; ++j) {
+                const int n = n0 + wn * 64 + j * 16 + 4 * (lane >> 4);
+                if (n >= a.H) continue;
+                float4* p = reinterpret_cast<float4*>(a.slots + ((int64_t)part * a.n_max + m) * a.H + n);
+                float4 o = make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
+                if (!a.first) {
+                    const float4 b = *p;
+                    o.x += b.x; o.y += b.y; o.z += b.z; o.w += b.w;
                 }
+                *p = o;
+            }
         }
     }
 }
 
 template <bool MAIN> __global__ __launch_bounds__(256) void head_dtable_f32_kernel(DtableArgs a) {
-    __shared__ __align__(16) float As[2][F32_STEP][F32_LD], Bs[2][F32_STEP][F32_LD];
+    __shared__ __align__(16) unsigned char smem[F32_SMEM];
     const int rows = live_rows(a.n_max, a.n_dev), tm = (a.K + 127) / 128, tn = (a.H + 127) / 128;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
     for (int64_t w = blockIdx.x; w < (int64_t)tm * tn; w += gridDim.x) {
         const int m0 = (int)(w / tn) * 128, n0 = (int)(w % tn) * 128;
         const F32Tile t{(const float*)a.e, (const float*)a.xs, a.lde, a.H, a.lde, a.H, 0, rows, m0, n0};
-        f32x16_t acc[2][2];
-        f32_tile<1>(t, As, Bs, acc);
+        f32x4_t acc[4][4];
+        f32_tile<1>(t, smem, acc);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int m = m0 + wm * 64 + i * 32 + (lane & 31);
+        for (int i = 0; i < 4; ++i) {
+            const int m = m0 + wm * 64 + i * 16 + (lane & 15);
             if (m >= a.K) continue;
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int n = n0 + wn * 64 + j * 32 + 8 * q + 4 * (lane >> 5);
-                    if (n >= a.H) continue;
-                    float4* p = reinterpret_cast<float4*>((float*)a.out + (int64_t)m * a.H + n);
-                    float4 o = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-                    if (MAIN) {
-                        const float4 b = *p;
-                        o.x += b.x; o.y += b.y; o.z += b.z; o.w += b.w;
-                    }
-                    *p = o;
+            for (int j = 0; j < 4; ++j) {
+                const int n = n0 + wn * 64 + j * 16 + 4 * (lane >> 4);
+                if (n >= a.H) continue;
+                float4* p = reinterpret_cast<float4*>((float*)a.out + (int64_t)m * a.H + n);
+                float4 o = make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
+                if (MAIN) {
+                    const float4 b = *p;
+                    o.x += b.x; o.y += b.y; o.z += b.z; o.w += b.w;
                 }
+                *p = o;
+            }
         }
     }
 }
 
 // ---- workspace and launches --------------------------------------------------------------------------------
 
-// Parts of dx's contraction over the vocabulary: the fewest rounds of the CUs per part, a part and its slot costing a hundredth of a whole contraction.
-static int dx_parts(int64_t tiles, int V, int n_cu) {
+// Parts of dx's contraction over the vocabulary: the fewest rounds of the blocks that are resident at a time per part.  A part costs its slot (written and read at
+// 5 TB/s) and a start of three microseconds; a whole contraction of a 256x256 bf16 tile takes V * 26 ns, of a 128x128 fp32 one V * 100 ns.
+static int dx_parts(int64_t tiles, int V, int dtype, int n_cu) {
+    const int64_t resident = (int64_t)n_cu * (dtype == CF_F32 ? 2 : 1);
+    const double part = (dtype == CF_F32 ? 0.25 * (double)tiles + 30.0 : 4.0 * (double)tiles + 115.0) / V;
     int best = 1;
     double least = 1e30;
     for (int s = 1; s <= 64 && (s == 1 || (int64_t)V >= (int64_t)s * 512); ++s) {
-        const double cost = (double)((tiles * s + n_cu - 1) / n_cu) / s + 0.01 * s;
+        const double cost = (double)((tiles * s + resident - 1) / resident) / s + part * s;
         if (cost < least - 1e-9) { least = cost; best = s; }
     }
     return best;
@@ -834,14 +868,17 @@ struct HeadWs {
         sums = take((size_t)(n <= FEW_ROWS ? std::max(strips, compute_units()) : strips) * ldn * 4);
         xs = take(need_dt ? (size_t)n * H * es : 0);
         tile = dtype == CF_F32 || n <= 128 ? 128 : 256;
-        parts = need_dx ? dx_parts((int64_t)ceil_div(n, tile) * ceil_div(H, tile), V, compute_units()) : 0;
+        parts = need_dx ? dx_parts((int64_t)ceil_div(n, tile) * ceil_div(H, tile), V, dtype, compute_units()) : 0;
         slots = take((size_t)parts * n * H * 4);
         e = at;
         cap = 0;
         total = at;
         if (!need_dx && !need_dt) return;
         int64_t whole = (int64_t)align_up((size_t)V, 256), least = std::min<int64_t>(whole, 2048), most = whole;
-        if (dtype == CF_BF16) {     // matrices below 2 GiB: 32-bit offsets
+        if (dtype == CF_F32) {      // 32-bit offsets within a tile's 128 rows
+            most = std::min<int64_t>(most, 1 << 21);
+            least = std::min(least, most);
+        } else {                    // matrices below 2 GiB: 32-bit offsets
             const int64_t lim = ((int64_t)1 << 31) - 1;
             most = std::min({most, lim / (2 * std::max<int64_t>(n, 256)) / 256 * 256, (lim / (2 * (int64_t)H) - 256) / 256 * 256});
             least = std::min(least, most);
@@ -896,7 +933,7 @@ template <> struct HeadLaunch<bf16_t> {
     }
 };
 template <> struct HeadLaunch<float> {
-    static int grid(int64_t items) { return (int)std::min<int64_t>(items, 2 * compute_units()); }
+    static int grid(int64_t items) { return (int)std::min<int64_t>(items, MAX_GRID); }
     template <int KIND> static hipError_t logits(const HeadArgs& a, hipStream_t st) {
         head_logits_f32_kernel<KIND><<<grid((int64_t)ceil_div(a.n_max, 128) * ceil_div(a.c1 - a.c0, 128)), 256, 0, st>>>(a);
         return hipGetLastError();
