@@ -40,10 +40,13 @@ struct TileRef {
 };
 
 // What becomes of a finished tile: a kernel's own epilogue, called with the accumulators and the tile, or by default the product's write-out.  Its
-// accumulators: lane l holds, of fragment (i, j) of its wave tile, row l % 16 and the columns 4 * (l / 16) .. +3.  LDA: see GemmArgs.
+// accumulators: lane l holds, of fragment (i, j) of its wave tile, row l % 16 and the columns 4 * (l / 16) .. +3.  rows: what it reads
+// from memory, before the next tile's loads go out, behind which it would have to wait.  LDA: see GemmArgs.
 struct Product {
     static constexpr bool OWN = false, LDA = false;
-    template <int TM, int TN> __device__ void operator()(f32x4_t (&)[2 * TM][2 * TN], const TileRef&, unsigned char*, int, int) const {}
+    struct Rows {};
+    template <int TM> __device__ Rows rows(const TileRef&, int) const { return {}; }
+    template <int TM, int TN> __device__ void operator()(f32x4_t (&)[2 * TM][2 * TN], const TileRef&, const Rows&, unsigned char*, int, int) const {}
 };
 
 // How the tiles of the last, partial round are cut.  The cost of a round of sub-tiles
@@ -524,6 +527,7 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs& g, const int K0x, con
             asm volatile("s_nop 15\n\ts_nop 15");
         }
         const TileRef ep = ld;          // the tile that leaves
+        const auto leave_rows = leave.template rows<TM>(ep, wm);
         const bool has_next = next_tile(ld);
         if (OVERLAP) {
             lds_barrier();              // every wave has read its last fragments: the stages are free
@@ -532,7 +536,7 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs& g, const int K0x, con
         const int m0 = ep.m0, n0 = ep.n0, Mx = ep.M;
 
     if constexpr (Leave::OWN) {
-        leave.template operator()<TM, TN>(acc, ep, smem, wm, wn);
+        leave.template operator()<TM, TN>(acc, ep, leave_rows, smem, wm, wn);
         if (!has_next) break;
         continue;
     }

@@ -85,57 +85,75 @@ __global__ __launch_bounds__(256) void head_rows_kernel(HeadArgs a, LossArgs l) 
 template <int KIND> struct LeaveLogits {
     static constexpr bool OWN = true, LDA = false;
     HeadArgs a;
-    int rows;
+    int n_rows;
+    struct Rows {
+        float ref[8], ey[KIND == VALUES ? 8 : 1];
+        int y[KIND == VALUES ? 8 : 1];
+    };
+    template <int TM> __device__ __forceinline__ Rows rows(const TileRef& t, int wm) const {
+        Rows r;
+#pragma unroll
+        for (int i = 0; i < 2 * TM; ++i) {
+            const int m = t.m0 + wm * (32 * TM) + i * 16 + (threadIdx.x & 15), at = min(m, n_rows - 1);
+            const float ref = a.ref[at];
+            r.ref[i] = m < n_rows ? ref : INFINITY;
+            if constexpr (KIND == VALUES) { r.y[i] = a.y[at]; r.ey[i] = a.ey[at]; }
+        }
+        // arrived ahead of whatever is asked for next
+#pragma unroll
+        for (int i = 0; i < 2 * TM; ++i) {
+            asm volatile("" : "+v"(r.ref[i]));
+            if constexpr (KIND == VALUES) { asm volatile("" : "+v"(r.y[i])); asm volatile("" : "+v"(r.ey[i])); }
+        }
+        return r;
+    }
     template <int TM, int TN>
-    __device__ __forceinline__ void operator()(f32x4_t (&acc)[2 * TM][2 * TN], const TileRef& t, unsigned char* smem, int wm, int wn) const {
-        constexpr int FM = 2 * TM, FN = 2 * TN, NS = FN / 4;
+    __device__ __forceinline__ void operator()(f32x4_t (&acc)[2 * TM][2 * TN], const TileRef& t, const Rows& row, unsigned char* smem, int wm, int wn) const {
+        // Columns behind the last one, in the last column of tiles, have a copy of the code of their own: a write to the accumulators, or a branch around a part of
+        // this, would have all of them copied to vector registers, and others spilled
+        if (t.n0 + 64 * TN > a.V) write_out<TM, TN, true>(acc, t, row, smem, wm, wn);
+        else write_out<TM, TN, false>(acc, t, row, smem, wm, wn);
+    }
+    template <int TM, int TN, bool EDGE>
+    __device__ __forceinline__ void write_out(f32x4_t (&acc)[2 * TM][2 * TN], const TileRef& t, const Rows& row, unsigned char* smem, int wm, int wn) const {
+        constexpr int FN = 2 * TN, NS = FN / 4;
+        const int rows = n_rows;
         int ln = threadIdx.x & 63;
         asm volatile("" : "+v"(ln));            // rebuilt for each tile, not carried through the products
         const int l16 = ln & 15, g4 = ln >> 4;
-        const int n0 = t.n0 + wn * (32 * TN), mw = t.m0 + wm * (32 * TM);
-        if (t.n0 + 64 * TN > a.V) {             // columns behind the last: the product's zeros become probabilities of 0
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int j = 0; j < FN; ++j)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v)
-                        if (n0 + j * 16 + 4 * g4 + v >= a.V) acc[i][j][v] = -INFINITY;
-        }
+        const int n0 = t.n0 + wn * (32 * TN), mw = t.m0 + wm * (32 * TM), left = a.V - n0 - 4 * g4;
         const bool store = KIND != MAXIMA && t.n0 < a.store_end;
         constexpr int RBY = 64 * TN, CPR = RBY / 16, RPP = 64 / CPR, NP = 32 / RPP, NV = CPR / RPP;     // as in the products' own write-out
         unsigned char* stg = smem + GEMM_RING + ((wm * 2 + wn) * 8192);
         const int c = ln % CPR, rl = ln / CPR, col = n0 + c * 8;
         const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(
-            (bf16_t*)a.e + (int64_t)mw * a.lde, 0, max(0, min(rows - mw, 32 * TM)) * a.lde * 2, 0x00020000);
+            (bf16_t*)a.e + (int64_t)mw * a.lde, 0, store ? max(0, min(rows - mw, 32 * TM)) * a.lde * 2 : 0, 0x00020000);       // nothing is stored: an empty range
         const unsigned voff = col - a.c0 < a.lde ? (unsigned)(rl * a.lde + (col - a.c0)) * 2u : 0x80000000u;
         const unsigned char* rd[NV];
 #pragma unroll
         for (int v = 0; v < NV; ++v) rd[v] = stg + rl * RBY + ((c ^ ((rl + RPP * v) & (CPR - 1))) << 4);
         unsigned char* const wr = stg + l16 * RBY + (g4 & 1) * 8;
         const int wsw = l16 & (CPR - 1), wch = g4 >> 1;
+        float* const sums = a.sums + (int64_t)(n0 / STRIP) * a.ldn + mw + l16;
+        bool beyond = false;
 #pragma unroll
         for (int i2 = 0; i2 < TM; ++i2) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int i = 2 * i2 + h, m = mw + i * 16 + l16;
-                const float ref = m < rows ? a.ref[m] : INFINITY;
+                const int i = 2 * i2 + h;
+                const float ref = row.ref[i];
                 const bool dead = ref == INFINITY;
-                int yrel = -1;
-                float ey = 0.f;
-                if (KIND == VALUES && m < rows) {
-                    yrel = a.y[m] - n0 - 4 * g4;
-                    ey = a.ey[m];
-                }
+                const int yrel = KIND == VALUES ? row.y[KIND == VALUES ? i : 0] - n0 - 4 * g4 : -1;
+                const float ey = row.ey[KIND == VALUES ? i : 0];
                 const unsigned mask = dead ? 0u : ~0u;          // whatever such a row holds, NaN included
 #pragma unroll
                 for (int z = 0; z < NS; ++z) {
                     float s = 0.f, mx = -INFINITY;
-                    if (KIND == MAXIMA) {
+                    if constexpr (KIND == MAXIMA) {
 #pragma unroll
                         for (int j = 4 * z; j < 4 * z + 4; ++j)
 #pragma unroll
-                            for (int v = 0; v < 4; ++v) mx = fmaxf(mx, acc[i][j][v]);
+                            for (int v = 0; v < 4; ++v) mx = !EDGE || j * 16 + v < left ? fmaxf(mx, acc[i][j][v]) : mx;
                         mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
                         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
                         mx *= a.k;
@@ -147,35 +165,37 @@ template <int KIND> struct LeaveLogits {
 #pragma unroll
                         for (int v = 0; v < 4; ++v) {
                             e[v] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][v], a.k, -r));
-                            if (KIND != VALUES) s += e[v];
+                            if constexpr (EDGE) e[v] = j * 16 + v < left ? e[v] : 0.f;
+                            if constexpr (KIND != VALUES) s += e[v];
                             else e[v] = yrel == j * 16 + v ? ey : e[v];
                         }
-                        if (store) {
+                        if constexpr (KIND != MAXIMA) {
                             uint2 o;
                             o.x = pack_bf16x2(e[0], e[1]) & mask;
                             o.y = pack_bf16x2(e[2], e[3]) & mask;
                             *reinterpret_cast<uint2*>(wr + h * 16 * RBY + (((2 * j + wch) ^ wsw) << 4)) = o;
                         }
                     }
-                    if (KIND != VALUES) {
+                    if constexpr (KIND != VALUES) {
                         s += __shfl_xor(s, 16, 64);
                         s += __shfl_xor(s, 32, 64);
-                        if (g4 == 0 && m < rows && n0 + z * STRIP < a.V) {
-                            a.sums[(int64_t)(n0 / STRIP + z) * a.ldn + m] = KIND == MAXIMA ? mx + log2f(s) : s;
-                            if (KIND == SUMS && !dead && !(s <= FLAG_ABOVE)) a.flags[0] = a.flags[1 + (m >> 8)] = 1;
-                        }
+                        if (KIND == SUMS) beyond |= !dead && !(s <= FLAG_ABOVE);
+                        if (g4 == 0 && mw + i * 16 + l16 < rows && (!EDGE || n0 + z * STRIP < a.V)) sums[(int64_t)z * a.ldn + i * 16] = KIND == MAXIMA ? mx + log2f(s) : s;
                     }
+                    CF_SCHED_FENCE();       // strip by strip: what is spilled comes back behind the next tile's loads
                 }
             }
-            if (store) {
+            if constexpr (KIND != MAXIMA) {
                 u32x4_t val[NP];
 #pragma unroll
                 for (int q = 0; q < NP; ++q) val[q] = *reinterpret_cast<const u32x4_t*>(rd[q % NV] + q * RPP * RBY);
 #pragma unroll
                 for (int q = 0; q < NP; ++q)
                     __builtin_amdgcn_raw_buffer_store_b128(val[q], rc, voff + (unsigned)((i2 * 32 + q * RPP) * a.lde) * 2u, 0, 0);
+                CF_SCHED_FENCE();
             }
         }
+        if (KIND == SUMS && beyond) a.flags[0] = a.flags[1 + (t.m0 >> 8)] = 1;
     }
 };
 
@@ -486,27 +506,33 @@ struct LeaveSlots {
     static constexpr bool OWN = true, LDA = true;
     float* slot;
     bool first;
+    struct Rows {};
+    template <int TM> __device__ __forceinline__ Rows rows(const TileRef&, int) const { return {}; }
     template <int TM, int TN>
-    __device__ __forceinline__ void operator()(f32x4_t (&acc)[2 * TM][2 * TN], const TileRef& t, unsigned char*, int wm, int wn) const {
+    __device__ __forceinline__ void operator()(f32x4_t (&acc)[2 * TM][2 * TN], const TileRef& t, const Rows&, unsigned char*, int wm, int wn) const {
         constexpr int FM = 2 * TM, FN = 2 * TN;
         int ln = threadIdx.x & 63;
         asm volatile("" : "+v"(ln));
-        const int mw = t.m0 + wm * (32 * TM), n = t.n0 + wn * (32 * TN) + 4 * (ln >> 4);
+        const int mw = t.m0 + wm * (32 * TM), have = min(t.M - mw, 32 * TM), n = t.n0 + wn * (32 * TN) + 4 * (ln >> 4);
+        const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(slot + (int64_t)mw * t.N, 0, have > 0 ? have * t.N * 4 : 0, 0x00020000);
+        const unsigned row_bytes = (unsigned)t.N * 4u, voff = (unsigned)(ln & 15) * row_bytes + (unsigned)n * 4u;
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-            const int m = mw + i * 16 + (ln & 15);
-            if (m >= t.M) continue;
-            float* p = slot + (int64_t)m * t.N + n;
+            u32x4_t old[FN];
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
-                if (n + j * 16 >= t.N) continue;
-                float4 o = make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
-                if (!first) {
-                    const float4 b = *reinterpret_cast<const float4*>(p + j * 16);
-                    o.x += b.x; o.y += b.y; o.z += b.z; o.w += b.w;
-                }
-                *reinterpret_cast<float4*>(p + j * 16) = o;
+                old[j] = u32x4_t{0u, 0u, 0u, 0u};
+                if (!first)
+                    old[j] = __builtin_amdgcn_raw_buffer_load_b128(rc, n + j * 16 < t.N ? voff + (unsigned)(i * 16) * row_bytes + j * 64u : 0x80000000u, 0, 0);
             }
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                u32x4_t o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(acc[i][j][e] + __uint_as_float(old[j][e]));
+                __builtin_amdgcn_raw_buffer_store_b128(o, rc, n + j * 16 < t.N ? voff + (unsigned)(i * 16) * row_bytes + j * 64u : 0x80000000u, 0, 0);
+            }
+            CF_SCHED_FENCE();
         }
     }
 };
