@@ -703,7 +703,7 @@ def embed_fwd(table, tokens, scale: float = 1.0, out=None):
     V, H = table.shape
     shape = (*tokens.shape, H)
     if out is None:
-        out = torch.empty(shape, dtype=table.dtype, device=table.device)
+        out = table.new_empty(shape)
     else:
         _dense(out, table.dtype, shape, "out")
         _need(not _ranges_meet(out, table), "out must not overlap table")
@@ -758,7 +758,7 @@ def norm_fwd(x, g, b=None, eps: float = 1e-5, layer: bool = False, idx=None, n_k
     n = max_kept if max_kept is not None else rows if idx is None else idx.numel()
     _kept_count(idx, n_kept_dev, rows, n)
     if out is None:
-        out = torch.empty((n, H), dtype=x.dtype, device=x.device)
+        out = x.new_empty((n, H))
     else:
         _dense(out, x.dtype, (n, H), "out")
         _need(not _ranges_meet(out, x) or (idx is None and out.data_ptr() == x.data_ptr()), "out must not overlap x, or be x without idx")

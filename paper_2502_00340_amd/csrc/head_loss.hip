@@ -475,7 +475,14 @@ __global__ __launch_bounds__(1024) void head_finish_kernel(HeadArgs a, LossArgs 
             // e of the other columns is relative to exp(lp) (flagged: to 1)
             const float by = flagged ? 1.f : s;
             fy = -rl.coef * l.scale / by;
-            const float ey = expm1f(lp) * by;
+            float ey = expm1f(lp) * by;
+            if constexpr (sizeof(T) == 2) {
+                // The target's e is most of a row's gradient.  Its rounding goes over to the row's factor, so that factor times e is exact at the target and
+                // off by that rounding, and their own, at the other columns: gradients 1.4 times as far off as one rounding instead of 1.7.
+                const float r = bf16_to_f32(narrow_one<bf16_t>(ey)), by_r = ey / r;
+                if (by_r > 0.5f && by_r < 2.f) fy *= by_r;
+                ey = r;
+            }
             a.ey[j] = ey;
             if (a.e != nullptr && !flagged && y < a.store_end) ((T*)a.e)[(int64_t)j * a.lde + y] = narrow_one<T>(ey);
         }

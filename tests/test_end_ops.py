@@ -457,13 +457,15 @@ def _head_check(got, x, table, y, dtype, policy=None, w=None, scale=1.0, norm=0.
     hot[ok, y[ok]] = 1.0
     shape = torch.where(dead[:, None], torch.zeros((), dtype=F64, device=DEV), (p - hot).abs())
     err = d.abs() * rel[:, None] + extra * shape + cw * p * (dlp * slope)[:, None] * ~dead[:, None]
+    # bf16: the target's e is exact, with its rounding taken over by the row's factor, so that the other columns have two: that one and their own
+    re = torch.where(hot > 0, 0.0, 2 * EPS[dtype]) if dtype is BF else EPS[dtype]
     if got[2] is not None:
         # below 2^-126, the smallest normal number of both types, a stored e (times a factor of at most cw and its row of the table) or a result may be 0
-        tol = (d.abs() * (EPS[dtype] + V * U) + err + 2.0 ** -126 * cw) @ at + dx.abs() * EPS[dtype] + 2.0 ** -126
+        tol = (d.abs() * (re + V * U) + err + 2.0 ** -126 * cw) @ at + dx.abs() * EPS[dtype] + 2.0 ** -126
         close(got[2], dx, tol, "dx")
     if got[3] is not None:
         # the same for e (times x) and for a scaled input, times an e of at most 2^58 in each of a strip's columns
-        tol = (d.abs() * (2 * EPS[dtype] + (n + 4) * U) + err + 2.0 ** -126 * cw).T @ ax + n * 2.0 ** (58 - 126) + 2.0 ** -126
+        tol = (d.abs() * (re + EPS[dtype] + (n + 4) * U) + err + 2.0 ** -126 * cw).T @ ax + n * 2.0 ** (58 - 126) + 2.0 ** -126
         want = dt if main is None else dt + main.to(F64)
         close(got[3], want, tol + want.abs() * (EPS[dtype] if main is None else U), "dtable")
 
