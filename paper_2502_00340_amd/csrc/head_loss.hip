@@ -634,10 +634,12 @@ __global__ __launch_bounds__(256) void head_dx_sum_kernel(const float* __restric
 // The same steps with fp32 operands on the bf16 matrix cores: a value is the sum of three bf16 numbers, each the rounded rest of what is ahead of it, x = x1 + x2 + x3
 // but for 2^-27 of x, and a product the sum of the six of the nine partial ones that are not below 2^-26 of it: x1 y1 + x1 y2 + x2 y1 + x2 y2 + x1 y3 + x3 y1, all in
 // one fp32 accumulator.  That is fp32 accuracy at a sixth of the bf16 rate, 2.7 times that of the fp32 matrix instruction (values beyond 3.39e38 round to infinity).
-// Tiles of 128x128, four waves of 64x64, steps of 32 k: operands go from memory to registers, a step ahead, and from there, split, to three planes in LDS; two
+// Tiles of 128x128, four waves of 64x64, steps of 32 k: operands go from memory to registers, a step ahead, and from there, split, to three planes in LDS; three
 // blocks a CU cover each other's barriers.  MODE 0: A and B with k contiguous, 1: both k-major, 2: A contiguous, B k-major.  Planes of a k-contiguous operand are
 // [row][32 k], 16-byte chunks XOR-ed with a function of the row that keeps the 16 lanes of one pass of a ds_read_b128 apart; of a k-major one [k][row], read
 // transposed.  D = B-frag x A-frag: lane l holds row l % 16 and columns 4 * (l / 16) .. +3 of a fragment, as in the bf16 products.
+// three blocks a CU at the price of a few spilled registers: logits 227 -> 208 us, the table's gradient 207 -> 193 (301 rows, [50257, 840])
+#define F32_BOUNDS __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3)))
 constexpr int F32_STEP = 32, F32_PLANE = 128 * F32_STEP * 2, F32_SMEM = 6 * F32_PLANE;
 
 struct F32Tile {
@@ -725,7 +727,7 @@ template <int MODE> __device__ __forceinline__ void f32_tile(const F32Tile& t, u
         put(ra, sa, AK);
         put(rb, sb, BK);
         lds_barrier();
-        // Nothing behind the last step.  One step ahead is enough with two blocks a CU (two: 284 and 277 us for 225 and 201, in 236 registers)
+        // Nothing behind the last step.  One step ahead is enough with several blocks a CU (two, in 236 registers: dx 284 us for 225)
         fetch(ra, t.A, t.lda, t.m0, t.M, va, k + F32_STEP, AK);
         fetch(rb, t.B, t.ldb, t.n0, t.N, vb, k + F32_STEP, BK);
         CF_SCHED_FENCE();
@@ -749,7 +751,7 @@ template <int MODE> __device__ __forceinline__ void f32_tile(const F32Tile& t, u
     }
 }
 
-template <int KIND> __global__ __launch_bounds__(256) void head_logits_f32_kernel(HeadArgs a) {
+template <int KIND> __global__ F32_BOUNDS void head_logits_f32_kernel(HeadArgs a) {
     __shared__ __align__(16) unsigned char smem[F32_SMEM];
     if (a.flagged_only && a.flags[0] == 0) return;
     const int rows = live_rows(a.n_max, a.n_dev), tm = (rows + 127) / 128, tn = (a.c1 - a.c0 + 127) / 128;
@@ -806,7 +808,7 @@ template <int KIND> __global__ __launch_bounds__(256) void head_logits_f32_kerne
     }
 }
 
-__global__ __launch_bounds__(256) void head_dx_f32_kernel(DxArgs a) {
+__global__ F32_BOUNDS void head_dx_f32_kernel(DxArgs a) {
     __shared__ __align__(16) unsigned char smem[F32_SMEM];
     const int rows = live_rows(a.n_max, a.n_dev), tm = (rows + 127) / 128, tn = (a.H + 127) / 128, tiles = tm * tn, items = tiles * a.parts;
     const int steps = (a.K + F32_STEP - 1) / F32_STEP, per = (steps + a.parts - 1) / a.parts;
@@ -837,7 +839,7 @@ __global__ __launch_bounds__(256) void head_dx_f32_kernel(DxArgs a) {
     }
 }
 
-template <bool MAIN> __global__ __launch_bounds__(256) void head_dtable_f32_kernel(DtableArgs a) {
+template <bool MAIN> __global__ F32_BOUNDS void head_dtable_f32_kernel(DtableArgs a) {
     __shared__ __align__(16) unsigned char smem[F32_SMEM];
     const int rows = live_rows(a.n_max, a.n_dev), tm = (a.K + 127) / 128, tn = (a.H + 127) / 128;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
@@ -871,7 +873,7 @@ template <bool MAIN> __global__ __launch_bounds__(256) void head_dtable_f32_kern
 // Parts of dx's contraction over the vocabulary: the fewest rounds of the blocks that are resident at a time per part.  A part costs its slot (written and read at
 // 5 TB/s) and a start of three microseconds; a whole contraction of a 256x256 bf16 tile takes V * 26 ns, of a 128x128 fp32 one V * 100 ns.
 static int dx_parts(int64_t tiles, int V, int dtype, int n_cu) {
-    const int64_t resident = (int64_t)n_cu * (dtype == CF_F32 ? 2 : 1);
+    const int64_t resident = (int64_t)n_cu * (dtype == CF_F32 ? 3 : 1);
     const double part = (dtype == CF_F32 ? 0.25 * (double)tiles + 30.0 : 4.0 * (double)tiles + 115.0) / V;
     int best = 1;
     double least = 1e30;
