@@ -269,6 +269,7 @@ template <int KIND> __global__ __launch_bounds__(256) void head_logits_kernel(He
 template <int NF, int P> __global__ __launch_bounds__(512) void head_few_kernel(HeadArgs a) {
     constexpr int R = P + 1, ROWS = 16 * NF, SLOT = ROWS * 128, XL = NF > 4 ? NF / 4 : 1, NB = 2;            // XL, NB: loads of a wave and step
     extern __shared__ __align__(16) unsigned char smem[];
+    unsigned char* const stage = smem + R * SLOT;       // a tile's exponentials, [row][128 columns], 16-byte chunks XOR-ed with the row
     __shared__ float red[8][ROWS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
     const int rows = __builtin_amdgcn_readfirstlane(live_rows(a.n_max, a.n_dev)), H = a.H, steps = (H + 63) / 64;
@@ -339,14 +340,20 @@ template <int NF, int P> __global__ __launch_bounds__(512) void head_few_kernel(
                 e[v] = c + v < a.V ? e[v] : 0.f;
                 sum[i] += e[v];
             }
-            const int m = i * 16 + l16;
-            if (a.store_end > 0 && m < rows && c < a.lde) {         // zeros behind the last column, too
+            if (a.store_end > 0) {
                 const bool dead = ref[i] == INFINITY;
                 uint2 o;
                 o.x = dead ? 0u : pack_bf16x2(e[0], e[1]);
                 o.y = dead ? 0u : pack_bf16x2(e[2], e[3]);
-                *reinterpret_cast<uint2*>((bf16_t*)a.e + (int64_t)m * a.lde + c) = o;
+                *reinterpret_cast<uint2*>(stage + (i * 16 + l16) * 256 + (((2 * wave + (g4 >> 1)) ^ l16) << 4) + (g4 & 1) * 8) = o;
             }
+        }
+        if (a.store_end == 0 || tile * TILE >= a.lde) return;
+        lds_barrier();          // the next one that writes here has the barrier of a step ahead of it
+        for (int v = threadIdx.x; v < rows * 16; v += 512) {            // whole rows of the tile; zeros behind the last column, too
+            const int m = v >> 4, ch = v & 15, col = tile * TILE + ch * 8;
+            if (col < a.lde)
+                *reinterpret_cast<u32x4_t*>((bf16_t*)a.e + (int64_t)m * a.lde + col) = *reinterpret_cast<const u32x4_t*>(stage + m * 256 + ((ch ^ (m & 15)) << 4));
         }
     };
     const int frag = l16 * 128, ch0 = (g4 ^ nt_swz(l16)) << 4, ch1 = ((4 + g4) ^ nt_swz(l16)) << 4;
@@ -598,6 +605,98 @@ template <bool CF32> __global__ __launch_bounds__(256) void head_dtable_kernel(D
         t = TileRef{0, 0, a.K, a.H, a.e, a.xs, a.out};
         tile_coords(l, tm, tn, bm, bn);
     }, smem);
+}
+
+// The same for few rows, a write of the gradient with little to compute: a block holds the fragments of x' for 256 columns in its registers and walks through
+// tiles of 64 rows of the table, whose exponentials it reads transposed from LDS.  A lane's four fragments of x' are columns 16 * (l / 16) + 4 j .. +3 of its wave's 64,
+// so that it ends up with 16 adjacent columns of a row of the gradient.
+constexpr int DT_FEW_ROWS = 128, DT_TILE = 64;
+template <int KS, bool CF32> __global__ __launch_bounds__(256) void head_dtable_few_kernel(DtableArgs a, int per) {
+    constexpr int ROWS = 32 * KS;
+    __shared__ __align__(16) unsigned char xs[ROWS * 512];          // [row][256 columns], then twice [row][64 columns of e]
+    const int rows = live_rows(a.n_max, a.n_dev), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, g4 = lane >> 4;
+    const int hb = (a.H + 255) / 256, h0 = (int)blockIdx.x % hb * 256, tiles = (a.K + DT_TILE - 1) / DT_TILE;
+    const int first = (int)blockIdx.x / hb * per, end = min(tiles, first + per);
+    if (first >= end) return;
+    // fragments are read transposed; of a row's chunks of 16 bytes those of 64 are XOR-ed with its number, so that the four rows of a read fall into different banks
+    auto swz = [](int k, bool wide) { return wide ? (k & 3) << 2 : (k & 2) << 1; };
+    auto frag = [&](unsigned char* s, bool wide, int ks, int col0) __attribute__((always_inline)) {
+        const int row_bytes = wide ? 512 : 128, kl = ks * 32 + 8 * g4 + (l16 >> 2), ch = col0 / 8 + ((lane & 3) >> 1);
+        unsigned char* p = s + kl * row_bytes + ((ch ^ swz(kl, wide)) << 4) + (lane & 1) * 8;
+        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(__attribute__((address_space(3))) unsigned char*)p);
+        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(__attribute__((address_space(3))) unsigned char*)(p + 4 * row_bytes));
+        return __builtin_bit_cast(bf16x8_t, (s16x8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    const u32x4_t zero = {0u, 0u, 0u, 0u};
+    for (int v = tid; v < ROWS * 32; v += 256) {
+        const int k = v >> 5, c = v & 31, h = h0 + c * 8;
+        u32x4_t w = zero;
+        if (k < rows && h < a.H) w = *reinterpret_cast<const u32x4_t*>((const bf16_t*)a.xs + (int64_t)k * a.H + h);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {          // four columns u of a group of 64: column 16 q + 4 j of them stands at 16 j + 4 q
+            const int u = (c & 7) * 2 + half, at = (u & 3) * 4 + (u >> 2), ch = (c >> 3) * 8 + (at >> 1);
+            *reinterpret_cast<uint2*>(xs + k * 512 + ((ch ^ swz(k, true)) << 4) + (at & 1) * 8) = half == 0 ? make_uint2(w.x, w.y) : make_uint2(w.z, w.w);
+        }
+    }
+    u32x4_t e[KS];
+    auto fetch = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < KS; ++u) {
+            const int k = (tid >> 3) + 32 * u, col = t * DT_TILE + (tid & 7) * 8;
+            e[u] = zero;
+            if (k < rows && col < a.lde && t < end) e[u] = *reinterpret_cast<const u32x4_t*>((const bf16_t*)a.e + (int64_t)k * a.lde + col);
+        }
+    };
+    fetch(first);
+    __syncthreads();
+    bf16x8_t fx[4][KS];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) fx[j][ks] = frag(xs, true, ks, wave * 64 + j * 16);
+    __syncthreads();
+    const int h = h0 + wave * 64 + g4 * 16;
+    for (int t = first; t < end; ++t) {
+        unsigned char* s = xs + (t & 1) * (ROWS * 128);
+#pragma unroll
+        for (int u = 0; u < KS; ++u) {
+            const int k = (tid >> 3) + 32 * u;
+            *reinterpret_cast<u32x4_t*>(s + k * 128 + (((tid & 7) ^ swz(k, false)) << 4)) = e[u];
+        }
+        lds_barrier();
+        fetch(t + 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f32x4_t acc[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const bf16x8_t fe = frag(s, false, ks, i * 16);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[j][ks], fe, acc[j], 0, 0, 0);
+            }
+            const int c = t * DT_TILE + i * 16 + l16;
+            if (c >= a.K) continue;
+            const int64_t at = (int64_t)c * a.H + h;
+            if constexpr (CF32) {
+                float4* p = reinterpret_cast<float4*>((float*)a.out + at);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (h + 4 * j < a.H) {
+                        const float4 b = p[j];
+                        p[j] = make_float4(b.x + acc[j][0], b.y + acc[j][1], b.z + acc[j][2], b.w + acc[j][3]);
+                    }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; j += 2)
+                    if (h + 4 * j < a.H)
+                        *reinterpret_cast<u32x4_t*>((bf16_t*)a.out + at + 4 * j) =
+                            u32x4_t{pack_bf16x2(acc[j][0], acc[j][1]), pack_bf16x2(acc[j][2], acc[j][3]), pack_bf16x2(acc[j + 1][0], acc[j + 1][1]),
+                                    pack_bf16x2(acc[j + 1][2], acc[j + 1][3])};
+            }
+        }
+    }
 }
 
 // ---- 5. dx -------------------------------------------------------------------------------------------------
@@ -936,7 +1035,7 @@ template <> struct HeadLaunch<bf16_t> {
     }
     template <int NF> static hipError_t few(const HeadArgs& a, hipStream_t st) {
         static std::atomic<uint64_t> lds_ok{0};
-        constexpr int P = 8, lds = (P + 1) * NF * 16 * 128;
+        constexpr int P = NF > 4 ? 6 : 8, lds = (P + 1) * NF * 16 * 128 + NF * 16 * 256;
         const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&head_few_kernel<NF, P>), lds, lds_ok);
         if (e != hipSuccess) return e;
         head_few_kernel<NF, P><<<a.strips, 512, lds, st>>>(a);
@@ -956,7 +1055,14 @@ template <> struct HeadLaunch<bf16_t> {
         head_dx_kernel<<<(int)std::min<int64_t>(items, compute_units()), 256, GEMM_SMEM, st>>>(a);
         return hipGetLastError();
     }
+    template <int KS> static hipError_t dtable_few(const DtableArgs& a, bool main, hipStream_t st) {
+        const int hb = ceil_div(a.H, 256), tiles = ceil_div(a.K, DT_TILE), per = ceil_div(tiles, std::max(1, 4 * compute_units() / hb)), grid = hb * ceil_div(tiles, per);
+        if (main) head_dtable_few_kernel<KS, true><<<grid, 256, 0, st>>>(a, per);
+        else head_dtable_few_kernel<KS, false><<<grid, 256, 0, st>>>(a, per);
+        return hipGetLastError();
+    }
     static hipError_t dtable(DtableArgs a, bool main, hipStream_t st) {
+        if (a.n_max <= DT_FEW_ROWS) return a.n_max <= 32 ? dtable_few<1>(a, main, st) : a.n_max <= 64 ? dtable_few<2>(a, main, st) : dtable_few<4>(a, main, st);
         static std::atomic<uint64_t> lds_ok[2];
         void (*const kernel)(DtableArgs) = main ? head_dtable_kernel<true> : head_dtable_kernel<false>;
         const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), GEMM_SMEM, lds_ok[main]);
