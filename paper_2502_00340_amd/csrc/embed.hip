@@ -404,6 +404,67 @@ __global__ __launch_bounds__(256) void embed_join_kernel(SumArgs a) {
     }
 }
 
+// ---- few rows ------------------------------------------------------------------------------------------------
+// One launch instead of three: each row's block finds the rows with its token among up to 256, leaves if one of them is ahead, and adds them up in order.
+constexpr int FEW_ROWS = 256;
+
+template <typename T, bool MAIN>
+__global__ __launch_bounds__(256) void embed_few_kernel(SumArgs a, const int64_t* __restrict__ tokens, const int32_t* __restrict__ idx) {
+    constexpr int VN = Vec<T>::N, U = 8;
+    __shared__ int key[FEW_ROWS], list[FEW_ROWS];
+    __shared__ uint64_t same[4];
+    const int n_rows = live_rows(a.n_max, a.n_dev), tid = threadIdx.x, wave = tid >> 6, vpr = a.H / VN, tiles = (vpr + 255) / 256, j = (int)blockIdx.x / tiles;
+    if (j >= n_rows) return;
+    int mine = a.V;
+    if (tid < n_rows) {
+        const int64_t t = tokens[idx != nullptr ? idx[tid] : tid];
+        if (t >= 0 && t < a.V) mine = (int)t;
+    }
+    key[tid] = mine;
+    __syncthreads();
+    const int t = key[j];
+    const bool hit = mine == t;
+    const uint64_t b = __ballot(hit);
+    if ((tid & 63) == 0) same[wave] = b;
+    __syncthreads();
+    if (t >= a.V) return;
+    int at = __popcll(b & ((1ull << (tid & 63)) - 1ull)), n = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const int c = __popcll(same[w]);
+        at += w < wave ? c : 0;
+        n += c;
+    }
+    if (hit) list[at] = tid;
+    __syncthreads();
+    if (list[0] != j) return;
+    const int v = (int)blockIdx.x % tiles * 256 + tid;
+    if (v >= vpr) return;
+    const int c = v * VN;
+    float old[VN] = {}, s[VN] = {};
+    if constexpr (MAIN) {
+        const float4* p = reinterpret_cast<const float4*>((const float*)a.out + (int64_t)t * a.H + c);
+#pragma unroll
+        for (int q = 0; q < VN / 4; ++q) {
+            const float4 w = p[q];
+            old[4 * q] = w.x; old[4 * q + 1] = w.y; old[4 * q + 2] = w.z; old[4 * q + 3] = w.w;
+        }
+    }
+    for (int k = 0; k < n; k += U) {
+        u32x4_t x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const u32x4_t*>((const T*)a.dx + (int64_t)list[min(k + u, n - 1)] * a.H + c);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float o[VN];
+            Vec<T>::load(reinterpret_cast<const T*>(&x[u]), o);
+#pragma unroll
+            for (int e = 0; e < VN; ++e) s[e] += k + u < n ? o[e] : 0.f;
+        }
+    }
+    embed_out<T, MAIN>(a, t, c, s, old);
+}
+
 // workspace: the order (twice where spans have to be merged), then the parts
 struct EmbedWs {
     size_t order, part, total;
@@ -430,16 +491,20 @@ static hipError_t launch_embed_bwd(SumArgs a, SortArgs so, unsigned char* ws, hi
         const int64_t blocks = MAIN ? 0 : (so.n_zero + threads - 1) / threads;
         return (int)(blocks < MAX_GRID / 2 ? blocks : MAX_GRID / 2);
     };
+    if (n <= FEW_ROWS) {
+        if (!MAIN) embed_rank_kernel<<<fill(RANK_THREADS), RANK_THREADS, 0, st>>>(so, 0);      // clears the table
+        if (n > 0) embed_few_kernel<T, MAIN><<<n * ceil_div(a.H / Vec<T>::N, 256), 256, 0, st>>>(a, so.tokens, so.idx);
+        return hipGetLastError();
+    }
     if (n <= SPAN) {
         const int rank_blocks = ceil_div(n, RANK_ROWS), grid = rank_blocks + fill(RANK_THREADS);
-        if (grid > 0) embed_rank_kernel<<<grid, RANK_THREADS, 0, st>>>(so, rank_blocks);
+        embed_rank_kernel<<<grid, RANK_THREADS, 0, st>>>(so, rank_blocks);
     } else {
         static std::atomic<uint64_t> lds_ok{0};
         const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&embed_sort_kernel), SORT_LDS, lds_ok);
         if (e != hipSuccess) return e;
         embed_sort_kernel<<<so.spans + fill(SORT_THREADS), SORT_THREADS, SORT_LDS, st>>>(so);
     }
-    if (n == 0) return hipGetLastError();
     a.tok = so.tok;
     a.row = so.row;
     if (so.spans > 1) {

@@ -656,6 +656,7 @@ template <int KS, bool CF32> __global__ __launch_bounds__(256) void head_dtable_
         for (int ks = 0; ks < KS; ++ks) fx[j][ks] = frag(xs, true, ks, wave * 64 + j * 16);
     __syncthreads();
     const int h = h0 + wave * 64 + g4 * 16;
+    unsigned char* const stage = xs + 2 * ROWS * 128 + wave * 2048;
     for (int t = first; t < end; ++t) {
         unsigned char* s = xs + (t & 1) * (ROWS * 128);
 #pragma unroll
@@ -676,11 +677,10 @@ template <int KS, bool CF32> __global__ __launch_bounds__(256) void head_dtable_
 #pragma unroll
                 for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[j][ks], fe, acc[j], 0, 0, 0);
             }
-            const int c = t * DT_TILE + i * 16 + l16;
-            if (c >= a.K) continue;
-            const int64_t at = (int64_t)c * a.H + h;
             if constexpr (CF32) {
-                float4* p = reinterpret_cast<float4*>((float*)a.out + at);
+                const int c = t * DT_TILE + i * 16 + l16;
+                if (c >= a.K) continue;
+                float4* p = reinterpret_cast<float4*>((float*)a.out + (int64_t)c * a.H + h);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     if (h + 4 * j < a.H) {
@@ -688,12 +688,19 @@ template <int KS, bool CF32> __global__ __launch_bounds__(256) void head_dtable_
                         p[j] = make_float4(b.x + acc[j][0], b.y + acc[j][1], b.z + acc[j][2], b.w + acc[j][3]);
                     }
             } else {
+                // by way of 2 KB of the wave's own to whole lines past the caches: what stays in the last one has to leave it under the next call's reading
+                // of the table (64 rows, [128256, 4096]: this and that 193 + 257 us cached, 203 + 200 so; 16 rows, [50257, 2048] 37 + 54, 40 + 39)
 #pragma unroll
                 for (int j = 0; j < 4; j += 2)
-                    if (h + 4 * j < a.H)
-                        *reinterpret_cast<u32x4_t*>((bf16_t*)a.out + at + 4 * j) =
-                            u32x4_t{pack_bf16x2(acc[j][0], acc[j][1]), pack_bf16x2(acc[j][2], acc[j][3]), pack_bf16x2(acc[j + 1][0], acc[j + 1][1]),
-                                    pack_bf16x2(acc[j + 1][2], acc[j + 1][3])};
+                    *reinterpret_cast<u32x4_t*>(stage + l16 * 128 + (((2 * g4 + (j >> 1)) ^ (l16 & 7)) << 4)) =
+                        u32x4_t{pack_bf16x2(acc[j][0], acc[j][1]), pack_bf16x2(acc[j][2], acc[j][3]), pack_bf16x2(acc[j + 1][0], acc[j + 1][1]),
+                                pack_bf16x2(acc[j + 1][2], acc[j + 1][3])};
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int r = half * 8 + (lane >> 3), c = t * DT_TILE + i * 16 + r, col = h0 + wave * 64 + (lane & 7) * 8;
+                    const u32x4_t w = *reinterpret_cast<const u32x4_t*>(stage + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
+                    if (c < a.K && col < a.H) __builtin_nontemporal_store(w, reinterpret_cast<u32x4_t*>((bf16_t*)a.out + (int64_t)c * a.H + col));
+                }
             }
         }
     }
@@ -1056,7 +1063,7 @@ template <> struct HeadLaunch<bf16_t> {
         return hipGetLastError();
     }
     template <int KS> static hipError_t dtable_few(const DtableArgs& a, bool main, hipStream_t st) {
-        const int hb = ceil_div(a.H, 256), tiles = ceil_div(a.K, DT_TILE), per = ceil_div(tiles, std::max(1, 4 * compute_units() / hb)), grid = hb * ceil_div(tiles, per);
+        const int hb = ceil_div(a.H, 256), tiles = ceil_div(a.K, DT_TILE), per = ceil_div(tiles, std::max(1, 8 * compute_units() / hb)), grid = hb * ceil_div(tiles, per);
         if (main) head_dtable_few_kernel<KS, true><<<grid, 256, 0, st>>>(a, per);
         else head_dtable_few_kernel<KS, false><<<grid, 256, 0, st>>>(a, per);
         return hipGetLastError();
