@@ -391,8 +391,8 @@ cf_status cf_token_loss(const cf_loss_desc* desc, const void* logits, int64_t lo
  * a multiple of 8 in CF_BF16 and of 4 in CF_F32; tensors of elements are dense and 16-byte aligned; workspaces 256-byte aligned.
  *
  * cf_embed_fwd: out[t,:] = scale * table[tokens[t],:], table [V,H], out [n,H]; 0 for a token outside [0,V).  out must not overlap table.
- * cf_embed_bwd: dtable[c,:] = scale * sum of the rows j of dx_kept [max_kept,H] with tokens[idx[j]] == c, in ascending order of j with fp32 sums: a function
- *   of the inputs alone, with no atomics.  main_grad 0: all of dtable [V,H] is written in the storage dtype, zeros where no row has the token.  main_grad 1:
+ * cf_embed_bwd: dtable[c,:] = scale * sum of the rows j of dx_kept [max_kept,H] with tokens[idx[j]] == c, fp32 sums in an
+ *   order that tokens, idx and max_kept fix (no atomics).  main_grad 0: all of dtable [V,H] is written in the storage dtype, zeros where no row has the token.  main_grad 1:
  *   dtable is fp32 and is added to; rows without a token are not touched.  dx rows whose token lies outside [0,V) count for nothing, whatever they hold. */
 cf_status cf_embed_fwd(const void* table, int32_t V, int32_t H, int32_t dtype, const int64_t* tokens, int64_t n, float scale, void* out,
                        cf_stream stream);
@@ -424,7 +424,8 @@ cf_status cf_norm_bwd(const cf_norm_desc* desc, const void* x, const void* g, co
  *   so that a tied table's two gradients share one buffer).
  * The logits are fp32 values that are never stored.  What is kept of them for the gradients is bounded by the workspace: exponentials, in the storage
  * dtype, of as many columns as it has room for; those of the others are computed again, piece by piece.  A larger workspace is faster; logp and stats do not
- * depend on it, gradients by the order of fp32 sums.  For the same rows logp has the same bits with and without gradients.
+ * depend on it, gradients by the order of fp32 sums.  For the same rows and max_kept logp has the same bits with and without
+ * gradients.  max_kept at most 2^22; in CF_BF16 x_kept stays below 2 GiB; the table may be larger.
  *   cf_head_loss_workspace_bytes: what to provide for a call with (need_dx, need_dtable): as much as is of use, at most `limit`, or the least that will do
  *   where that is more.  0 for sizes that are refused. */
 size_t cf_head_loss_workspace_bytes(const cf_loss_desc* desc, int32_t H, int32_t max_kept, int32_t need_dx, int32_t need_dtable, size_t limit);

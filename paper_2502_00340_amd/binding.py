@@ -834,6 +834,7 @@ def head_loss(x, table, targets, old_logp=None, advantages=None, ref_logp=None, 
     for t in (old_logp, advantages, ref_logp, weights):
         if t is not None and not (t.dtype is torch.float32 and t.shape == (rows,) and t.is_contiguous()):
             raise ValueError("old_logp, advantages, ref_logp and weights have to be fp32 [%d]" % rows)
+    _need(ws_limit >= 0, "ws_limit counts bytes")
     code, dev = _dtype_code(x), x.device
     dx = dt = None
     if dx_out is not None:

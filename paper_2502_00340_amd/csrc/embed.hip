@@ -530,6 +530,11 @@ static hipError_t launch_embed_bwd(SumArgs a, SortArgs so, unsigned char* ws, hi
 
 using namespace cf;
 
+static bool ranges_meet(const void* a, uint64_t an, const void* b, uint64_t bn) {
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return an && bn && x < y + bn && y < x + an;
+}
+
 static bool off16(const void* p) { return (uintptr_t)p % 16 != 0; }
 
 static cf_status embed_sizes(int32_t V, int32_t H, int32_t dtype) {
@@ -547,6 +552,8 @@ cf_status cf_embed_fwd(const void* table, int32_t V, int32_t H, int32_t dtype, c
     if (ok != CF_OK) return ok;
     if (n < 0 || n > ((int64_t)1 << 40) / H || !(scale - scale == 0.f)) return CF_ERR_SHAPE;
     if (off16(table) || off16(out) || (uintptr_t)tokens % 8 != 0) return CF_ERR_SHAPE;
+    const uint64_t row = (uint64_t)H * dtype_size(dtype);
+    if (ranges_meet(out, n * row, table, V * row)) return CF_ERR_SHAPE;
     if (n == 0) return CF_OK;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     if (dtype == CF_F32) launch_embed_fwd<float>(table, tokens, n, V, H, scale, out, st);
@@ -567,6 +574,8 @@ cf_status cf_embed_bwd(const int64_t* tokens, const void* dx_kept, int32_t V, in
     if (ok != CF_OK) return ok;
     if (max_kept < 0 || max_kept > (1 << 30) || (main_grad != 0 && main_grad != 1) || !(scale - scale == 0.f)) return CF_ERR_SHAPE;
     if (off16(dx_kept) || off16(dtable) || (uintptr_t)tokens % 8 != 0 || (uintptr_t)idx % 4 != 0 || (uintptr_t)n_kept_dev % 4 != 0) return CF_ERR_SHAPE;
+    const uint64_t es = dtype_size(dtype);
+    if (ranges_meet(dtable, (uint64_t)V * H * (main_grad ? 4 : es), dx_kept, (uint64_t)max_kept * H * es)) return CF_ERR_SHAPE;
     if (!ws || (uintptr_t)ws % 256 != 0 || ws_bytes < cf_embed_bwd_workspace_bytes(H, max_kept)) return CF_ERR_WORKSPACE;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     int passes = 0;

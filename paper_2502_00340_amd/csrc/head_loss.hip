@@ -1021,7 +1021,7 @@ struct HeadWs {
             least = std::min(least, most);
         } else {                    // matrices below 2 GiB: 32-bit offsets
             const int64_t lim = ((int64_t)1 << 31) - 1;
-            most = std::min({most, lim / (2 * std::max<int64_t>(n, 256)) / 256 * 256, (lim / (2 * (int64_t)H) - 256) / 256 * 256});
+            most = std::min({most, lim / (2 * (std::max<int64_t>(n, 256) + 64)) / 256 * 256, (lim / (2 * (int64_t)H) - 256) / 256 * 256});
             least = std::min(least, most);
         }
         if (most < 256) { cap = -1; return; }
@@ -1161,7 +1161,8 @@ static cf_status head_sizes(const cf_loss_desc* d, int32_t H, int32_t max_kept) 
     if (!d) return CF_ERR_NULL;
     if (d->dtype != CF_BF16 && d->dtype != CF_F32) return CF_ERR_DTYPE;
     if (d->V <= 0 || d->V > (1 << 30) || H <= 0 || H % (d->dtype == CF_F32 ? 4 : 8) != 0 || max_kept < 0 || max_kept > (1 << 30)) return CF_ERR_SHAPE;
-    if (H > (1 << 20)) return CF_ERR_UNSUPPORTED;
+    // tiles, and threads of a launch, are counted in 32 bits
+    if (H > (1 << 20) || max_kept > (1 << 22) || (int64_t)ceil_div(max_kept, 256) * ceil_div(d->V, 256) >= (1 << 29)) return CF_ERR_UNSUPPORTED;
     if (d->dtype == CF_BF16 && (int64_t)max_kept * H * 2 >= ((int64_t)1 << 31)) return CF_ERR_UNSUPPORTED;
     return CF_OK;
 }

@@ -387,6 +387,8 @@ cf_status cf_norm_bwd(const cf_norm_desc* desc, const void* x, const void* g, co
     const uint64_t bytes = (uint64_t)max_kept * desc->H * dtype_size(desc->dtype);
     if (dx_kept != dy_kept && overlap(dx_kept, bytes, dy_kept, bytes)) return CF_ERR_SHAPE;
     if (dx_kept == x ? idx != nullptr : !idx && overlap(dx_kept, bytes, x, bytes)) return CF_ERR_SHAPE;
+    const uint64_t gb = (uint64_t)desc->H * (main_grad ? 4 : dtype_size(desc->dtype));
+    if (overlap(dg, gb, db, gb) || overlap(dg, gb, dx_kept, bytes) || overlap(db, gb, dx_kept, bytes)) return CF_ERR_SHAPE;
     if (dg && (!ws || off_by(ws, 256) || ws_bytes < cf_norm_bwd_workspace_bytes(desc, max_kept))) return CF_ERR_WORKSPACE;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     const int rpb = NormShape(desc->dtype, desc->H).rpb;

@@ -110,15 +110,17 @@ def test_embedding_refusals(L):
     assert f(dt=2) == 3
     assert f(V=0) == f(V=(1 << 30) + 1) == f(H=0) == f(H=12) == f(H=-8) == f(n=-1) == f(n=1 << 60) == 2
     assert f(s=math.inf) == f(s=math.nan) == f(table=FAKE + 2) == f(out=FAKE + 8) == f(tok=FAKE + 4) == f(dt=1, H=6) == 2
+    assert f(out=FAKE + 32) == f(out=FAKE) == 2             # overlaps
     assert f(n=0) == 0
     need = L.cf_embed_bwd_workspace_bytes
     assert need(0, 4) == need(16, -1) == need(1 << 21, 4) == need(16, (1 << 30) + 1) == 0
     assert need(16, 0) > 0 and need(16, 8192) < need(16, 8193)
-    b = lambda tok=FAKE, dx=FAKE, V=10, H=16, dt=0, idx=None, nd=None, n=4, s=1.0, out=FAKE, main=0, ws=FAKE, wsb=1 << 20: \
+    b = lambda tok=FAKE, dx=FAKE, V=10, H=16, dt=0, idx=None, nd=None, n=4, s=1.0, out=2 * FAKE, main=0, ws=FAKE, wsb=1 << 20: \
         L.cf_embed_bwd(tok, dx, V, H, dt, idx, nd, n, s, out, main, ws, wsb, None)
     assert b(tok=None) == b(dx=None) == b(out=None) == 1
     assert b(dt=-1) == 3
     assert b(V=0) == b(H=4) == b(n=-1) == b(n=(1 << 30) + 1) == b(main=2) == b(s=math.inf) == b(idx=FAKE + 2) == b(nd=FAKE + 1) == b(dx=FAKE + 4) == 2
+    assert b(out=FAKE + 64) == b(dx=2 * FAKE + 304) == 2 and b(dx=2 * FAKE + 320, main=1, ws=None) == 2
     assert b(ws=None) == b(ws=FAKE + 16) == b(wsb=need(16, 4) - 1) == 4
 
 
@@ -138,6 +140,7 @@ def test_norm_refusals(L):
         L.cf_norm_bwd(d, x, g, dy, idx, nd, n, dx, dg, db, main, ws, wsb, None)
     assert b(d=None) == b(x=None) == b(g=None) == b(dy=None) == b(dx=None) == 1
     assert b(db=FAKE) == b(d=D(layer=1), dg=None, db=FAKE) == b(main=-1) == b(dx=2 * FAKE + 64) == b(dx=FAKE, idx=FAKE) == b(dx=FAKE + 64) == 2
+    assert b(d=D(layer=1), db=FAKE + 16) == b(dg=3 * FAKE + 96) == 2
     assert b(dg=FAKE + 4) == b(nd=FAKE + 2) == b(n=(1 << 30) + 1) == 2
     assert b(ws=None) == b(ws=FAKE + 128) == b(wsb=need(D(), 4) - 1) == 4
 
@@ -154,7 +157,7 @@ def test_head_loss_refusals(L):
     assert f(H=0) == f(H=12) == f(n=-1) == f(n=(1 << 30) + 1) == f(main=2) == f(x=FAKE + 8) == f(y=FAKE + 4) == f(lp=FAKE + 2) == f(dt=FAKE + 4) == 2
     assert f(dx=FAKE + 64) == f(dx=8 * FAKE) == f(dt=8 * FAKE + 1600) == f(dt=FAKE) == f(dt=2 * FAKE) == 2        # overlaps
     assert f(d=T(kind=1, lo=1.5), old=FAKE, adv=FAKE) == f(d=T(kind=1, kl=0.1), old=FAKE, adv=FAKE) == 2
-    assert f(n=1 << 27) == f(H=1 << 21) == 5
+    assert f(n=1 << 27) == f(n=(1 << 22) + 1) == f(d=T(V=1 << 30), n=1 << 20) == f(H=1 << 21) == 5
     assert f(ws=None) == f(ws=FAKE + 64) == f(wsb=need(T(), 16, 4, 1, 1, 0) - 1) == 4
     assert need(T(), 12, 4, 1, 1, 0) == need(T(V=0), 16, 4, 1, 1, 0) == need(T(), 16, 1 << 27, 1, 1, 0) == 0
     # as much as is of use, at most the limit, never less than will do
@@ -477,7 +480,8 @@ def _head_check(got, x, table, y, dtype, policy=None, w=None, scale=1.0, norm=0.
 
 
 # one row, one column; rows around 16, 32, 64, 128 and tiles of 256; odd vocabularies; a width of one vector; wide; more columns than a least piece
-HEAD = [(1, 8, 1), (1, 64, 300), (3, 16, 7), (17, 40, 999), (33, 72, 130), (64, 256, 1003), (65, 328, 4100), (128, 520, 2500), (129, 840, 2049), (300, 264, 5001), (513, 128, 33000), (257, 1032, 257)]
+HEAD = [(1, 8, 1), (1, 64, 300), (3, 16, 7), (17, 40, 999), (33, 72, 130), (64, 256, 1003), (65, 328, 4100), (128, 520, 2500), (129, 840, 2049), (300, 264, 5001), (513, 128, 33000), (257, 1032, 257), (200, 8, 600),
+        (140, 24, 5000), (3000, 64, 9)]
 
 
 @gpu
@@ -506,6 +510,18 @@ def test_head_loss(dtype, n, H, V, policy):
     again = Bn.head_loss(x, table, y, **kw)
     for s, t in zip(again, got):
         assert torch.equal(s, t)
+
+
+@gpu
+def test_widths_of_four_in_fp32():
+    for n, H, V in ((70, 20, 333), (300, 12, 2500)):
+        x, table, y, _, g0 = _head_case(n, F32, n, H, V)
+        _head_check(Bn.head_loss(x, table, y, ws_limit=0), x, table, y, F32)
+        g, dy = randn(g0, H), randn(g0, n, H)
+        dx, _, _, big, _, _ = norm_ref_bwd(x, g, dy, 1e-5, False)
+        close(Bn.norm_bwd(x, g, dy)[0], dx, dx.abs() * U + big * 80 * U, "dx")
+        want, mag = embed_ref_bwd(y, dy, V, 1.0)
+        close(Bn.embed_bwd(y, dy, V), want, mag * U * (n + 2) + want.abs() * U, "dE")
 
 
 @gpu
@@ -575,9 +591,10 @@ def test_head_loss_of_rows_that_are_left_out(dtype):
 @gpu
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("gap", [50.0, 200.0, 5000.0])
-def test_head_loss_of_improbable_targets(dtype, gap):
+@pytest.mark.parametrize("n", [100, 600])
+def test_head_loss_of_improbable_targets(dtype, gap, n):
     """Targets whose logit lies far below the row's largest: their exponentials leave the range in which the target is the reference."""
-    n, H, V = 600, 64, 3000
+    H, V = 64, 3000
     x, table, y, _, g0 = _head_case(9, dtype, n, H, V)
     z = torch.arange(0, n, 37, device=DEV)              # rows of two of the three row tiles
     z = z[z < 300]
