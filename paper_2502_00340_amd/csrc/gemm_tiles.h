@@ -120,6 +120,13 @@ __device__ __forceinline__ void tile_coords(int l, int tiles_m, int tiles_n, int
     bn = r / gsize;
 }
 
+// ... and back
+__device__ __forceinline__ int tile_number(int bm, int bn, int tiles_m, int tiles_n) {
+    constexpr int GROUP_M = 8;
+    const int first_m = bm / GROUP_M * GROUP_M;
+    return first_m * tiles_n + bn * min(GROUP_M, tiles_m - first_m) + bm - first_m;
+}
+
 template <typename P>
 __device__ __forceinline__ P* uniform_ptr(P* p) {
     const uint64_t v = reinterpret_cast<uint64_t>(p);

@@ -514,11 +514,41 @@ __global__ __launch_bounds__(1024) void head_finish_kernel(HeadArgs a, LossArgs 
 
 // ---- 4. products of a piece --------------------------------------------------------------------------------
 
-// dx: e [n, K] times the piece's rows of the table [K, H], in `parts` parts of the contraction, each into a slot [n, H] of its own, which the first piece writes
-// and the others add to.
+// dx: e [n, K] times the piece's rows of the table [K, H], fp32 tiles that the first piece writes and the others add to.  The tiles that do not fill a round of the
+// resident blocks have their contraction cut into parts: the first part lies with the whole tiles in slots [n, H], the others in tiles of their own, for
+// head_dx_sum_kernel to add up.  All of it is a function of the live rows: kernels agree on it whoever knows the count.  (4096 rows, [65536, 4160], 272 tiles: all
+// of them in parts 2395 us, 1804 so.)
+struct DxPlan {
+    int tm, tn, n_full, rem, parts;
+    __device__ DxPlan(int rows, int H, int V, int tile, int resident) {
+        tm = (rows + tile - 1) / tile;
+        tn = (H + tile - 1) / tile;
+        n_full = tm * tn / resident * resident;
+        rem = tm * tn - n_full;
+        parts = 1;
+        if (rem > 0) {          // one round, or two where these are shorter
+            const int one = resident / rem, two = 2 * resident / rem;
+            parts = 20 * one < 17 * (two - one) ? two : one;
+            parts = max(1, min(min(parts, 64), V / 512));
+        }
+    }
+    __device__ int items() const { return n_full + rem * parts; }
+    // item -> tile (in the order of tile_coords) and part
+    __device__ void item(int w, int& tile, int& part) const {
+        part = 0;
+        if (w < n_full) { tile = xcd_order(w, n_full); return; }
+        const int l = xcd_order(w - n_full, rem * parts);
+        part = l / rem;
+        tile = n_full + l - part * rem;
+    }
+    // where an element (row, col) of a part lies: offset from `more` of parts 1 .. for one of the tiles behind the whole ones
+    __device__ int64_t more(int tile, int part, int side) const { return ((int64_t)(tile - n_full) * (parts - 1) + part - 1) * side * side; }
+};
+
 struct LeaveSlots {
     static constexpr bool OWN = true, LDA = true;
-    float* slot;
+    float* origin;              // of the tile
+    int ld;
     bool first;
     struct Rows {};
     template <int TM> __device__ __forceinline__ Rows rows(const TileRef&, int) const { return {}; }
@@ -527,9 +557,9 @@ struct LeaveSlots {
         constexpr int FM = 2 * TM, FN = 2 * TN;
         int ln = threadIdx.x & 63;
         asm volatile("" : "+v"(ln));
-        const int mw = t.m0 + wm * (32 * TM), have = min(t.M - mw, 32 * TM), n = t.n0 + wn * (32 * TN) + 4 * (ln >> 4);
-        const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(slot + (int64_t)mw * t.N, 0, have > 0 ? have * t.N * 4 : 0, 0x00020000);
-        const unsigned row_bytes = (unsigned)t.N * 4u, voff = (unsigned)(ln & 15) * row_bytes + (unsigned)n * 4u;
+        const int mw = t.m0 + wm * (32 * TM), have = min(t.M - mw, 32 * TM), col = wn * (32 * TN) + 4 * (ln >> 4), n = t.n0 + col;
+        const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(origin + (int64_t)(wm * (32 * TM)) * ld, 0, have > 0 ? have * ld * 4 : 0, 0x00020000);
+        const unsigned row_bytes = (unsigned)ld * 4u, voff = (unsigned)(ln & 15) * row_bytes + (unsigned)col * 4u;
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
             u32x4_t old[FN];
@@ -554,27 +584,29 @@ struct DxArgs {
     const void *e, *table;      // the piece's rows of the table
     int lde, K, H, n_max;
     const int32_t* n_dev;
-    float* slots;
-    int parts, tile;            // 256 or 128
+    float *slots, *more;
+    int V, tile, resident;      // tile: 256 or 128
     bool first;
 };
 __global__ __launch_bounds__(256) void head_dx_kernel(DxArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
     const int rows = __builtin_amdgcn_readfirstlane(live_rows(a.n_max, a.n_dev));
-    const int tm = (rows + a.tile - 1) / a.tile, tn = (a.H + a.tile - 1) / a.tile, tiles = tm * tn, items = tiles * a.parts;
-    const int pairs = (a.K + 63) / 64, per = (pairs + a.parts - 1) / a.parts;
+    const DxPlan plan(rows, a.H, a.V, a.tile, a.resident);
+    const int items = plan.items(), pairs = (a.K + 63) / 64;
     GemmArgs g;
     g.A[0] = a.e; g.B[0] = a.table; g.K[0] = a.K; g.nseg = 1; g.C = nullptr; g.M = rows; g.N = a.H; g.alpha = 1.f; g.beta = 0.f;
     g.a_idx = nullptr; g.a_rows = 0; g.n_dev = nullptr; g.lda = a.lde;
     auto none = [](TileRef&) { return false; };
     for (int w = blockIdx.x; w < items; w += gridDim.x) {
-        const int l = xcd_order(w, items);
-        const int part = __builtin_amdgcn_readfirstlane(l / tiles);
-        int bm, bn;
-        tile_coords(l - part * tiles, tm, tn, bm, bn);
+        int tile, part, bm, bn;
+        plan.item(w, tile, part);
+        tile = __builtin_amdgcn_readfirstlane(tile);
+        part = __builtin_amdgcn_readfirstlane(part);
+        tile_coords(tile, plan.tm, plan.tn, bm, bn);
         TileRef t{__builtin_amdgcn_readfirstlane(bm * a.tile), __builtin_amdgcn_readfirstlane(bn * a.tile), rows, a.H, uniform_ptr(a.e),
                   uniform_ptr(a.table), nullptr};
-        const LeaveSlots leave{a.slots + (int64_t)part * a.n_max * a.H, a.first};
+        const LeaveSlots leave{part == 0 ? a.slots + (int64_t)t.m0 * a.H + t.n0 : a.more + plan.more(tile, part, a.tile), part == 0 ? a.H : a.tile, a.first};
+        const int per = tile < plan.n_full ? pairs : (pairs + plan.parts - 1) / plan.parts;
         const int pbeg = min(pairs, part * per), pend = min(pairs, pbeg + per);
         if (a.tile == 256) gemm_tiles<2, 4, 4, true, false>(g, a.K, t, none, smem, pbeg, pend, nullptr, leave);
         else gemm_tiles<2, 2, 2, true, false>(g, a.K, t, none, smem, pbeg, pend, nullptr, leave);
@@ -709,23 +741,32 @@ template <int KS, bool CF32> __global__ __launch_bounds__(256) void head_dtable_
 // ---- 5. dx -------------------------------------------------------------------------------------------------
 
 template <typename T>
-__global__ __launch_bounds__(256) void head_dx_sum_kernel(const float* __restrict__ slots, int parts, const float* __restrict__ fac,
-                                                          const int32_t* __restrict__ y, int n_max, const int32_t* __restrict__ n_dev, int H,
-                                                          T* __restrict__ dx) {
+__global__ __launch_bounds__(256) void head_dx_sum_kernel(DxArgs a, const float* __restrict__ fac, const int32_t* __restrict__ y, T* __restrict__ dx) {
     constexpr int VN = Vec<T>::N;
-    const int n_rows = live_rows(n_max, n_dev), vpr = H / VN;
-    const int64_t total = (int64_t)n_rows * vpr, slot = (int64_t)n_max * H;
+    const int rows = live_rows(a.n_max, a.n_dev), vpr = a.H / VN;
+    if (rows == 0) return;
+    const DxPlan plan(rows, a.H, a.V, a.tile, a.resident);
+    const int64_t total = (int64_t)rows * vpr;
     for (int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x; v < total; v += (int64_t)gridDim.x * 256) {
-        const int j = (int)(v / vpr);
-        const float* p = slots + v * VN;
+        const int j = (int)(v / vpr), c = (int)(v - (int64_t)j * vpr) * VN;
         float s[VN];
-#pragma unroll
-        for (int e = 0; e < VN; ++e) s[e] = 0.f;
-        for (int k = 0; k < parts; ++k, p += slot) {
+        auto add = [&](const float* p) __attribute__((always_inline)) {
 #pragma unroll
             for (int q = 0; q < VN / 4; ++q) {
                 const float4 w = reinterpret_cast<const float4*>(p)[q];
                 s[4 * q] += w.x; s[4 * q + 1] += w.y; s[4 * q + 2] += w.z; s[4 * q + 3] += w.w;
+            }
+        };
+#pragma unroll
+        for (int e = 0; e < VN; ++e) s[e] = 0.f;
+        add(a.slots + v * VN);
+        if (plan.parts > 1) {
+            const int tile = tile_number(j / a.tile, c / a.tile, plan.tm, plan.tn);
+            if (tile >= plan.n_full) {
+                const int64_t side = (int64_t)a.tile * a.tile;
+                const float* p = a.more + plan.more(tile, 1, a.tile) + (j % a.tile) * a.tile + c % a.tile;
+#pragma unroll 4
+                for (int k = 1; k < plan.parts; ++k, p += side) add(p);
             }
         }
         const float f = fac[j];
@@ -916,24 +957,30 @@ template <int KIND> __global__ F32_BOUNDS void head_logits_f32_kernel(HeadArgs a
 
 __global__ F32_BOUNDS void head_dx_f32_kernel(DxArgs a) {
     __shared__ __align__(16) unsigned char smem[F32_SMEM];
-    const int rows = live_rows(a.n_max, a.n_dev), tm = (rows + 127) / 128, tn = (a.H + 127) / 128, tiles = tm * tn, items = tiles * a.parts;
-    const int steps = (a.K + F32_STEP - 1) / F32_STEP, per = (steps + a.parts - 1) / a.parts;
+    const int rows = live_rows(a.n_max, a.n_dev);
+    if (rows == 0) return;
+    const DxPlan plan(rows, a.H, a.V, 128, a.resident);
+    const int items = plan.items(), steps = (a.K + F32_STEP - 1) / F32_STEP;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
     for (int w = blockIdx.x; w < items; w += gridDim.x) {
-        const int part = w / tiles, l = w - part * tiles, m0 = (l % tm) * 128, n0 = (l / tm) * 128;
+        int tile, part, bm, bn;
+        plan.item(w, tile, part);
+        tile_coords(tile, plan.tm, plan.tn, bm, bn);
+        const int m0 = bm * 128, n0 = bn * 128, per = tile < plan.n_full ? steps : (steps + plan.parts - 1) / plan.parts, ld = part == 0 ? a.H : 128;
+        float* const origin = part == 0 ? a.slots + (int64_t)m0 * a.H + n0 : a.more + plan.more(tile, part, 128);
         const F32Tile t{(const float*)a.e, (const float*)a.table, a.lde, a.H, rows, a.H, min(steps, part * per) * F32_STEP,
                         min(a.K, min(steps, part * per + per) * F32_STEP), m0, n0};
         f32x4_t acc[4][4];
         f32_tile<2>(t, smem, acc);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int m = m0 + wm * 64 + i * 16 + (lane & 15);
-            if (m >= rows) continue;
+            const int r = wm * 64 + i * 16 + (lane & 15);
+            if (m0 + r >= rows) continue;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int n = n0 + wn * 64 + j * 16 + 4 * (lane >> 4);
-                if (n >= a.H) continue;
-                float4* p = reinterpret_cast<float4*>(a.slots + ((int64_t)part * a.n_max + m) * a.H + n);
+                const int c = wn * 64 + j * 16 + 4 * (lane >> 4);
+                if (n0 + c >= a.H) continue;
+                float4* p = reinterpret_cast<float4*>(origin + (int64_t)r * ld + c);
                 float4 o = make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
                 if (!a.first) {
                     const float4 b = *p;
@@ -976,23 +1023,9 @@ template <bool MAIN> __global__ F32_BOUNDS void head_dtable_f32_kernel(DtableArg
 
 // ---- workspace and launches --------------------------------------------------------------------------------
 
-// Parts of dx's contraction over the vocabulary: the fewest rounds of the blocks that are resident at a time per part.  A part costs its slot (written and read at
-// 5 TB/s) and a start of three microseconds; a whole contraction of a 256x256 bf16 tile takes V * 26 ns, of a 128x128 fp32 one V * 100 ns.
-static int dx_parts(int64_t tiles, int V, int dtype, int n_cu) {
-    const int64_t resident = (int64_t)n_cu * (dtype == CF_F32 ? 3 : 1);
-    const double part = (dtype == CF_F32 ? 0.25 * (double)tiles + 30.0 : 4.0 * (double)tiles + 115.0) / V;
-    int best = 1;
-    double least = 1e30;
-    for (int s = 1; s <= 64 && (s == 1 || (int64_t)V >= (int64_t)s * 512); ++s) {
-        const double cost = (double)((tiles * s + resident - 1) / resident) / s + part * s;
-        if (cost < least - 1e-9) { least = cost; best = s; }
-    }
-    return best;
-}
-
 struct HeadWs {
-    int strips, ldn, tile, parts, cap;          // cap: columns of e (0: too little room, or no gradient)
-    size_t ref, a, ey, y, terms, flags, sums, xs, slots, e, total;
+    int strips, ldn, tile, resident, cap;       // of dx: a tile's rows and columns, blocks that are resident at a time.  cap: columns of e (0: too little room, or no gradient)
+    size_t ref, a, ey, y, terms, flags, sums, xs, slots, more, e, total;
     HeadWs(int V, int H, int n_rows, int dtype, bool need_dx, bool need_dt, size_t bytes) {
         const int n = n_rows > 0 ? n_rows : 1;
         const size_t es = dtype_size(dtype);
@@ -1009,8 +1042,9 @@ struct HeadWs {
         sums = take((size_t)(n <= FEW_ROWS ? std::max(strips, compute_units()) : strips) * ldn * 4);
         xs = take(need_dt ? (size_t)n * H * es : 0);
         tile = dtype == CF_F32 || n <= 128 ? 128 : 256;
-        parts = need_dx ? dx_parts((int64_t)ceil_div(n, tile) * ceil_div(H, tile), V, dtype, compute_units()) : 0;
-        slots = take((size_t)parts * n * H * 4);
+        resident = compute_units() * (dtype == CF_F32 ? 3 : 1);
+        slots = take(need_dx ? (size_t)n * H * 4 : 0);
+        more = take(need_dx ? (size_t)2 * resident * tile * tile * 4 : 0);         // at most two rounds of parts
         e = at;
         cap = 0;
         total = at;
@@ -1058,8 +1092,7 @@ template <> struct HeadLaunch<bf16_t> {
         static std::atomic<uint64_t> lds_ok{0};
         const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&head_dx_kernel), GEMM_SMEM, lds_ok);
         if (e != hipSuccess) return e;
-        const int64_t items = (int64_t)ceil_div(a.n_max, a.tile) * ceil_div(a.H, a.tile) * a.parts;
-        head_dx_kernel<<<(int)std::min<int64_t>(items, compute_units()), 256, GEMM_SMEM, st>>>(a);
+        head_dx_kernel<<<a.resident, 256, GEMM_SMEM, st>>>(a);
         return hipGetLastError();
     }
     template <int KS> static hipError_t dtable_few(const DtableArgs& a, bool main, hipStream_t st) {
@@ -1088,7 +1121,7 @@ template <> struct HeadLaunch<float> {
     }
     static hipError_t sums(HeadArgs& a, hipStream_t st) { return logits<SUMS>(a, st); }
     static hipError_t dx(const DxArgs& a, hipStream_t st) {
-        head_dx_f32_kernel<<<grid((int64_t)ceil_div(a.n_max, 128) * ceil_div(a.H, 128) * a.parts), 256, 0, st>>>(a);
+        head_dx_f32_kernel<<<2 * a.resident, 256, 0, st>>>(a);
         return hipGetLastError();
     }
     static hipError_t dtable(const DtableArgs& a, bool main, hipStream_t st) {
@@ -1131,19 +1164,20 @@ static hipError_t launch_head(HeadArgs a, LossArgs l, const HeadWs& L, unsigned 
         CF_TRY(HeadLaunch<T>::template logits<MAXIMA>(a, st));
         head_finish_kernel<T><<<ceil_div(n, 16), 1024, 0, st>>>(a, l, xs);
         CF_TRY(hipGetLastError());
+        DxArgs d{};
         for (int c = 0; grads && c < V; c += L.cap) {
             const int w = std::min(L.cap, V - c);
             a.c0 = c; a.c1 = c + w; a.lde = (int)align_up((size_t)w, 8); a.store_end = c + w; a.flagged_only = c == 0;
             CF_TRY(HeadLaunch<T>::template logits<VALUES>(a, st));
             if (dx != nullptr)
-                CF_TRY(HeadLaunch<T>::dx(DxArgs{a.e, (const T*)a.table + (int64_t)c * H, a.lde, w, H, n, a.n_dev, (float*)(ws + L.slots), L.parts, L.tile, c == 0}, st));
+                CF_TRY(HeadLaunch<T>::dx(d = DxArgs{a.e, (const T*)a.table + (int64_t)c * H, a.lde, w, H, n, a.n_dev, (float*)(ws + L.slots), (float*)(ws + L.more), V, L.tile,
+                                                    L.resident, c == 0}, st));
             if (dtable != nullptr)
                 CF_TRY(HeadLaunch<T>::dtable(DtableArgs{a.e, xs, (char*)dtable + (int64_t)c * H * (main ? 4 : (int)sizeof(T)), a.lde, w, H, n, a.n_dev, 0, 1}, main, st));
         }
         if (dx != nullptr) {
             const int64_t vecs = (int64_t)n * (H / Vec<T>::N);
-            head_dx_sum_kernel<T><<<(int)std::min<int64_t>((vecs + 255) / 256, 32 * compute_units()), 256, 0, st>>>(
-                (const float*)(ws + L.slots), L.parts, a.a, a.y, n, a.n_dev, H, (T*)dx);
+            head_dx_sum_kernel<T><<<(int)std::min<int64_t>((vecs + 255) / 256, 32 * compute_units()), 256, 0, st>>>(d, a.a, a.y, (T*)dx);
             CF_TRY(hipGetLastError());
         }
     } else if (dtable != nullptr && !main) {
