@@ -273,31 +273,7 @@ struct SumArgs {
     float scale;
     void* out;
     float* part;
-    int sum_blocks, clear_from;     // blocks behind the first ones clear the table's rows from clear_from on that no row adds to
 };
-
-// Zeros for the rows from clear_from on whose token nobody has, eight at a time by waves `wave`, `wave` + `waves`, ...: the ordered tokens say which.  64 samples of them
-// bound where a group's stand.
-template <typename T> __device__ __forceinline__ void clear_untouched(const SumArgs& a, int64_t wave, int64_t waves) {
-    const int n_rows = live_rows(a.n_max, a.n_dev), lane = threadIdx.x & 63, step = (n_rows + 63) / 64, vpr = a.H / Vec<T>::N;
-    const int sample = lane * step < n_rows ? a.tok[lane * step] : a.V;
-    for (int64_t g = wave; a.clear_from + g * 8 < a.V; g += waves) {
-        const int r = a.clear_from + (int)g * 8, ahead = __popcll(__ballot(sample < r));
-        unsigned touched = 0;
-        for (int p = ahead > 0 ? (ahead - 1) * step : 0; p < n_rows; p += 64) {
-            const int t = p + lane < n_rows ? a.tok[p + lane] : a.V;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) touched |= __ballot(t == r + k) != 0 ? 1u << k : 0u;
-            if (__ballot(t >= r + 8) != 0) break;
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            if (r + k >= a.V || (touched >> k & 1u)) continue;
-            u32x4_t* row = reinterpret_cast<u32x4_t*>((T*)a.out + (int64_t)(r + k) * a.H);
-            for (int v = lane; v < vpr; v += 64) row[v] = u32x4_t{0u, 0u, 0u, 0u};
-        }
-    }
-}
 
 template <typename T, bool MAIN>
 __device__ __forceinline__ void embed_out(const SumArgs& a, int t, int c, const float (&s)[Vec<T>::N], const float (&old)[Vec<T>::N]) {
@@ -317,16 +293,9 @@ __device__ __forceinline__ void embed_out(const SumArgs& a, int t, int c, const 
 template <typename T, int NT, bool MAIN>
 __global__ __launch_bounds__(NT) void embed_sum_kernel(SumArgs a) {
     constexpr int VN = Vec<T>::N;
-    if constexpr (!MAIN) {
-        if ((int)blockIdx.x >= a.sum_blocks) {
-            constexpr int W = NT / 64;
-            clear_untouched<T>(a, (int64_t)((int)blockIdx.x - a.sum_blocks) * W + (threadIdx.x >> 6), (int64_t)((int)gridDim.x - a.sum_blocks) * W);
-            return;
-        }
-    }
     const int n_rows = live_rows(a.n_max, a.n_dev), vpr = a.H / VN, tiles = (vpr + NT - 1) / NT;
     const int64_t units = (int64_t)((n_rows + CH - 1) / CH) * tiles;
-    for (int64_t u = blockIdx.x; u < units; u += a.sum_blocks) {
+    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
         const int chunk = (int)(u / tiles), p0 = chunk * CH, v = (int)(u % tiles) * NT + threadIdx.x;
         int t[CH + 2];              // tokens of rows p0 - 1 .. p0 + CH; V: none
 #pragma unroll
@@ -496,10 +465,6 @@ __global__ __launch_bounds__(256) void embed_few_kernel(SumArgs a, const int64_t
     embed_out<T, MAIN>(a, t, c, s, old);
 }
 
-// Bytes of the table that are cleared beside the ordering of the rows, about 6 us; the others beside the sums (8 tables of 169 MB in turn: 38.3 us a call; 8 MB ahead 42.0,
-// 64 MB 38.6, all of it 40.7)
-constexpr int64_t CLEAR_AHEAD = (int64_t)32 << 20;
-
 // workspace: the order (twice where spans have to be merged), then the parts
 struct EmbedWs {
     size_t order, part, total;
@@ -531,11 +496,6 @@ static hipError_t launch_embed_bwd(SumArgs a, SortArgs so, unsigned char* ws, hi
         if (n > 0) embed_few_kernel<T, MAIN><<<n * ceil_div(a.H / Vec<T>::N, 256), 256, 0, st>>>(a, so.tokens, so.idx);
         return hipGetLastError();
     }
-    if (!MAIN) {        // what the launch that puts the rows in order has time to clear; the sums' launch clears the others
-        const int64_t rows = CLEAR_AHEAD / ((int64_t)a.H * (int64_t)sizeof(T)) + 1;
-        a.clear_from = (int)(rows < a.V ? rows : a.V);
-        so.n_zero = (int64_t)a.clear_from * a.H * (int64_t)sizeof(T) / 16;
-    }
     if (n <= SPAN) {
         const int rank_blocks = ceil_div(n, RANK_ROWS), grid = rank_blocks + fill(RANK_THREADS);
         embed_rank_kernel<<<grid, RANK_THREADS, 0, st>>>(so, rank_blocks);
@@ -554,13 +514,11 @@ static hipError_t launch_embed_bwd(SumArgs a, SortArgs so, unsigned char* ws, hi
         a.row = row;
     }
     a.part = (float*)(ws + L.part);
-    const int vpr = a.H / Vec<T>::N, chunks = ceil_div(n, CH), nt = vpr <= 64 ? 64 : vpr <= 128 ? 128 : 256;
-    const int64_t units = (int64_t)chunks * ((vpr + nt - 1) / nt), groups = MAIN ? 0 : ((int64_t)a.V - a.clear_from + 7) / 8, clear = (groups + nt / 64 - 1) / (nt / 64);
-    a.sum_blocks = (int)(units < MAX_GRID / 2 ? units : MAX_GRID / 2);
-    const int grid = a.sum_blocks + (int)(clear < MAX_GRID / 2 ? clear : MAX_GRID / 2);
-    if (nt == 64) embed_sum_kernel<T, 64, MAIN><<<grid, 64, 0, st>>>(a);
-    else if (nt == 128) embed_sum_kernel<T, 128, MAIN><<<grid, 128, 0, st>>>(a);
-    else embed_sum_kernel<T, 256, MAIN><<<grid, 256, 0, st>>>(a);
+    const int vpr = a.H / Vec<T>::N, chunks = ceil_div(n, CH);
+    const auto blocks = [&](int nt) { const int64_t u = (int64_t)chunks * ((vpr + nt - 1) / nt); return (int)(u < MAX_GRID ? u : MAX_GRID); };
+    if (vpr <= 64) embed_sum_kernel<T, 64, MAIN><<<blocks(64), 64, 0, st>>>(a);
+    else if (vpr <= 128) embed_sum_kernel<T, 128, MAIN><<<blocks(128), 128, 0, st>>>(a);
+    else embed_sum_kernel<T, 256, MAIN><<<blocks(256), 256, 0, st>>>(a);
     if (chunks > 1) {
         const int64_t waves = (int64_t)(chunks - 1) * ((a.H + 255) / 256), blocks = (waves + 3) / 4, most = 16 * compute_units();
         embed_join_kernel<T, MAIN><<<(int)(blocks < most ? blocks : most), 256, 0, st>>>(a);
@@ -622,7 +580,7 @@ cf_status cf_embed_bwd(const int64_t* tokens, const void* dx_kept, int32_t V, in
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     int passes = 0;
     for (int64_t v = V; v > 0; v >>= DIGIT_BITS) ++passes;
-    SumArgs a{nullptr, nullptr, n_kept_dev, max_kept, V, H, dx_kept, scale, dtable, nullptr, 0, 0};
+    SumArgs a{nullptr, nullptr, n_kept_dev, max_kept, V, H, dx_kept, scale, dtable, nullptr};
     SortArgs so{tokens, idx, n_kept_dev, max_kept, V, passes, nullptr, nullptr, 0, nullptr, 0};
     unsigned char* w = (unsigned char*)ws;
     hipError_t e;
