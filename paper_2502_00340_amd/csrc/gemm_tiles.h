@@ -42,8 +42,9 @@ struct TileRef {
 // What becomes of a finished tile: a kernel's own epilogue, called with the accumulators and the tile, or by default the product's write-out.  Its
 // accumulators: lane l holds, of fragment (i, j) of its wave tile, row l % 16 and the columns 4 * (l / 16) .. +3.  rows: what it reads
 // from memory, before the next tile's loads go out, behind which it would have to wait.  LDA: see GemmArgs.
+// STREAM: the bf16 write-out goes past the caches.
 struct Product {
-    static constexpr bool OWN = false, LDA = false;
+    static constexpr bool OWN = false, LDA = false, STREAM = false;
     struct Rows {};
     template <int TM> __device__ Rows rows(const TileRef&, int) const { return {}; }
     template <int TM, int TN> __device__ void operator()(f32x4_t (&)[2 * TM][2 * TN], const TileRef&, const Rows&, unsigned char*, int, int) const {}
@@ -168,6 +169,7 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs& g, const int K0x, con
     constexpr int PAIR = 2 * STAGE, PWIN = 65536 / PAIR;    // bytes of a pair, pairs within reach of one LDS base register
     // MODE 0 (NT): both operands lie with K contiguous in memory; 1 (TN): both K-major; 2 (NN): A K-contiguous, B K-major
     constexpr bool AK = MODE != 1, BK = MODE == 0;
+    constexpr int STORE = Leave::STREAM ? 2 : 0;      // the bf16 write-out, past the caches or through them
     constexpr int A_BYTES = BM * KB * 2, B_BYTES = BN * KB * 2;     // of one K-step; a pair holds A's two K-steps, then B's
     constexpr int NU = TM + TN;                         // 1 KB wave-loads per wave per K-step: TM for A, TN for B
     constexpr int FM = 2 * TM, FN = 2 * TN;             // 16-row fragments of the wave tile along M and N
@@ -668,7 +670,7 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs& g, const int K0x, con
             }
 #pragma unroll
             for (int q = 0; q < NP; ++q)
-                __builtin_amdgcn_raw_buffer_store_b128(val[q], rc, voff + (unsigned)(i * 32 + q * RPP) * row_bytes, 0, 0);
+                __builtin_amdgcn_raw_buffer_store_b128(val[q], rc, voff + (unsigned)(i * 32 + q * RPP) * row_bytes, 0, STORE);
         }
     }
     if (!has_next) break;

@@ -83,7 +83,7 @@ __global__ __launch_bounds__(256) void head_rows_kernel(HeadArgs a, LossArgs l) 
 // ---- 2. tiles of logits ------------------------------------------------------------------------------------
 
 template <int KIND> struct LeaveLogits {
-    static constexpr bool OWN = true, LDA = false;
+    static constexpr bool OWN = true, LDA = false, STREAM = false;
     HeadArgs a;
     int n_rows;
     struct Rows {
@@ -546,7 +546,7 @@ struct DxPlan {
 };
 
 struct LeaveSlots {
-    static constexpr bool OWN = true, LDA = true;
+    static constexpr bool OWN = true, LDA = true, STREAM = false;
     float* origin;              // of the tile
     int ld;
     bool first;
@@ -615,9 +615,10 @@ __global__ __launch_bounds__(256) void head_dx_kernel(DxArgs a) {
     }
 }
 
-// the table's gradient: e^T x' over the live rows, bf16 written or fp32 added to
+// the table's gradient: e^T x' over the live rows, bf16 written (past the caches: nothing here reads it, and e and x' stay in them; whole calls 0.985 to 0.997 of
+// the time) or fp32 added to
 struct WideA : Product {
-    static constexpr bool LDA = true;
+    static constexpr bool LDA = true, STREAM = true;
 };
 struct DtableArgs {
     const void *e, *xs;
