@@ -7,6 +7,7 @@
 namespace cf {
 
 // ---- forward -------------------------------------------------------------------------------------------------
+// 8192 rows of [128256, 4096] bf16: 17.6 us, 5.6 TB/s; a copy of as much in one piece reaches 6.3.
 
 template <typename T>
 __global__ __launch_bounds__(256) void embed_fwd_kernel(const T* __restrict__ table, const int64_t* __restrict__ tokens, int64_t n, int V, int vpr,
@@ -50,7 +51,7 @@ static void launch_embed_fwd(const void* table, const int64_t* tokens, int64_t n
 // ---- the rows in the order (token, row) ----------------------------------------------------------------------
 // A block sorts a span of up to 8192 rows in LDS: passes of nine bits, lowest first, each keeping the order of what is equal.  A wave takes a
 // contiguous part of the span, 64 rows at a time; rows of one wave and round that share a digit find each other by nine ballots.  Two passes do for
-// 2^18 tokens.  Spans are merged by rank: a row's place is its place in its span and, for each other span, the number of rows there that go ahead of it.
+// 2^18 tokens (4096 rows in one block: 16.8 us).  Spans are merged by rank: a row's place is its place in its span and, for each other span, the number of rows there that go ahead of it.
 
 constexpr int SPAN = 8192, DIGIT_BITS = 9, DIGITS = 1 << DIGIT_BITS, SORT_WAVES = 16, SORT_THREADS = 64 * SORT_WAVES, PER_THREAD = SPAN / SORT_THREADS;
 constexpr int SORT_LDS = SPAN * 4 + SPAN * 2 + SORT_WAVES * DIGITS * 2 + 64;
@@ -180,7 +181,8 @@ __global__ __launch_bounds__(SORT_THREADS) void embed_sort_kernel(SortArgs a) {
 }
 
 // Up to a span the rows are put in order by counting instead, on all CUs in one launch: a row's place is the number of rows with a smaller token and of rows
-// ahead of it with the same one.  n^2 comparisons of keys in LDS; a wave takes a row.
+// ahead of it with the same one.  n^2 comparisons of keys in LDS; a wave takes a row.  4096 rows 6.0 us, of
+// which the keys' loads through the index are half; with 16 lanes a row in blocks of 256 threads 10.9.
 constexpr int RANK_ROWS = 16, RANK_THREADS = 64 * RANK_ROWS;
 
 __global__ __launch_bounds__(RANK_THREADS) void embed_rank_kernel(SortArgs a, int rank_blocks) {
@@ -265,6 +267,7 @@ __global__ __launch_bounds__(256) void embed_merge_kernel(const int32_t* __restr
 // A block takes CH rows of that order, and TILE columns.  All its loads are asked for at once (rows, and the main gradient's old values); then the
 // rows are added up one by one, and a token's sum leaves where its last row has been added.  A token whose rows reach over the border of a block leaves parts: [chunk][0]
 // of one that began ahead of the chunk, [chunk][1] of one that begins here and goes on.  embed_join_kernel adds these up in order.
+// 4096 rows of 4096 bf16, log-uniform tokens, into an fp32 table: 110 MB in 21 us, 5.2 TB/s.
 constexpr int CH = 8;
 
 struct SumArgs {
@@ -360,7 +363,7 @@ __global__ __launch_bounds__(NT) void embed_sum_kernel(SumArgs a) {
 }
 
 // The tokens whose rows reach over chunks.  A wave takes a chunk and 256 columns; it has work where a token begins in the chunk that goes on in the next one.
-// Parts are added in order, 16 of them in flight.
+// Parts are added in order, 16 of them in flight.  Those rows: 6.1 us, latency; blocks of 16 waves that share a token 14.6.
 template <typename T, bool MAIN>
 __global__ __launch_bounds__(256) void embed_join_kernel(SumArgs a) {
     const int n_rows = live_rows(a.n_max, a.n_dev), chunks = (n_rows + CH - 1) / CH, tiles = (a.H + 255) / 256, lane = threadIdx.x & 63;

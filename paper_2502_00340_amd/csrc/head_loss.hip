@@ -14,6 +14,9 @@
 // 2^t is at most exp(-lp), so that nothing leaves fp32's or bf16's range unless the target has a probability below exp(-40).  A strip whose sum says so raises its
 // row tile's flag; head_logits then goes over the flagged tiles again with strips' maxima, and the row's log-sum-exp becomes its reference.
 //
+// What bounds it: the matrix cores under the chip's power limit from some hundred rows on (4096 rows, H = 4096, V = 128256 bf16: logits, dx and the table's gradient
+// 3.04, 3.01 and 3.08 ms, 1.40 to 1.43 PFLOP/s), the table's traffic for few rows.  Keeping e makes that three products instead of four.
+//
 // Roundings: logits, sums, lp and both gradients' sums are fp32; e, and x' = a*x, are rounded to the storage type once each (2^-8 relative in bf16), dx and
 // the table's gradient once where they are stored.
 #include <math.h>

@@ -2,7 +2,8 @@
 //   n = (x - mu) * rstd,  rstd = (mean((x - mu)^2) + eps)^(-1/2),  y = n * g + b
 //   u = dy * g,  dx = rstd * (u - [layer] mean(u) - n * mean(u * n)),  dg = sum over rows of dy * n,  db = sum of dy
 // HBM-bound: rows in, rows out; a row stays in registers from its statistics to its output, and the next row is asked for ahead of them.  The statistics are
-// centred sums (the mean first), in fp32: no difference of two large sums.
+// centred sums (the mean first), in fp32: no difference of two large sums.  4096 rows of 4096 bf16 through an index: forward 11.6 us, 5.8 TB/s, backward 19.5, 5.1 TB/s, and 4 for
+// the gains' second launch.
 #include "common.h"
 #include "mfma_util.h"
 
@@ -292,7 +293,7 @@ __global__ __launch_bounds__(256) void norm_gains_kernel(const float* pg, const 
     }
 }
 
-// Threads a row: a wave up to four vectors a lane, which needs no barrier; then the smallest block whose threads hold a row in four.
+// Threads a row (a function of the width and the type, so that sums have one order): a wave up to four vectors a lane, which needs no barrier; then the smallest block whose threads hold a row in four.
 struct NormShape {
     int nt, rpb;
     NormShape(int dtype, int H) {
@@ -301,7 +302,8 @@ struct NormShape {
         rpb = nt == 64 ? 4 : 1;
     }
 };
-constexpr int NORM_BWD_BLOCKS = 512;        // and so the parts of a gain's gradient
+// Blocks of the backward, and so the parts of a gain's gradient: 512, 768 and 1024 take 19.5, 19.8 and 22.2 us (4593 fp32 rows of 840, layer norm: 12.9, 13.4, 15.2)
+constexpr int NORM_BWD_BLOCKS = 512;
 
 template <typename T, bool LAYER, bool BWD> static void launch_norm(const NormArgs& a, hipStream_t st) {
     const NormShape s(Vec<T>::N == 4 ? CF_F32 : CF_BF16, a.H);

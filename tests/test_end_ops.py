@@ -6,11 +6,13 @@ terms by (its depth, at most n) * 2^-24 of the sum of their absolute values, a f
 import ctypes as C
 import math
 
+import numpy as np
 import pytest
 import torch
 
 from paper_2502_00340_amd import binding as Bn
-from tests.test_step_ops import BF, DEV, EPS, F32, F64, FAKE, U, close, gen, gpu, loss_ref, randn, say
+from tests import harness as Hn
+from tests.test_step_ops import BF, DEV, EPS, EPS_N, F32, F64, FAKE, U, _layer_qk_device, _layer_qk_problem, close, gen, gpu, loss_ref, qk_ref, randn, say
 
 
 @pytest.fixture(scope="module")
@@ -686,7 +688,7 @@ def test_ends_of_a_step_together(dtype, tied):
     tol = {BF: 12 * EPS[BF], F32: 200 * U}[dtype]
     for got, ref in zip(main, want):
         assert float((got.to(F64) - ref).norm()) <= tol * float(ref.norm())
-    assert abs(float(stats[0]) - float(loss)) <= tol * float(loss)
+    assert abs(float(stats[0]) - loss.item()) <= tol * loss.item()
 
 
 @gpu
@@ -733,3 +735,62 @@ def test_ends_of_a_step_in_a_graph_and_on_another_stream(dtype):
         assert torch.equal(stats, out[0]) and torch.equal(logp[:n], out[1][:n])
         for s, t in zip(main, eager):
             assert torch.equal(s, t)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("tied", [False, True])
+def test_whole_model_step(dtype, tied):
+    """Embeddings, a layer, the last norm and the loss, and back into main gradients, with every token kept: the gradients of the whole function, which torch
+    differentiates in 64 bits."""
+    say("model step", dtype, tied)
+    V = 520
+    shape, W, sv, tabs, rng = _layer_qk_problem(dtype, seed=41)
+    B, S, H, Hq, Hkv, d = shape.B, shape.S, shape.H, shape.Hq, shape.Hkv, shape.d
+    T = shape.T
+    tok = torch.from_numpy(rng.permutation(V)[:T])                      # the layer's input is given: a row of the table each
+    table = Hn.quantize(0.05 * rng.standard_normal((V, H)), shape.dtype)
+    table[tok.numpy()] = sv["x"]
+    wh = table if tied else Hn.quantize(0.05 * rng.standard_normal((V, H)), shape.dtype)
+    gf = Hn.quantize(1.0 + 0.2 * rng.standard_normal(H), shape.dtype)
+    y = torch.from_numpy(rng.integers(0, V, T))
+    # the whole function in 64 bits
+    P = {n: torch.from_numpy(v.astype(np.float64)).requires_grad_() for n, v in {**W, "table": table, "gf": gf}.items()}
+    head = P["table"] if tied else torch.from_numpy(wh.astype(np.float64)).requires_grad_()
+    rms = lambda x, g: x / (x.square().mean(-1, keepdim=True) + 1e-5).sqrt() * g
+    x = P["table"][tok]
+    cos, sin, pos = torch.from_numpy(tabs[0]), torch.from_numpy(tabs[1]), torch.arange(T) % S
+    h1 = rms(x, P["g1"])
+    q, k, v = qk_ref(h1 @ P["wq"], P["gq"], d, EPS_N, cos, sin, pos), qk_ref(h1 @ P["wk"], P["gk"], d, EPS_N, cos, sin, pos), h1 @ P["wv"]
+    heads = lambda t, n: t.view(B, S, n, d).transpose(1, 2)
+    kk, vv = (heads(t, Hkv).repeat_interleave(Hq // Hkv, 1) for t in (k, v))
+    sc = (heads(q, Hq) @ kk.transpose(2, 3) / math.sqrt(d)).masked_fill(torch.triu(torch.ones(S, S, dtype=torch.bool), 1), -math.inf)
+    r = x + (torch.softmax(sc, -1) @ vv).transpose(1, 2).reshape(T, -1) @ P["wo"]
+    h2 = rms(r, P["g2"])
+    out = r + (torch.nn.functional.silu(h2 @ P["wg"]) * (h2 @ P["wu"])) @ P["wd"]
+    loss = torch.nn.functional.cross_entropy(rms(out, P["gf"]) @ head.T, y)
+    loss.backward()
+    # the same through the library
+    to = lambda a: Hn.to_dev(a, shape.dtype)
+    dsv, dW = _layer_qk_device(shape, W, sv, tabs)
+    dtab, dgf, dwh, tok, y = to(table), to(gf), to(wh), tok.to(DEV), y.to(DEV)
+    assert torch.equal(Bn.embed_fwd(dtab, tok), dsv["x"])
+    top = to(Hn.quantize(out.detach().numpy(), shape.dtype))
+    idx, cu, nd, n = Bn.build_keep_index(torch.ones((B, S), dtype=torch.uint8, device=DEV))
+    plan = Bn.LayerBackward(Bn.make_desc(B, S, H, Hq, Hkv, d, shape.F, shape.dtype), main_grad=True, qk_norm_eps=EPS_N)
+    z = lambda *s: torch.zeros(s, device=DEV)
+    gtab, ggf = z(V, H), z(H)
+    gwh = gtab if tied else z(V, H)
+    hz = Bn.norm_fwd(top, dgf, idx=idx, n_kept_dev=nd)
+    stats, _, dz, _ = Bn.head_loss(hz, dwh, y, idx=idx, n_kept_dev=nd, main_grad=gwh, dx_out=hz)
+    dy, _, _ = Bn.norm_bwd(top, dgf, dz, idx=idx, n_kept_dev=nd, main_grads=(ggf, None), out=dz)
+    plan.compact_dev(dsv, dW, dy, idx, cu, nd)
+    Bn.embed_bwd(tok, plan.grads["dx"], V, idx=idx, n_kept_dev=nd, main_grad=gtab)
+    tol = 4 * Hn.TOL[shape.dtype]           # the layer's, the norm's, the head's and the loss's one after the other
+    assert abs(float(stats[0]) - loss.item()) < tol
+    want = {"d" + m: t.grad.numpy() for m, t in P.items()}
+    got = {m: plan.grads[m] for m in Hn.GRADS + ("dgq", "dgk")} | {"dtable": gtab, "dgf": ggf}
+    if not tied:
+        want["dhead"], got["dhead"] = head.grad.numpy(), gwh
+    for m, t in got.items():
+        assert Hn.rel_fro(Hn.to_np(t), want[m]) <= tol, (m, Hn.rel_fro(Hn.to_np(t), want[m]))
