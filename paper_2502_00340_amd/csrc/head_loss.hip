@@ -409,14 +409,18 @@ static int few_blocks(int V, int n_cu) { return std::min(ceil_div(V, 128), n_cu)
 constexpr int FEW_ROWS = 128;
 
 // ---- 3. the rows' ends -------------------------------------------------------------------------------------
-// A block takes 16 rows: 64 groups of 16 lanes add their strips up, one lane a row ends it, and the block scales the rows of x.
+// A block takes 16 rows: 64 groups of 16 lanes add their strips up, one lane a row ends it, and the block scales the rows of x.  A single block has all terms, and leaves
+// the statistics, too.
 template <typename T>
-__global__ __launch_bounds__(1024) void head_finish_kernel(HeadArgs a, LossArgs l, void* xs) {
+__global__ __launch_bounds__(1024) void head_finish_kernel(HeadArgs a, LossArgs l, void* xs, float* stats) {
     constexpr int VN = Vec<T>::N;
     __shared__ float red[2][16][16];
-    __shared__ float fac[16];
+    __shared__ float fac[16], terms[16][4];
     const int n_rows = live_rows(a.n_max, a.n_dev), j0 = blockIdx.x * 16, tid = threadIdx.x, r = tid & 15, grp = tid >> 4, j = j0 + r;
-    if (j0 >= n_rows) return;
+    if (j0 >= n_rows) {
+        if (stats != nullptr && tid < 4) stats[tid] = 0.f;
+        return;
+    }
     const bool flagged = a.flags[1 + (j0 >> 8)] != 0;           // the same for the 16 rows
     const int strips = flagged ? (a.V + STRIP - 1) / STRIP : a.strips;
     float m = 0.f, s = 0.f;
@@ -500,10 +504,17 @@ __global__ __launch_bounds__(1024) void head_finish_kernel(HeadArgs a, LossArgs 
         fac[r] = fy;
         if (l.logp != nullptr) l.logp[j] = lp;
         l.terms[j] = rl.terms;
+        terms[r][0] = rl.terms.x; terms[r][1] = rl.terms.y; terms[r][2] = rl.terms.z; terms[r][3] = rl.terms.w;
     }
-    if (xs == nullptr) return;
+    if (xs == nullptr && stats == nullptr) return;
     __syncthreads();
     const int vpr = a.H / VN, rows = min(16, n_rows - j0);
+    if (stats != nullptr && tid < 4) {
+        double t = 0.;
+        for (int i = 0; i < rows; ++i) t += terms[i][tid];
+        stats[tid] = (float)(t / (l.norm != 0.f ? (double)l.norm : (double)n_rows));
+    }
+    if (xs == nullptr) return;
     for (int v = tid; v < rows * vpr; v += 1024) {
         const int q = v / vpr;
         const int64_t at = (int64_t)(j0 + q) * a.H + (v - q * vpr) * VN;
@@ -1166,7 +1177,7 @@ static hipError_t launch_head(HeadArgs a, LossArgs l, const HeadWs& L, unsigned 
         CF_TRY(HeadLaunch<T>::sums(a, st));
         a.flagged_only = true;
         CF_TRY(HeadLaunch<T>::template logits<MAXIMA>(a, st));
-        head_finish_kernel<T><<<ceil_div(n, 16), 1024, 0, st>>>(a, l, xs);
+        head_finish_kernel<T><<<ceil_div(n, 16), 1024, 0, st>>>(a, l, xs, n <= 16 ? stats : nullptr);
         CF_TRY(hipGetLastError());
         DxArgs d{};
         for (int c = 0; grads && c < V; c += L.cap) {
@@ -1187,7 +1198,7 @@ static hipError_t launch_head(HeadArgs a, LossArgs l, const HeadWs& L, unsigned 
     } else if (dtable != nullptr && !main) {
         CF_TRY(launch_fill_zero(dtable, (size_t)V * H * sizeof(T), st));
     }
-    if (stats != nullptr) launch_loss_stats((const float4*)(ws + L.terms), n, a.n_dev, l.norm, stats, st);
+    if (stats != nullptr && (n == 0 || n > 16)) launch_loss_stats((const float4*)(ws + L.terms), n, a.n_dev, l.norm, stats, st);
     return hipGetLastError();
 }
 
