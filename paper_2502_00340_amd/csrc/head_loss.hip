@@ -1036,6 +1036,189 @@ template <bool MAIN> __global__ F32_BOUNDS void head_dtable_f32_kernel(DtableArg
     }
 }
 
+// ---- fp32, up to 16 rows -----------------------------------------------------------------------------------
+// The table's traffic counts, as for few bf16 rows, and is met with fp32 arithmetic (one row of [151936, 8192], 4.98 GB: logits 817 us, 6.1 TB/s, dx 775, the table's gradient 829; as
+// products of tiles 3.8 ms in all): the logits by the fp32 matrix instruction (16x16x4; a lane's four adjacent k are four
+// instructions, each with an accumulator of its own, so that a sum of H products has chains of H / 16), dx and the table's gradient, whose other operand is
+// a few numbers, by fused multiply-adds.
+constexpr int F32_FEW_ROWS = 16, F32_DX_FEW_ROWS = 4;       // dx of 16 rows so 871 us, as a product of tiles 146 ([50257, 2048])
+
+__global__ __launch_bounds__(512) void head_few_f32_kernel(HeadArgs a) {
+    constexpr int P = 6, R = P + 1, SLOT = 16 * 256, TILE = 128;
+    __shared__ __align__(16) unsigned char smem[R * SLOT];
+    __shared__ float red[8][16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
+    const int rows = __builtin_amdgcn_readfirstlane(live_rows(a.n_max, a.n_dev)), H = a.H, steps = (H + 63) / 64;
+    if (rows == 0) return;
+    const int tiles = (a.V + TILE - 1) / TILE, rot = (int)(blockIdx.x * 37u) % steps;
+    constexpr unsigned OOB = 0x80000000u;
+    // x: four rows of 64 k a load, chunks of 16 bytes XOR-ed with the row; two waves load the same part
+    const i32x4_t rx = make_rsrc(a.x, (int64_t)rows * H * 4);
+    const int part = wave & 3, xrow = part * 4 + (lane >> 4), xk = ((lane & 15) ^ xrow) * 4;
+    const unsigned xoff = (unsigned)xrow * (unsigned)H * 4u + xk * 4u, xdst = __builtin_amdgcn_readfirstlane(lds_addr_of(smem) + part * 1024);
+    int lt = blockIdx.x, ls = 0, slot_in = 0;
+    __amdgpu_buffer_rsrc_t rb;
+    auto open = [&]() __attribute__((always_inline)) {
+        const int64_t v0 = (int64_t)lt * TILE, have = lt < tiles ? min((int64_t)TILE, a.V - v0) : 0;
+        rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>((const float*)a.table + (lt < tiles ? v0 : 0) * H), 0, (int)(have * H * 4), 0x00020000);
+    };
+    open();
+    const unsigned boff = (unsigned)(wave * 16 + l16) * (unsigned)H * 4u + g4 * 16u;
+    u32x4_t b[P][4];
+    auto fetch = [&](u32x4_t (&to)[4]) __attribute__((always_inline)) {
+        const int k0 = (ls + rot >= steps ? ls + rot - steps : ls + rot) * 64;
+        dma16s(xdst + slot_in * SLOT, rx, k0 + xk < H ? xoff : OOB, (unsigned)k0 * 4u);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) to[c] = __builtin_amdgcn_raw_buffer_load_b128(rb, k0 + c * 16 + g4 * 4 < H ? boff : OOB, (k0 + c * 16) * 4, 0);
+        CF_SCHED_FENCE();
+        slot_in = slot_in + 1 == R ? 0 : slot_in + 1;
+        if (++ls == steps) {
+            ls = 0;
+            lt += (int)gridDim.x;
+            open();
+        }
+    };
+    const float ref = l16 < rows ? a.ref[l16] : INFINITY;
+    const bool dead = ref == INFINITY;
+    float sum = 0.f;
+#pragma unroll
+    for (int p = 0; p < P; ++p) fetch(b[p]);
+    f32x4_t acc[4];
+#pragma unroll
+    for (int m = 0; m < 4; ++m) acc[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    int tile = blockIdx.x, s = 0, slot = 0;
+    const int mine = (tiles - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
+    for (int64_t left = (int64_t)mine * steps; left > 0; left -= P) {           // whole rounds, as for bf16
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            wait_vmcnt<(P - 1) * 5>();
+            lds_barrier();
+            const unsigned char* xs = smem + slot * SLOT + l16 * 256;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const float4 fa = *reinterpret_cast<const float4*>(xs + (((c * 4 + g4) ^ l16) << 4));
+                const float* fx = reinterpret_cast<const float*>(&fa);
+#pragma unroll
+                for (int m = 0; m < 4; ++m) acc[m] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b[p][c][m]), fx[m], acc[m], 0, 0, 0);
+            }
+            CF_SCHED_FENCE();
+            fetch(b[p]);
+            slot = slot + 1 == R ? 0 : slot + 1;
+            if (++s == steps) {
+                const int col = tile * TILE + wave * 16 + 4 * g4;
+                float e[4];
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const float l = (acc[0][v] + acc[1][v]) + (acc[2][v] + acc[3][v]);
+                    e[v] = col + v < a.V ? __builtin_amdgcn_exp2f(fmaf(l, a.k, -ref)) : 0.f;
+                    sum += tile < tiles ? e[v] : 0.f;
+                    acc[0][v] = acc[1][v] = acc[2][v] = acc[3][v] = 0.f;
+                }
+                if (a.store_end > 0 && l16 < rows && tile < tiles && col < a.lde)
+                    *reinterpret_cast<float4*>((float*)a.e + (int64_t)l16 * a.lde + col) = dead ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(e[0], e[1], e[2], e[3]);
+                s = 0;
+                tile += (int)gridDim.x;
+            }
+        }
+    }
+    wait_vmcnt<0>();
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    if (g4 == 0) red[wave][l16] = sum;
+    __syncthreads();
+    if ((int)threadIdx.x < rows) {
+        float t = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) t += red[w][threadIdx.x];
+        a.sums[(int64_t)blockIdx.x * a.ldn + threadIdx.x] = t;
+        if (a.ref[threadIdx.x] != INFINITY && !(t <= FLAG_ABOVE)) a.flags[0] = a.flags[1] = 1;
+    }
+}
+
+// what is the same for all threads, and not written during the kernel
+__device__ __forceinline__ float uniform_load(const float* p) { return *(const __attribute__((address_space(4))) float*)(uintptr_t)p; }
+
+// dx, split over the piece's rows of the table: split s of block's columns leaves [s][n_max, H] in the slots
+template <int N> __global__ __launch_bounds__(256) void head_dx_few_f32_kernel(DxArgs a, int splits) {
+    constexpr int U = 8;
+    const int rows = live_rows(a.n_max, a.n_dev), hb = (a.H / 4 + 255) / 256, v = (int)blockIdx.x % hb * 256 + threadIdx.x, split = (int)blockIdx.x / hb;
+    if (rows == 0 || v >= a.H / 4) return;
+    const int per = (a.K + splits - 1) / splits, c0 = min(a.K, split * per), c1 = min(a.K, c0 + per);
+    const float4* t = reinterpret_cast<const float4*>((const float*)a.table) + v;
+    const int64_t ld = a.H / 4;
+    float4 acc[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto take = [&](const float4& w, int c) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float e = uniform_load((const float*)a.e + (int64_t)min(j, rows - 1) * a.lde + c);
+            acc[j].x = fmaf(e, w.x, acc[j].x); acc[j].y = fmaf(e, w.y, acc[j].y); acc[j].z = fmaf(e, w.z, acc[j].z); acc[j].w = fmaf(e, w.w, acc[j].w);
+        }
+    };
+    int c = c0;
+    for (; c + U <= c1; c += U) {
+        float4 w[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) w[u] = t[(c + u) * ld];
+#pragma unroll
+        for (int u = 0; u < U; ++u) take(w[u], c + u);
+    }
+    for (; c < c1; ++c) take(t[c * ld], c);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        if (j >= rows) break;
+        float4* p = reinterpret_cast<float4*>(a.slots + ((int64_t)split * a.n_max + j) * a.H) + v;
+        if (!a.first) {
+            const float4 o = *p;
+            acc[j].x += o.x; acc[j].y += o.y; acc[j].z += o.z; acc[j].w += o.w;
+        }
+        *p = acc[j];
+    }
+}
+__global__ __launch_bounds__(256) void head_dx_few_sum_f32_kernel(DxArgs a, int splits, const float* __restrict__ fac, const int32_t* __restrict__ y, float* __restrict__ dx) {
+    const int rows = live_rows(a.n_max, a.n_dev), ld = a.H / 4, v = blockIdx.x * 256 + threadIdx.x;
+    if (v >= rows * ld) return;
+    const float4* p = reinterpret_cast<const float4*>(a.slots) + v;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 16
+    for (int k = 0; k < splits; ++k) {
+        const float4 w = p[(int64_t)k * a.n_max * ld];
+        s.x += w.x; s.y += w.y; s.z += w.z; s.w += w.w;
+    }
+    const float f = fac[v / ld];
+    const bool live = y[v / ld] >= 0;
+    reinterpret_cast<float4*>(dx)[v] = live ? make_float4(f * s.x, f * s.y, f * s.z, f * s.w) : make_float4(0.f, 0.f, 0.f, 0.f);
+}
+
+template <int N, bool MAIN> __global__ __launch_bounds__(256) void head_dtable_few_f32_kernel(DtableArgs a, int per) {
+    const int rows = live_rows(a.n_max, a.n_dev), hb = (a.H / 4 + 255) / 256, v = (int)blockIdx.x % hb * 256 + threadIdx.x, c0 = (int)blockIdx.x / hb * per;
+    if (v >= a.H / 4 || (MAIN && rows == 0)) return;
+    float4 x[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        x[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (j < rows) x[j] = reinterpret_cast<const float4*>((const float*)a.xs + (int64_t)j * a.H)[v];
+    }
+    const int c1 = min(a.K, c0 + per);
+#pragma unroll 2
+    for (int c = c0; c < c1; ++c) {
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float e = rows > 0 ? uniform_load((const float*)a.e + (int64_t)min(j, rows - 1) * a.lde + c) : 0.f;
+            o.x = fmaf(e, x[j].x, o.x); o.y = fmaf(e, x[j].y, o.y); o.z = fmaf(e, x[j].z, o.z); o.w = fmaf(e, x[j].w, o.w);
+        }
+        float4* p = reinterpret_cast<float4*>((float*)a.out + (int64_t)c * a.H) + v;
+        if constexpr (MAIN) {
+            const float4 b = *p;
+            *p = make_float4(b.x + o.x, b.y + o.y, b.z + o.z, b.w + o.w);
+        } else {
+            __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, o), reinterpret_cast<u32x4_t*>(p));
+        }
+    }
+}
+
 // ---- workspace and launches --------------------------------------------------------------------------------
 
 struct HeadWs {
@@ -1080,6 +1263,11 @@ struct HeadWs {
     }
 };
 
+template <typename T> static void launch_dx_sum(const DxArgs& a, const float* fac, const int32_t* y, void* dx, hipStream_t st) {
+    const int64_t vecs = (int64_t)a.n_max * (a.H / Vec<T>::N);
+    head_dx_sum_kernel<T><<<(int)std::min<int64_t>((vecs + 255) / 256, 32 * compute_units()), 256, 0, st>>>(a, fac, y, (T*)dx);
+}
+
 template <typename T> struct HeadLaunch;
 template <> struct HeadLaunch<bf16_t> {
     template <int KIND> static hipError_t logits(const HeadArgs& a, hipStream_t st) {
@@ -1095,6 +1283,10 @@ template <> struct HeadLaunch<bf16_t> {
         const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&head_few_kernel<NF, P>), lds, lds_ok);
         if (e != hipSuccess) return e;
         head_few_kernel<NF, P><<<a.strips, 512, lds, st>>>(a);
+        return hipGetLastError();
+    }
+    static hipError_t dx_sum(const DxArgs& a, const float* fac, const int32_t* y, bf16_t* dx, hipStream_t st) {
+        launch_dx_sum<bf16_t>(a, fac, y, dx, st);
         return hipGetLastError();
     }
     // sums of the whole vocabulary; sets the number of sums a row has
@@ -1134,12 +1326,41 @@ template <> struct HeadLaunch<float> {
         head_logits_f32_kernel<KIND><<<grid((int64_t)ceil_div(a.n_max, 128) * ceil_div(a.c1 - a.c0, 128)), 256, 0, st>>>(a);
         return hipGetLastError();
     }
-    static hipError_t sums(HeadArgs& a, hipStream_t st) { return logits<SUMS>(a, st); }
+    static hipError_t sums(HeadArgs& a, hipStream_t st) {
+        if (a.n_max > F32_FEW_ROWS) return logits<SUMS>(a, st);
+        a.strips = few_blocks(a.V, compute_units());
+        head_few_f32_kernel<<<a.strips, 512, 0, st>>>(a);
+        return hipGetLastError();
+    }
+    // parts of dx's sum over the vocabulary: eight blocks a CU, each with as much to read as it leaves, in the slots there are
+    static int splits(const DxArgs& a) {
+        const int hb = ceil_div(a.H / 4, 256);
+        const int64_t room = ((int64_t)a.n_max * a.H + (int64_t)2 * a.resident * a.tile * a.tile) / ((int64_t)a.n_max * a.H);
+        return (int)std::max<int64_t>(1, std::min({(int64_t)8 * compute_units() / hb, room, (int64_t)a.V / (16 * a.n_max)}));
+    }
+    static hipError_t dx_sum(const DxArgs& a, const float* fac, const int32_t* y, float* dx, hipStream_t st) {
+        if (a.n_max <= F32_DX_FEW_ROWS) head_dx_few_sum_f32_kernel<<<ceil_div((int64_t)a.n_max * (a.H / 4), 256), 256, 0, st>>>(a, splits(a), fac, y, dx);
+        else launch_dx_sum<float>(a, fac, y, dx, st);
+        return hipGetLastError();
+    }
     static hipError_t dx(const DxArgs& a, hipStream_t st) {
+        if (a.n_max <= F32_DX_FEW_ROWS) {
+            const int s = splits(a), g = s * ceil_div(a.H / 4, 256);
+            if (a.n_max <= 1) head_dx_few_f32_kernel<1><<<g, 256, 0, st>>>(a, s);
+            else head_dx_few_f32_kernel<4><<<g, 256, 0, st>>>(a, s);
+            return hipGetLastError();
+        }
         head_dx_f32_kernel<<<2 * a.resident, 256, 0, st>>>(a);
         return hipGetLastError();
     }
+    template <int N> static hipError_t dtable_few(const DtableArgs& a, bool main, hipStream_t st) {
+        const int hb = ceil_div(a.H / 4, 256), per = ceil_div(a.K, std::max(1, 16 * compute_units() / hb)), g = hb * ceil_div(a.K, per);
+        if (main) head_dtable_few_f32_kernel<N, true><<<g, 256, 0, st>>>(a, per);
+        else head_dtable_few_f32_kernel<N, false><<<g, 256, 0, st>>>(a, per);
+        return hipGetLastError();
+    }
     static hipError_t dtable(const DtableArgs& a, bool main, hipStream_t st) {
+        if (a.n_max <= F32_FEW_ROWS) return a.n_max <= 1 ? dtable_few<1>(a, main, st) : a.n_max <= 4 ? dtable_few<4>(a, main, st) : dtable_few<16>(a, main, st);
         const int g = grid((int64_t)ceil_div(a.K, 128) * ceil_div(a.H, 128));
         if (main) head_dtable_f32_kernel<true><<<g, 256, 0, st>>>(a);
         else head_dtable_f32_kernel<false><<<g, 256, 0, st>>>(a);
@@ -1190,11 +1411,7 @@ static hipError_t launch_head(HeadArgs a, LossArgs l, const HeadWs& L, unsigned 
             if (dtable != nullptr)
                 CF_TRY(HeadLaunch<T>::dtable(DtableArgs{a.e, xs, (char*)dtable + (int64_t)c * H * (main ? 4 : (int)sizeof(T)), a.lde, w, H, n, a.n_dev, 0, 1}, main, st));
         }
-        if (dx != nullptr) {
-            const int64_t vecs = (int64_t)n * (H / Vec<T>::N);
-            head_dx_sum_kernel<T><<<(int)std::min<int64_t>((vecs + 255) / 256, 32 * compute_units()), 256, 0, st>>>(d, a.a, a.y, (T*)dx);
-            CF_TRY(hipGetLastError());
-        }
+        if (dx != nullptr) CF_TRY(HeadLaunch<T>::dx_sum(d, a.a, a.y, (T*)dx, st));
     } else if (dtable != nullptr && !main) {
         CF_TRY(launch_fill_zero(dtable, (size_t)V * H * sizeof(T), st));
     }

@@ -482,7 +482,7 @@ def _head_check(got, x, table, y, dtype, policy=None, w=None, scale=1.0, norm=0.
 
 
 # one row, one column; rows around 16, 32, 64, 128 and tiles of 256; odd vocabularies; a width of one vector; wide; more columns than a least piece
-HEAD = [(1, 8, 1), (1, 64, 300), (3, 16, 7), (17, 40, 999), (33, 72, 130), (64, 256, 1003), (65, 328, 4100), (128, 520, 2500), (129, 840, 2049), (300, 264, 5001), (513, 128, 33000), (257, 1032, 257), (200, 8, 600),
+HEAD = [(1, 8, 1), (1, 64, 300), (3, 16, 7), (1, 1032, 5000), (4, 264, 2100), (13, 1096, 3001), (16, 64, 40000), (17, 40, 999), (33, 72, 130), (64, 256, 1003), (65, 328, 4100), (128, 520, 2500), (129, 840, 2049), (300, 264, 5001), (513, 128, 33000), (257, 1032, 257), (200, 8, 600),
         (140, 24, 5000), (3000, 64, 9)]
 
 
@@ -547,11 +547,11 @@ def test_head_loss_on_kept_rows_into_a_main_gradient(dtype):
 @gpu
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("limit", [0, 1 << 30])
-@pytest.mark.parametrize("n", [100, 600])
+@pytest.mark.parametrize("n", [12, 100, 600])
 def test_head_loss_with_the_count_on_the_device(dtype, limit, n):
     H, V = 72, 3001
     x, table, y, _, g0 = _head_case(6, dtype, n, H, V)
-    for live in (0, 1, 33, n, n + 9) if n == 100 else (0, 1, 100, 129, 257, 600, 609):
+    for live in (0, 1, n // 3, n, n + 9) if n <= 100 else (0, 1, 100, 129, 257, 600, 609):
         say("head count", dtype, live, limit)
         m = min(live, n)
         dev = torch.tensor([live], dtype=torch.int32, device=DEV)
@@ -578,6 +578,9 @@ def test_head_loss_of_rows_that_are_left_out(dtype):
     y[0:40:4], y[1:41:4], y[2] = -1, V, 1 << 40
     w[3:200:16] = 0.0
     dead = (y < 0) | (y >= V) | (w == 0)
+    for few in (16, 9, 1):          # the first rows alone
+        got = Bn.head_loss(torch.where(dead[:, None], float("nan"), x)[:few].contiguous(), table, y[:few].contiguous(), weights=w[:few].contiguous())
+        _head_check(got, x[:few], table, y[:few], dtype, w=w[:few])
     clean = torch.where(dead[:, None], torch.zeros((), dtype=dtype, device=DEV), x)
     want = Bn.head_loss(clean, table, y, weights=w)
     x[dead] = torch.tensor([float("nan"), float("inf"), -float("inf"), 3e38], device=DEV, dtype=dtype).repeat(H // 4)
@@ -593,7 +596,7 @@ def test_head_loss_of_rows_that_are_left_out(dtype):
 @gpu
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("gap", [50.0, 200.0, 5000.0])
-@pytest.mark.parametrize("n", [100, 600])
+@pytest.mark.parametrize("n", [12, 100, 600])
 def test_head_loss_of_improbable_targets(dtype, gap, n):
     """Targets whose logit lies far below the row's largest: their exponentials leave the range in which the target is the reference."""
     H, V = 64, 3000
