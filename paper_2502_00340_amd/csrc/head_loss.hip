@@ -1036,25 +1036,27 @@ template <bool MAIN> __global__ F32_BOUNDS void head_dtable_f32_kernel(DtableArg
     }
 }
 
-// ---- fp32, up to 16 rows -----------------------------------------------------------------------------------
+// ---- fp32, few rows -----------------------------------------------------------------------------------
 // The table's traffic counts, as for few bf16 rows, and is met with fp32 arithmetic (one row of [151936, 8192], 4.98 GB: logits 817 us, 6.1 TB/s, dx 775, the table's gradient 829; as
 // products of tiles 3.8 ms in all): the logits by the fp32 matrix instruction (16x16x4; a lane's four adjacent k are four
 // instructions, each with an accumulator of its own, so that a sum of H products has chains of H / 16), dx and the table's gradient, whose other operand is
 // a few numbers, by fused multiply-adds.
-constexpr int F32_FEW_ROWS = 16, F32_DX_FEW_ROWS = 4;       // dx of 16 rows so 871 us, as a product of tiles 146 ([50257, 2048])
+// Up to how many rows: the logits (32 rows, [32000, 4096], 139 to 157 us, tiles 240; 64 rows, [50257, 2048], 187 and 177), the table's gradient, dx (16 rows, [50257, 2048], 871 and 146)
+constexpr int F32_SUMS_FEW_ROWS = 32, F32_FEW_ROWS = 16, F32_DX_FEW_ROWS = 4;
 
-__global__ __launch_bounds__(512) void head_few_f32_kernel(HeadArgs a) {
-    constexpr int P = 6, R = P + 1, SLOT = 16 * 256, TILE = 128;
-    __shared__ __align__(16) unsigned char smem[R * SLOT];
-    __shared__ float red[8][16];
+template <int NF, int P> __global__ __launch_bounds__(512) void head_few_f32_kernel(HeadArgs a) {
+    constexpr int R = P + 1, ROWS = 16 * NF, SLOT = ROWS * 256, TILE = 128;
+    static_assert(NF <= 2, "a load of x a wave and step");
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ float red[8][ROWS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
     const int rows = __builtin_amdgcn_readfirstlane(live_rows(a.n_max, a.n_dev)), H = a.H, steps = (H + 63) / 64;
     if (rows == 0) return;
     const int tiles = (a.V + TILE - 1) / TILE, rot = (int)(blockIdx.x * 37u) % steps;
     constexpr unsigned OOB = 0x80000000u;
-    // x: four rows of 64 k a load, chunks of 16 bytes XOR-ed with the row; two waves load the same part
+    // x: four rows of 64 k a load, chunks of 16 bytes XOR-ed with the row; with few rows two waves load the same part
     const i32x4_t rx = make_rsrc(a.x, (int64_t)rows * H * 4);
-    const int part = wave & 3, xrow = part * 4 + (lane >> 4), xk = ((lane & 15) ^ xrow) * 4;
+    const int part = wave % (4 * NF), xrow = part * 4 + (lane >> 4), xk = ((lane ^ xrow) & 15) * 4;
     const unsigned xoff = (unsigned)xrow * (unsigned)H * 4u + xk * 4u, xdst = __builtin_amdgcn_readfirstlane(lds_addr_of(smem) + part * 1024);
     int lt = blockIdx.x, ls = 0, slot_in = 0;
     __amdgpu_buffer_rsrc_t rb;
@@ -1078,14 +1080,19 @@ __global__ __launch_bounds__(512) void head_few_f32_kernel(HeadArgs a) {
             open();
         }
     };
-    const float ref = l16 < rows ? a.ref[l16] : INFINITY;
-    const bool dead = ref == INFINITY;
-    float sum = 0.f;
+    float ref[NF], sum[NF];
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+        ref[i] = i * 16 + l16 < rows ? a.ref[i * 16 + l16] : INFINITY;
+        sum[i] = 0.f;
+    }
 #pragma unroll
     for (int p = 0; p < P; ++p) fetch(b[p]);
-    f32x4_t acc[4];
+    f32x4_t acc[NF][4];
 #pragma unroll
-    for (int m = 0; m < 4; ++m) acc[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < NF; ++i)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) acc[i][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     int tile = blockIdx.x, s = 0, slot = 0;
     const int mine = (tiles - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
     for (int64_t left = (int64_t)mine * steps; left > 0; left -= P) {           // whole rounds, as for bf16
@@ -1095,36 +1102,45 @@ __global__ __launch_bounds__(512) void head_few_f32_kernel(HeadArgs a) {
             lds_barrier();
             const unsigned char* xs = smem + slot * SLOT + l16 * 256;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const float4 fa = *reinterpret_cast<const float4*>(xs + (((c * 4 + g4) ^ l16) << 4));
-                const float* fx = reinterpret_cast<const float*>(&fa);
+            for (int c = 0; c < 4; ++c)
 #pragma unroll
-                for (int m = 0; m < 4; ++m) acc[m] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b[p][c][m]), fx[m], acc[m], 0, 0, 0);
-            }
+                for (int i = 0; i < NF; ++i) {
+                    const f32x4_t fa = *reinterpret_cast<const f32x4_t*>(xs + i * 4096 + (((c * 4 + g4) ^ l16) << 4));
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) acc[i][m] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b[p][c][m]), fa[m], acc[i][m], 0, 0, 0);
+                }
             CF_SCHED_FENCE();
             fetch(b[p]);
             slot = slot + 1 == R ? 0 : slot + 1;
             if (++s == steps) {
                 const int col = tile * TILE + wave * 16 + 4 * g4;
-                float e[4];
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const float l = (acc[0][v] + acc[1][v]) + (acc[2][v] + acc[3][v]);
-                    e[v] = col + v < a.V ? __builtin_amdgcn_exp2f(fmaf(l, a.k, -ref)) : 0.f;
-                    sum += tile < tiles ? e[v] : 0.f;
-                    acc[0][v] = acc[1][v] = acc[2][v] = acc[3][v] = 0.f;
+                for (int i = 0; i < NF; ++i) {
+                    float e[4];
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const float l = (acc[i][0][v] + acc[i][1][v]) + (acc[i][2][v] + acc[i][3][v]);
+                        e[v] = col + v < a.V ? __builtin_amdgcn_exp2f(fmaf(l, a.k, -ref[i])) : 0.f;
+                        sum[i] += tile < tiles ? e[v] : 0.f;
+                        acc[i][0][v] = acc[i][1][v] = acc[i][2][v] = acc[i][3][v] = 0.f;
+                    }
+                    const int m = i * 16 + l16;
+                    if (a.store_end > 0 && m < rows && tile < tiles && col < a.lde)
+                        *reinterpret_cast<float4*>((float*)a.e + (int64_t)m * a.lde + col) =
+                            ref[i] == INFINITY ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(e[0], e[1], e[2], e[3]);
                 }
-                if (a.store_end > 0 && l16 < rows && tile < tiles && col < a.lde)
-                    *reinterpret_cast<float4*>((float*)a.e + (int64_t)l16 * a.lde + col) = dead ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(e[0], e[1], e[2], e[3]);
                 s = 0;
                 tile += (int)gridDim.x;
             }
         }
     }
     wait_vmcnt<0>();
-    sum += __shfl_xor(sum, 16, 64);
-    sum += __shfl_xor(sum, 32, 64);
-    if (g4 == 0) red[wave][l16] = sum;
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+        sum[i] += __shfl_xor(sum[i], 16, 64);
+        sum[i] += __shfl_xor(sum[i], 32, 64);
+        if (g4 == 0) red[wave][i * 16 + l16] = sum[i];
+    }
     __syncthreads();
     if ((int)threadIdx.x < rows) {
         float t = 0.f;
@@ -1327,9 +1343,16 @@ template <> struct HeadLaunch<float> {
         return hipGetLastError();
     }
     static hipError_t sums(HeadArgs& a, hipStream_t st) {
-        if (a.n_max > F32_FEW_ROWS) return logits<SUMS>(a, st);
+        if (a.n_max > F32_SUMS_FEW_ROWS) return logits<SUMS>(a, st);
         a.strips = few_blocks(a.V, compute_units());
-        head_few_f32_kernel<<<a.strips, 512, 0, st>>>(a);
+        return a.n_max <= 16 ? few<1>(a, st) : few<2>(a, st);
+    }
+    template <int NF> static hipError_t few(const HeadArgs& a, hipStream_t st) {
+        static std::atomic<uint64_t> lds_ok{0};
+        constexpr int P = 6, lds = (P + 1) * NF * 16 * 256;
+        const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&head_few_f32_kernel<NF, P>), lds, lds_ok);
+        if (e != hipSuccess) return e;
+        head_few_f32_kernel<NF, P><<<a.strips, 512, lds, st>>>(a);
         return hipGetLastError();
     }
     // parts of dx's sum over the vocabulary: eight blocks a CU, each with as much to read as it leaves, in the slots there are
