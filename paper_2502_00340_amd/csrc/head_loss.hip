@@ -2,10 +2,10 @@
 // tile in the matrix cores' accumulators and never leave them.  What leaves is bounded by the caller's workspace:
 //
 //   1. head_rows      the target's logit of every row, a dot product: ref = s*log2(e) * x.E_y
-//   2. head_logits    tiles of x E^T; with t = s*log2(e)*l - ref, strips of 64 columns leave sum(2^t), and, for the first columns (as many as the
-//                     workspace has room for), e = 2^t in the storage type
-//   3. head_finish    per row lp = -log(sum over c of 2^t), the loss and its slope; a = -w/norm * dL/dlp * s * exp(lp) is the row's factor: the gradient of logit c is
-//                     a * e_c, and a * e'_y with e'_y = expm1(lp) / exp(lp) at the target.  x' = a * x for the table's gradient
+//   2. head_logits    tiles of x E^T; with t = s*log2(e)*l - ref, strips of 64 columns leave sum(2^t) of the columns that are not the target, and, for the first columns
+//                     (as many as the workspace has room for), e = 2^t in the storage type
+//   3. head_finish    per row, with q the sum of its strips, lp = -log(1 + q), the loss and its slope; a = -w/norm * dL/dlp * s * exp(lp) is the row's factor: the gradient
+//                     of logit c is a * e_c, and a * e'_y with e'_y = expm1(lp) / exp(lp) = -q at the target.  x' = a * x for the table's gradient
 //   4. for each piece of the columns (the first one is there already, the others are made again by head_logits):
 //      head_dx        slots (+)= e E, fp32          head_dtable   dE (+)= e^T x'
 //   5. head_dx_sum    dx = a * sum of the slots
@@ -13,6 +13,8 @@
 // Taking the target's logit as the reference (not the row's maximum, which is not known ahead of the product) makes e a number that needs no second scaling:
 // 2^t is at most exp(-lp), so that nothing leaves fp32's or bf16's range unless the target has a probability below exp(-40).  A strip whose sum says so raises its
 // row tile's flag; head_logits then goes over the flagged tiles again with strips' maxima, and the row's log-sum-exp becomes its reference.
+// The target's own exponential, 1, stays out of the sums: step 1's order of sums is not that of the products, so that 2^t at the target would be 1 + d with a d of some 1e-6, and
+// what an almost certain target leaves to the others, 1 - p, would drown in it.  So it keeps all digits, and a row's gradients add up to 0 but for their roundings.
 //
 // What bounds it: the matrix cores under the chip's power limit from some hundred rows on (4096 rows, H = 4096, V = 128256 bf16: logits, dx and the table's gradient
 // 3.04, 3.01 and 3.08 ms, 1.40 to 1.43 PFLOP/s), the table's traffic for few rows.  Keeping e makes that three products instead of four.
@@ -91,7 +93,7 @@ template <int KIND> struct LeaveLogits {
     int n_rows;
     struct Rows {
         float ref[8], ey[KIND == VALUES ? 8 : 1];
-        int y[KIND == VALUES ? 8 : 1];
+        int y[8];
     };
     template <int TM> __device__ __forceinline__ Rows rows(const TileRef& t, int wm) const {
         Rows r;
@@ -99,25 +101,32 @@ template <int KIND> struct LeaveLogits {
         for (int i = 0; i < 2 * TM; ++i) {
             const int m = t.m0 + wm * (32 * TM) + i * 16 + (threadIdx.x & 15), at = min(m, n_rows - 1);
             const float ref = a.ref[at];
+            const int y = a.y[at];
             r.ref[i] = m < n_rows ? ref : INFINITY;
-            if constexpr (KIND == VALUES) { r.y[i] = a.y[at]; r.ey[i] = a.ey[at]; }
+            r.y[i] = m < n_rows ? y : -1;
+            if constexpr (KIND == VALUES) r.ey[i] = a.ey[at];
         }
         // arrived ahead of whatever is asked for next
 #pragma unroll
         for (int i = 0; i < 2 * TM; ++i) {
             asm volatile("" : "+v"(r.ref[i]));
-            if constexpr (KIND == VALUES) { asm volatile("" : "+v"(r.y[i])); asm volatile("" : "+v"(r.ey[i])); }
+            asm volatile("" : "+v"(r.y[i]));
+            if constexpr (KIND == VALUES) asm volatile("" : "+v"(r.ey[i]));
         }
         return r;
     }
     template <int TM, int TN>
     __device__ __forceinline__ void operator()(f32x4_t (&acc)[2 * TM][2 * TN], const TileRef& t, const Rows& row, unsigned char* smem, int wm, int wn) const {
-        // Columns behind the last one, in the last column of tiles, have a copy of the code of their own: a write to the accumulators, or a branch around a part of
-        // this, would have all of them copied to vector registers, and others spilled
-        if (t.n0 + 64 * TN > a.V) write_out<TM, TN, true>(acc, t, row, smem, wm, wn);
-        else write_out<TM, TN, false>(acc, t, row, smem, wm, wn);
+        // Columns behind the last one, in the last column of tiles, and targets among a wave's rows and columns have a copy of the code of their own: a write to the
+        // accumulators, or a branch around a part of this, would have all of them copied to vector registers, and others spilled
+        bool hit = false;
+#pragma unroll
+        for (int i = 0; i < 2 * TM; ++i) hit |= (unsigned)(row.y[i] - (t.n0 + wn * (32 * TN))) < 32u * TN;
+        if (t.n0 + 64 * TN > a.V) write_out<TM, TN, true, true>(acc, t, row, smem, wm, wn);
+        else if (__any(hit)) write_out<TM, TN, false, true>(acc, t, row, smem, wm, wn);
+        else write_out<TM, TN, false, false>(acc, t, row, smem, wm, wn);
     }
-    template <int TM, int TN, bool EDGE>
+    template <int TM, int TN, bool EDGE, bool TARGETS>
     __device__ __forceinline__ void write_out(f32x4_t (&acc)[2 * TM][2 * TN], const TileRef& t, const Rows& row, unsigned char* smem, int wm, int wn) const {
         constexpr int FN = 2 * TN, NS = FN / 4;
         const int rows = n_rows;
@@ -146,7 +155,7 @@ template <int KIND> struct LeaveLogits {
                 const int i = 2 * i2 + h;
                 const float ref = row.ref[i];
                 const bool dead = ref == INFINITY;
-                const int yrel = KIND == VALUES ? row.y[KIND == VALUES ? i : 0] - n0 - 4 * g4 : -1;
+                const int yrel = row.y[i] - n0 - 4 * g4;
                 const float ey = row.ey[KIND == VALUES ? i : 0];
                 const unsigned mask = dead ? 0u : ~0u;          // whatever such a row holds, NaN included
 #pragma unroll
@@ -156,7 +165,7 @@ template <int KIND> struct LeaveLogits {
 #pragma unroll
                         for (int j = 4 * z; j < 4 * z + 4; ++j)
 #pragma unroll
-                            for (int v = 0; v < 4; ++v) mx = !EDGE || j * 16 + v < left ? fmaxf(mx, acc[i][j][v]) : mx;
+                            for (int v = 0; v < 4; ++v) mx = (!EDGE || j * 16 + v < left) && (!TARGETS || j * 16 + v != yrel) ? fmaxf(mx, acc[i][j][v]) : mx;
                         mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
                         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
                         mx *= a.k;
@@ -169,8 +178,8 @@ template <int KIND> struct LeaveLogits {
                         for (int v = 0; v < 4; ++v) {
                             e[v] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][v], a.k, -r));
                             if constexpr (EDGE) e[v] = j * 16 + v < left ? e[v] : 0.f;
+                            if constexpr (TARGETS) e[v] = yrel == j * 16 + v ? (KIND == VALUES ? ey : 0.f) : e[v];
                             if constexpr (KIND != VALUES) s += e[v];
-                            else e[v] = yrel == j * 16 + v ? ey : e[v];
                         }
                         if constexpr (KIND != MAXIMA) {
                             uint2 o;
@@ -320,10 +329,12 @@ template <int NF, int P> __global__ __launch_bounds__(512) void head_few_kernel(
         }
     };
     float ref[NF], sum[NF];
+    int y[NF];
 #pragma unroll
     for (int i = 0; i < NF; ++i) {
         const int m = i * 16 + l16;
         ref[i] = m < rows ? a.ref[m] : INFINITY;
+        y[i] = m < rows ? a.y[m] : -1;
         sum[i] = 0.f;
     }
 #pragma unroll
@@ -340,7 +351,7 @@ template <int NF, int P> __global__ __launch_bounds__(512) void head_few_kernel(
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 e[v] = __builtin_amdgcn_exp2f(fmaf(acc[i][v], a.k, -ref[i]));
-                e[v] = c + v < a.V ? e[v] : 0.f;
+                e[v] = c + v < a.V && c + v != y[i] ? e[v] : 0.f;
                 sum[i] += e[v];
             }
             if (a.store_end > 0) {
@@ -465,16 +476,23 @@ __global__ __launch_bounds__(1024) void head_finish_kernel(HeadArgs a, LossArgs 
         float lp = 0.f, fy = 0.f;
         RowLoss rl{make_float4(0.f, 0.f, 0.f, 0.f), 0.f};
         if (y >= 0) {
-            // lp = ln(2) * (target - log2(sum)), with the sum relative to ref or, flagged, to m
-            const float ref = a.ref[j], ln2 = 0.6931471805599453f, rest = ln2 * a.ey[j];
+            // q: what the other columns' exponentials add up to relative to the target's own, lp = -log(1 + q).  s is relative to ref, the target's logit but for its
+            // rounding r, or, flagged, to m
+            const float ref = a.ref[j], ln2 = 0.6931471805599453f, r = ln2 * a.ey[j];
+            float fy0, ey;          // the row's factor is the slope times fy0
             if (!flagged) {
-                lp = rest - logf(s);
+                const float by = expf(-r), q = s * by;
+                lp = -log1pf(q);
+                fy0 = by / (1.f + q);
+                ey = -s;
             } else {
-                lp = ln2 * (ref - m) + (rest - logf(s));
-                const float lse = m + log2f(s);
+                const float t = ln2 * (m - ref) + (logf(s) - r), small = log1pf(expf(-fabsf(t))), log2e = 1.4426950408889634f;         // t = log(q)
+                lp = -(fmaxf(t, 0.f) + small);
+                const float lse = (t > 0.f ? m + log2f(s) : ref) + small * log2e;
                 a.ref[j] = lse == INFINITY ? NAN : lse;
+                fy0 = 1.f;
+                ey = expm1f(lp);
             }
-            lp = lp > 0.f ? 0.f : lp;           // the target's logit comes from another order of sums than the strips'
             RowHead h;
             h.row = l.idx != nullptr ? l.idx[j] : j;
             h.y = y;
@@ -486,16 +504,13 @@ __global__ __launch_bounds__(1024) void head_finish_kernel(HeadArgs a, LossArgs 
                 if (l.ref_logp != nullptr) h.ref = l.ref_logp[h.row];
             }
             rl = row_loss(l, h, lp, 1.f / (l.norm != 0.f ? l.norm : (float)n_rows));
-            // e of the other columns is relative to exp(lp) (flagged: to 1)
-            const float by = flagged ? 1.f : s;
-            fy = -rl.coef * l.scale / by;
-            float ey = expm1f(lp) * by;
+            fy = -rl.coef * l.scale * fy0;
             if constexpr (sizeof(T) == 2) {
                 // The target's e is most of a row's gradient.  Its rounding goes over to the row's factor, so that factor times e is exact at the target and
                 // off by that rounding, and their own, at the other columns: gradients 1.4 times as far off as one rounding instead of 1.7.
-                const float r = bf16_to_f32(narrow_one<bf16_t>(ey)), by_r = ey / r;
-                if (by_r > 0.5f && by_r < 2.f) fy *= by_r;
-                ey = r;
+                const float near = bf16_to_f32(narrow_one<bf16_t>(ey)), by = ey / near;
+                if (by > 0.5f && by < 2.f) fy *= by;
+                ey = near;
             }
             a.ey[j] = ey;
             if (a.e != nullptr && !flagged && y < a.store_end) ((T*)a.e)[(int64_t)j * a.lde + y] = narrow_one<T>(ey);
@@ -933,12 +948,13 @@ template <int KIND> __global__ F32_BOUNDS void head_logits_f32_kernel(HeadArgs a
             const bool dead = ref == INFINITY;
             float s = 0.f, mx = -INFINITY, ey = 0.f;
             int y = -1;
-            if (KIND == VALUES && m < rows) { y = a.y[m]; ey = a.ey[m]; }
+            if (m < rows) { y = a.y[m]; ey = KIND == VALUES ? a.ey[m] : 0.f; }
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    if (c + j * 16 + 4 * g4 + v >= a.V) acc[i][j][v] = -INFINITY;
+                    const int col = c + j * 16 + 4 * g4 + v;
+                    if (col >= a.V || (KIND == MAXIMA && col == y)) acc[i][j][v] = -INFINITY;
                     mx = fmaxf(mx, acc[i][j][v]);
                 }
             mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
@@ -951,8 +967,8 @@ template <int KIND> __global__ F32_BOUNDS void head_logits_f32_kernel(HeadArgs a
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
                     e[v] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][v], a.k, -r));
+                    if (col + v == y) e[v] = ey;
                     s += e[v];
-                    if (KIND == VALUES && col + v == y) e[v] = ey;
                     if (dead) e[v] = 0.f;
                 }
                 if (store && m < rows && col - a.c0 < a.lde)
@@ -1081,9 +1097,11 @@ template <int NF, int P> __global__ __launch_bounds__(512) void head_few_f32_ker
         }
     };
     float ref[NF], sum[NF];
+    int y[NF];
 #pragma unroll
     for (int i = 0; i < NF; ++i) {
         ref[i] = i * 16 + l16 < rows ? a.ref[i * 16 + l16] : INFINITY;
+        y[i] = i * 16 + l16 < rows ? a.y[i * 16 + l16] : -1;
         sum[i] = 0.f;
     }
 #pragma unroll
@@ -1120,7 +1138,7 @@ template <int NF, int P> __global__ __launch_bounds__(512) void head_few_f32_ker
 #pragma unroll
                     for (int v = 0; v < 4; ++v) {
                         const float l = (acc[i][0][v] + acc[i][1][v]) + (acc[i][2][v] + acc[i][3][v]);
-                        e[v] = col + v < a.V ? __builtin_amdgcn_exp2f(fmaf(l, a.k, -ref[i])) : 0.f;
+                        e[v] = col + v < a.V && col + v != y[i] ? __builtin_amdgcn_exp2f(fmaf(l, a.k, -ref[i])) : 0.f;
                         sum[i] += tile < tiles ? e[v] : 0.f;
                         acc[i][0][v] = acc[i][1][v] = acc[i][2][v] = acc[i][3][v] = 0.f;
                     }

@@ -1,0 +1,88 @@
+"""Digits and paths of the operators at the ends of the stack of layers that bounds by absolute sums are too wide for: targets that are almost certain, fp32 products
+whose exact result fp32 holds, plans of tiles and rings that small sizes do not reach.
+
+Tolerances count roundings: a stored value is off by half a step of its type (EPS: half of finfo.eps, relative), an fp32 sum of n
+terms by (its depth, at most n) * 2^-24 of the sum of their absolute values, a function of the hardware or the library by a few 2^-24."""
+import math
+
+import pytest
+import torch
+
+from paper_2502_00340_amd import binding as Bn
+from tests.test_step_ops import BF, DEV, EPS, F32, F64, U, close, gen, gpu, randn, say
+
+
+# ---- targets that are almost certain -----------------------------------------------------------------------
+
+def _dlogits(l, y, n):
+    """(logp, dlogits of the mean NLL) for logits l [n, V] in 64 bits, from the other columns' share alone: no digit of 1 - p is lost."""
+    at = y[:, None]
+    others = (l - l.gather(1, at)).exp().scatter_(1, at, 0.0)
+    rest = others.sum(1, keepdim=True)
+    d = others / (1.0 + rest)
+    return -torch.log1p(rest).squeeze(1), d.scatter(1, at, -rest / (1.0 + rest)) / n
+
+
+def test_share_of_the_other_columns_reference():
+    g0 = gen(1)
+    l, y = randn(g0, 5, 7, std=2.0, dtype=F64, device="cpu").requires_grad_(), torch.tensor([0, 6, 3, 3, 1])
+    loss = torch.nn.functional.cross_entropy(l, y)
+    loss.backward()
+    lp, d = _dlogits(l.detach(), y, 5)
+    close(d, l.grad, 1e-14, "d")
+    assert abs(float(-lp.mean()) - loss.item()) < 1e-14
+
+
+def _certain_case(dtype, n, H, V, improbable):
+    """Rows whose targets have 1 - p of some 1e-2 down to 1e-11.  The first columns of x are the identity, those of the table 0: the table's gradient holds there what
+    the logits' gradient is, row by row."""
+    g0, K = gen(n + H + V), (n + 7) // 8 * 8
+    table = randn(g0, V, H, std=2.0 / math.sqrt(H))
+    y = torch.randint(0, V - 1, (n,), generator=g0).to(DEV)
+    x = randn(g0, n, H) + table[y] * torch.linspace(3.2, 8.0, n)[torch.randperm(n, generator=g0)][:, None].to(DEV)
+    if improbable:          # the first row's tile is gone over again with another reference; its other rows stay what they are
+        x[:, 0], table[:, 0] = 0.0, 0.0
+        x[0], table[V - 1, 0] = 0.0, 200.0
+        x[0, 0] = 1.0
+    x = torch.cat((torch.eye(n, K, device=DEV), x), 1).to(dtype).contiguous()
+    table = torch.cat((torch.zeros(V, K, device=DEV), table), 1).to(dtype).contiguous()
+    return x, table, y
+
+
+# rows of each form: up to 16, 32, 64 and 128, whole tiles; columns beyond a piece of the least size; more tiles than CUs
+@gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n,H,V", [(1, 264, 3000), (12, 1096, 3000), (24, 1096, 3000), (60, 264, 3001), (100, 264, 2500), (300, 520, 3000), (12, 264, 40000), (24, 264, 40000), (60, 264, 40000),
+                                   (100, 264, 40000)])
+@pytest.mark.parametrize("improbable", [False, True])
+def test_head_loss_of_almost_certain_targets(dtype, n, H, V, improbable):
+    say("certain", dtype, n, H, V, improbable)
+    x, table, y = _certain_case(dtype, n, H, V, improbable)
+    x64, t64 = x.to(F64), table.to(F64)
+    l = x64 @ t64.T
+    lp, d = _dlogits(l, y, n)
+    # the difference of two logits, sums of H products each (the identity adds none), its scaling and its exponential; sums of 64 columns and of these strips
+    big = float((x64.abs() @ t64.abs().T).max())
+    rel = 2 * (H + 4) * U * big + (4 * float((l - l.gather(1, y[:, None])).abs().max()) + V / 64 + 64) * U
+    got = [Bn.head_loss(x, table, y, ws_limit=limit) for limit in (1 << 30, 0)]
+    got.append(Bn.head_loss(x, table, y, need_dx=False, need_dtable=False))
+    for k, (_, glp, dx, dt) in enumerate(got):
+        # 1 - p and its logarithm: both relative to themselves
+        close(glp, lp, (2 * rel + 8 * U) * lp.abs() + 2.0 ** -126, "logp")
+        if dt is None:
+            continue
+        # e, the row's factor, the scaled input, the result; bf16: the target's e is exact, its rounding the factor's
+        gd = dt[:, :n].T.to(F64)
+        hot = torch.zeros_like(d, dtype=torch.bool).scatter_(1, y[:, None], True)
+        tol = d.abs() * (2 * rel + 16 * U + 1.01 * EPS[dtype] * torch.where(hot, 2.0, 4.0)) + 2.0 ** -120
+        close(gd, d, tol, "dlogits")
+        # what a row's gradient adds up to is nothing but roundings
+        own = d.abs().sum(1)
+        if dtype is F32 and not improbable and k == 0:
+            over = gd.sum(1).abs() - own * (V / 64 + 128) * U
+        else:
+            over = gd.sum(1).abs() - own * (2 * rel + 16 * U + 4.04 * EPS[dtype])
+        assert float(over.max()) <= 2.0 ** -120 * V, float((gd.sum(1).abs() / own).max())
+        want = d @ t64
+        if dtype is F32:
+            close(dx, want, (d.abs() * (2 * rel + (V + 16) * U)) @ t64.abs() + 2.0 ** -120, "dx")
