@@ -48,6 +48,8 @@ struct HeadArgs {
     int lde, c0, c1;        // the launch's columns: c0 .. c1 - 1
     int store_end;          // columns below it are stored
     bool flagged_only;
+    float* part;            // fp32: [parts] tiles' accumulators of each part of the contraction, where it is cut
+    int parts;
 };
 enum HeadKind { SUMS = 0, MAXIMA = 1, VALUES = 2 };
 
@@ -928,62 +930,120 @@ template <int MODE> __device__ __forceinline__ void f32_tile(const F32Tile& t, u
     }
 }
 
+// What becomes of 16 rows' logits in a strip of columns from c on: lane l has row m = m0' + l % 16 and, in acc[j], columns c + 16 j + 4 * (l / 16) .. +3
+template <int KIND> __device__ __forceinline__ void leave_f32(const HeadArgs& a, int rows, f32x4_t (&acc)[4], int m, int c, bool store) {
+    const int g4 = (threadIdx.x & 63) >> 4;
+    const float ref = m < rows ? a.ref[m] : INFINITY;
+    const bool dead = ref == INFINITY;
+    float s = 0.f, mx = -INFINITY, ey = 0.f;
+    int y = -1;
+    if (m < rows) { y = a.y[m]; ey = KIND == VALUES ? a.ey[m] : 0.f; }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int col = c + j * 16 + 4 * g4 + v;
+            if (col >= a.V || (KIND == MAXIMA && col == y)) acc[j][v] = -INFINITY;
+            mx = fmaxf(mx, acc[j][v]);
+        }
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * a.k;
+    const float r = KIND == MAXIMA ? (mx == -INFINITY ? 0.f : mx) : ref;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int col = c + j * 16 + 4 * g4;
+        float e[4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            e[v] = __builtin_amdgcn_exp2f(fmaf(acc[j][v], a.k, -r));
+            if (col + v == y) e[v] = ey;
+            s += e[v];
+            if (dead) e[v] = 0.f;
+        }
+        if (store && m < rows && col - a.c0 < a.lde)
+            *reinterpret_cast<float4*>((float*)a.e + (int64_t)m * a.lde + (col - a.c0)) = make_float4(e[0], e[1], e[2], e[3]);
+    }
+    if (KIND != VALUES) {
+        s += __shfl_xor(s, 16, 64);
+        s += __shfl_xor(s, 32, 64);
+        if (g4 == 0 && m < rows && c < a.V) {
+            a.sums[(int64_t)(c / STRIP) * a.ldn + m] = KIND == MAXIMA ? mx + log2f(s) : s;
+            if (KIND == SUMS && !dead && !(s <= FLAG_ABOVE)) a.flags[0] = a.flags[1 + (m >> 8)] = 1;
+        }
+    }
+}
+
 template <int KIND> __global__ F32_BOUNDS void head_logits_f32_kernel(HeadArgs a) {
     __shared__ __align__(16) unsigned char smem[F32_SMEM];
     if (a.flagged_only && a.flags[0] == 0) return;
     const int rows = live_rows(a.n_max, a.n_dev), tm = (rows + 127) / 128, tn = (a.c1 - a.c0 + 127) / 128;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, l16 = lane & 15, g4 = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
     for (int64_t w = blockIdx.x; w < (int64_t)tm * tn; w += gridDim.x) {
         const int bm = (int)(w % tm), m0 = bm * 128, n0 = a.c0 + (int)(w / tm) * 128;
         if (a.flagged_only && a.flags[1 + (m0 >> 8)] == 0) continue;
         const F32Tile t{(const float*)a.x, (const float*)a.table, a.H, a.H, rows, min(a.c1, a.V), 0, a.H, m0, n0};
         f32x4_t acc[4][4];
         f32_tile<0>(t, smem, acc);
-        const int c = n0 + wn * 64;             // a strip
-        const bool store = KIND != MAXIMA && n0 < a.store_end;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int m = m0 + wm * 64 + i * 16 + l16;
-            const float ref = m < rows ? a.ref[m] : INFINITY;
-            const bool dead = ref == INFINITY;
-            float s = 0.f, mx = -INFINITY, ey = 0.f;
-            int y = -1;
-            if (m < rows) { y = a.y[m]; ey = KIND == VALUES ? a.ey[m] : 0.f; }
+        for (int i = 0; i < 4; ++i)
+            leave_f32<KIND>(a, rows, acc[i], m0 + wm * 64 + i * 16 + (lane & 15), n0 + wn * 64, KIND != MAXIMA && n0 < a.store_end);
+    }
+}
+
+// Fewer tiles than blocks that are resident at a time: a block takes a part of a tile's contraction and leaves its accumulators as they lie in its lanes; a wave a
+// fragment row of a tile adds the parts up in order and does with the sum what the whole tile would.  A flagged tile is added up again, not multiplied.
+// Whole calls, no gradients, without and with parts: 33 rows of [300, 8192] 455 and 43 us, 300 of [2500, 8192] 460 and 113, 300 of [12000, 2048] (282 tiles, two parts) 164 and
+// 135, 600 of [2000, 512] (four steps a part) 46 and 34.
+struct F32Parts {
+    int tiles, parts, per;          // per: steps of 32 k a part; parts 1: whole tiles
+    F32Parts(int n, int V, int H, int resident) {
+        const int steps = ceil_div(H, F32_STEP);
+        const int64_t t = (int64_t)ceil_div(n, 128) * ceil_div(V, 128);
+        tiles = (int)std::min<int64_t>(t, 1 << 30);
+        parts = std::max(1, std::min(resident / tiles, steps / 4));
+        per = ceil_div(steps, parts);
+        parts = ceil_div(steps, per);
+    }
+};
+__global__ F32_BOUNDS void head_logits_part_f32_kernel(HeadArgs a, int tm, int tiles, int per) {
+    __shared__ __align__(16) unsigned char smem[F32_SMEM];
+    const int rows = live_rows(a.n_max, a.n_dev), tile = (int)blockIdx.x % tiles, part = (int)blockIdx.x / tiles, m0 = tile % tm * 128;
+    if (m0 >= rows) return;
+    const int k0 = part * per * F32_STEP;
+    const F32Tile t{(const float*)a.x, (const float*)a.table, a.H, a.H, rows, a.V, k0, min(a.H, k0 + per * F32_STEP), m0, tile / tm * 128};
+    f32x4_t acc[4][4];
+    f32_tile<0>(t, smem, acc);
+    f32x4_t* p = reinterpret_cast<f32x4_t*>(a.part) + (int64_t)blockIdx.x * 4096 + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) p[(i * 4 + j) * 256] = acc[i][j];
+}
+template <int KIND> __global__ __launch_bounds__(64) void head_logits_join_f32_kernel(HeadArgs a, int tm, int tiles) {
+    if (a.flagged_only && a.flags[0] == 0) return;
+    const int rows = live_rows(a.n_max, a.n_dev), tile = (int)blockIdx.x >> 4, i = (int)blockIdx.x & 3, wave = ((int)blockIdx.x >> 2) & 3;
+    const int m0 = tile % tm * 128, n0 = tile / tm * 128, m = m0 + (wave >> 1) * 64 + i * 16;
+    if (m >= rows || n0 >= a.c1 || (a.flagged_only && a.flags[1 + (m0 >> 8)] == 0)) return;
+    const f32x4_t* p = reinterpret_cast<const f32x4_t*>(a.part) + (int64_t)tile * 4096 + i * 1024 + wave * 64 + threadIdx.x;
+    const int64_t step = (int64_t)tiles * 4096;
+    f32x4_t acc[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    constexpr int U = 8;
+    for (int q = 0; q < a.parts; q += U) {
+        f32x4_t w[U][4];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[u][j] = p[min(q + u, a.parts - 1) * step + j * 256];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const int col = c + j * 16 + 4 * g4 + v;
-                    if (col >= a.V || (KIND == MAXIMA && col == y)) acc[i][j][v] = -INFINITY;
-                    mx = fmaxf(mx, acc[i][j][v]);
-                }
-            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * a.k;
-            const float r = KIND == MAXIMA ? (mx == -INFINITY ? 0.f : mx) : ref;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int col = c + j * 16 + 4 * g4;
-                float e[4];
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    e[v] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][v], a.k, -r));
-                    if (col + v == y) e[v] = ey;
-                    s += e[v];
-                    if (dead) e[v] = 0.f;
-                }
-                if (store && m < rows && col - a.c0 < a.lde)
-                    *reinterpret_cast<float4*>((float*)a.e + (int64_t)m * a.lde + (col - a.c0)) = make_float4(e[0], e[1], e[2], e[3]);
-            }
-            if (KIND != VALUES) {
-                s += __shfl_xor(s, 16, 64);
-                s += __shfl_xor(s, 32, 64);
-                if (g4 == 0 && m < rows && c < a.V) {
-                    a.sums[(int64_t)(c / STRIP) * a.ldn + m] = KIND == MAXIMA ? mx + log2f(s) : s;
-                    if (KIND == SUMS && !dead && !(s <= FLAG_ABOVE)) a.flags[0] = a.flags[1 + (m >> 8)] = 1;
-                }
-            }
-        }
+                for (int v = 0; v < 4; ++v) acc[j][v] += q + u < a.parts ? w[u][j][v] : 0.f;
     }
+    leave_f32<KIND>(a, rows, acc, m + ((int)threadIdx.x & 15), n0 + (wave & 1) * 64, KIND != MAXIMA && n0 < a.store_end);
 }
 
 __global__ F32_BOUNDS void head_dx_f32_kernel(DxArgs a) {
@@ -1257,7 +1317,7 @@ template <int N, bool MAIN> __global__ __launch_bounds__(256) void head_dtable_f
 
 struct HeadWs {
     int strips, ldn, tile, resident, cap;       // of dx: a tile's rows and columns, blocks that are resident at a time.  cap: columns of e (0: too little room, or no gradient)
-    size_t ref, a, ey, y, terms, flags, sums, xs, slots, more, e, total;
+    size_t ref, a, ey, y, terms, flags, sums, xs, slots, more, part, e, total;
     HeadWs(int V, int H, int n_rows, int dtype, bool need_dx, bool need_dt, size_t bytes) {
         const int n = n_rows > 0 ? n_rows : 1;
         const size_t es = dtype_size(dtype);
@@ -1277,6 +1337,9 @@ struct HeadWs {
         resident = compute_units() * (dtype == CF_F32 ? 3 : 1);
         slots = take(need_dx ? (size_t)n * H * 4 : 0);
         more = take(need_dx ? (size_t)2 * resident * tile * tile * 4 : 0);         // at most two rounds of parts
+        // fp32 logits in parts, at most a round of them: gone before dx begins
+        const F32Parts P(n, V, H, resident);
+        part = need_dx ? more : take(dtype == CF_F32 && n > F32_SUMS_FEW_ROWS && P.parts > 1 ? (size_t)P.tiles * P.parts * 65536 : 0);
         e = at;
         cap = 0;
         total = at;
@@ -1356,12 +1419,26 @@ template <> struct HeadLaunch<bf16_t> {
 };
 template <> struct HeadLaunch<float> {
     static int grid(int64_t items) { return (int)std::min<int64_t>(items, MAX_GRID); }
+    // of the launch's columns, or of the flagged tiles, whose parts are still there
     template <int KIND> static hipError_t logits(const HeadArgs& a, hipStream_t st) {
+        if (a.parts > 1 && a.flagged_only) return join<KIND>(a, st);
         head_logits_f32_kernel<KIND><<<grid((int64_t)ceil_div(a.n_max, 128) * ceil_div(a.c1 - a.c0, 128)), 256, 0, st>>>(a);
         return hipGetLastError();
     }
+    template <int KIND> static hipError_t join(const HeadArgs& a, hipStream_t st) {
+        const int tm = ceil_div(a.n_max, 128), tiles = tm * ceil_div(a.V, 128);
+        head_logits_join_f32_kernel<KIND><<<16 * tiles, 64, 0, st>>>(a, tm, tiles);
+        return hipGetLastError();
+    }
     static hipError_t sums(HeadArgs& a, hipStream_t st) {
-        if (a.n_max > F32_SUMS_FEW_ROWS) return logits<SUMS>(a, st);
+        if (a.n_max > F32_SUMS_FEW_ROWS) {
+            const F32Parts P(a.n_max, a.V, a.H, 3 * compute_units());
+            a.parts = P.parts;
+            if (P.parts == 1) return logits<SUMS>(a, st);
+            head_logits_part_f32_kernel<<<P.tiles * P.parts, 256, 0, st>>>(a, ceil_div(a.n_max, 128), P.tiles, P.per);
+            const hipError_t e = hipGetLastError();
+            return e != hipSuccess ? e : join<SUMS>(a, st);
+        }
         a.strips = few_blocks(a.V, compute_units());
         return a.n_max <= 16 ? few<1>(a, st) : few<2>(a, st);
     }
@@ -1433,6 +1510,8 @@ static hipError_t launch_head(HeadArgs a, LossArgs l, const HeadWs& L, unsigned 
         const int first = std::min(V, L.cap);           // columns whose exponentials are kept
         a.c0 = 0; a.c1 = V; a.lde = (int)align_up((size_t)first, 8); a.store_end = grads ? first : 0; a.e = grads ? ws + L.e : nullptr;
         a.flagged_only = false;
+        a.part = (float*)(ws + L.part);
+        a.parts = 1;
         const int blocks = ceil_div(n, 4);
         head_rows_kernel<T><<<std::min(blocks, 8 * compute_units()), 256, 0, st>>>(a, l);
         CF_TRY(hipGetLastError());

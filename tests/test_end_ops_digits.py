@@ -9,6 +9,7 @@ import pytest
 import torch
 
 from paper_2502_00340_amd import binding as Bn
+from tests.test_end_ops import _head_case, _head_check
 from tests.test_step_ops import BF, DEV, EPS, F32, F64, U, close, gen, gpu, randn, say
 
 
@@ -86,3 +87,50 @@ def test_head_loss_of_almost_certain_targets(dtype, n, H, V, improbable):
         want = d @ t64
         if dtype is F32:
             close(dx, want, (d.abs() * (2 * rel + (V + 16) * U)) @ t64.abs() + 2.0 ** -120, "dx")
+
+
+# ---- fp32 logits whose contraction is cut into parts --------------------------------------------------------
+
+# few tiles of 128 columns, wide inputs: parts that come out even and that do not, one row more than the streamed form takes, more rows than a flag's
+@gpu
+@pytest.mark.parametrize("n,H,V", [(33, 8192, 300), (64, 8192, 2400), (100, 4100, 6000), (300, 4096, 2500), (130, 8192, 1), (600, 2052, 130)])
+def test_fp32_logits_of_few_tiles(n, H, V):
+    say("parts", n, H, V)
+    x, table, y, _, _ = _head_case(n + V, F32, n, H, V)
+    got = Bn.head_loss(x, table, y)
+    _head_check(got, x, table, y, F32)
+    for kw in (dict(need_dx=False, need_dtable=False), dict(need_dx=False), dict(ws_limit=0)):
+        o = Bn.head_loss(x, table, y, **kw)
+        assert torch.equal(o[0], got[0]) and torch.equal(o[1], got[1])
+        _head_check(o, x, table, y, F32)
+    for s, t in zip(Bn.head_loss(x, table, y), got):
+        assert torch.equal(s, t)
+
+
+@gpu
+@pytest.mark.parametrize("improbable", [False, True])
+def test_fp32_logits_of_few_tiles_of_live_rows(improbable):
+    """The count on the device, rows that are left out whatever they hold, targets far below their row's largest logit."""
+    n, H, V = 300, 520, 2500
+    x, table, y, _, g0 = _head_case(3, F32, n, H, V)
+    if improbable:
+        x[:, 0], table[:, 0] = 0.0, 0.0
+        table[V - 1, 0] = 300.0
+        x[7], y[7] = 0.0, 11
+        x[7, 0] = 1.0
+    for live in (0, 1, 9, 128, 129, 300, 310):
+        m = min(live, n)
+        x2, y2 = x.clone(), y.clone()
+        x2[m:] = float("nan")
+        if m > 20:
+            x2[3], y2[3], x2[20], y2[20] = float("nan"), -100, float("inf"), V
+        dev = torch.tensor([live], dtype=torch.int32, device=DEV)
+        dx = torch.full((n, H), 7.0, device=DEV)
+        got = Bn.head_loss(x2, table, y2, n_kept_dev=dev, dx_out=dx)
+        assert dx[m:].eq(7.0).all()
+        if m == 0:
+            assert got[0].eq(0).all() and got[3].eq(0).all()
+            continue
+        _head_check((got[0], got[1][:m], dx[:m], got[3]), x2[:m], table, y2[:m], F32)
+    if improbable:
+        assert float(got[1][7]) < -290.0
