@@ -403,6 +403,7 @@ cf_status cf_embed_bwd(const int64_t* tokens, const void* dx_kept, int32_t V, in
 
 /* cf_norm_fwd: y[j,:] = n * g + b of row idx[j] of x, n = (x - mu) * rstd, rstd = (mean((x - mu)^2) + eps)^(-1/2); mu is the row's mean (layer 1) or 0
  *   (layer 0: root mean square norm).  b (layer 1 only, nullable): biases.  y [max_kept,H] may be x itself without idx; no other overlap.
+ *   (Overlaps are refused as far as extents are known; which rows of x an index names is not, beyond the first: y, and dx and the gradients below, have to lie elsewhere.)
  * cf_norm_bwd: with u = dy * g,  dx = rstd * (u - [layer 1] mean(u) - n * mean(u * n)),  dg = sum over rows of dy * n,  db = sum of dy (layer 1).
  *   The statistics are made again from x.  dx_kept [max_kept,H] may be dy_kept itself, without idx x itself; no other overlap.  dg, db [H] (nullable; db
  *   with dg only): in the storage dtype, overwritten, or (main_grad 1) fp32 and added to.  The sums' order depends on the sizes alone.  ws is needed for dg and db only.

@@ -364,7 +364,9 @@ cf_status cf_norm_fwd(const cf_norm_desc* desc, const void* x, const void* g, co
     if (b && !desc->layer) return CF_ERR_SHAPE;
     if (off_by(x, 16) || off_by(g, 16) || off_by(b, 16) || off_by(y, 16) || off_by(idx, 4) || off_by(n_kept_dev, 4)) return CF_ERR_SHAPE;
     const uint64_t bytes = (uint64_t)max_kept * desc->H * dtype_size(desc->dtype);
-    if (x == y ? idx != nullptr : !idx && overlap(x, bytes, y, bytes)) return CF_ERR_SHAPE;
+    const uint64_t row = (uint64_t)desc->H * dtype_size(desc->dtype), known = idx ? row : bytes;          // of x: an index may name few rows
+    if (x == y ? idx != nullptr : overlap(x, known, y, bytes)) return CF_ERR_SHAPE;
+    if (overlap(y, bytes, g, row) || overlap(y, bytes, b, row)) return CF_ERR_SHAPE;
     if (max_kept == 0) return CF_OK;
     NormArgs a{x, g, b, nullptr, idx, n_kept_dev, max_kept, desc->H, desc->eps, y, nullptr, nullptr, 0};
     launch_norm_any<false>(*desc, a, reinterpret_cast<hipStream_t>(stream));
@@ -388,10 +390,14 @@ cf_status cf_norm_bwd(const cf_norm_desc* desc, const void* x, const void* g, co
     if (off_by(idx, 4) || off_by(n_kept_dev, 4)) return CF_ERR_SHAPE;
     const uint64_t bytes = (uint64_t)max_kept * desc->H * dtype_size(desc->dtype);
     if (dx_kept != dy_kept && overlap(dx_kept, bytes, dy_kept, bytes)) return CF_ERR_SHAPE;
-    if (dx_kept == x ? idx != nullptr : !idx && overlap(dx_kept, bytes, x, bytes)) return CF_ERR_SHAPE;
+    const uint64_t row = (uint64_t)desc->H * dtype_size(desc->dtype), known = max_kept == 0 ? 0 : idx ? row : bytes;
+    if (dx_kept == x ? idx != nullptr : overlap(dx_kept, bytes, x, known)) return CF_ERR_SHAPE;
+    if (overlap(dx_kept, bytes, g, row)) return CF_ERR_SHAPE;
     const uint64_t gb = (uint64_t)desc->H * (main_grad ? 4 : dtype_size(desc->dtype));
     if (overlap(dg, gb, db, gb) || overlap(dg, gb, dx_kept, bytes) || overlap(db, gb, dx_kept, bytes)) return CF_ERR_SHAPE;
     if (dg && (!ws || off_by(ws, 256) || ws_bytes < cf_norm_bwd_workspace_bytes(desc, max_kept))) return CF_ERR_WORKSPACE;
+    for (const void* p : {(const void*)dg, (const void*)db})
+        if (overlap(p, gb, g, row) || overlap(p, gb, dy_kept, bytes) || overlap(p, gb, x, known)) return CF_ERR_SHAPE;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     const int rpb = NormShape(desc->dtype, desc->H).rpb;
     const int used = norm_bwd_used(max_kept > 0 ? max_kept : 1, rpb, NORM_BWD_BLOCKS);

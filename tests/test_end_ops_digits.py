@@ -3,6 +3,7 @@ whose exact result fp32 holds, plans of tiles and rings that small sizes do not 
 
 Tolerances count roundings: a stored value is off by half a step of its type (EPS: half of finfo.eps, relative), an fp32 sum of n
 terms by (its depth, at most n) * 2^-24 of the sum of their absolute values, a function of the hardware or the library by a few 2^-24."""
+import ctypes as C
 import math
 
 import pytest
@@ -11,6 +12,29 @@ import torch
 from paper_2502_00340_amd import binding as Bn
 from tests.test_end_ops import _head_case, _head_check
 from tests.test_step_ops import BF, DEV, EPS, F32, F64, U, close, gen, gpu, randn, say
+
+
+# ---- overlaps (CPU) ----------------------------------------------------------------------------------------
+
+def test_norm_refuses_overlaps_of_known_extents():
+    """Blocks read the gains, and the backward's last launch writes their gradients, while and after others write rows."""
+    L = Bn.lib()
+    A, N = 1 << 20, 4 * 16 * 2           # far apart; bytes of four rows of 16
+    D = lambda layer=1: C.byref(Bn.NormDesc(16, 0, layer, 1e-5))
+    idx = 9 * A
+    f = lambda x=A, g=2 * A, b=3 * A, i=None, n=4, y=4 * A: L.cf_norm_fwd(D(), x, g, b, i, None, n, y, None)
+    for y in (2 * A, 2 * A + 16, 3 * A, 3 * A - N + 16, 2 * A - N + 16):
+        assert f(y=y) == f(y=y, i=idx) == 2
+    assert f(i=idx, y=A) == 2 and f(i=idx, y=A + 16) == 2          # the first of the rows that an index may name
+    need = L.cf_norm_bwd_workspace_bytes(D(), 4)
+    b = lambda x=A, g=2 * A, dy=3 * A, i=None, dx=4 * A, dg=5 * A, db=6 * A, main=0: L.cf_norm_bwd(D(), x, g, dy, i, None, 4, dx, dg, db, main, 7 * A, need, None)
+    for i in (None, idx):
+        for main in (0, 1):
+            wide = 64 if main else 32
+            for at, size in ((2 * A, 32), (3 * A, N)):              # the gains, dy
+                assert b(dg=at, i=i, main=main) == b(dg=at + size - 16, i=i, main=main) == b(db=at - wide + 16, i=i, main=main) == 2
+            assert b(dx=2 * A, i=i, main=main) == b(dx=2 * A - N + 16, i=i, main=main) == 2
+    assert b(dg=A) == b(db=A + N - 16) == b(dg=A + 16, i=idx) == b(dx=A + 16, i=idx) == 2
 
 
 # ---- targets that are almost certain -----------------------------------------------------------------------
