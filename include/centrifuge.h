@@ -426,7 +426,10 @@ cf_status cf_norm_bwd(const cf_norm_desc* desc, const void* x, const void* g, co
  * The logits are fp32 values that are never stored.  What is kept of them for the gradients is bounded by the workspace: exponentials, in the storage
  * dtype, of as many columns as it has room for; those of the others are computed again, piece by piece.  A larger workspace is faster; logp and stats do not
  * depend on it, gradients by the order of fp32 sums.  For the same rows and max_kept logp has the same bits with and without
- * gradients.  max_kept at most 2^22; in CF_BF16 x_kept stays below 2 GiB; the table may be larger.
+ * gradients.  max_kept at most 2^22, in CF_BF16 with a gradient 2^22 - 65; in CF_BF16 x_kept stays below 2 GiB; the table may be larger.
+ * In CF_BF16 the exponentials and the rows of x_kept times their row's factor are operands of matrix products and rounded to bf16 once each: dtable is off by up to
+ * four roundings of 2^-8 a term, dx by three.  In CF_F32 products take their operands in three bf16 parts (2^-26 a product): magnitudes above 3.39e38 count as
+ * infinite, and an infinite operand of a row that counts may give NaN where a sum of fp32 products is infinite.
  *   cf_head_loss_workspace_bytes: what to provide for a call with (need_dx, need_dtable): as much as is of use, at most `limit`, or the least that will do
  *   where that is more.  0 for sizes that are refused. */
 size_t cf_head_loss_workspace_bytes(const cf_loss_desc* desc, int32_t H, int32_t max_kept, int32_t need_dx, int32_t need_dtable, size_t limit);

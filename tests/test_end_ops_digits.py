@@ -37,6 +37,17 @@ def test_norm_refuses_overlaps_of_known_extents():
     assert b(dg=A) == b(db=A + N - 16) == b(dg=A + 16, i=idx) == b(dx=A + 16, i=idx) == 2
 
 
+# ---- bounds (CPU) ------------------------------------------------------------------------------------------
+
+def test_head_loss_bounds_of_rows():
+    need = lambda n, dx, dt, code=0: Bn.lib().cf_head_loss_workspace_bytes(C.byref(Bn.LossDesc(0, 300, code, 1.0, 0.0, 0.0, 0.0, 0.0)), 8, n, dx, dt, 0)
+    most = 1 << 22
+    for dx, dt in ((1, 0), (0, 1), (1, 1)):
+        assert need(most - 65, dx, dt) > 0 and need(most - 64, dx, dt) == 0
+        assert need(most, dx, dt, 1) > 0 and need(most + 1, dx, dt, 1) == 0
+    assert need(most, 0, 0) > 0 and need(most + 1, 0, 0) == 0
+
+
 # ---- targets that are almost certain -----------------------------------------------------------------------
 
 def _dlogits(l, y, n):
