@@ -9,7 +9,7 @@
 
 namespace cf {
 
-struct NormArgs {
+struct RowNormArgs {
     const void *x, *g, *b, *dy;
     const int32_t *idx, *n_dev;
     int n_max, H;
@@ -46,7 +46,7 @@ template <typename T> __device__ __forceinline__ void unpack(const u32x4_t& w, f
 
 // NT threads a row, NV vectors of 16 bytes a thread; blocks of 256 (or NT) threads, so that NT = 64 has four rows a block at a time
 template <typename T, int NT, int NV, bool LAYER>
-__global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_fwd_kernel(NormArgs a) {
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_fwd_kernel(RowNormArgs a) {
     constexpr int VN = Vec<T>::N, BT = NT < 256 ? 256 : NT, RPB = BT / NT;
     __shared__ float red[2][NT > 64 ? NT / 64 : 1];
     const int n_rows = live_rows(a.n_max, a.n_dev), H = a.H, vpr = H / VN, tid = threadIdx.x % NT;
@@ -123,7 +123,7 @@ __host__ __device__ inline int norm_bwd_used(int n_rows, int rpb, int blocks) {
 }
 
 template <typename T, int NT, int NV, bool LAYER>
-__global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_bwd_kernel(NormArgs a) {
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_bwd_kernel(RowNormArgs a) {
     constexpr int VN = Vec<T>::N, BT = NT < 256 ? 256 : NT, RPB = BT / NT, W = NT > 64 ? NT / 64 : 1;
     __shared__ float red[2][3 * W];
     const int n_rows = live_rows(a.n_max, a.n_dev), H = a.H, vpr = H / VN, tid = threadIdx.x % NT;
@@ -305,7 +305,7 @@ struct NormShape {
 // Blocks of the backward, and so the parts of a gain's gradient: 512, 768 and 1024 take 19.5, 19.8 and 22.2 us (4593 fp32 rows of 840, layer norm: 12.9, 13.4, 15.2)
 constexpr int NORM_BWD_BLOCKS = 512;
 
-template <typename T, bool LAYER, bool BWD> static void launch_norm(const NormArgs& a, hipStream_t st) {
+template <typename T, bool LAYER, bool BWD> static void launch_norm(const RowNormArgs& a, hipStream_t st) {
     const NormShape s(Vec<T>::N == 4 ? CF_F32 : CF_BF16, a.H);
     const int vpr = a.H / Vec<T>::N, nv = (vpr + s.nt - 1) / s.nt;
     const int need = ceil_div(a.n_max, s.rpb), most = BWD ? a.blocks : compute_units() * (s.nt == 1024 ? 2 : 8);
@@ -329,7 +329,7 @@ template <typename T, bool LAYER, bool BWD> static void launch_norm(const NormAr
 #undef CF_NORM
 }
 
-template <bool BWD> static void launch_norm_any(const cf_norm_desc& d, const NormArgs& a, hipStream_t st) {
+template <bool BWD> static void launch_norm_any(const cf_norm_desc& d, const RowNormArgs& a, hipStream_t st) {
     if (d.dtype == CF_F32) d.layer ? launch_norm<float, true, BWD>(a, st) : launch_norm<float, false, BWD>(a, st);
     else d.layer ? launch_norm<bf16_t, true, BWD>(a, st) : launch_norm<bf16_t, false, BWD>(a, st);
 }
@@ -368,7 +368,7 @@ cf_status cf_norm_fwd(const cf_norm_desc* desc, const void* x, const void* g, co
     if (x == y ? idx != nullptr : overlap(x, known, y, bytes)) return CF_ERR_SHAPE;
     if (overlap(y, bytes, g, row) || overlap(y, bytes, b, row)) return CF_ERR_SHAPE;
     if (max_kept == 0) return CF_OK;
-    NormArgs a{x, g, b, nullptr, idx, n_kept_dev, max_kept, desc->H, desc->eps, y, nullptr, nullptr, 0};
+    RowNormArgs a{x, g, b, nullptr, idx, n_kept_dev, max_kept, desc->H, desc->eps, y, nullptr, nullptr, 0};
     launch_norm_any<false>(*desc, a, reinterpret_cast<hipStream_t>(stream));
     return hipGetLastError() == hipSuccess ? CF_OK : CF_ERR_HIP;
 }
@@ -403,7 +403,7 @@ cf_status cf_norm_bwd(const cf_norm_desc* desc, const void* x, const void* g, co
     const int used = norm_bwd_used(max_kept > 0 ? max_kept : 1, rpb, NORM_BWD_BLOCKS);
     float* pg = dg ? (float*)ws : nullptr;
     float* pb = db ? pg + (size_t)used * desc->H : nullptr;
-    NormArgs a{x, g, nullptr, dy_kept, idx, n_kept_dev, max_kept, desc->H, desc->eps, dx_kept, pg, pb, NORM_BWD_BLOCKS};
+    RowNormArgs a{x, g, nullptr, dy_kept, idx, n_kept_dev, max_kept, desc->H, desc->eps, dx_kept, pg, pb, NORM_BWD_BLOCKS};
     if (max_kept > 0) launch_norm_any<true>(*desc, a, st);
     if (dg) {
         const dim3 grid(ceil_div(desc->H, 32), db ? 2 : 1);
