@@ -105,6 +105,12 @@ constexpr int MAX_GRID = 1 << 20;
 
 static inline int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 static inline size_t dtype_size(int dtype) { return dtype == CF_F32 ? 4 : 2; }
+// whether two ranges of bytes share an address; nothing and an empty range share none
+static inline bool ranges_meet(const void* a, uint64_t an, const void* b, uint64_t bn) {
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return a && b && an && bn && x < y + bn && y < x + an;
+}
+static inline bool off_by(const void* p, size_t a) { return (uintptr_t)p % a != 0; }
 
 // Number of live rows of a launch (kept tokens).  dev == nullptr: exactly n, known to the host.
 // Otherwise the count lives on the device (the index build earlier on the same stream wrote it) and

@@ -534,13 +534,6 @@ static hipError_t launch_embed_bwd(SumArgs a, SortArgs so, unsigned char* ws, hi
 
 using namespace cf;
 
-static bool ranges_meet(const void* a, uint64_t an, const void* b, uint64_t bn) {
-    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    return an && bn && x < y + bn && y < x + an;
-}
-
-static bool off16(const void* p) { return (uintptr_t)p % 16 != 0; }
-
 static cf_status embed_sizes(int32_t V, int32_t H, int32_t dtype) {
     if (dtype != CF_BF16 && dtype != CF_F32) return CF_ERR_DTYPE;
     if (V <= 0 || V > (1 << 30) || H <= 0 || H > (1 << 20) || H % (dtype == CF_F32 ? 4 : 8) != 0) return CF_ERR_SHAPE;
@@ -555,7 +548,7 @@ cf_status cf_embed_fwd(const void* table, int32_t V, int32_t H, int32_t dtype, c
     const cf_status ok = embed_sizes(V, H, dtype);
     if (ok != CF_OK) return ok;
     if (n < 0 || n > ((int64_t)1 << 40) / H || !(scale - scale == 0.f)) return CF_ERR_SHAPE;
-    if (off16(table) || off16(out) || (uintptr_t)tokens % 8 != 0) return CF_ERR_SHAPE;
+    if (off_by(table, 16) || off_by(out, 16) || off_by(tokens, 8)) return CF_ERR_SHAPE;
     const uint64_t row = (uint64_t)H * dtype_size(dtype);
     if (ranges_meet(out, n * row, table, V * row)) return CF_ERR_SHAPE;
     if (n == 0) return CF_OK;
@@ -577,10 +570,10 @@ cf_status cf_embed_bwd(const int64_t* tokens, const void* dx_kept, int32_t V, in
     const cf_status ok = embed_sizes(V, H, dtype);
     if (ok != CF_OK) return ok;
     if (max_kept < 0 || max_kept > (1 << 30) || (main_grad != 0 && main_grad != 1) || !(scale - scale == 0.f)) return CF_ERR_SHAPE;
-    if (off16(dx_kept) || off16(dtable) || (uintptr_t)tokens % 8 != 0 || (uintptr_t)idx % 4 != 0 || (uintptr_t)n_kept_dev % 4 != 0) return CF_ERR_SHAPE;
+    if (off_by(dx_kept, 16) || off_by(dtable, 16) || off_by(tokens, 8) || off_by(idx, 4) || off_by(n_kept_dev, 4)) return CF_ERR_SHAPE;
     const uint64_t es = dtype_size(dtype);
     if (ranges_meet(dtable, (uint64_t)V * H * (main_grad ? 4 : es), dx_kept, (uint64_t)max_kept * H * es)) return CF_ERR_SHAPE;
-    if (!ws || (uintptr_t)ws % 256 != 0 || ws_bytes < cf_embed_bwd_workspace_bytes(H, max_kept)) return CF_ERR_WORKSPACE;
+    if (!ws || off_by(ws, 256) || ws_bytes < cf_embed_bwd_workspace_bytes(H, max_kept)) return CF_ERR_WORKSPACE;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     int passes = 0;
     for (int64_t v = V; v > 0; v >>= DIGIT_BITS) ++passes;

@@ -1553,11 +1553,6 @@ static cf_status head_sizes(const cf_loss_desc* d, int32_t H, int32_t max_kept) 
     return CF_OK;
 }
 
-static bool ranges_meet(const void* a, uint64_t an, const void* b, uint64_t bn) {
-    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    return a && b && an && bn && x < y + bn && y < x + an;
-}
-
 extern "C" {
 
 size_t cf_head_loss_workspace_bytes(const cf_loss_desc* desc, int32_t H, int32_t max_kept, int32_t need_dx, int32_t need_dtable, size_t limit) {
@@ -1576,11 +1571,10 @@ cf_status cf_head_loss(const cf_loss_desc* desc, int32_t H, const void* x_kept, 
     if (ok == CF_OK) ok = head_sizes(desc, H, max_kept);
     if (ok != CF_OK) return ok;
     if (main_grad != 0 && main_grad != 1) return CF_ERR_SHAPE;
-    const auto off = [](const void* p, size_t a) { return (uintptr_t)p % a != 0; };
-    if (off(x_kept, 16) || off(table, 16) || off(dx_kept, 16) || off(dtable, 16) || off(targets, 8)) return CF_ERR_SHAPE;
+    if (off_by(x_kept, 16) || off_by(table, 16) || off_by(dx_kept, 16) || off_by(dtable, 16) || off_by(targets, 8)) return CF_ERR_SHAPE;
     for (const void* p : {(const void*)old_logp, (const void*)ref_logp, (const void*)advantages, (const void*)weights, (const void*)idx,
                           (const void*)n_kept_dev, (const void*)logp, (const void*)stats})
-        if (off(p, 4)) return CF_ERR_SHAPE;
+        if (off_by(p, 4)) return CF_ERR_SHAPE;
     const uint64_t es = dtype_size(desc->dtype), xb = (uint64_t)max_kept * H * es, tb = (uint64_t)desc->V * H * es;
     const uint64_t db = (uint64_t)desc->V * H * (main_grad ? 4 : es);
     if ((dx_kept != x_kept && ranges_meet(dx_kept, xb, x_kept, xb)) || ranges_meet(dx_kept, xb, table, tb) || ranges_meet(dtable, db, table, tb) ||
@@ -1588,7 +1582,7 @@ cf_status cf_head_loss(const cf_loss_desc* desc, int32_t H, const void* x_kept, 
         return CF_ERR_SHAPE;
     const HeadWs L(desc->V, H, max_kept, desc->dtype, dx_kept != nullptr, dtable != nullptr, ws_bytes);
     if (L.cap < 0) return CF_ERR_UNSUPPORTED;
-    if (!ws || off(ws, 256) || ws_bytes < L.total) return CF_ERR_WORKSPACE;
+    if (!ws || off_by(ws, 256) || ws_bytes < L.total) return CF_ERR_WORKSPACE;
     const LossArgs l = loss_args(desc, targets, old_logp, ref_logp, advantages, weights, idx, n_kept_dev, max_kept, logp);
     HeadArgs a{};
     a.x = x_kept; a.table = table; a.H = H; a.V = desc->V; a.n_max = max_kept; a.n_dev = n_kept_dev; a.k = l.k;

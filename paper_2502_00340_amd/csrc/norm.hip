@@ -347,13 +347,6 @@ static cf_status norm_check(const cf_norm_desc* d, int32_t max_kept) {
     return d->H > 4096 * vn ? CF_ERR_UNSUPPORTED : CF_OK;       // a row stays in the registers of a block
 }
 
-static bool overlap(const void* a, uint64_t an, const void* b, uint64_t bn) {
-    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    return a && b && an && bn && x < y + bn && y < x + an;
-}
-
-static bool off_by(const void* p, size_t a) { return (uintptr_t)p % a != 0; }
-
 extern "C" {
 
 cf_status cf_norm_fwd(const cf_norm_desc* desc, const void* x, const void* g, const void* b, const int32_t* idx, const int32_t* n_kept_dev,
@@ -365,8 +358,8 @@ cf_status cf_norm_fwd(const cf_norm_desc* desc, const void* x, const void* g, co
     if (off_by(x, 16) || off_by(g, 16) || off_by(b, 16) || off_by(y, 16) || off_by(idx, 4) || off_by(n_kept_dev, 4)) return CF_ERR_SHAPE;
     const uint64_t bytes = (uint64_t)max_kept * desc->H * dtype_size(desc->dtype);
     const uint64_t row = (uint64_t)desc->H * dtype_size(desc->dtype), known = idx ? row : bytes;          // of x: an index may name few rows
-    if (x == y ? idx != nullptr : overlap(x, known, y, bytes)) return CF_ERR_SHAPE;
-    if (overlap(y, bytes, g, row) || overlap(y, bytes, b, row)) return CF_ERR_SHAPE;
+    if (x == y ? idx != nullptr : ranges_meet(x, known, y, bytes)) return CF_ERR_SHAPE;
+    if (ranges_meet(y, bytes, g, row) || ranges_meet(y, bytes, b, row)) return CF_ERR_SHAPE;
     if (max_kept == 0) return CF_OK;
     RowNormArgs a{x, g, b, nullptr, idx, n_kept_dev, max_kept, desc->H, desc->eps, y, nullptr, nullptr, 0};
     launch_norm_any<false>(*desc, a, reinterpret_cast<hipStream_t>(stream));
@@ -389,15 +382,15 @@ cf_status cf_norm_bwd(const cf_norm_desc* desc, const void* x, const void* g, co
         if (off_by(p, 16)) return CF_ERR_SHAPE;
     if (off_by(idx, 4) || off_by(n_kept_dev, 4)) return CF_ERR_SHAPE;
     const uint64_t bytes = (uint64_t)max_kept * desc->H * dtype_size(desc->dtype);
-    if (dx_kept != dy_kept && overlap(dx_kept, bytes, dy_kept, bytes)) return CF_ERR_SHAPE;
+    if (dx_kept != dy_kept && ranges_meet(dx_kept, bytes, dy_kept, bytes)) return CF_ERR_SHAPE;
     const uint64_t row = (uint64_t)desc->H * dtype_size(desc->dtype), known = max_kept == 0 ? 0 : idx ? row : bytes;
-    if (dx_kept == x ? idx != nullptr : overlap(dx_kept, bytes, x, known)) return CF_ERR_SHAPE;
-    if (overlap(dx_kept, bytes, g, row)) return CF_ERR_SHAPE;
+    if (dx_kept == x ? idx != nullptr : ranges_meet(dx_kept, bytes, x, known)) return CF_ERR_SHAPE;
+    if (ranges_meet(dx_kept, bytes, g, row)) return CF_ERR_SHAPE;
     const uint64_t gb = (uint64_t)desc->H * (main_grad ? 4 : dtype_size(desc->dtype));
-    if (overlap(dg, gb, db, gb) || overlap(dg, gb, dx_kept, bytes) || overlap(db, gb, dx_kept, bytes)) return CF_ERR_SHAPE;
+    if (ranges_meet(dg, gb, db, gb) || ranges_meet(dg, gb, dx_kept, bytes) || ranges_meet(db, gb, dx_kept, bytes)) return CF_ERR_SHAPE;
     if (dg && (!ws || off_by(ws, 256) || ws_bytes < cf_norm_bwd_workspace_bytes(desc, max_kept))) return CF_ERR_WORKSPACE;
     for (const void* p : {(const void*)dg, (const void*)db})
-        if (overlap(p, gb, g, row) || overlap(p, gb, dy_kept, bytes) || overlap(p, gb, x, known)) return CF_ERR_SHAPE;
+        if (ranges_meet(p, gb, g, row) || ranges_meet(p, gb, dy_kept, bytes) || ranges_meet(p, gb, x, known)) return CF_ERR_SHAPE;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     const int rpb = NormShape(desc->dtype, desc->H).rpb;
     const int used = norm_bwd_used(max_kept > 0 ? max_kept : 1, rpb, NORM_BWD_BLOCKS);

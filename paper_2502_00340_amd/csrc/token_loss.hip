@@ -30,10 +30,6 @@ template <> __device__ __forceinline__ Bytes16 narrow<float>(const float (&o)[4]
 template <> __device__ __forceinline__ Bytes16 narrow<bf16_t>(const float (&o)[8]) {
     return Bytes16{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]), pack_bf16x2(o[4], o[5]), pack_bf16x2(o[6], o[7])};
 }
-template <typename T> __device__ __forceinline__ T one_from_f32(float v);
-template <> __device__ __forceinline__ float one_from_f32<float>(float v) { return v; }
-template <> __device__ __forceinline__ bf16_t one_from_f32<bf16_t>(float v) { return (bf16_t)pack_bf16x2(v, 0.f); }     // NaN stays NaN
-
 // What a block knows of a row apart from its logits.  The same for all its threads, which the compiler cannot know of what it loads:
 // these go through the scalar path, apart from the vectors in flight (nothing in them is written during the kernel before it is read).
 template <typename U> __device__ __forceinline__ U scalar_load(const U* p) {
@@ -167,7 +163,7 @@ template <typename T, int NT> __device__ __forceinline__ void stream_row(const L
         }
     }
     if (int c = nv * VN + tid; c < V)
-        dl[c] = one_from_f32<T>(!r.live() ? 0.f : c == r.y ? end.at_y : end.neg * expo<EXACT>(ex, to_f32<T>(l[c])));
+        dl[c] = narrow_one<T>(!r.live() ? 0.f : c == r.y ? end.at_y : end.neg * expo<EXACT>(ex, to_f32<T>(l[c])));
 }
 
 template <typename T, int NT>
@@ -304,7 +300,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NV <= 4 ? 8 
             char* dl = (char*)((T*)a.dlogits + (int64_t)j * a.dstride);
             const unsigned yv = (unsigned)(r.y >> (VN == 8 ? 3 : 2)) * 16u;
             const int ye = r.y & (VN - 1);
-            if (ct < V) ((T*)dl)[ct] = one_from_f32<T>(!r.live() ? 0.f : ct == r.y ? at_y : grad(tail));
+            if (ct < V) ((T*)dl)[ct] = narrow_one<T>(!r.live() ? 0.f : ct == r.y ? at_y : grad(tail));
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 if (i < FULL || i * NT < nv) {
