@@ -990,17 +990,23 @@ template <int KIND> __global__ F32_BOUNDS void head_logits_f32_kernel(HeadArgs a
     }
 }
 
-// Fewer tiles than blocks that are resident at a time: a block takes a part of a tile's contraction and leaves its accumulators as they lie in its lanes; a wave a
-// fragment row of a tile adds the parts up in order and does with the sum what the whole tile would.  A flagged tile is added up again, not multiplied.
-// Whole calls, no gradients, without and with parts: 33 rows of [300, 8192] 455 and 43 us, 300 of [2500, 8192] 460 and 113, 300 of [12000, 2048] (282 tiles, two parts) 164 and
-// 135, 600 of [2000, 512] (four steps a part) 46 and 34.
+// Fewer tiles than blocks that can be resident: a block takes a part of a tile's contraction and leaves its accumulators as they lie in its lanes; a wave a
+// fragment row of a tile adds the parts up in order and does with the sum what the whole tile would.  A flagged tile is added up again, not multiplied.  The number of parts
+// is that of the least cost: a step of 32 k takes 1.5, 2.1 or 2.6 us where one, two or three blocks share a CU, the second launch 3 us, 64 KB out and in 14 ns.
+// Whole calls, no gradients, whole and in parts: 33 rows of [300, 8192] 453 and 45 us, 300 of [2500, 8192] 461 and 110, 1000 of [4096, 4096] (256 tiles) 242 and 190, 300
+// of [12000, 2048] (282 tiles) 164 and 132, 600 of [4096, 512] 47 and 42; 1000 of [4096, 512] stays whole, 47 (in three parts 50).
 struct F32Parts {
-    int tiles, parts, per;          // per: steps of 32 k a part; parts 1: whole tiles
-    F32Parts(int n, int V, int H, int resident) {
+    int tiles, parts, per;          // per: steps a part; parts 1: whole tiles
+    F32Parts(int n, int V, int H, int n_cu) {
+        constexpr int64_t ns[4] = {0, 1500, 2100, 2600};
         const int steps = ceil_div(H, F32_STEP);
-        const int64_t t = (int64_t)ceil_div(n, 128) * ceil_div(V, 128);
-        tiles = (int)std::min<int64_t>(t, 1 << 30);
-        parts = std::max(1, std::min(resident / tiles, steps / 4));
+        tiles = (int)std::min<int64_t>((int64_t)ceil_div(n, 128) * ceil_div(V, 128), 1 << 24);
+        parts = 1;
+        int64_t best = tiles <= 3 * n_cu ? steps * ns[ceil_div(tiles, n_cu)] : 0;
+        for (int p = 2; p * tiles <= 3 * n_cu && 4 * p <= steps; ++p) {
+            const int64_t cost = ceil_div(steps, p) * ns[ceil_div(tiles * p, n_cu)] + 3000 + 14 * tiles * p;
+            if (cost < best) { best = cost; parts = p; }
+        }
         per = ceil_div(steps, parts);
         parts = ceil_div(steps, per);
     }
@@ -1337,8 +1343,8 @@ struct HeadWs {
         resident = compute_units() * (dtype == CF_F32 ? 3 : 1);
         slots = take(need_dx ? (size_t)n * H * 4 : 0);
         more = take(need_dx ? (size_t)2 * resident * tile * tile * 4 : 0);         // at most two rounds of parts
-        // fp32 logits in parts, at most a round of them: gone before dx begins
-        const F32Parts P(n, V, H, resident);
+        // fp32 logits in parts, at most three a CU: gone before dx begins
+        const F32Parts P(n, V, H, compute_units());
         part = need_dx ? more : take(dtype == CF_F32 && n > F32_SUMS_FEW_ROWS && P.parts > 1 ? (size_t)P.tiles * P.parts * 65536 : 0);
         e = at;
         cap = 0;
@@ -1432,7 +1438,7 @@ template <> struct HeadLaunch<float> {
     }
     static hipError_t sums(HeadArgs& a, hipStream_t st) {
         if (a.n_max > F32_SUMS_FEW_ROWS) {
-            const F32Parts P(a.n_max, a.V, a.H, 3 * compute_units());
+            const F32Parts P(a.n_max, a.V, a.H, compute_units());
             a.parts = P.parts;
             if (P.parts == 1) return logits<SUMS>(a, st);
             head_logits_part_f32_kernel<<<P.tiles * P.parts, 256, 0, st>>>(a, ceil_div(a.n_max, 128), P.tiles, P.per);
