@@ -819,10 +819,10 @@ def _head_ws_bytes(V, code, H, n, dx, dt, limit, device):
 def head_loss(x, table, targets, old_logp=None, advantages=None, ref_logp=None, weights=None, clip=(0.2, 0.2), kl_coef: float = 0.0,
               logit_scale: float = 1.0, norm: float = 0.0, idx=None, n_kept_dev=None, need_dx: bool = True, need_dtable: bool = True, main_grad=None,
               dx_out=None, ws_limit: int = 2 << 30):
-    """The losses of token_loss straight from the head's input x [n, H] (compact: row j belongs to targets[idx[j]], and so on) and its table [V, H], with no
-    logits in memory.  Returns (stats [4], logp [n], dx [n, H] or None, dtable [V, H] or None).  main_grad: fp32 [V, H] that the table's gradient is added to.
+    """The losses of token_loss straight from the head's input x [n, H] (compact: row j belongs to targets[idx[j]], and so on) and its table [V, H]; logits are
+    not stored.  Returns (stats [4], logp [n], dx [n, H] or None, dtable [V, H] or None).  main_grad: fp32 [V, H] that the table's gradient is added to.
     dx_out: to write dx to, x itself too.  n_kept_dev: only the first min(*n_kept_dev, n) rows.  ws_limit: bytes of scratch that the call may
-    allocate; exponentials of logits that do not fit are computed twice."""
+    allocate, or the least that will do; a call with gradients keeps an exponential of every logit there, in x's type, and computes those that do not fit twice."""
     _need(x.dim() == 2 and x.is_contiguous() and table.dim() == 2 and table.is_contiguous(), "x has to be [n, H] and table [V, H], contiguous")
     (n, H), V = x.shape, table.shape[0]
     _dense(table, x.dtype, (V, H), "table")

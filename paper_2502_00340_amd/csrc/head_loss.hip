@@ -1,5 +1,6 @@
 // Loss of kept tokens straight from the head's input x [n, H] and the table E [V, H], with the gradients towards both: the logits s * x E^T are made tile by
-// tile in the matrix cores' accumulators and never leave them.  What leaves is bounded by the caller's workspace:
+// tile in the matrix cores' accumulators and are used up there (but for few fp32 tiles, whose accumulators leave in parts).  What leaves is bounded by the caller's
+// workspace:
 //
 //   1. head_rows      the target's logit of every row, a dot product: ref = s*log2(e) * x.E_y
 //   2. head_logits    tiles of x E^T; with t = s*log2(e)*l - ref, strips of 64 columns leave sum(2^t) of the columns that are not the target, and, for the first columns
@@ -17,7 +18,7 @@
 // what an almost certain target leaves to the others, 1 - p, would drown in it.  So it keeps all digits, and a row's gradients add up to 0 but for their roundings.
 //
 // What bounds it: the matrix cores under the chip's power limit from some hundred rows on (4096 rows, H = 4096, V = 128256 bf16: logits, dx and the table's gradient
-// 3.04, 3.01 and 3.08 ms, 1.40 to 1.43 PFLOP/s), the table's traffic for few rows.  Keeping e makes that three products instead of four.
+// 3.07, 3.08 and 3.13 ms, 1.38 to 1.40 PFLOP/s, medians of 12 passes in a row), the table's traffic for few rows.  Keeping e makes that three products instead of four.
 //
 // Roundings: logits, sums, lp and both gradients' sums are fp32; e, and x' = a*x, are rounded to the storage type once each (2^-8 relative in bf16), dx and
 // the table's gradient once where they are stored.
